@@ -10,6 +10,7 @@
  *   slkv_compress_overlapped / slkv_join   the same, successive layers overlapped on the GPU
  *   slkv_cp_*            the same for one sequence whose keys are split over ranks (context parallel)
  *   slkv_row_lse         the window rows' log-sum-exp over their softmax domain       (Eq. 3-4, Eq. 7)
+ *   slkv_q4_*            the compressed cache in decoding: held in 4 bits, attended to, evicted from
  *
  * Conventions
  *   - "dev" pointers are device memory of the current CUDA device, "host" pointers are host memory.
@@ -255,7 +256,7 @@ int slkv_compress(const slkv_params* p, const void* q_win, const void* k, const 
  *     queued and makes `stream` wait for every overlapped call made so far on the current device (no host wait);
  *     consume outputs, or free / overwrite any input, output or workspace buffer -- q_win, k, v, cu_seqlens_dev
  *     and budgets included -- only behind it.  cu_seqlens_host is read during the call only.  Any other slkv_*
- *     call that uses a workspace joins by itself first.
+ *     call that uses a workspace joins by itself first, except the slkv_q4_* calls: join before packing.
  *   - Streams and host threads: the calls made on one stream form one sequence (queue, workspace);
  *     calls made on another stream -- by another host thread or the same one -- form another, and the two do not
  *     disturb each other as long as each has its own workspace (calls on two streams that share a workspace are
@@ -416,8 +417,122 @@ int slkv_score_noalloc(const slkv_params* p, const void* q_win, const void* k, c
 size_t slkv_noalloc_scratch_bytes(void);      /* = SLKV_NOALLOC_SCRATCH_BYTES */
 int slkv_noalloc_last_cuda_error(void);
 
-/* Number of kernels the most recent slkv_score / slkv_compress / slkv_compress_host call on this
- * thread enqueued (launch accounting for benchmarks). */
+/*
+ * The compressed cache in decoding (no counterpart in the paper, which ends with the prefill): the rows that slkv_compress kept, held in
+ * 4 bits, attended to by new tokens, and kept within their heads' budgets while tokens come in.
+ *
+ * A cache has n_seqs * n_kv_heads segments, seg = s * n_kv_heads + h as in the packed output.  Segment seg owns the slots
+ * starts[seg] .. starts[seg+1]-1; the first lens[seg] of them are filled.  starts with no slack is slkv_compress' offsets; with slack,
+ * tokens can be appended.  starts and lens are device arrays that the host never reads: lengths that do not fit their segments and
+ * segments that do not fit the cache are cut to what fits.  Per slot:
+ *   records  slkv_q4_record_bytes(head_dim) = head_dim * 5 / 4 bytes: the token's K and V row in groups of 32 channels.  A group has a
+ *            scale and a zero in bf16, a channel a 4-bit code; it stands for zero + scale * code.
+ *              zero = the group's minimum rounded down to bf16, scale = (maximum - zero) / 15 rounded up to bf16,
+ *              code = (x - zero) / scale rounded to the nearest integer, ties to even, within 0 .. 15
+ *            so that |x - value| <= scale / 2 up to fp32 rounding.  A group with a NaN or an infinity, or with a range that fp32 does
+ *            not hold, stands for NaN throughout.
+ *            Layout: head_dim/2 bytes K codes, head_dim/2 bytes V codes, then head_dim/32 bf16 each of K scales, K zeros, V scales and
+ *            V zeros.  K codes: 32-bit word t * head_dim/32 + j has channels 32 j + 8 t + e in its nibbles e = 0 .. 7, lowest first; V
+ *            codes: 16-bit unit g * head_dim/32 + j has channels 32 j + 4 g + e in its nibbles e = 0 .. 3.
+ *   pos      the token's position in its sequence (kept_idx).  Slots need not be in the order of their positions.
+ *   weight   the attention the row has received: 0 when it comes in, added to by slkv_q4_attend, read by slkv_q4_evict.  May be NULL
+ *            for callers that never evict.
+ * Everything is enqueued on `stream`, nothing is allocated, every call can be captured.  Results are the same bit for bit from call
+ * to call.  n_seqs * n_kv_heads <= 16384, 1 <= capacity_rows < 2^31; records, rows and workspaces 16-byte aligned.
+ */
+typedef struct slkv_q4_cache {
+  int32_t n_seqs, n_kv_heads, head_dim;   /* head_dim 64 or 128 */
+  int32_t reserved;
+  int64_t capacity_rows;                  /* slots of the arrays below */
+  void* records;                          /* dev */
+  int32_t* pos;                           /* dev */
+  float* weight;                          /* dev, optional */
+  const int32_t* starts;                  /* dev, int32[n_seqs*n_kv_heads + 1], ascending */
+  int32_t* lens;                          /* dev, int32[n_seqs*n_kv_heads] */
+} slkv_q4_cache;
+
+size_t slkv_q4_record_bytes(int32_t head_dim);   /* 0 for a head_dim that is not supported */
+
+/*
+ * A packed layer into the cache: rows offsets[seg] .. offsets[seg+1]-1 of k, v (the k_out, v_out, offsets and kept_idx of slkv_compress)
+ * become the segment's first rows, lens[seg] their number, their positions kept_idx, their weights 0.
+ *   k, v       dev, [n_rows, head_dim] elements of dtype (SLKV_F32 | SLKV_BF16), contiguous; n_rows: rows that may be read
+ *   offsets    dev, int32[n_seqs*n_kv_heads + 1];  kept_idx dev, int32[n_rows]
+ *   status     dev, optional: SLKV_ERR_CAPACITY if a segment has more rows than slots, or offsets run past n_rows (the rest is dropped)
+ */
+int slkv_q4_pack(const slkv_q4_cache* c, int32_t dtype, const void* k, const void* v, int64_t n_rows, const int32_t* offsets,
+                 const int32_t* kept_idx, int32_t* status, void* stream);
+
+/*
+ * New tokens' rows behind the filled slots of every segment.
+ *   k, v       dev: element (s, i, h, p) at s*stride_seq + i*stride_tok + h*stride_head + p, i < n_tokens <= 65536
+ *   pos        dev, int32[n_seqs][n_tokens]: the tokens' positions
+ *   lens_out   dev, optional: takes the new lengths in place of c->lens, which then keeps the old ones (tokens that are drafted, and
+ *              may have to go again)
+ *   status     dev, optional: SLKV_ERR_CAPACITY if a segment has not enough slots left (it takes the tokens that fit)
+ */
+int slkv_q4_append(const slkv_q4_cache* c, int32_t dtype, const void* k, const void* v, int32_t n_tokens, int64_t k_stride_seq,
+                   int64_t k_stride_tok, int64_t k_stride_head, int64_t v_stride_seq, int64_t v_stride_tok, int64_t v_stride_head,
+                   const int32_t* pos, int32_t* lens_out, int32_t* status, void* stream);
+
+/*
+ * The values that records stand for, as rows of dtype (rounded to nearest for bf16).
+ *   slots_opt    dev, optional, int32[n]: row i of k_out, v_out [n, head_dim] is slot slots_opt[i]'s; entries outside the cache are
+ *                padding.  NULL: row i is slot i's, for the filled slots (n is capacity_rows whatever is passed).
+ * Rows of padding and of slots that are not filled are left as they are.
+ */
+int slkv_q4_unpack(const slkv_q4_cache* c, int32_t dtype, const int32_t* slots_opt, int64_t n, void* k_out, void* v_out, void* stream);
+
+/*
+ * Attention of n_tokens new tokens per sequence over the cache (their own rows appended or not).  For query head qh of KV head h and
+ * token i, over the filled slots r of segment (s, h):
+ *     x[r] = scale * q . K[r];  softcap > 0: x = softcap * tanh(x / softcap);  slopes: x += slopes[qh] * (pos[r] - q_pos[s][i])
+ *     visible: every filled slot; with q_pos those with pos[r] <= q_pos[s][i]
+ *     out = sum p V, p = softmax of x over the visible slots;  lse = log sum exp x
+ * A query that sees no slot gets zeros and -infinity.  A slot that is not visible to a query gives it nothing, whatever it holds.
+ *   q, out     dev, elements of dtype: element (s, i, qh, p) at s*stride_seq + i*stride_tok + qh*stride_head + p
+ *   q_pos_opt  dev, optional, int32[n_seqs][n_tokens];  slopes_opt dev, optional, float[n_q_heads] (needs q_pos_opt)
+ *   lse_opt    dev, optional out, float[n_seqs][n_q_heads][n_tokens] in lse_units
+ *   accumulate 1: weight[r] = weight_decay * weight[r] + (1/G) sum over the G query heads of h and over the tokens of p[r], for every
+ *              filled slot (the reduction slkv_score uses over window rows and heads)
+ *   status     dev, optional: SLKV_ERR_DEVICE_TIMEOUT if a bounded wait inside the kernel ran out
+ * Limits: n_q_heads / n_kv_heads * n_tokens <= 256.  Positions are >= 0.  fp32 accumulation throughout; with bf16 rows, probabilities
+ * times scales are rounded to bf16 for the product with V, with fp32 rows they keep 24 bits.
+ */
+typedef struct slkv_q4_attend_params {
+  int32_t n_q_heads;        /* multiple of the cache's n_kv_heads */
+  int32_t n_tokens;         /* per sequence, >= 1 */
+  int32_t dtype;            /* SLKV_F32 | SLKV_BF16: q and out */
+  int32_t lse_units;        /* SLKV_LSE_LN | SLKV_LSE_LOG2 */
+  float scale;              /* 1 / sqrt(head_dim), usually */
+  float softcap;            /* 0: none */
+  float weight_decay;       /* 1: a plain sum */
+  int32_t reserved;
+  int64_t q_stride_seq, q_stride_tok, q_stride_head;
+  int64_t o_stride_seq, o_stride_tok, o_stride_head;
+} slkv_q4_attend_params;
+size_t slkv_q4_attend_workspace_bytes(const slkv_q4_cache* c, const slkv_q4_attend_params* p, int32_t accumulate);   /* 0: bad arguments */
+int slkv_q4_attend(const slkv_q4_cache* c, const slkv_q4_attend_params* p, const void* q, const int32_t* q_pos_opt,
+                   const float* slopes_opt, void* out, float* lse_opt, int32_t accumulate, int32_t* status, void* workspace,
+                   size_t workspace_bytes, void* stream);
+
+/*
+ * Eviction: segment (s, h) with len rows keeps kept = min(len, max(budgets[h], window)) of them -- the rows with
+ * pos > newest[s] - window first, then those with the largest weights (NaN counts as less than any number; ties: lower slot first).
+ * Slot i < kept of the result holds row i where that is kept; the slots of rows that go take the kept rows from slots kept, kept + 1, ..
+ * in ascending order.  to->lens[seg] = kept.
+ *   from, to   the same cache (in place: records, pos, weight, starts and capacity the same, lens the same array or another), or another
+ *              one with the same numbers of sequences and heads that shares no memory with it and may lay out its segments otherwise.
+ *              Slots behind the kept rows are left as they are.
+ *   budgets    dev, int32[n_kv_heads];  newest dev, int32[n_seqs]: the position of the sequence's newest token;  window >= 1
+ *   status     dev, optional: SLKV_ERR_CAPACITY if a segment of `to` has fewer slots than rows are kept (it takes the first ones)
+ */
+size_t slkv_q4_evict_workspace_bytes(const slkv_q4_cache* from);     /* 0: bad arguments */
+int slkv_q4_evict(const slkv_q4_cache* from, const slkv_q4_cache* to, const int32_t* budgets, int32_t window, const int32_t* newest,
+                  int32_t* status, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Number of kernels the most recent slkv_score / slkv_compress / slkv_compress_host / slkv_q4_* call on
+ * this thread enqueued (launch accounting for benchmarks). */
 int slkv_last_launch_count(void);
 
 /*

@@ -40,6 +40,18 @@ class SlkvAllocOptions(C.Structure):
     _fields_ = [("head_normaliser", C.c_int32), ("rounding", C.c_int32), ("cap", C.c_int64)]
 
 
+class SlkvQ4Cache(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_seqs", "n_kv_heads", "head_dim", "reserved")] + [("capacity_rows", C.c_int64)] + \
+               [(n, C.c_void_p) for n in ("records", "pos", "weight", "starts", "lens")]
+
+
+class SlkvQ4AttendParams(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_q_heads", "n_tokens", "dtype", "lse_units")] + \
+               [(n, C.c_float) for n in ("scale", "softcap", "weight_decay")] + [("reserved", C.c_int32)] + \
+               [(n, C.c_int64) for n in ("q_stride_seq", "q_stride_tok", "q_stride_head", "o_stride_seq", "o_stride_tok",
+                                         "o_stride_head")]
+
+
 SLKV_NORM_GLOBAL, SLKV_NORM_WITHIN_LAYER = 0, 1
 SLKV_ROUND_SUM_EXACT, SLKV_ROUND_PAPER = 0, 1
 
@@ -133,6 +145,23 @@ def lib() -> C.CDLL:
         L.slkv_cp_emit.restype = C.c_int
         L.slkv_cp_emit.argtypes = [pp, vp, vp, i64, vp, i64, i32, i32, i64, vp, vp, vp, i32, i32, i32, i64, vp, vp, i64,
                                    vp, vp, vp, vp, sz, vp]
+        cp, ap = C.POINTER(SlkvQ4Cache), C.POINTER(SlkvQ4AttendParams)
+        L.slkv_q4_record_bytes.restype = sz
+        L.slkv_q4_record_bytes.argtypes = [i32]
+        L.slkv_q4_pack.restype = C.c_int
+        L.slkv_q4_pack.argtypes = [cp, i32, vp, vp, i64, vp, vp, vp, vp]
+        L.slkv_q4_append.restype = C.c_int
+        L.slkv_q4_append.argtypes = [cp, i32, vp, vp, i32, i64, i64, i64, i64, i64, i64, vp, vp, vp, vp]
+        L.slkv_q4_unpack.restype = C.c_int
+        L.slkv_q4_unpack.argtypes = [cp, i32, vp, i64, vp, vp, vp]
+        L.slkv_q4_attend_workspace_bytes.restype = sz
+        L.slkv_q4_attend_workspace_bytes.argtypes = [cp, ap, i32]
+        L.slkv_q4_attend.restype = C.c_int
+        L.slkv_q4_attend.argtypes = [cp, ap, vp, vp, vp, vp, vp, i32, vp, vp, sz, vp]
+        L.slkv_q4_evict_workspace_bytes.restype = sz
+        L.slkv_q4_evict_workspace_bytes.argtypes = [cp]
+        L.slkv_q4_evict.restype = C.c_int
+        L.slkv_q4_evict.argtypes = [cp, cp, vp, i32, vp, vp, vp, sz, vp]
         _lib = L
     return _lib
 
@@ -465,3 +494,136 @@ def slkv_cp_emit(params: SlkvParams, k: torch.Tensor, v: torch.Tensor, rows: int
                                int(pos0), threshold, need, ties_all, ties_all.size(0), int(part), int(window_rows),
                                int(window_pos0), k_out, v_out, k_out.size(0), offsets, kept_idx, status, workspace,
                                workspace.numel()), "slkv_cp_emit")
+
+
+# ---- the compressed cache in decoding, held in 4 bits: thin wrappers, see include/slkv.h ------------------------------------
+def slkv_q4_record_bytes(head_dim: int) -> int:
+    return int(lib().slkv_q4_record_bytes(int(head_dim)))
+
+
+def make_q4_cache(records: torch.Tensor, pos: torch.Tensor, weight: Optional[torch.Tensor], starts: torch.Tensor,
+                  lens: torch.Tensor, n_kv_heads: int) -> SlkvQ4Cache:
+    """records uint8 [slots, slkv_q4_record_bytes], pos int32 [slots], weight float32 [slots] or None, starts int32 [n_seg + 1],
+    lens int32 [n_seg], all contiguous.  The structure keeps the tensors alive and belongs to their device."""
+    head_dim = {80: 64, 160: 128}[records.size(1)]
+    assert records.dtype == torch.uint8 and pos.dtype == starts.dtype == lens.dtype == torch.int32
+    assert weight is None or weight.dtype == torch.float32
+    tensors = [t for t in (records, pos, weight, starts, lens) if t is not None]
+    for t in tensors:
+        assert t.is_contiguous() and t.device == records.device and t.dim() == (2 if t is records else 1)
+    rows, n_seg = records.size(0), lens.numel()
+    assert pos.numel() == rows and (weight is None or weight.numel() == rows) and starts.numel() == n_seg + 1
+    assert n_kv_heads >= 1 and n_seg % n_kv_heads == 0
+    c = SlkvQ4Cache(n_seg // n_kv_heads, n_kv_heads, head_dim, 0, rows, records.data_ptr(), pos.data_ptr(),
+                    weight.data_ptr() if weight is not None else None, starts.data_ptr(), lens.data_ptr())
+    c.tensors, c.device, c.lens_tensor = tensors, records.device, lens
+    return c
+
+
+def _q4_device(cache: SlkvQ4Cache, *tensors: Optional[torch.Tensor]) -> None:
+    """Calls are enqueued on a stream of the current device: that has to be the cache's and the tensors'."""
+    d = cache.device
+    assert d.type == "cuda" and d.index == torch.cuda.current_device(), "the cache is not on the current device"
+    for t in tensors:
+        assert t is None or t.device == d, "a tensor is not on the cache's device"
+
+
+def slkv_q4_pack(cache: SlkvQ4Cache, k: torch.Tensor, v: torch.Tensor, offsets: torch.Tensor, kept_idx: torch.Tensor,
+                 status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """k, v [rows, head_dim], offsets, kept_idx: as slkv_compress wrote them."""
+    _q4_device(cache, k, v, offsets, kept_idx, status)
+    rows = k.size(0)
+    assert k.is_contiguous() and v.is_contiguous() and k.dtype == v.dtype and k.shape == v.shape == (rows, cache.head_dim)
+    assert offsets.dtype == kept_idx.dtype == torch.int32 and offsets.is_contiguous() and kept_idx.is_contiguous()
+    assert offsets.numel() == cache.n_seqs * cache.n_kv_heads + 1 and kept_idx.numel() >= rows
+    _check(_fn["slkv_q4_pack"](stream, cache, _DTYPES[k.dtype], k, v, rows, offsets, kept_idx, status), "slkv_q4_pack")
+
+
+def slkv_q4_append(cache: SlkvQ4Cache, k: torch.Tensor, v: torch.Tensor, pos: torch.Tensor, after: Optional[SlkvQ4Cache] = None,
+                   status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """k, v [n_seqs, n_tokens, n_kv_heads, head_dim] (any strides over a contiguous last dimension), pos int32 [n_seqs, n_tokens].
+    after: the same cache with lengths of its own, which take the new ones."""
+    _q4_device(cache, k, v, pos, status)
+    n = k.size(1)
+    assert k.shape == v.shape == (cache.n_seqs, n, cache.n_kv_heads, cache.head_dim) and k.dtype == v.dtype
+    assert pos.dtype == torch.int32 and pos.is_contiguous() and pos.shape == (cache.n_seqs, n)
+    (ks, kt, kh, k1), (vs, vt, vh, v1) = k.stride(), v.stride()
+    assert k1 == v1 == 1
+    if after is not None:
+        assert after.records == cache.records and after.starts == cache.starts and after.pos == cache.pos
+    _check(_fn["slkv_q4_append"](stream, cache, _DTYPES[k.dtype], k, v, n, ks, kt, kh, vs, vt, vh, pos,
+                                 after.lens_tensor if after is not None else None, status), "slkv_q4_append")
+
+
+def slkv_q4_unpack(cache: SlkvQ4Cache, k_out: torch.Tensor, v_out: torch.Tensor, slots: Optional[torch.Tensor] = None,
+                   stream=None) -> None:
+    """k_out, v_out [n, head_dim]: the rows of the slots given (int32 [n], entries outside the cache are padding), or of every
+    filled slot at its own place (n = slots of the cache)."""
+    _q4_device(cache, k_out, v_out, slots)
+    n = k_out.size(0)
+    assert k_out.is_contiguous() and v_out.is_contiguous() and k_out.dtype == v_out.dtype
+    assert k_out.shape == v_out.shape == (n, cache.head_dim)
+    assert n == (cache.capacity_rows if slots is None else slots.numel())
+    assert slots is None or (slots.dtype == torch.int32 and slots.is_contiguous())
+    _check(_fn["slkv_q4_unpack"](stream, cache, _DTYPES[k_out.dtype], slots, n, k_out, v_out), "slkv_q4_unpack")
+
+
+def make_q4_attend(cache: SlkvQ4Cache, q: torch.Tensor, out: torch.Tensor, scale: Optional[float] = None, softcap: float = 0.0,
+                   weight_decay: float = 1.0, lse_units: int = SLKV_LSE_LN) -> SlkvQ4AttendParams:
+    """Shapes and strides from the tensors: q, out [n_seqs, n_tokens, n_q_heads, head_dim] (last dim contiguous)."""
+    assert q.shape == out.shape and q.dim() == 4 and q.dtype == out.dtype and q.stride(3) == 1 and out.stride(3) == 1
+    assert q.size(0) == cache.n_seqs and q.size(3) == cache.head_dim
+    return SlkvQ4AttendParams(q.size(2), q.size(1), _DTYPES[q.dtype], lse_units, cache.head_dim ** -0.5 if scale is None else scale,
+                              softcap, weight_decay, 0, *q.stride()[:3], *out.stride()[:3])
+
+
+def slkv_q4_attend_workspace_bytes(cache: SlkvQ4Cache, params: SlkvQ4AttendParams, accumulate: bool = False) -> int:
+    return int(lib().slkv_q4_attend_workspace_bytes(C.byref(cache), C.byref(params), int(accumulate)))
+
+
+def new_q4_workspace(cache: SlkvQ4Cache, params: SlkvQ4AttendParams, accumulate: bool = False) -> torch.Tensor:
+    n = slkv_q4_attend_workspace_bytes(cache, params, accumulate)
+    if n == 0:
+        raise SlkvError(ERR["BAD_SHAPE"], "slkv_q4_attend_workspace_bytes")
+    return torch.empty(n, dtype=torch.uint8, device=cache.device)
+
+
+def slkv_q4_attend(cache: SlkvQ4Cache, params: SlkvQ4AttendParams, q: torch.Tensor, out: torch.Tensor, workspace: torch.Tensor,
+                   q_pos: Optional[torch.Tensor] = None, slopes: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                   accumulate: bool = False, status: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """q, out: the shapes and strides params was made from.  q_pos int32 [n_seqs, n_tokens], slopes float32 [n_q_heads],
+    lse float32 [n_seqs, n_q_heads, n_tokens]; accumulate adds to the cache's weights."""
+    _q4_device(cache, q, out, workspace, q_pos, slopes, lse, status)
+    shape = (cache.n_seqs, params.n_tokens, params.n_q_heads, cache.head_dim)
+    assert q.shape == out.shape == shape and _DTYPES[q.dtype] == _DTYPES[out.dtype] == params.dtype
+    assert q.stride() == (params.q_stride_seq, params.q_stride_tok, params.q_stride_head, 1)
+    assert out.stride() == (params.o_stride_seq, params.o_stride_tok, params.o_stride_head, 1)
+    assert q_pos is None or (q_pos.dtype == torch.int32 and q_pos.is_contiguous() and q_pos.numel() == shape[0] * shape[1])
+    assert slopes is None or (slopes.dtype == torch.float32 and slopes.is_contiguous() and slopes.numel() == shape[2])
+    assert lse is None or (lse.dtype == torch.float32 and lse.is_contiguous() and lse.numel() == shape[0] * shape[1] * shape[2])
+    _check(_fn["slkv_q4_attend"](stream, cache, params, q, q_pos, slopes, out, lse, int(accumulate), status, workspace,
+                                 workspace.numel()), "slkv_q4_attend")
+    return out
+
+
+def slkv_q4_evict_workspace_bytes(cache: SlkvQ4Cache) -> int:
+    return int(lib().slkv_q4_evict_workspace_bytes(C.byref(cache)))
+
+
+def new_q4_evict_workspace(cache: SlkvQ4Cache, to: Optional[SlkvQ4Cache] = None) -> torch.Tensor:
+    """For evictions from `cache` (to whichever cache)."""
+    n = slkv_q4_evict_workspace_bytes(cache)
+    if n == 0:
+        raise SlkvError(ERR["BAD_SHAPE"], "slkv_q4_evict_workspace_bytes")
+    return torch.empty(n, dtype=torch.uint8, device=cache.device)
+
+
+def slkv_q4_evict(cache: SlkvQ4Cache, to: SlkvQ4Cache, budgets: torch.Tensor, window: int, newest: torch.Tensor,
+                  workspace: torch.Tensor, status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """budgets int32 [n_kv_heads], newest int32 [n_seqs]; to: `cache` itself, or another cache."""
+    _q4_device(cache, budgets, newest, workspace, status)
+    assert to.device == cache.device
+    assert budgets.dtype == newest.dtype == torch.int32 and budgets.is_contiguous() and newest.is_contiguous()
+    assert budgets.numel() == cache.n_kv_heads and newest.numel() == cache.n_seqs
+    _check(_fn["slkv_q4_evict"](stream, cache, to, budgets, int(window), newest, status, workspace, workspace.numel()),
+           "slkv_q4_evict")

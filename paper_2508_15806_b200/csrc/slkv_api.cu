@@ -559,6 +559,11 @@ unsigned long long next_launch_tag() {
   return n * 0x9E3779B97F4A7C15ull;
 }
 
+int report(cudaError_t e, int launches) {
+  g_last_launches = launches;
+  return e == cudaSuccess ? SLKV_OK : cuda_fail(e);
+}
+
 void expire_next_layer_wait(int on) { g_expire_next_layer_wait = on; }
 int take_expire_next_layer_wait(bool sums) {
   const int v = g_expire_next_layer_wait;
@@ -633,7 +638,8 @@ int slkv_profile_collect(float* total_ms, int32_t* launches, int32_t n_kernels) 
 const char* slkv_kernel_name(int kernel_id) {
   static const char* names[KID_COUNT] = {"k_setup", "k_score_lse", "k_score_vote", "k_pool", "k_select",
                                          "k_gather", "k_alloc", "k_score_fused", "k_score_list", "k_window_stats",
-                                         "k_merge_lse", "k_behavior", "k_cp", "k_layer", "k_score_bound"};
+                                         "k_merge_lse", "k_behavior", "k_cp", "k_layer", "k_score_bound",
+                                         "k_q4_rows", "k_q4_attend", "k_q4_join", "k_q4_evict"};
   return (kernel_id >= 0 && kernel_id < KID_COUNT) ? names[kernel_id] : "";
 }
 
@@ -646,7 +652,7 @@ int slkv_trace_set_buffer(void* dev_buf, size_t bytes) {
 
 int slkv_last_cuda_error(void) { return g_last_cuda_error; }
 int slkv_last_launch_count(void) { return g_last_launches; }
-int slkv_version(void) { return 300; }
+int slkv_version(void) { return 400; }
 
 int slkv_debug_list_way(int way) {
   set_list_way(way == 1 || way == 2 ? way : 0);

@@ -131,7 +131,7 @@ struct Problem {
 };
 
 // kernel ids for launch accounting / per-kernel timing
-enum KernelId { KID_SETUP = 0, KID_SCORE_LSE, KID_SCORE_VOTE, KID_POOL, KID_SELECT, KID_GATHER, KID_ALLOC, KID_SCORE_FUSED, KID_SCORE_LIST, KID_WINDOW_STATS, KID_MERGE_LSE, KID_BEHAVIOR, KID_CP, KID_LAYER, KID_SCORE_BOUND, KID_COUNT };
+enum KernelId { KID_SETUP = 0, KID_SCORE_LSE, KID_SCORE_VOTE, KID_POOL, KID_SELECT, KID_GATHER, KID_ALLOC, KID_SCORE_FUSED, KID_SCORE_LIST, KID_WINDOW_STATS, KID_MERGE_LSE, KID_BEHAVIOR, KID_CP, KID_LAYER, KID_SCORE_BOUND, KID_Q4_ROWS, KID_Q4_ATTEND, KID_Q4_JOIN, KID_Q4_EVICT, KID_COUNT };
 
 // Brackets one kernel launch: counts it and, when per-kernel timing is on for this thread, records a
 // CUDA event pair around it on the launch stream.
@@ -310,6 +310,35 @@ cudaError_t launch_layer_fma(const Problem& pb, int cs, const TailLayer* tail, f
                              int* launches);
 cudaError_t launch_layer_tc(const Problem& pb, int cs, const TailLayer* tail, float* pooled, int32_t* status, cudaStream_t st,
                             int* launches);
+// ---- the 4-bit cache (slkv_q4.cu, slkv_q4_attend.cu, slkv_q4_evict.cu) --------------------------------------------------
+constexpr int kMaxQ4Columns = 256;               // query heads of a KV head times tokens
+constexpr int kMaxQ4Ctas = 160 * 6;              // of an attention launch: what the workspace has room for
+struct Q4CacheView {                             // slkv_q4_cache for the kernels
+  unsigned char* records;
+  int32_t* pos;
+  float* weight;                                 // may be null
+  const int32_t* starts;
+  int32_t* lens;
+  long long capacity;
+  int n_seg;
+};
+cudaError_t launch_q4_pack(const Q4CacheView& c, int head_dim, bool f32, const void* k, const void* v, long long n_rows,
+                           const int32_t* offsets, const int32_t* kept_idx, int32_t* status, cudaStream_t st, int* launches);
+cudaError_t launch_q4_append(const Q4CacheView& c, int n_kv_heads, int head_dim, bool f32, const void* k, const void* v, int n_tokens,
+                             const int64_t (&stride)[6], const int32_t* pos, int32_t* lens_out, int32_t* status, cudaStream_t st,
+                             int* launches);
+cudaError_t launch_q4_unpack(const Q4CacheView& c, int head_dim, bool f32, const int32_t* slots, long long n, void* k_out,
+                             void* v_out, cudaStream_t st, int* launches);
+size_t q4_attend_workspace(int n_seg, int head_dim, int columns, long long capacity, bool accumulate);
+cudaError_t launch_q4_attend(const Q4CacheView& c, const slkv_q4_cache& cache, const slkv_q4_attend_params& p, const void* q,
+                             const int32_t* q_pos, const float* slopes, void* out, float* lse, bool accumulate, int32_t* status,
+                             void* workspace, cudaStream_t st, int* launches);
+size_t q4_evict_workspace(int n_seg, long long capacity);
+cudaError_t launch_q4_evict(const Q4CacheView& from, const Q4CacheView& to, int n_kv_heads, int head_dim, const int32_t* budgets, int window,
+                            const int32_t* newest, int32_t* status, void* workspace, cudaStream_t st, int* launches);
+// A call's status for the caller, its CUDA error and its launches kept for this thread.
+int report(cudaError_t e, int launches);
+
 // Timeline buffer of this thread (diagnostics), or null: kTraceSlots words per CTA.
 unsigned long long* tensor_trace_buffer(int n_cta);
 // Diagnostics: arm / consume the one-shot switches that make an inter-CTA wait of this thread's next launch run out: a wait for words

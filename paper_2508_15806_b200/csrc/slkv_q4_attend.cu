@@ -1,0 +1,730 @@
+// Attention of new tokens over the 4-bit cache: out = softmax(f(scale q.k)) v per query head, its log-sum-exp, and the rows'
+// accumulated weights.
+//
+// One pass over the records with a running maximum and sum (base 2, fp32).  Four bits become matrix operands in registers:
+//   scores  a K nibble c, shifted to the top of a bf16 mantissa under the exponent of one, is 1 + c / 16, exactly; the
+//           accumulator of a group's product starts at -sum of the group's queries, so that what comes out is sum q c / 16.
+//           The score is 16 * sum over groups of scale * that, plus sum over groups of zero * (sum of queries), which is one
+//           more product: the zeros as they lie in the record against the query sums split in three bf16 parts.
+//   output  a V nibble under the exponent of 128 is 128 + c; less 136 it is c - 8, exactly.  Probabilities times the group's
+//           scale, rounded to bf16, are the other operand.  zero + 8 scale goes with the unrounded probabilities, in fp32.
+// Keys are the products' long side (m16), the query heads of a KV head and its tokens the short one (n8): with four heads to a
+// KV head nothing wider would be used.  The scores' accumulators hold keys along the lanes, the second product wants
+// them along the other axis: one 8 x 8 transposition by the matrix unit's own instruction per 8 keys and group.
+// fp32 queries and probabilities go through the same products in three bf16 parts, which is exact (8 + 8 + 8 bits); sums over
+// 16 keys are then added in fp32 outside the matrix unit, whose own accumulation cuts off.
+//
+// Work: a (segment, block of columns) is a unit of 32-row tiles; the tiles of all units form one line, cut evenly over the
+// CTAs, whatever the lengths.  A unit that lies in one CTA is finished there; the others leave a maximum, a sum and an
+// unscaled output per piece, which a second launch joins.  In a CTA each warp takes every fourth tile with its own ring of
+// bulk copies, so that no warp waits for another before a piece ends.
+// The weights need the final log-sum-exps: the scores are kept in the workspace, the second launch turns them into
+// probabilities.
+// What bounds it: the arithmetic between DRAM and the products (unpacking, scales).
+#include <atomic>
+
+#include "slkv_q4_device.cuh"
+
+namespace slkv {
+namespace {
+
+constexpr int kAttendWarps = 4, kTileRows = 32, kCols = 8;
+constexpr int kFewestTiles = 4;         // a CTA's share, at least: a tile for each warp
+constexpr unsigned long long kQ4WaitNs = 1000ull * 1000ull * 1000ull;
+
+struct Q4AttendArgs {
+  Q4CacheView c;
+  const void* q;
+  void* out;
+  float* lse;                           // optional, [n_seqs][n_q_heads][n_tokens]
+  const int32_t* q_pos;                 // optional
+  const float* slopes;                  // optional
+  int32_t* status;
+  long long q_seq, q_tok, q_head, o_seq, o_tok, o_head;      // elements
+  int n_kv_heads, n_q_heads, n_tokens, G, R, n_cb, n_cta, accumulate;
+  float scale, softcap, decay, lse_unit;                     // lse_unit: of a base-2 logarithm
+  // workspace
+  int* head;                            // tiles per CTA, tiles
+  int* unit_tile;                       // [n_units] first tile of a unit
+  int4* walk;                           // [n_cta] where a CTA's share begins: segment, block of columns, tile in it
+  float2* ml;                           // [n_cta][2][8] maximum and sum of a piece's columns
+  float* part;                          // [n_cta][2][8][HD] their unscaled outputs
+  float* lse2;                          // [n_seg][R] of units that lie in one CTA, base 2
+  float* scores;                        // [capacity][R] base 2 (accumulate)
+};
+
+__device__ __forceinline__ uint32_t smem_at(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+// generic accesses to shared memory before it, bulk copies after it
+__device__ __forceinline__ void async_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+// Whether the copies of a barrier's phase are there, within a second.
+__device__ __forceinline__ bool copies_there(uint32_t bar, uint32_t parity) {
+  unsigned long long began = 0;
+  for (;;) {
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    if (ok) return true;
+    unsigned long long now;
+    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(now));
+    if (!began) began = now;
+    if (now - began > kQ4WaitNs) return false;
+  }
+}
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ void mma16816(float (&d)[4], unsigned a0, unsigned a1, unsigned a2, unsigned a3, unsigned b0, unsigned b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ unsigned transpose8(unsigned x) {
+  unsigned y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+__device__ __forceinline__ unsigned pack2(float lo, float hi) {
+  const __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const unsigned*>(&b);
+}
+__device__ __forceinline__ float lo_f(unsigned w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float hi_f(unsigned w) { return __uint_as_float(w & 0xffff0000u); }
+// nibbles I and I + 4 of a word as 1 + c / 16
+template <int I>
+__device__ __forceinline__ unsigned k_pair(unsigned w) {
+  const unsigned s = I == 0 ? w << 3 : w >> (I == 0 ? 0 : 4 * I - 3);
+  return (s & 0x00780078u) | 0x3f803f80u;
+}
+// nibbles I of both halves as c - 8
+template <int I>
+__device__ __forceinline__ unsigned v_pair(unsigned w) {
+  const unsigned x = ((w >> (4 * I)) & 0x000f000fu) | 0x43004300u;
+  const __nv_bfloat16 off = __ushort_as_bfloat16(0x4308);  // 136
+  const __nv_bfloat162 y = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&x), __nv_bfloat162(off, off));
+  return *reinterpret_cast<const unsigned*>(&y);
+}
+// Key of a product's row r: neighbours apart, so that the lanes of one shared-memory access meet all banks.
+__device__ __forceinline__ int key_of(int r) { return (r & 8) | ((0x57463120u >> (4 * (r & 7))) & 7); }      // 0 2 1 3 6 4 7 5
+__device__ __forceinline__ int tiles_of(int len) { return (len + kTileRows - 1) / kTileRows; }
+// N 32-bit words from shared memory
+template <int N>
+__device__ __forceinline__ void load_words(const unsigned char* p, unsigned (&w)[N]) {
+  if constexpr (N == 4) {
+    const uint4 u = *reinterpret_cast<const uint4*>(p);
+    w[0] = u.x; w[1] = u.y; w[2] = u.z; w[3] = u.w;
+  } else if constexpr (N == 2) {
+    const uint2 u = *reinterpret_cast<const uint2*>(p);
+    w[0] = u.x; w[1] = u.y;
+  } else {
+    w[0] = *reinterpret_cast<const unsigned*>(p);
+  }
+}
+
+template <int HD> constexpr int kQ4Stages = HD == 128 ? 2 : 4;
+template <int HD> constexpr int kQ4Smem = kAttendWarps * kQ4Stages<HD> * kTileRows * q4_record_bytes(HD);
+
+template <int HD, int PARTS, bool MASK>
+__global__ void __launch_bounds__(kAttendWarps * 32) k_q4_attend(const __grid_constant__ Q4AttendArgs a) {
+  constexpr int NG = HD / 32, RB = q4_record_bytes(HD), kStages = kQ4Stages<HD>, kStageBytes = kTileRows * RB;
+  extern __shared__ __align__(128) unsigned char smem[];
+  __shared__ __align__(8) unsigned long long bars[kAttendWarps][kStages];
+  __shared__ int found[kAttendWarps];
+  __shared__ float merge_m[kAttendWarps][kCols], merge_l[kAttendWarps][kCols];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
+  unsigned char* ring = smem + warp * (kStages * kStageBytes);
+  const uint32_t bar0 = smem_at(bars[warp]);
+  if (lane < kStages) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bar0 + 8 * lane) : "memory");
+  asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  pdl_launch_dependents();
+  pdl_wait();
+
+  // ---- the CTA's share of the line of tiles
+  const int n_seg = a.c.n_seg, per_thread = (n_seg + kAttendWarps * 32 - 1) / (kAttendWarps * 32);
+  const int first = min(tid * per_thread, n_seg), last = min(first + per_thread, n_seg);
+  int mine = 0;
+  for (int s = first; s < last; ++s) mine += tiles_of(q4_segment(a.c.starts, a.c.lens, s, a.c.capacity).len) * a.n_cb;
+  int sum = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int x = __shfl_up_sync(0xffffffffu, sum, o);
+    if (lane >= o) sum += x;
+  }
+  if (lane == 31) found[warp] = sum;
+  __syncthreads();
+  for (int w = 0; w < warp; ++w) sum += found[w];
+  int total = found[0];
+  for (int w = 1; w < kAttendWarps; ++w) total += found[w];
+  const int per = max((total + a.n_cta - 1) / a.n_cta, kFewestTiles);
+  const long long t0 = (long long)blockIdx.x * per;
+  if (blockIdx.x == 0 && tid == 0) { a.head[0] = per; a.head[1] = total; }
+  __syncthreads();
+  if (t0 >= total) return;
+  if (sum - mine <= t0 && t0 < sum) {                      // the one thread whose segments the share begins in
+    int u = sum - mine, s = first, n = 0;
+    for (; s < last; ++s) {
+      n = tiles_of(q4_segment(a.c.starts, a.c.lens, s, a.c.capacity).len);
+      if (t0 < u + n * a.n_cb) break;
+      u += n * a.n_cb;
+    }
+    found[0] = s; found[1] = ((int)t0 - u) / n; found[2] = ((int)t0 - u) % n;
+    a.walk[blockIdx.x] = make_int4(s, found[1], found[2], 0);
+  }
+  __syncthreads();
+  int seg = found[0], cb = found[1], from = found[2];
+  int left = (int)min((long long)per, total - t0);
+  int line = (int)t0;                                      // tile on the line
+  unsigned issued = 0, used = 0, lost = 0;                 // copies of this warp's ring
+  bool dead = false;
+
+  while (left > 0 && seg < n_seg) {
+    const Q4Segment sg = q4_segment(a.c.starts, a.c.lens, seg, a.c.capacity);
+    const int tiles = tiles_of(sg.len);
+    if (tiles == 0) { ++seg; cb = 0; from = 0; continue; }
+    const int to = min(tiles, from + left);
+    const unsigned char* rows = a.c.records + (long long)sg.begin * RB;
+    if (from == 0 && tid == 0) a.unit_tile[seg * a.n_cb + cb] = line;
+
+    // the ring's first copies
+    auto issue = [&](int tile) {
+      const int n = min(kTileRows, sg.len - tile * kTileRows), slot = issued % kStages;
+      if (lane == 0) {
+        const uint32_t bar = bar0 + 8 * slot;
+        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(n * RB) : "memory");
+        asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
+                         smem_at(ring + slot * kStageBytes)),
+                     "l"(rows + (long long)tile * kStageBytes), "r"(n * RB), "r"(bar) : "memory");
+      }
+      ++issued;
+    };
+    int next = from + warp;
+    if (!dead)
+      for (int i = 0; i < kStages && next < to; ++i, next += kAttendWarps) issue(next);
+
+    // ---- the unit's queries: fragments, and sums per group
+    const int s = seg / a.n_kv_heads, h = seg - s * a.n_kv_heads;
+    unsigned bq[PARTS][NG][2][2], bz[2] = {0u, 0u};
+    float init[NG][2];
+    {
+      const int col = cb * kCols + g;
+      const bool there = col < a.R;
+      const int tok = there ? col / a.G : 0, qh = h * a.G + (there ? col - tok * a.G : 0);
+      const long long at = s * a.q_seq + tok * a.q_tok + qh * a.q_head + 8 * t;
+      float qs[NG];
+#pragma unroll
+      for (int j = 0; j < NG; ++j) {
+        float x[8];
+        if constexpr (PARTS == 1) {
+          uint4 w = make_uint4(0, 0, 0, 0);
+          if (there) w = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.q) + at + 32 * j);
+          bq[0][j][0][0] = __byte_perm(w.x, w.z, 0x5410); bq[0][j][0][1] = __byte_perm(w.x, w.z, 0x7632);
+          bq[0][j][1][0] = __byte_perm(w.y, w.w, 0x5410); bq[0][j][1][1] = __byte_perm(w.y, w.w, 0x7632);
+          x[0] = lo_f(w.x); x[1] = hi_f(w.x); x[2] = lo_f(w.y); x[3] = hi_f(w.y);
+          x[4] = lo_f(w.z); x[5] = hi_f(w.z); x[6] = lo_f(w.w); x[7] = hi_f(w.w);
+        } else {
+          float4 u = make_float4(0, 0, 0, 0), v = u;
+          if (there) {
+            const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(a.q) + at + 32 * j);
+            u = p[0]; v = p[1];
+          }
+          x[0] = u.x; x[1] = u.y; x[2] = u.z; x[3] = u.w; x[4] = v.x; x[5] = v.y; x[6] = v.z; x[7] = v.w;
+          float r[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) r[e] = x[e];
+#pragma unroll
+          for (int p = 0; p < PARTS; ++p)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const unsigned w = pack2(r[e], r[e + 4]);
+              bq[p][j][e >> 1][e & 1] = w;
+              r[e] -= lo_f(w);
+              r[e + 4] -= hi_f(w);
+            }
+        }
+        qs[j] = ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+        qs[j] += __shfl_xor_sync(0xffffffffu, qs[j], 1);
+        qs[j] += __shfl_xor_sync(0xffffffffu, qs[j], 2);
+        init[j][0] = -__shfl_sync(0xffffffffu, qs[j], 8 * t);              // of columns 2 t and 2 t + 1
+        init[j][1] = -__shfl_sync(0xffffffffu, qs[j], 8 * t + 4);
+      }
+      // the query sums / 16 in three parts: lane t holds part t of all groups, where the zeros' fragments expect them
+#pragma unroll
+      for (int jj = 0; jj < NG / 2; ++jj) {
+        float x = qs[2 * jj] * 0.0625f, y = qs[2 * jj + 1] * 0.0625f;
+        unsigned w = 0;
+#pragma unroll
+        for (int p = 0; p < 3; ++p) {
+          const unsigned v = pack2(x, y);
+          if (p == t) w = v;
+          x -= lo_f(v);
+          y -= hi_f(v);
+        }
+        bz[jj] = w;                                        // lane t = 3: zeros
+      }
+    }
+    const float to_log2 = a.scale * (16.0f * kLog2e), cap_in = a.softcap > 0.0f ? 16.0f * a.scale / a.softcap : 0.0f;
+    int qp[2] = {0, 0};
+    float slope[2] = {0.0f, 0.0f};
+    if (MASK) {
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const int col = cb * kCols + 2 * t + c, tok = col < a.R ? col / a.G : 0;
+        qp[c] = a.q_pos[s * a.n_tokens + tok];
+        if (a.slopes) slope[c] = a.slopes[h * a.G + (col < a.R ? col - tok * a.G : 0)] * kLog2e;
+      }
+    }
+
+    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f};
+    float o[NG][2][4], zacc[NG][2];
+#pragma unroll
+    for (int j = 0; j < NG; ++j) {
+      zacc[j][0] = zacc[j][1] = 0.0f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) o[j][i >> 2][i & 3] = 0.0f;
+    }
+    const int* pos_rows = a.c.pos + sg.begin;
+    int pos_next = 0;
+    if (MASK && from + warp < to) pos_next = pos_rows[min((from + warp) * kTileRows + lane, sg.len - 1)];
+
+    for (int tile = from + warp; tile < to; tile += kAttendWarps) {
+      const int n = min(kTileRows, sg.len - tile * kTileRows), slot = used % kStages;
+      const int pos_here = pos_next;
+      if (MASK && tile + kAttendWarps < to) pos_next = pos_rows[min((tile + kAttendWarps) * kTileRows + lane, sg.len - 1)];
+      unsigned char* buf = ring + slot * kStageBytes;
+      if (!dead) {                                         // a copy that does not come in a second is not waited for again
+        dead = __any_sync(0xffffffffu, !copies_there(bar0 + 8 * slot, (used / kStages) & 1));
+        if (dead) {
+          lost = used;
+          if (lane == 0 && a.status) *a.status = SLKV_ERR_DEVICE_TIMEOUT;
+        }
+      }
+      ++used;
+      if (n < kTileRows) {                                 // what lies behind the last row must be finite: scales and zeros
+        if (lane >= n) {
+#pragma unroll
+          for (int i = 0; i < RB - HD; i += 16) *reinterpret_cast<uint4*>(buf + lane * RB + HD + i) = make_uint4(0, 0, 0, 0);
+          async_fence();
+        }
+        __syncwarp();
+      }
+      float sc[2][4];
+      // ---- scores: rows key_of(g) and key_of(g + 8) of each half, columns 2 t and 2 t + 1
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const int r0 = half * 16 + key_of(g), r1 = r0 + 8;
+        const unsigned char *p0 = buf + r0 * RB, *p1 = buf + r1 * RB;
+        unsigned w0[NG], w1[NG], x0[NG], x1[NG];           // codes; scales and zeros
+        load_words(p0 + 4 * NG * t, w0);
+        load_words(p1 + 4 * NG * t, w1);
+        load_words(p0 + HD, x0);
+        load_words(p1 + HD, x1);
+        float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        mma16816(acc, x0[NG / 2], x1[NG / 2], NG == 4 ? x0[NG - 1] : 0u, NG == 4 ? x1[NG - 1] : 0u, bz[0], bz[1]);
+#pragma unroll
+        for (int j = 0; j < NG; ++j) {
+          float d[4] = {init[j][0], init[j][1], init[j][0], init[j][1]};
+          const unsigned a00 = k_pair<0>(w0[j]), a01 = k_pair<1>(w0[j]), a02 = k_pair<2>(w0[j]), a03 = k_pair<3>(w0[j]);
+          const unsigned a10 = k_pair<0>(w1[j]), a11 = k_pair<1>(w1[j]), a12 = k_pair<2>(w1[j]), a13 = k_pair<3>(w1[j]);
+#pragma unroll
+          for (int p = 0; p < PARTS; ++p) {
+            mma16816(d, a00, a10, a01, a11, bq[p][j][0][0], bq[p][j][0][1]);
+            mma16816(d, a02, a12, a03, a13, bq[p][j][1][0], bq[p][j][1][1]);
+          }
+          const float s0 = j & 1 ? hi_f(x0[j >> 1]) : lo_f(x0[j >> 1]), s1 = j & 1 ? hi_f(x1[j >> 1]) : lo_f(x1[j >> 1]);
+          acc[0] = fmaf(s0, d[0], acc[0]); acc[1] = fmaf(s0, d[1], acc[1]);
+          acc[2] = fmaf(s1, d[2], acc[2]); acc[3] = fmaf(s1, d[3], acc[3]);
+        }
+        int pos0 = 0, pos1 = 0;
+        if (MASK) {
+          pos0 = __shfl_sync(0xffffffffu, pos_here, r0);
+          pos1 = __shfl_sync(0xffffffffu, pos_here, r1);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float x = a.softcap > 0.0f ? a.softcap * kLog2e * tanhf(acc[i] * cap_in) : acc[i] * to_log2;
+          bool visible = (i < 2 ? r0 : r1) < n;
+          if (MASK) {
+            const int pos = i < 2 ? pos0 : pos1;
+            x = fmaf(slope[i & 1], (float)(pos - qp[i & 1]), x);
+            visible = visible && pos <= qp[i & 1];
+          }
+          sc[half][i] = visible ? x : -INFINITY;
+        }
+        if (a.accumulate) {
+          const int col = cb * kCols + 2 * t;
+          float* to_row = a.scores + ((long long)sg.begin + tile * kTileRows) * a.R + col;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int r = i < 2 ? r0 : r1;
+            if (r < n && col + (i & 1) < a.R) to_row[r * a.R + (i & 1)] = sc[half][i];
+          }
+        }
+      }
+      // ---- running maximum and sum
+      float p[2][4], up[2];
+      bool grew = false;
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        float x = fmaxf(fmaxf(sc[0][c], sc[0][c + 2]), fmaxf(sc[1][c], sc[1][c + 2]));
+        x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
+        x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
+        x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
+        up[c] = 1.0f;
+        if (x > m[c]) {
+          up[c] = ex2(m[c] - x);
+          m[c] = x;
+          grew = true;
+        }
+      }
+      if (__any_sync(0xffffffffu, grew)) {
+#pragma unroll
+        for (int j = 0; j < NG; ++j) {
+          zacc[j][0] *= up[0]; zacc[j][1] *= up[1];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) o[j][i >> 2][i & 3] *= up[i & 1];
+        }
+        l[0] *= up[0]; l[1] *= up[1];
+      }
+      const float base[2] = {m[0] == -INFINITY ? 0.0f : m[0], m[1] == -INFINITY ? 0.0f : m[1]};
+#pragma unroll
+      for (int half = 0; half < 2; ++half)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          p[half][i] = ex2(sc[half][i] - base[i & 1]);
+          l[i & 1] += p[half][i];
+        }
+      // ---- output
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const int r0 = half * 16 + key_of(g), r1 = r0 + 8;
+        unsigned x0[NG], x1[NG];
+        load_words(buf + r0 * RB + HD + 4 * NG, x0);
+        load_words(buf + r1 * RB + HD + 4 * NG, x1);
+        const int k0 = half * 16 + key_of(2 * t), k1 = half * 16 + key_of(2 * t + 1);
+        unsigned va[4][NG / 2];                            // keys 2 t, 2 t + 1, 2 t + 8, 2 t + 9
+#pragma unroll
+        for (int i = 0; i < 4; ++i) load_words(buf + ((i & 1 ? k1 : k0) + (i & 2 ? 8 : 0)) * RB + HD / 2 + g * (HD / 16), va[i]);
+        bool seen[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) seen[i] = !MASK || sc[half][i] != -INFINITY;
+#pragma unroll
+        for (int j = 0; j < NG; ++j) {
+          const float s0 = j & 1 ? hi_f(x0[j >> 1]) : lo_f(x0[j >> 1]), s1 = j & 1 ? hi_f(x1[j >> 1]) : lo_f(x1[j >> 1]);
+          const unsigned zw0 = x0[(NG + j) >> 1], zw1 = x1[(NG + j) >> 1];
+          const float z0 = fmaf(8.0f, s0, j & 1 ? hi_f(zw0) : lo_f(zw0)), z1 = fmaf(8.0f, s1, j & 1 ? hi_f(zw1) : lo_f(zw1));
+          float y[4];
+          // a row that a column does not see gives it nothing, whatever its scales hold
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float zz = seen[i] ? (i < 2 ? z0 : z1) : 0.0f;
+            zacc[j][i & 1] = fmaf(p[half][i], zz, zacc[j][i & 1]);
+            y[i] = seen[i] ? p[half][i] * (i < 2 ? s0 : s1) : 0.0f;
+          }
+          const unsigned t01 = __byte_perm(va[0][j >> 1], va[1][j >> 1], j & 1 ? 0x7632 : 0x5410);
+          const unsigned t89 = __byte_perm(va[2][j >> 1], va[3][j >> 1], j & 1 ? 0x7632 : 0x5410);
+          const unsigned f0[4] = {v_pair<0>(t01), v_pair<1>(t01), v_pair<0>(t89), v_pair<1>(t89)};
+          const unsigned f1[4] = {v_pair<2>(t01), v_pair<3>(t01), v_pair<2>(t89), v_pair<3>(t89)};
+          if constexpr (PARTS == 1) {
+            const unsigned b0 = transpose8(pack2(y[0], y[1])), b1 = transpose8(pack2(y[2], y[3]));
+            mma16816(o[j][0], f0[0], f0[1], f0[2], f0[3], b0, b1);
+            mma16816(o[j][1], f1[0], f1[1], f1[2], f1[3], b0, b1);
+          } else {
+            float d0[4] = {0.0f, 0.0f, 0.0f, 0.0f}, d1[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int part = 0; part < PARTS; ++part) {
+              const unsigned w0 = pack2(y[0], y[1]), w1 = pack2(y[2], y[3]);
+              y[0] -= lo_f(w0); y[1] -= hi_f(w0); y[2] -= lo_f(w1); y[3] -= hi_f(w1);
+              const unsigned b0 = transpose8(w0), b1 = transpose8(w1);
+              mma16816(d0, f0[0], f0[1], f0[2], f0[3], b0, b1);
+              mma16816(d1, f1[0], f1[1], f1[2], f1[3], b0, b1);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { o[j][0][i] += d0[i]; o[j][1][i] += d1[i]; }
+          }
+        }
+      }
+      __syncwarp();
+      if (next < to) {
+        if (!dead) issue(next);
+        next += kAttendWarps;
+      }
+    }
+    // ---- the piece's end: the warps' shares together.  A warp's ring is empty now and takes its output.
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+#pragma unroll
+      for (int d = 4; d < 32; d <<= 1) {
+        l[c] += __shfl_xor_sync(0xffffffffu, l[c], d);
+#pragma unroll
+        for (int j = 0; j < NG; ++j) zacc[j][c] += __shfl_xor_sync(0xffffffffu, zacc[j][c], d);
+      }
+      if (g == 0) {
+        merge_m[warp][2 * t + c] = m[c];
+        merge_l[warp][2 * t + c] = l[c];
+      }
+    }
+    float* mine_o = reinterpret_cast<float*>(ring);        // [column][HD + 4]
+    constexpr int kPitch = HD + 4;
+#pragma unroll
+    for (int j = 0; j < NG; ++j)
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+        *reinterpret_cast<float4*>(mine_o + (2 * t + c) * kPitch + 32 * j + 4 * g) =
+            make_float4(o[j][0][c] + zacc[j][c], o[j][0][c + 2] + zacc[j][c], o[j][1][c] + zacc[j][c], o[j][1][c + 2] + zacc[j][c]);
+    async_fence();
+    __syncthreads();
+    const bool whole = from == 0 && to == tiles;
+    const int part = from == 0 ? 1 : 0;                    // a CTA's share ends in at most one unit that begins in it
+    for (int i = tid; i < kCols * HD / 4; i += kAttendWarps * 32) {
+      const int c = i / (HD / 4), ch = 4 * (i % (HD / 4)), col = cb * kCols + c;
+      if (col >= a.R) continue;
+      float top = merge_m[0][c];
+#pragma unroll
+      for (int w = 1; w < kAttendWarps; ++w) top = fmaxf(top, merge_m[w][c]);
+      const float base = top == -INFINITY ? 0.0f : top;
+      float sum_l = 0.0f;
+      float4 v = make_float4(0, 0, 0, 0);
+#pragma unroll
+      for (int w = 0; w < kAttendWarps; ++w) {
+        const float f = ex2(merge_m[w][c] - base);         // 0 for a warp without rows
+        const float4 x = *reinterpret_cast<const float4*>(smem + w * (kStages * kStageBytes) + (c * kPitch + ch) * 4);
+        sum_l = fmaf(merge_l[w][c], f, sum_l);
+        v.x = fmaf(x.x, f, v.x); v.y = fmaf(x.y, f, v.y); v.z = fmaf(x.z, f, v.z); v.w = fmaf(x.w, f, v.w);
+      }
+      if (whole) {
+        const int tok = col / a.G, qh = h * a.G + col - tok * a.G;
+        const float inv = sum_l == 0.0f ? 0.0f : 1.0f / sum_l;             // no visible row: zeros
+        const long long at = s * a.o_seq + tok * a.o_tok + qh * a.o_head + ch;
+        if constexpr (PARTS == 1) {
+          *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.out) + at) = make_uint2(pack2(v.x * inv, v.y * inv), pack2(v.z * inv, v.w * inv));
+        } else {
+          *reinterpret_cast<float4*>(static_cast<float*>(a.out) + at) = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
+        }
+        if (ch == 0) {
+          const float z = top + log2f(sum_l);
+          if (a.lse) a.lse[((long long)s * a.n_q_heads + qh) * a.n_tokens + tok] = z * a.lse_unit;
+          a.lse2[(long long)seg * a.R + col] = z;
+        }
+      } else {
+        const long long at = ((long long)blockIdx.x * 2 + part) * kCols + c;
+        if (ch == 0) a.ml[at] = make_float2(top, sum_l);
+        *reinterpret_cast<float4*>(a.part + at * HD + ch) = v;
+      }
+    }
+    __syncthreads();                                       // the rings and the sums are free again
+    line += to - from;
+    left -= to - from;
+    from = 0;
+    if (++cb == a.n_cb) { cb = 0; ++seg; }
+  }
+  if (dead)                                                // what is still in flight lands before the memory is another CTA's
+    for (unsigned i = lost; i < issued; ++i) copies_there(bar0 + 8 * (i % kStages), (i / kStages) & 1);
+}
+
+// ---- the pieces of units that lie in several CTAs, and the weights ---------------------------------------------------
+constexpr int kJoinThreads = 128;
+
+// Pieces of a unit: CTAs first .. last of the launch before; one CTA has finished it by itself.
+struct Q4Pieces { int first, last; };
+__device__ __forceinline__ Q4Pieces pieces_of(const Q4AttendArgs& a, int unit, int tiles) {
+  const int per = a.head[0], at = a.unit_tile[unit];
+  return {at / per, (at + tiles - 1) / per};
+}
+__device__ __forceinline__ long long piece_at(const Q4Pieces& p, int i, int c) {
+  return ((long long)i * 2 + (i == p.first ? 1 : 0)) * kCols + c;
+}
+// Maximum and sum over a unit's pieces for one column; whole warp.
+__device__ __forceinline__ float2 join_ml(const Q4AttendArgs& a, const Q4Pieces& p, int c, int lane) {
+  float m = -INFINITY, l = 0.0f;
+  for (int i = p.first + lane; i <= p.last; i += 32) {
+    const float2 x = a.ml[piece_at(p, i, c)];
+    const float top = fmaxf(m, x.x), base = top == -INFINITY ? 0.0f : top;
+    l = l * ex2(m - base) + x.y * ex2(x.x - base);
+    m = top;
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    const float om = __shfl_xor_sync(0xffffffffu, m, o), ol = __shfl_xor_sync(0xffffffffu, l, o);
+    const float top = fmaxf(m, om), base = top == -INFINITY ? 0.0f : top;
+    l = l * ex2(m - base) + ol * ex2(om - base);
+    m = top;
+  }
+  return make_float2(m, l);
+}
+
+template <int HD, bool F32>
+__global__ void __launch_bounds__(kJoinThreads) k_q4_join(const __grid_constant__ Q4AttendArgs a) {
+  constexpr int kWarps = kJoinThreads / 32, V = HD / 32;   // channels per lane
+  __shared__ float shares[kWarps][HD], lse_of[kMaxQ4Columns];
+  pdl_launch_dependents();
+  pdl_wait();
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int n_out = a.c.n_seg * a.R;
+  if ((int)blockIdx.x < n_out) {                           // one segment's column
+    const int seg = blockIdx.x / a.R, col = blockIdx.x - seg * a.R, cb = col / kCols, c = col - cb * kCols;
+    const int s = seg / a.n_kv_heads, h = seg - s * a.n_kv_heads, tok = col / a.G, qh = h * a.G + col - tok * a.G;
+    const int tiles = tiles_of(q4_segment(a.c.starts, a.c.lens, seg, a.c.capacity).len);
+    Q4Pieces p = {0, 0};
+    if (tiles > 0) {
+      p = pieces_of(a, seg * a.n_cb + cb, tiles);
+      if (p.first == p.last) return;
+    }
+    float2 ml = make_float2(-INFINITY, 0.0f);
+    float acc[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) acc[e] = 0.0f;
+    if (tiles > 0) {
+      ml = join_ml(a, p, c, lane);
+      const float base = ml.x == -INFINITY ? 0.0f : ml.x;
+#pragma unroll 4
+      for (int i = p.first + warp; i <= p.last; i += kWarps) {
+        const long long at = piece_at(p, i, c);
+        const float f = ex2(a.ml[at].x - base);
+#pragma unroll
+        for (int e = 0; e < V; ++e) acc[e] = fmaf(a.part[at * HD + lane + 32 * e], f, acc[e]);
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < V; ++e) shares[warp][lane + 32 * e] = acc[e];
+    __syncthreads();
+    if (tid < HD) {
+      float v = 0.0f;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) v += shares[w][tid];
+      v *= ml.y == 0.0f ? 0.0f : 1.0f / ml.y;
+      const long long at = s * a.o_seq + tok * a.o_tok + qh * a.o_head + tid;
+      if (F32) static_cast<float*>(a.out)[at] = v;
+      else static_cast<__nv_bfloat16*>(a.out)[at] = __float2bfloat16_rn(v);
+    }
+    if (tid == 0 && a.lse) a.lse[((long long)s * a.n_q_heads + qh) * a.n_tokens + tok] = (ml.x + log2f(ml.y)) * a.lse_unit;
+    return;
+  }
+  // the weights of the rows of one CTA's share: a row has its scores of all columns, so the first block of columns does it
+  const int cta = blockIdx.x - n_out, per = a.head[0];
+  if ((long long)cta * per >= a.head[1]) return;
+  const int4 w = a.walk[cta];
+  int seg = w.x, cb = w.y, from = w.z, left = min(per, a.head[1] - cta * per);
+  const float inv_g = 1.0f / (float)a.G;
+  while (left > 0 && seg < a.c.n_seg) {
+    const Q4Segment sg = q4_segment(a.c.starts, a.c.lens, seg, a.c.capacity);
+    const int tiles = tiles_of(sg.len);
+    if (tiles == 0) { ++seg; cb = 0; from = 0; continue; }
+    const int to = min(tiles, from + left);
+    if (cb == 0) {
+      __syncthreads();
+      for (int col = warp; col < a.R; col += kWarps) {
+        const Q4Pieces p = pieces_of(a, seg * a.n_cb + col / kCols, tiles);
+        float z;
+        if (p.first == p.last) {
+          z = a.lse2[(long long)seg * a.R + col];
+        } else {
+          const float2 ml = join_ml(a, p, col % kCols, lane);
+          z = ml.x + log2f(ml.y);
+        }
+        if (lane == 0) lse_of[col] = z == -INFINITY ? INFINITY : z;        // a column that sees nothing gives nothing
+      }
+      __syncthreads();
+      const int end = min(to * kTileRows, sg.len);
+      for (int r = from * kTileRows + tid; r < end; r += kJoinThreads) {
+        const long long slot = (long long)sg.begin + r;
+        const float* x = a.scores + slot * a.R;
+        float sum = 0.0f;
+        if ((a.R & 3) == 0) {
+          for (int c = 0; c < a.R; c += 4) {
+            const float4 v = *reinterpret_cast<const float4*>(x + c);
+            sum += (ex2(v.x - lse_of[c]) + ex2(v.y - lse_of[c + 1])) + (ex2(v.z - lse_of[c + 2]) + ex2(v.w - lse_of[c + 3]));
+          }
+        } else {
+          for (int c = 0; c < a.R; ++c) sum += ex2(x[c] - lse_of[c]);
+        }
+        a.c.weight[slot] = fmaf(a.decay, a.c.weight[slot], sum * inv_g);
+      }
+    }
+    left -= to - from;
+    from = 0;
+    if (++cb == a.n_cb) { cb = 0; ++seg; }
+  }
+}
+
+constexpr size_t kAlign = 256;
+size_t up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
+
+struct Q4Workspace {
+  size_t unit_tile, walk, ml, part, lse2, scores, total;
+  Q4Workspace(int n_seg, int head_dim, int R, long long capacity, bool accumulate) {
+    const size_t n_cb = (size_t)(R + kCols - 1) / kCols, ctas = kMaxQ4Ctas;
+    unit_tile = kAlign;
+    walk = unit_tile + up(n_seg * n_cb * sizeof(int));
+    ml = walk + up(ctas * sizeof(int4));
+    part = ml + up(ctas * 2 * kCols * sizeof(float2));
+    lse2 = part + up(ctas * 2 * kCols * head_dim * sizeof(float));
+    scores = lse2 + up((size_t)n_seg * R * sizeof(float));
+    total = scores + (accumulate ? up((size_t)capacity * R * sizeof(float)) : 0);
+  }
+};
+
+template <int HD, int PARTS, bool MASK>
+cudaError_t launch_attend(Q4AttendArgs& a, cudaStream_t st, int* launches) {
+  auto kernel = k_q4_attend<HD, PARTS, MASK>;
+  static std::atomic<int> per_sm[16];                      // of each device; found once
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  int n = dev < 16 ? per_sm[dev].load(std::memory_order_relaxed) : 0;
+  if (n == 0) {
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kQ4Smem<HD>);
+    if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, kAttendWarps * 32, kQ4Smem<HD>);
+    if (e != cudaSuccess) return e;
+    if (n < 1) return cudaErrorLaunchOutOfResources;
+    if (dev < 16) per_sm[dev].store(n, std::memory_order_relaxed);
+  }
+  const int most = sm_count() * n;
+  a.n_cta = most < kMaxQ4Ctas ? most : kMaxQ4Ctas;
+  {
+    LaunchScope scope(KID_Q4_ATTEND, st, launches);
+    e = launch_pdl(kernel, dim3((unsigned)a.n_cta), dim3(kAttendWarps * 32), kQ4Smem<HD>, st, 1, a);
+  }
+  if (e != cudaSuccess) return e;
+  LaunchScope scope(KID_Q4_JOIN, st, launches);
+  const unsigned grid = (unsigned)(a.c.n_seg * a.R + (a.accumulate ? a.n_cta : 0));
+  return launch_pdl(k_q4_join<HD, (PARTS > 1)>, dim3(grid), dim3(kJoinThreads), 0, st, 1, a);
+}
+
+template <int HD>
+cudaError_t launch_attend_of(Q4AttendArgs& a, bool f32, cudaStream_t st, int* launches) {
+  if (f32) return a.q_pos ? launch_attend<HD, 3, true>(a, st, launches) : launch_attend<HD, 3, false>(a, st, launches);
+  return a.q_pos ? launch_attend<HD, 1, true>(a, st, launches) : launch_attend<HD, 1, false>(a, st, launches);
+}
+
+}  // namespace
+
+size_t q4_attend_workspace(int n_seg, int head_dim, int columns, long long capacity, bool accumulate) {
+  return Q4Workspace(n_seg, head_dim, columns, capacity, accumulate).total;
+}
+
+cudaError_t launch_q4_attend(const Q4CacheView& c, const slkv_q4_cache& cache, const slkv_q4_attend_params& p, const void* q,
+                             const int32_t* q_pos, const float* slopes, void* out, float* lse, bool accumulate, int32_t* status,
+                             void* workspace, cudaStream_t st, int* launches) {
+  Q4AttendArgs a = {};
+  a.c = c; a.q = q; a.out = out; a.lse = lse; a.q_pos = q_pos; a.slopes = slopes; a.status = status;
+  a.q_seq = p.q_stride_seq; a.q_tok = p.q_stride_tok; a.q_head = p.q_stride_head;
+  a.o_seq = p.o_stride_seq; a.o_tok = p.o_stride_tok; a.o_head = p.o_stride_head;
+  a.n_kv_heads = cache.n_kv_heads; a.n_q_heads = p.n_q_heads; a.n_tokens = p.n_tokens;
+  a.G = p.n_q_heads / cache.n_kv_heads; a.R = a.G * p.n_tokens; a.n_cb = (a.R + kCols - 1) / kCols;
+  a.accumulate = accumulate;
+  a.scale = p.scale; a.softcap = p.softcap; a.decay = p.weight_decay;
+  a.lse_unit = p.lse_units == SLKV_LSE_LOG2 ? 1.0f : 0.69314718055994531f;
+  const Q4Workspace w(c.n_seg, cache.head_dim, a.R, c.capacity, accumulate);
+  char* ws = static_cast<char*>(workspace);
+  a.head = reinterpret_cast<int*>(ws);
+  a.unit_tile = reinterpret_cast<int*>(ws + w.unit_tile);
+  a.walk = reinterpret_cast<int4*>(ws + w.walk);
+  a.ml = reinterpret_cast<float2*>(ws + w.ml);
+  a.part = reinterpret_cast<float*>(ws + w.part);
+  a.lse2 = reinterpret_cast<float*>(ws + w.lse2);
+  a.scores = accumulate ? reinterpret_cast<float*>(ws + w.scores) : nullptr;
+  return cache.head_dim == 128 ? launch_attend_of<128>(a, p.dtype == SLKV_F32, st, launches)
+                               : launch_attend_of<64>(a, p.dtype == SLKV_F32, st, launches);
+}
+
+}  // namespace slkv

@@ -1,0 +1,492 @@
+"""The 4-bit cache on the GPU against its definition in 64 bits: packing, appending, unpacking, attention, eviction, and a run of them."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import q4_reference as R
+from paper_2508_15806_b200 import binding as B
+
+pytestmark = pytest.mark.gpu
+DEV = torch.device("cuda:0") if torch.cuda.is_available() else torch.device("cpu")
+
+
+def cache_of(c, n_kv_heads, **kw):
+    c = {**c, **kw}
+    return B.make_q4_cache(c["records"], c["pos"], c["weight"], c["starts"], c["lens"], n_kv_heads)
+
+
+def empty_cache(rooms, d, n_kv_heads, fill=0xAB):
+    starts = [0]
+    for r in rooms:
+        starts.append(starts[-1] + r)
+    n = max(starts[-1], 1)
+    t = dict(records=torch.full((n, d + d // 4), fill, dtype=torch.uint8, device=DEV), pos=torch.full((n,), -7, dtype=torch.int32, device=DEV),
+             weight=torch.full((n,), 5.0, device=DEV), starts=torch.tensor(starts, dtype=torch.int32, device=DEV),
+             lens=torch.full((len(rooms),), 12345, dtype=torch.int32, device=DEV))
+    return t, cache_of(t, n_kv_heads)
+
+
+def expected_record(k, v):
+    """Bytes of the records of rows k, v (float64 arrays [n, d])."""
+    n, d = k.shape
+    ng = d // 32
+    out = np.zeros((n, d + d // 4), np.uint8)
+    for r in range(n):
+        parts = []
+        for x, lanes, per in ((k[r], 4, 8), (v[r], 8, 4)):
+            code, scale, zero = R.quantise_row(x)
+            c = code.reshape(ng, lanes, per).transpose(1, 0, 2).reshape(-1)
+            parts.append(((c[0::2] | (c[1::2] << 4)).astype(np.uint8), scale, zero))
+        s = np.concatenate([parts[0][1], parts[0][2], parts[1][1], parts[1][2]]).astype(np.float32)
+        bits = (s.view(np.uint32) >> 16).astype(np.uint16)
+        bits[np.isnan(s)] = 0x7FFF
+        out[r] = np.concatenate([parts[0][0], parts[1][0], bits.view(np.uint8)])
+    return out
+
+
+def rows(seed, n, d, dtype):
+    g = torch.Generator().manual_seed(seed)
+    k, v = torch.randn(n, d, generator=g) * 1.5 + torch.randn(d, generator=g), torch.randn(n, d, generator=g)
+    return k.to(dtype), v.to(dtype)
+
+
+# ---- rows in and out -------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("lens,hkv,slack", [([1], 1, 0), ([0, 5, 0, 33, 1, 0], 2, 3), ([7, 130, 64], 3, 0), ([0, 0], 1, 2)])
+def test_pack_writes_the_defined_records(d, dtype, lens, hkv, slack):
+    n = sum(lens)
+    k, v = rows(n + d, max(n, 1), d, dtype)
+    offsets = torch.tensor([0] + list(np.cumsum(lens)), dtype=torch.int32, device=DEV)
+    kept = torch.arange(max(n, 1), dtype=torch.int32, device=DEV) * 3 + 1
+    t, c = empty_cache([x + slack for x in lens], d, hkv)
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    B.slkv_q4_pack(c, k.to(DEV), v.to(DEV), offsets, kept, status)
+    assert status.item() == 0 and t["lens"].tolist() == lens
+    want = expected_record(k.double().numpy(), v.double().numpy())
+    slots = [int(t["starts"][s]) + i for s, m in enumerate(lens) for i in range(m)]
+    got = t["records"].cpu().numpy()
+    assert np.array_equal(got[slots], want[:n])
+    assert np.array_equal(t["pos"].cpu().numpy()[slots], kept.cpu().numpy()[:n]) and np.all(t["weight"].cpu().numpy()[slots] == 0)
+    rest = np.setdiff1d(np.arange(got.shape[0]), slots)              # slots behind the rows stay as they were
+    assert np.all(got[rest] == 0xAB) and np.all(t["pos"].cpu().numpy()[rest] == -7) and np.all(t["weight"].cpu().numpy()[rest] == 5.0)
+
+    # and back: every filled slot, then some slots with padding between them
+    K, V, _ = R.decode(t["records"][slots], d)
+    for out_dtype in (torch.float32, torch.bfloat16):
+        ko, vo = (torch.full((got.shape[0], d), 77.0, dtype=out_dtype, device=DEV) for _ in range(2))
+        B.slkv_q4_unpack(c, ko, vo)
+        for o, x in ((ko, K), (vo, V)):
+            assert torch.equal(o.cpu()[slots], torch.from_numpy(x).float().to(out_dtype)) and torch.all(o.cpu()[rest] == 77.0)
+    pick = torch.tensor(slots[::-1][:5] + [-1, got.shape[0], 2 ** 31 - 1], dtype=torch.int32, device=DEV)
+    ko, vo = (torch.full((pick.numel(), d), 77.0, device=DEV) for _ in range(2))
+    B.slkv_q4_unpack(c, ko, vo, slots=pick)
+    m = pick.numel() - 3
+    assert torch.equal(ko.cpu()[:m], torch.from_numpy(K[::-1][:m].copy()).float()) and torch.all(ko[m:] == 77.0)
+    assert torch.equal(vo.cpu()[:m], torch.from_numpy(V[::-1][:m].copy()).float()) and torch.all(vo[m:] == 77.0)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_groups_that_are_not_ordinary(dtype):
+    big, inf, nan = 3.0e38, float("inf"), float("nan")
+    k, v = rows(3, 16, 128, torch.float32)
+    k[0, :32] = 0.75                                   # one value
+    k[1, 32:64] = 0.0
+    k[1, 40] = -0.0
+    k[2, 5], k[3, 70], k[4, 127] = nan, inf, -inf
+    k[5, 3], k[5, 9] = -big, big                       # a range over fp32's
+    k[6, 64:96] = big                                  # large, but one value
+    k[7, :32] = torch.arange(32) * 1e-40               # subnormal
+    k[8, :32] = torch.arange(32) * 2.0 ** -125
+    k[9, :32] = 1000.0 + torch.arange(32) / 64         # small steps far from zero
+    k[10, :32] = torch.arange(32) % 16                 # exact codes, and ties between them
+    k[11, :32] = (torch.arange(32) % 31) / 2
+    k[12, :32] = -torch.arange(32) * 3.7e36
+    k[13, 0], k[13, 1] = 2.0 ** -130, -2.0 ** -133
+    k, v = k.to(dtype), v.to(dtype)
+    t, c = empty_cache([16], 128, 1)
+    B.slkv_q4_pack(c, k.to(DEV), v.to(DEV), torch.tensor([0, 16], dtype=torch.int32, device=DEV), torch.zeros(16, dtype=torch.int32, device=DEV))
+    want = expected_record(k.double().numpy(), v.double().numpy())
+    assert np.array_equal(t["records"].cpu().numpy(), want)
+    ko, vo = (torch.zeros(16, 128, device=DEV) for _ in range(2))
+    B.slkv_q4_unpack(c, ko, vo)
+    x, y = k.double().numpy().reshape(16, 4, 32), ko.double().cpu().numpy().reshape(16, 4, 32)
+    poisoned = {(2, 0), (3, 2), (4, 3), (5, 0)}
+    for r in range(16):
+        for j in range(4):
+            if (r, j) in poisoned:
+                assert np.all(np.isnan(y[r, j]))
+            else:                                      # half a step, the fp32 roundings of x - zero and of the value
+                step = R.quantise_row(x[r].reshape(-1))[1][j]
+                assert np.all(np.abs(x[r, j] - y[r, j]) <= step / 2 + 2.0 ** -22 * np.abs(x[r, j]).max() + 2.0 ** -148), (r, j)
+
+
+def test_pack_stops_at_the_segments_ends_and_says_so():
+    k, v = rows(5, 30, 128, torch.bfloat16)
+    t, c = empty_cache([4, 12, 9], 128, 1)
+    off = torch.tensor([0, 10, 22, 30], dtype=torch.int32, device=DEV)
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    B.slkv_q4_pack(c, k.to(DEV), v.to(DEV), off, torch.arange(30, dtype=torch.int32, device=DEV), status)
+    assert status.item() == B.ERR["CAPACITY"] and t["lens"].tolist() == [4, 12, 8]
+    want = expected_record(k.double().numpy(), v.double().numpy())
+    assert np.array_equal(t["records"].cpu().numpy()[:24], want[[0, 1, 2, 3] + list(range(10, 30))]) and torch.all(t["records"][24] == 0xAB)
+    # offsets past the rows that are there
+    status.zero_()
+    t, c = empty_cache([10, 12, 9], 128, 1)
+    B.slkv_q4_pack(c, k[:25].contiguous().to(DEV), v[:25].contiguous().to(DEV), off, torch.arange(25, dtype=torch.int32, device=DEV), status)
+    assert status.item() == B.ERR["CAPACITY"] and t["lens"].tolist() == [10, 12, 3] and torch.all(t["records"][25:] == 0xAB)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("n_tokens", [1, 2, 21])
+def test_append_behind_the_filled_slots(d, dtype, n_tokens):
+    ns, hkv = 3, 2
+    lens = [0, 4, 50, 1, 7, 30]
+    t, c = empty_cache([x + n_tokens + i % 2 for i, x in enumerate(lens)], d, hkv)
+    t["lens"].copy_(torch.tensor(lens))
+    k, v = rows(d + n_tokens, ns * n_tokens * hkv, d, dtype)
+    # K from a wider tensor, V with its heads outside the tokens
+    kt = torch.zeros(ns, n_tokens, hkv + 1, d + 32, dtype=dtype, device=DEV)[:, :, :hkv, :d]
+    kt.copy_(k.view(ns, n_tokens, hkv, d))
+    vt = torch.zeros(ns, hkv, n_tokens, d, dtype=dtype, device=DEV).transpose(1, 2)
+    vt.copy_(v.view(ns, n_tokens, hkv, d))
+    pos = torch.arange(ns * n_tokens, dtype=torch.int32, device=DEV).view(ns, n_tokens) + 1000
+    after_lens = torch.zeros(6, dtype=torch.int32, device=DEV)
+    before = t["records"].clone()
+    B.slkv_q4_append(c, kt, vt, pos, after=cache_of(t, hkv, lens=after_lens))
+    assert t["lens"].tolist() == lens and after_lens.tolist() == [x + n_tokens for x in lens]
+    want = expected_record(k.double().numpy(), v.double().numpy()).reshape(ns, n_tokens, hkv, -1)
+    for seg, n in enumerate(lens):
+        s, h = divmod(seg, hkv)
+        b = int(t["starts"][seg]) + n
+        assert np.array_equal(t["records"][b:b + n_tokens].cpu().numpy(), want[s, :, h])
+        assert t["pos"][b:b + n_tokens].tolist() == pos[s].tolist() and torch.all(t["weight"][b:b + n_tokens] == 0)
+        before[b:b + n_tokens] = t["records"][b:b + n_tokens]
+    assert torch.equal(before, t["records"])
+    # the lengths themselves move on; a second time not everything fits
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    B.slkv_q4_append(c, kt, vt, pos, status=status)
+    assert t["lens"].tolist() == after_lens.tolist() and status.item() == 0 and torch.equal(before, t["records"])
+    B.slkv_q4_append(c, kt, vt, pos, status=status)
+    assert status.item() == B.ERR["CAPACITY"] and t["lens"].tolist() == [x + n_tokens + i % 2 for i, x in enumerate(lens)]
+
+
+# ---- attention -------------------------------------------------------------------------------------------------------
+def attend(t, hkv, q, accumulate=False, q_pos=None, slopes=None, units=B.SLKV_LSE_LN, out=None, **kw):
+    q = q.to(DEV) if not q.is_cuda else q
+    c = cache_of(t, hkv)
+    out = torch.full_like(q, 9.0) if out is None else out
+    lse = torch.full((q.size(0), q.size(2), q.size(1)), 9.0, device=DEV)
+    p = B.make_q4_attend(c, q, out, lse_units=units, **kw)
+    ws = B.new_q4_workspace(c, p, accumulate)
+    ws.fill_(0xFF)
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    B.slkv_q4_attend(c, p, q, out, ws, q_pos=q_pos, slopes=slopes, lse=lse, accumulate=accumulate, status=status)
+    assert status.item() == 0
+    return out, lse
+
+
+def check(t, hkv, q, accumulate=False, q_pos=None, slopes=None, units=B.SLKV_LSE_LN, **kw):
+    ref = R.attend(t["records"], t["pos"], t["weight"], t["starts"], t["lens"], q, hkv, kw.get("scale", q.size(3) ** -0.5),
+                   kw.get("softcap", 0.0), None if q_pos is None else q_pos.cpu().numpy(), None if slopes is None else slopes.cpu().numpy(),
+                   kw.get("weight_decay", 1.0))
+    out, lse = attend(t, hkv, q, accumulate, q_pos, slopes, units, **kw)
+    R.check_attend(out, lse, ref, q.dtype == torch.bfloat16, math.log(2.0) if units == B.SLKV_LSE_LOG2 else 1.0, t["weight"] if accumulate else None)
+    return out, lse
+
+
+def queries(seed, ns, nt, hq, d, dtype, size=1.0):
+    return (size * torch.randn(ns, nt, hq, d, generator=torch.Generator().manual_seed(seed))).to(dtype)
+
+
+LENS = [[1], [0, 31, 32, 33], [0, 0, 128, 129], [300, 5, 64, 1000, 2, 17]]
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("lens,hkv", [(LENS[0], 1), (LENS[1], 2), (LENS[2], 4), (LENS[3], 2)])
+@pytest.mark.parametrize("G,nt", [(1, 1), (4, 1), (8, 1), (3, 3), (5, 7)])
+def test_attention_over_any_lengths_and_columns(d, dtype, lens, hkv, G, nt):
+    t = R.random_cache(sum(lens) + d, lens, d, hkv, device=DEV)
+    check(t, hkv, queries(d + G, len(lens) // hkv, nt, hkv * G, d, dtype), accumulate=True)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("kw", [dict(softcap=5.0), dict(softcap=30.0, weight_decay=0.9, scale=0.3), dict(slopes=True), dict(slopes=True, softcap=20.0),
+                                dict(units=B.SLKV_LSE_LOG2, weight_decay=0.0), dict(scale=-0.05)])
+def test_caps_biases_and_masks_by_position(d, dtype, kw):
+    kw = dict(kw)
+    hkv, G, nt = 2, 4, 3
+    lens = [70, 257, 0, 3, 1000, 33]
+    t = R.random_cache(11 + d, lens, d, hkv, device=DEV)
+    # tokens between the rows, before all of them (nothing to see), behind all of them
+    q_pos = torch.tensor([[0, 90, 500], [4, 5, 1], [10 ** 6, 1200, 17]], dtype=torch.int32, device=DEV)
+    slopes = torch.exp2(-torch.arange(hkv * G, device=DEV, dtype=torch.float32)) if kw.pop("slopes", False) else None
+    out, lse = check(t, hkv, queries(d, 3, nt, hkv * G, d, dtype), accumulate=True, q_pos=q_pos, slopes=slopes, **kw)
+    assert torch.all(out[0, 0] == 0) and torch.all(torch.isneginf(lse[0, :, 0]))
+    assert torch.all(out[1, :, :G] == 0)                    # an empty segment
+
+
+@pytest.mark.parametrize("d,dtype", [(128, torch.bfloat16), (64, torch.float32)])
+def test_long_segments_in_many_pieces(d, dtype):
+    lens = [40001, 12, 0, 33000]
+    t = R.random_cache(5, lens, d, 4, device=DEV)
+    check(t, 4, queries(1, 1, 2, 24, d, dtype, 2.0), accumulate=True, q_pos=torch.tensor([[60000, 200000]], dtype=torch.int32, device=DEV))
+
+
+def test_many_short_segments():
+    lens = [(i * 37) % 90 for i in range(3000)]
+    t = R.random_cache(6, lens, 64, 6, slack=0, device=DEV)
+    check(t, 6, queries(2, 500, 1, 6, 64, torch.bfloat16), accumulate=True)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_scores_far_apart_and_large_queries(dtype):
+    t = R.random_cache(8, [500, 90], 128, 1, device=DEV)
+    check(t, 1, queries(3, 2, 1, 4, 128, dtype, 40.0))
+    check(t, 1, queries(4, 2, 1, 4, 128, dtype, 1e-3))
+    check(t, 1, queries(4, 2, 1, 4, 128, dtype, 0.0))
+
+
+def test_rows_that_are_not_seen_give_nothing_whatever_they_hold():
+    lens, d, hkv = [100, 37], 128, 1
+    t = R.random_cache(9, lens, d, hkv, device=DEV)
+    q = queries(5, 2, 2, 4, d, torch.bfloat16)
+    hidden = [40, 41, int(t["starts"][1]) + 36]
+    t["pos"][hidden] = 5000
+    q_pos = torch.tensor([[1000, 2000], [1000, 4000]], dtype=torch.int32, device=DEV)
+    want = attend(t, hkv, q, q_pos=q_pos)
+    for bad in (float("nan"), float("inf"), -float("inf"), 3e38):
+        s = t["records"][hidden][:, d:].contiguous().view(torch.bfloat16)
+        t["records"][hidden, d:] = torch.full_like(s, bad).view(torch.uint8)
+        got = attend(t, hkv, q, q_pos=q_pos)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    # a row that is seen by the second token alone is that token's
+    q_pos[0, 1] = 6000
+    t["records"][hidden, d:] = torch.full_like(s, float("nan")).view(torch.uint8)
+    got = attend(t, hkv, q, q_pos=q_pos)
+    assert torch.all(torch.isnan(got[0][0, 1])) and torch.equal(got[0][0, 0], want[0][0, 0]) and torch.equal(got[0][1], want[0][1])
+
+
+def test_a_poisoned_value_group_and_a_poisoned_key():
+    d = 128
+    t = R.random_cache(10, [50], d, 1, device=DEV)
+    q = queries(6, 1, 1, 4, d, torch.float32)
+    want, lse0 = attend(t, 1, q)
+    s = t["records"][:, d:].view(torch.bfloat16).view(-1, 4, 4)
+    keep = s.clone()
+    s[7, 2:, 1] = float("nan")                             # V, channels 32 .. 63
+    got, lse = attend(t, 1, q)
+    assert torch.all(torch.isnan(got[..., 32:64])) and torch.equal(lse, lse0)
+    rest = torch.cat([got[..., :32], got[..., 64:]], -1)
+    assert torch.equal(rest, torch.cat([want[..., :32], want[..., 64:]], -1))
+    s.copy_(keep)
+    s[7, :2, 1] = float("nan")                             # K
+    got, lse = attend(t, 1, q)
+    assert torch.all(torch.isnan(got)) and torch.all(torch.isnan(lse))
+    s.copy_(keep)
+    s[:50, 1, 0] = float("nan")                            # every key
+    got, lse = attend(t, 1, q)
+    assert torch.all(torch.isnan(got)) and torch.all(torch.isnan(lse))
+
+
+def test_strided_queries_and_outputs():
+    lens, d, hkv, G = [60, 400, 9, 77], 64, 2, 3
+    t = R.random_cache(12, lens, d, hkv, device=DEV)
+    q = queries(7, 2, 2, hkv * G, d, torch.bfloat16)
+    want, _ = attend(t, hkv, q)
+    wide = torch.zeros(2, hkv * G + 2, 2, d + 8, dtype=q.dtype, device=DEV)
+    qs = wide.transpose(1, 2)[:, :, 1:1 + hkv * G, :d]
+    qs.copy_(q)
+    o = torch.full((2, hkv * G, 2, 2 * d), 3.0, dtype=q.dtype, device=DEV)
+    os_ = o.transpose(1, 2)[..., :d]
+    got, _ = attend(t, hkv, qs, out=os_)
+    assert torch.equal(got, want) and torch.all(o[..., d:] == 3.0)
+
+
+def test_lengths_and_starts_that_do_not_fit_are_cut():
+    t = R.random_cache(13, [40, 50, 60], 128, 1, slack=2, device=DEV)
+    t["records"][:, 128:] = t["records"][0, 128:]            # every slot holds something
+    q = queries(8, 3, 1, 4, 128, torch.bfloat16)
+    rows_ = t["records"].size(0)
+    bad = dict(t, lens=torch.tensor([10 ** 6, -5, 10 ** 9], dtype=torch.int32, device=DEV))
+    room = (t["starts"][1:] - t["starts"][:-1]).tolist()
+    fit = dict(t, lens=torch.tensor([room[0], 0, room[2]], dtype=torch.int32, device=DEV))
+    assert torch.equal(attend(bad, 1, q)[0], attend(fit, 1, q)[0])
+    bad = dict(t, starts=torch.tensor([0, 40, rows_ - 5, rows_ + 10 ** 6], dtype=torch.int32, device=DEV),
+               lens=torch.tensor([40, 20, 60], dtype=torch.int32, device=DEV))
+    fit = dict(bad, starts=torch.tensor([0, 40, rows_ - 5, rows_], dtype=torch.int32, device=DEV), lens=torch.tensor([40, 20, 5], dtype=torch.int32, device=DEV))
+    assert torch.equal(attend(bad, 1, q)[0], attend(fit, 1, q)[0])
+
+
+# ---- eviction --------------------------------------------------------------------------------------------------------
+def run_evict(t, hkv, budgets, window, newest, to=None, to_lens=None):
+    c = cache_of(t, hkv)
+    dst = c if to is None and to_lens is None else cache_of(t, hkv, lens=to_lens) if to is None else cache_of(to, hkv)
+    ws = B.new_q4_evict_workspace(c, dst)
+    ws.fill_(0xFF)
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    B.slkv_q4_evict(c, dst, torch.tensor(budgets, dtype=torch.int32, device=DEV), window, torch.tensor(newest, dtype=torch.int32, device=DEV), ws, status)
+    return status.item()
+
+
+def expect_evicted(before, lens, hkv, budgets, window, newest, starts_to, room_to, after):
+    """`after` (tensors on the CPU) holds what the definition says, and is elsewhere as it was."""
+    for seg, n in enumerate(lens):
+        b, dst = int(before["starts"][seg]), starts_to[seg]
+        kept = min(n, max(budgets[seg % hkv], window))
+        src = R.evict_order(before["weight"][b:b + n].tolist(), before["pos"][b:b + n].tolist(), newest[seg // hkv], window, kept)[:room_to[seg]]
+        idx = [b + i for i in src]
+        for name in ("records", "pos", "weight"):
+            got, want = after[name][dst:dst + len(src)], before[name][idx]
+            if name == "weight":
+                got, want = got.view(torch.int32), want.view(torch.int32)
+            assert torch.equal(got, want), (seg, name)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("lens,hkv,budgets,window", [
+    ([1], 1, [1], 1), ([0, 5, 3, 9], 2, [2, 4], 1), ([40, 41, 200, 100, 33, 1], 3, [33, 40, 100], 32), ([1000, 2500, 2049, 10], 2, [999, 1], 16),
+    ([90, 80], 1, [-3], 64), ([300, 400], 2, [10 ** 6, 400], 8), ([70000, 17000, 50000, 49153], 2, [30000, 100], 64)])
+@pytest.mark.parametrize("in_place", [True, False])
+def test_eviction_keeps_what_the_definition_says(d, lens, hkv, budgets, window, in_place):
+    t = R.random_cache(sum(lens), lens, d, hkv, device=DEV)
+    g = torch.Generator().manual_seed(1)
+    t["weight"].copy_(torch.where(torch.rand(t["weight"].shape, generator=g) < 0.3, torch.tensor(0.0), t["weight"].cpu()))       # many ties
+    special = [float("nan"), float("inf"), -float("inf"), -0.0, 0.0, -1.5, 1e-42, float("nan")]
+    for i, x in enumerate(special):
+        if t["weight"].numel() > 3 * i:
+            t["weight"][3 * i] = x
+    newest = [int(t["pos"].max())] * (len(lens) // hkv)
+    if len(newest) > 1:
+        newest[1] = 20                                   # its rows count as new, most of them
+    before = {k: v.cpu().clone() for k, v in t.items()}
+    kept = [min(n, max(budgets[s % hkv], window)) for s, n in enumerate(lens)]
+    if in_place:
+        other = torch.full_like(t["lens"], -1)
+        assert run_evict(t, hkv, budgets, window, newest, to_lens=other) == 0
+        assert other.tolist() == kept and t["lens"].tolist() == lens
+        t2 = {k: v.clone().to(DEV) for k, v in before.items()}
+        assert run_evict(t2, hkv, budgets, window, newest) == 0          # the lengths in place too
+        assert t2["lens"].tolist() == kept and torch.equal(t2["records"], t["records"])
+        after = {k: v.cpu() for k, v in t.items()}
+        expect_evicted(before, lens, hkv, budgets, window, newest, before["starts"].tolist(), kept, after)
+        for seg in range(len(lens)):                     # behind the kept rows nothing changes
+            b, e = int(before["starts"][seg]) + kept[seg], int(before["starts"][seg + 1])
+            assert torch.equal(after["records"][b:e], before["records"][b:e]) and torch.equal(after["pos"][b:e], before["pos"][b:e])
+    else:
+        to, _ = empty_cache([x + 2 for x in kept], d, hkv)
+        assert run_evict(t, hkv, budgets, window, newest, to=to) == 0
+        assert to["lens"].tolist() == kept and t["lens"].tolist() == lens and torch.equal(t["records"].cpu(), before["records"])
+        after = {k: v.cpu() for k, v in to.items()}
+        expect_evicted(before, lens, hkv, budgets, window, newest, after["starts"].tolist(), kept, after)
+        for seg in range(len(lens)):
+            b, e = int(after["starts"][seg]) + kept[seg], int(after["starts"][seg + 1])
+            assert torch.all(after["records"][b:e] == 0xAB) and torch.all(after["pos"][b:e] == -7)
+
+
+def test_eviction_into_a_cache_that_is_too_small():
+    lens = [50, 60]
+    t = R.random_cache(3, lens, 128, 1, device=DEV)
+    before = {k: v.cpu().clone() for k, v in t.items()}
+    to, _ = empty_cache([10, 40], 128, 1)
+    assert run_evict(t, 1, [30], 4, [10 ** 6] * 2, to=to) == B.ERR["CAPACITY"]
+    assert to["lens"].tolist() == [10, 30]
+    after = {k: v.cpu() for k, v in to.items()}
+    expect_evicted(before, lens, 1, [30], 4, [10 ** 6] * 2, [0, 10], [10, 40], after)
+    assert torch.all(after["records"][40:] == 0xAB)
+
+
+# ---- together --------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype,d", [(torch.bfloat16, 128), (torch.float32, 64)])
+def test_a_compressed_prefill_decoded_at_its_budget(dtype, d):
+    ns, hkv, G, w, steps = 2, 2, 4, 16, 12
+    hq, cu = hkv * G, [0, 700, 1000]
+    g = torch.Generator().manual_seed(d)
+    T = cu[-1]
+    k, v = (torch.randn(T, hkv, d, generator=g).to(dtype).to(DEV) for _ in range(2))
+    q_win = torch.randn(ns, w, hq, d, generator=g).to(dtype).to(DEV)
+    p = B.make_params(q_win, k, v, w, 5)
+    cu_dev = torch.tensor(cu, dtype=torch.int32, device=DEV)
+    budgets = B.slkv_alloc_budgets(torch.tensor([[0.4, 0.9]], device=DEV), 32, 300)[0]
+    cap = B.slkv_packed_rows_upper_bound(p, cu)
+    ko, vo = (torch.empty(cap, d, dtype=dtype, device=DEV) for _ in range(2))
+    off, kept = torch.empty(ns * hkv + 1, dtype=torch.int32, device=DEV), torch.empty(cap, dtype=torch.int32, device=DEV)
+    B.slkv_compress(p, q_win, k, v, cu_dev, cu, budgets, ko, vo, off, kept, B.new_workspace(p, cu, DEV))
+    t, c = empty_cache([int(x) + 4 for x in budgets] * ns, d, hkv)
+    B.slkv_q4_pack(c, ko, vo, off, kept)
+    assert torch.equal(t["lens"], off[1:] - off[:-1])
+
+    out, lse = torch.empty(ns, 2, hq, d, dtype=dtype, device=DEV), torch.empty(ns, hq, 2, device=DEV)
+    params = B.make_q4_attend(c, out, out, weight_decay=0.95)
+    ws, ews = B.new_q4_workspace(c, params, True), B.new_q4_evict_workspace(c)
+    for step in range(steps):
+        newest = torch.tensor([cu[1] + 2 * step + 1, cu[2] - cu[1] + 2 * step + 1], dtype=torch.int32, device=DEV)
+        q_pos = torch.stack([newest - 1, newest], 1).contiguous()
+        kn, vn = (torch.randn(ns, 2, hkv, d, generator=g).to(dtype).to(DEV) for _ in range(2))
+        q = torch.randn(ns, 2, hq, d, generator=g).to(dtype).to(DEV)
+        B.slkv_q4_append(c, kn, vn, q_pos)
+        before = {x: y.cpu().clone() for x, y in t.items()}
+        ref = R.attend(before["records"], before["pos"], before["weight"], before["starts"], before["lens"], q, hkv, d ** -0.5,
+                       q_pos=q_pos.cpu().numpy(), decay=float(np.float32(0.95)))
+        B.slkv_q4_attend(c, params, q, out, ws, q_pos=q_pos, lse=lse, accumulate=True)
+        R.check_attend(out, lse, ref, dtype == torch.bfloat16, got_weight=t["weight"])
+        before = {x: y.cpu().clone() for x, y in t.items()}
+        B.slkv_q4_evict(c, c, budgets, w, newest, ews)
+        n = before["lens"].tolist()
+        expect_evicted(before, n, hkv, budgets.tolist(), w, newest.tolist(), before["starts"].tolist(), n, {x: y.cpu() for x, y in t.items()})
+        assert t["lens"].tolist() == [min(x, max(int(b), w)) for x, b in zip(n, budgets.tolist() * ns)]
+
+
+def test_the_same_bits_every_time_on_two_streams_and_in_a_graph():
+    lens, d, hkv, G = [3000, 200, 900, 4100], 128, 2, 4
+    base = R.random_cache(21, lens, d, hkv, device=DEV)
+    q = queries(9, 2, 1, hkv * G, d, torch.bfloat16).to(DEV)
+    k, v = (queries(10 + i, 2, 1, hkv, d, torch.bfloat16).to(DEV) for i in range(2))
+    newest = torch.tensor([20000, 20000], dtype=torch.int32, device=DEV)
+    budgets = torch.tensor([700, 1500], dtype=torch.int32, device=DEV)
+
+    def prepare():
+        t = {x: y.clone() for x, y in base.items()}
+        c = cache_of(t, hkv)
+        out, lse = torch.empty_like(q), torch.empty(2, hkv * G, 1, device=DEV)
+        p = B.make_q4_attend(c, q, out)
+        return t, c, out, lse, p, B.new_q4_workspace(c, p, True).fill_(0xEE), B.new_q4_evict_workspace(c).fill_(0xEE)
+
+    def step(s):
+        t, c, out, lse, p, ws, ews = s
+        B.slkv_q4_append(c, k, v, newest.view(2, 1))
+        B.slkv_q4_attend(c, p, q, out, ws, lse=lse, accumulate=True)
+        B.slkv_q4_evict(c, c, budgets, 8, newest, ews)
+    one = prepare()
+    step(one)
+    step(one)
+    torch.cuda.synchronize()
+    runs = [prepare(), prepare()]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(2):
+        for s, r in zip(streams, runs):
+            with torch.cuda.stream(s):
+                step(r)
+    torch.cuda.synchronize()
+    graphed = prepare()
+    step(graphed)                                          # sets every kernel up
+    graphed[0]["lens"].copy_(base["lens"])
+    for x in ("records", "pos", "weight"):
+        graphed[0][x].copy_(base[x])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(graphed)
+    graph.replay()
+    graph.replay()
+    torch.cuda.synchronize()
+    for r in runs + [graphed]:
+        assert torch.equal(r[2], one[2]) and torch.equal(r[3], one[3])
+        for x in ("lens", "records", "pos"):
+            assert torch.equal(r[0][x], one[0][x]), x
+        assert torch.equal(r[0]["weight"].view(torch.int32), one[0]["weight"].view(torch.int32))
