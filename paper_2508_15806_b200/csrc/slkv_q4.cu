@@ -54,7 +54,7 @@ __device__ __forceinline__ unsigned q4_quantise(const float (&x)[8], unsigned& s
   }
   const unsigned lane = threadIdx.x & 31, all = __ballot_sync(0xffffffffu, fine);
   fine = ((all >> (lane & 28)) & 15u) == 15u;
-  const float zero = __bfloat162float(__float2bfloat16_rd(lo));
+  const float zero = __bfloat162float(__float2bfloat16_rd(lo)) + 0.0f;       // -0 as 0: which of the two comes out of a minimum is open
   const float span = hi - zero;
   fine = fine && span <= kLargest;
   const __nv_bfloat16 sb = __float2bfloat16_ru(__fdiv_rn(span, 15.0f));

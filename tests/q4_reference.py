@@ -25,7 +25,7 @@ def quantise_row(x):
         if not np.all(np.isfinite(g)):
             scale[j] = zero[j] = math.nan
             continue
-        z = bf16_towards(float(g.min()), up=False)
+        z = bf16_towards(float(g.min()), up=False) + 0.0                 # -0 is 0
         with np.errstate(over="ignore"):
             span = float(np.float32(np.float32(g.max()) - np.float32(z)))
         if not math.isfinite(span):

@@ -109,7 +109,7 @@ def test_groups_that_are_not_ordinary(dtype):
     t, c = empty_cache([16], 128, 1)
     B.slkv_q4_pack(c, k.to(DEV), v.to(DEV), torch.tensor([0, 16], dtype=torch.int32, device=DEV), torch.zeros(16, dtype=torch.int32, device=DEV))
     want = expected_record(k.double().numpy(), v.double().numpy())
-    assert np.array_equal(t["records"].cpu().numpy(), want)
+    assert [r for r in range(16) if not np.array_equal(t["records"][r].cpu().numpy(), want[r])] == []
     ko, vo = (torch.zeros(16, 128, device=DEV) for _ in range(2))
     B.slkv_q4_unpack(c, ko, vo)
     x, y = k.double().numpy().reshape(16, 4, 32), ko.double().cpu().numpy().reshape(16, 4, 32)
