@@ -428,7 +428,7 @@ int slkv_noalloc_last_cuda_error(void);
  *   records  slkv_q4_record_bytes(head_dim) = head_dim * 5 / 4 bytes: the token's K and V row in groups of 32 channels.  A group has a
  *            scale and a zero in bf16, a channel a 4-bit code; it stands for zero + scale * code.
  *              zero = the minimum of the group rounded down to bf16, scale = (maximum - zero) / 15 rounded up to bf16,
- *              code = (x - zero) / scale rounded to the nearest integer, ties to even, within 0 .. 15
+ *              code = (x - zero) / scale in fp32, rounded to the nearest integer, ties to even: 0 .. 15
  *            so that |x - value| <= scale / 2 up to fp32 rounding.  A group with a NaN or an infinity, or with a range that fp32 does
  *            not hold, stands for NaN throughout.
  *            Layout: head_dim/2 bytes K codes, head_dim/2 bytes V codes, then head_dim/32 bf16 each of K scales, K zeros, V scales and

@@ -520,52 +520,76 @@ def make_q4_cache(records: torch.Tensor, pos: torch.Tensor, weight: Optional[tor
     return c
 
 
-def _q4_device(cache: SlkvQ4Cache, *tensors: Optional[torch.Tensor]) -> None:
+# The calls of a decode step are issued at the rate the checks below allow: each looks at a tensor's properties once.
+def _q4_here(cache: SlkvQ4Cache, *tensors: torch.Tensor) -> None:
     """Calls are enqueued on a stream of the current device: that has to be the cache's and the tensors'."""
-    d = cache.device
-    assert d.type == "cuda" and d.index == torch.cuda.current_device(), "the cache is not on the current device"
-    for t in tensors:
-        assert t is None or t.device == d, "a tensor is not on the cache's device"
+    d = torch._C._cuda_getDevice() if cache.device.type == "cuda" else -2
+    if cache.device.index != d or [1 for t in tensors if t.get_device() != d]:
+        raise AssertionError("the cache and the tensors have to be on the current device")
+
+
+def _q4_status(cache: SlkvQ4Cache, status: torch.Tensor) -> None:
+    _q4_here(cache, status)
+    assert status.dtype is torch.int32 and status.numel() >= 1
+
+
+def _q4_int32(t: torch.Tensor, n: int) -> None:
+    assert t.dtype is torch.int32 and t.numel() == n and t.is_contiguous()
 
 
 def slkv_q4_pack(cache: SlkvQ4Cache, k: torch.Tensor, v: torch.Tensor, offsets: torch.Tensor, kept_idx: torch.Tensor,
                  status: Optional[torch.Tensor] = None, stream=None) -> None:
     """k, v [rows, head_dim], offsets, kept_idx: as slkv_compress wrote them."""
-    _q4_device(cache, k, v, offsets, kept_idx, status)
-    rows = k.size(0)
-    assert k.is_contiguous() and v.is_contiguous() and k.dtype == v.dtype and k.shape == v.shape == (rows, cache.head_dim)
-    assert offsets.dtype == kept_idx.dtype == torch.int32 and offsets.is_contiguous() and kept_idx.is_contiguous()
-    assert offsets.numel() == cache.n_seqs * cache.n_kv_heads + 1 and kept_idx.numel() >= rows
-    _check(_fn["slkv_q4_pack"](stream, cache, _DTYPES[k.dtype], k, v, rows, offsets, kept_idx, status), "slkv_q4_pack")
+    _q4_here(cache, k, v, offsets, kept_idx)
+    rows, dim = k.shape
+    assert dim == cache.head_dim and v.shape == (rows, dim) and k.dtype is v.dtype and k.is_contiguous() and v.is_contiguous()
+    _q4_int32(offsets, cache.n_seqs * cache.n_kv_heads + 1)
+    assert kept_idx.dtype is torch.int32 and kept_idx.is_contiguous() and kept_idx.numel() >= rows
+    if status is not None:
+        _q4_status(cache, status)
+    rc = _fn["slkv_q4_pack"](stream, cache, _DTYPES[k.dtype], k, v, rows, offsets, kept_idx, status)
+    if rc != SLKV_OK:
+        raise SlkvError(rc, "slkv_q4_pack")
 
 
 def slkv_q4_append(cache: SlkvQ4Cache, k: torch.Tensor, v: torch.Tensor, pos: torch.Tensor, after: Optional[SlkvQ4Cache] = None,
                    status: Optional[torch.Tensor] = None, stream=None) -> None:
     """k, v [n_seqs, n_tokens, n_kv_heads, head_dim] (any strides over a contiguous last dimension), pos int32 [n_seqs, n_tokens].
     after: the same cache with lengths of its own, which take the new ones."""
-    _q4_device(cache, k, v, pos, status)
-    n = k.size(1)
-    assert k.shape == v.shape == (cache.n_seqs, n, cache.n_kv_heads, cache.head_dim) and k.dtype == v.dtype
-    assert pos.dtype == torch.int32 and pos.is_contiguous() and pos.shape == (cache.n_seqs, n)
-    (ks, kt, kh, k1), (vs, vt, vh, v1) = k.stride(), v.stride()
+    _q4_here(cache, k, v, pos)
+    shape = ns, n, hkv, dim = k.shape
+    assert (ns, hkv, dim) == (cache.n_seqs, cache.n_kv_heads, cache.head_dim) and v.shape == shape and k.dtype is v.dtype
+    _q4_int32(pos, ns * n)
+    ks, kt, kh, k1 = k.stride()
+    vs, vt, vh, v1 = v.stride()
     assert k1 == v1 == 1
+    lens_out = None
     if after is not None:
         assert after.records == cache.records and after.starts == cache.starts and after.pos == cache.pos
-    _check(_fn["slkv_q4_append"](stream, cache, _DTYPES[k.dtype], k, v, n, ks, kt, kh, vs, vt, vh, pos,
-                                 after.lens_tensor if after is not None else None, status), "slkv_q4_append")
+        lens_out = after.lens_tensor
+    if status is not None:
+        _q4_status(cache, status)
+    rc = _fn["slkv_q4_append"](stream, cache, _DTYPES[k.dtype], k, v, n, ks, kt, kh, vs, vt, vh, pos, lens_out, status)
+    if rc != SLKV_OK:
+        raise SlkvError(rc, "slkv_q4_append")
 
 
 def slkv_q4_unpack(cache: SlkvQ4Cache, k_out: torch.Tensor, v_out: torch.Tensor, slots: Optional[torch.Tensor] = None,
                    stream=None) -> None:
     """k_out, v_out [n, head_dim]: the rows of the slots given (int32 [n], entries outside the cache are padding), or of every
     filled slot at its own place (n = slots of the cache)."""
-    _q4_device(cache, k_out, v_out, slots)
-    n = k_out.size(0)
-    assert k_out.is_contiguous() and v_out.is_contiguous() and k_out.dtype == v_out.dtype
-    assert k_out.shape == v_out.shape == (n, cache.head_dim)
-    assert n == (cache.capacity_rows if slots is None else slots.numel())
-    assert slots is None or (slots.dtype == torch.int32 and slots.is_contiguous())
-    _check(_fn["slkv_q4_unpack"](stream, cache, _DTYPES[k_out.dtype], slots, n, k_out, v_out), "slkv_q4_unpack")
+    _q4_here(cache, k_out, v_out)
+    shape = n, dim = k_out.shape
+    assert dim == cache.head_dim and v_out.shape == shape and k_out.dtype is v_out.dtype
+    assert k_out.is_contiguous() and v_out.is_contiguous()
+    if slots is None:
+        assert n == cache.capacity_rows
+    else:
+        _q4_here(cache, slots)
+        _q4_int32(slots, n)
+    rc = _fn["slkv_q4_unpack"](stream, cache, _DTYPES[k_out.dtype], slots, n, k_out, v_out)
+    if rc != SLKV_OK:
+        raise SlkvError(rc, "slkv_q4_unpack")
 
 
 def make_q4_attend(cache: SlkvQ4Cache, q: torch.Tensor, out: torch.Tensor, scale: Optional[float] = None, softcap: float = 0.0,
@@ -573,8 +597,10 @@ def make_q4_attend(cache: SlkvQ4Cache, q: torch.Tensor, out: torch.Tensor, scale
     """Shapes and strides from the tensors: q, out [n_seqs, n_tokens, n_q_heads, head_dim] (last dim contiguous)."""
     assert q.shape == out.shape and q.dim() == 4 and q.dtype == out.dtype and q.stride(3) == 1 and out.stride(3) == 1
     assert q.size(0) == cache.n_seqs and q.size(3) == cache.head_dim
-    return SlkvQ4AttendParams(q.size(2), q.size(1), _DTYPES[q.dtype], lse_units, cache.head_dim ** -0.5 if scale is None else scale,
-                              softcap, weight_decay, 0, *q.stride()[:3], *out.stride()[:3])
+    p = SlkvQ4AttendParams(q.size(2), q.size(1), _DTYPES[q.dtype], lse_units, cache.head_dim ** -0.5 if scale is None else scale,
+                           softcap, weight_decay, 0, *q.stride()[:3], *out.stride()[:3])
+    p.q_like, p.out_like = (q.shape, q.stride(), q.dtype), (out.shape, out.stride(), out.dtype)
+    return p
 
 
 def slkv_q4_attend_workspace_bytes(cache: SlkvQ4Cache, params: SlkvQ4AttendParams, accumulate: bool = False) -> int:
@@ -593,16 +619,24 @@ def slkv_q4_attend(cache: SlkvQ4Cache, params: SlkvQ4AttendParams, q: torch.Tens
                    accumulate: bool = False, status: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """q, out: the shapes and strides params was made from.  q_pos int32 [n_seqs, n_tokens], slopes float32 [n_q_heads],
     lse float32 [n_seqs, n_q_heads, n_tokens]; accumulate adds to the cache's weights."""
-    _q4_device(cache, q, out, workspace, q_pos, slopes, lse, status)
-    shape = (cache.n_seqs, params.n_tokens, params.n_q_heads, cache.head_dim)
-    assert q.shape == out.shape == shape and _DTYPES[q.dtype] == _DTYPES[out.dtype] == params.dtype
-    assert q.stride() == (params.q_stride_seq, params.q_stride_tok, params.q_stride_head, 1)
-    assert out.stride() == (params.o_stride_seq, params.o_stride_tok, params.o_stride_head, 1)
-    assert q_pos is None or (q_pos.dtype == torch.int32 and q_pos.is_contiguous() and q_pos.numel() == shape[0] * shape[1])
-    assert slopes is None or (slopes.dtype == torch.float32 and slopes.is_contiguous() and slopes.numel() == shape[2])
-    assert lse is None or (lse.dtype == torch.float32 and lse.is_contiguous() and lse.numel() == shape[0] * shape[1] * shape[2])
-    _check(_fn["slkv_q4_attend"](stream, cache, params, q, q_pos, slopes, out, lse, int(accumulate), status, workspace,
-                                 workspace.numel()), "slkv_q4_attend")
+    _q4_here(cache, q, out, workspace)
+    assert (q.shape, q.stride(), q.dtype) == params.q_like and (out.shape, out.stride(), out.dtype) == params.out_like
+    ns, nt, hq, _ = params.q_like[0]
+    if q_pos is not None:
+        _q4_here(cache, q_pos)
+        _q4_int32(q_pos, ns * nt)
+    if slopes is not None:
+        _q4_here(cache, slopes)
+        assert slopes.dtype is torch.float32 and slopes.numel() == hq and slopes.is_contiguous()
+    if lse is not None:
+        _q4_here(cache, lse)
+        assert lse.dtype is torch.float32 and lse.numel() == ns * nt * hq and lse.is_contiguous()
+    if status is not None:
+        _q4_status(cache, status)
+    rc = _fn["slkv_q4_attend"](stream, cache, params, q, q_pos, slopes, out, lse, 1 if accumulate else 0, status, workspace,
+                               workspace.numel())
+    if rc != SLKV_OK:
+        raise SlkvError(rc, "slkv_q4_attend")
     return out
 
 
@@ -621,9 +655,12 @@ def new_q4_evict_workspace(cache: SlkvQ4Cache, to: Optional[SlkvQ4Cache] = None)
 def slkv_q4_evict(cache: SlkvQ4Cache, to: SlkvQ4Cache, budgets: torch.Tensor, window: int, newest: torch.Tensor,
                   workspace: torch.Tensor, status: Optional[torch.Tensor] = None, stream=None) -> None:
     """budgets int32 [n_kv_heads], newest int32 [n_seqs]; to: `cache` itself, or another cache."""
-    _q4_device(cache, budgets, newest, workspace, status)
+    _q4_here(cache, budgets, newest, workspace)
     assert to.device == cache.device
-    assert budgets.dtype == newest.dtype == torch.int32 and budgets.is_contiguous() and newest.is_contiguous()
-    assert budgets.numel() == cache.n_kv_heads and newest.numel() == cache.n_seqs
-    _check(_fn["slkv_q4_evict"](stream, cache, to, budgets, int(window), newest, status, workspace, workspace.numel()),
-           "slkv_q4_evict")
+    _q4_int32(budgets, cache.n_kv_heads)
+    _q4_int32(newest, cache.n_seqs)
+    if status is not None:
+        _q4_status(cache, status)
+    rc = _fn["slkv_q4_evict"](stream, cache, to, budgets, int(window), newest, status, workspace, workspace.numel())
+    if rc != SLKV_OK:
+        raise SlkvError(rc, "slkv_q4_evict")

@@ -3,9 +3,9 @@
 //
 // One pass over the records with a running maximum and sum (base 2, fp32).  Four bits become matrix operands in registers:
 //   scores  a K nibble c, shifted to the top of a bf16 mantissa under the exponent of one, is 1 + c / 16, exactly; the
-//           accumulator of a group's product starts at -sum of the group's queries, so that what comes out is sum q c / 16.
-//           The score is 16 * sum over groups of scale * that, plus sum over groups of zero * (sum of queries), which is one
-//           more product: the zeros as they lie in the record against the query sums split in three bf16 parts.
+//           score is sum over groups of 16 scale * (product - sum of the group's queries) + zero * (sum of the group's queries);
+//           the last two are two more products, of scales and zeros as they lie in the record and the query sums in three
+//           bf16 parts, which is exact.
 //   output  a V nibble under the exponent of 128 is 128 + c; less 136 it is c - 8, exactly.  Probabilities times the group's
 //           scale, rounded to bf16, are the other operand.  zero + 8 scale goes with the unrounded probabilities, in fp32.
 // Keys are the products' long side (m16), the query heads of a KV head and its tokens the short one (n8): with four heads to a
@@ -29,6 +29,8 @@ namespace slkv {
 namespace {
 
 constexpr int kAttendWarps = 4, kTileRows = 32, kCols = 8;
+constexpr float kLowest = -3e38f;       // a maximum over nothing: below every score, and differences of two stay numbers
+constexpr float kSlack = 8.0f;
 constexpr int kFewestTiles = 4;         // a CTA's share, at least: a tile for each warp
 constexpr unsigned long long kQ4WaitNs = 1000ull * 1000ull * 1000ull;
 
@@ -76,12 +78,16 @@ __device__ __forceinline__ float ex2(float x) {
   return y;
 }
 __device__ __forceinline__ void mma16816(float (&d)[4], unsigned a0, unsigned a1, unsigned a2, unsigned a3, unsigned b0, unsigned b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma16816_from_zero(float (&d)[4], unsigned a0, unsigned a1, unsigned a2, unsigned a3, unsigned b0, unsigned b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+               : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.0f));
 }
 __device__ __forceinline__ unsigned transpose8(unsigned x) {
   unsigned y;
-  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
 }
 __device__ __forceinline__ unsigned pack2(float lo, float hi) {
@@ -90,18 +96,28 @@ __device__ __forceinline__ unsigned pack2(float lo, float hi) {
 }
 __device__ __forceinline__ float lo_f(unsigned w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float hi_f(unsigned w) { return __uint_as_float(w & 0xffff0000u); }
+// (x & mask) | under
+__device__ __forceinline__ unsigned put_under(unsigned x, unsigned mask, unsigned under) {
+  unsigned y;
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(y) : "r"(x), "r"(mask), "r"(under));
+  return y;
+}
+// A constant that stays in a register: the loop has no room for instructions that bring it there again and again.
+__device__ __forceinline__ unsigned held(unsigned x) {
+  unsigned y;
+  asm volatile("mov.b32 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
 // nibbles I and I + 4 of a word as 1 + c / 16
 template <int I>
-__device__ __forceinline__ unsigned k_pair(unsigned w) {
-  const unsigned s = I == 0 ? w << 3 : w >> (I == 0 ? 0 : 4 * I - 3);
-  return (s & 0x00780078u) | 0x3f803f80u;
+__device__ __forceinline__ unsigned k_pair(unsigned w, unsigned one) {
+  return put_under(I == 0 ? w << 3 : w >> (I == 0 ? 0 : 4 * I - 3), 0x00780078u, one);
 }
 // nibbles I of both halves as c - 8
 template <int I>
-__device__ __forceinline__ unsigned v_pair(unsigned w) {
-  const unsigned x = ((w >> (4 * I)) & 0x000f000fu) | 0x43004300u;
-  const __nv_bfloat16 off = __ushort_as_bfloat16(0x4308);  // 136
-  const __nv_bfloat162 y = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&x), __nv_bfloat162(off, off));
+__device__ __forceinline__ unsigned v_pair(unsigned w, unsigned h128, unsigned h136) {
+  const unsigned x = put_under(w >> (4 * I), 0x000f000fu, h128);
+  const __nv_bfloat162 y = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&x), *reinterpret_cast<const __nv_bfloat162*>(&h136));
   return *reinterpret_cast<const unsigned*>(&y);
 }
 // Key of a product's row r: neighbours apart, so that the lanes of one shared-memory access meet all banks.
@@ -109,23 +125,20 @@ __device__ __forceinline__ int key_of(int r) { return (r & 8) | ((0x57463120u >>
 __device__ __forceinline__ int tiles_of(int len) { return (len + kTileRows - 1) / kTileRows; }
 // N 32-bit words from shared memory
 template <int N>
-__device__ __forceinline__ void load_words(const unsigned char* p, unsigned (&w)[N]) {
-  if constexpr (N == 4) {
-    const uint4 u = *reinterpret_cast<const uint4*>(p);
-    w[0] = u.x; w[1] = u.y; w[2] = u.z; w[3] = u.w;
-  } else if constexpr (N == 2) {
-    const uint2 u = *reinterpret_cast<const uint2*>(p);
-    w[0] = u.x; w[1] = u.y;
-  } else {
-    w[0] = *reinterpret_cast<const unsigned*>(p);
-  }
+__device__ __forceinline__ void load_words(uint32_t at, unsigned (&w)[N]) {
+  if constexpr (N == 4)
+    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at) : "memory");
+  else if constexpr (N == 2)
+    asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(at) : "memory");
+  else
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w[0]) : "r"(at) : "memory");
 }
 
 template <int HD> constexpr int kQ4Stages = HD == 128 ? 2 : 4;
 template <int HD> constexpr int kQ4Smem = kAttendWarps * kQ4Stages<HD> * kTileRows * q4_record_bytes(HD);
 
 template <int HD, int PARTS, bool MASK>
-__global__ void __launch_bounds__(kAttendWarps * 32) k_q4_attend(const __grid_constant__ Q4AttendArgs a) {
+__global__ void __launch_bounds__(kAttendWarps * 32, PARTS == 1 ? 4 : HD == 64 ? 3 : 2) k_q4_attend(const __grid_constant__ Q4AttendArgs a) {
   constexpr int NG = HD / 32, RB = q4_record_bytes(HD), kStages = kQ4Stages<HD>, kStageBytes = kTileRows * RB;
   extern __shared__ __align__(128) unsigned char smem[];
   __shared__ __align__(8) unsigned long long bars[kAttendWarps][kStages];
@@ -133,7 +146,12 @@ __global__ void __launch_bounds__(kAttendWarps * 32) k_q4_attend(const __grid_co
   __shared__ float merge_m[kAttendWarps][kCols], merge_l[kAttendWarps][kCols];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
   unsigned char* ring = smem + warp * (kStages * kStageBytes);
-  const uint32_t bar0 = smem_at(bars[warp]);
+  const uint32_t bar0 = smem_at(bars[warp]), ring_at = smem_at(ring);
+  const unsigned one = held(0x3f803f80u), h128 = held(0x43004300u), h136 = held(0x43084308u);
+  // where a lane finds its keys in 16 rows: rows key_of(g) and that + 8 of the first product, key_of(2 t), key_of(2 t + 1) and
+  // those + 8 of the second
+  const uint32_t key_row = key_of(g) * RB, value_row[2] = {uint32_t(key_of(2 * t) * RB + HD / 2 + g * (HD / 16)),
+                                                          uint32_t(key_of(2 * t + 1) * RB + HD / 2 + g * (HD / 16))};
   if (lane < kStages) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bar0 + 8 * lane) : "memory");
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   pdl_launch_dependents();
@@ -203,8 +221,7 @@ __global__ void __launch_bounds__(kAttendWarps * 32) k_q4_attend(const __grid_co
 
     // ---- the unit's queries: fragments, and sums per group
     const int s = seg / a.n_kv_heads, h = seg - s * a.n_kv_heads;
-    unsigned bq[PARTS][NG][2][2], bz[2] = {0u, 0u};
-    float init[NG][2];
+    unsigned bq[PARTS][NG][2][2], bz[2] = {0u, 0u}, bs[2] = {0u, 0u};
     {
       const int col = cb * kCols + g;
       const bool there = col < a.R;
@@ -244,22 +261,21 @@ __global__ void __launch_bounds__(kAttendWarps * 32) k_q4_attend(const __grid_co
         qs[j] = ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
         qs[j] += __shfl_xor_sync(0xffffffffu, qs[j], 1);
         qs[j] += __shfl_xor_sync(0xffffffffu, qs[j], 2);
-        init[j][0] = -__shfl_sync(0xffffffffu, qs[j], 8 * t);              // of columns 2 t and 2 t + 1
-        init[j][1] = -__shfl_sync(0xffffffffu, qs[j], 8 * t + 4);
       }
-      // the query sums / 16 in three parts: lane t holds part t of all groups, where the zeros' fragments expect them
+      // the query sums in three parts: lane t holds part t of all groups, where the fragments of scales and zeros expect them
 #pragma unroll
       for (int jj = 0; jj < NG / 2; ++jj) {
-        float x = qs[2 * jj] * 0.0625f, y = qs[2 * jj + 1] * 0.0625f;
-        unsigned w = 0;
+        float x = -qs[2 * jj], y = -qs[2 * jj + 1];
 #pragma unroll
         for (int p = 0; p < 3; ++p) {
           const unsigned v = pack2(x, y);
-          if (p == t) w = v;
+          if (p == t) {                                    // lane t = 3: zeros
+            bs[jj] = v;
+            bz[jj] = pack2(-0.0625f * lo_f(v), -0.0625f * hi_f(v));
+          }
           x -= lo_f(v);
           y -= hi_f(v);
         }
-        bz[jj] = w;                                        // lane t = 3: zeros
       }
     }
     const float to_log2 = a.scale * (16.0f * kLog2e), cap_in = a.softcap > 0.0f ? 16.0f * a.scale / a.softcap : 0.0f;
@@ -274,7 +290,7 @@ __global__ void __launch_bounds__(kAttendWarps * 32) k_q4_attend(const __grid_co
       }
     }
 
-    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f};
+    float m[2] = {kLowest, kLowest}, l[2] = {0.0f, 0.0f};
     float o[NG][2][4], zacc[NG][2];
 #pragma unroll
     for (int j = 0; j < NG; ++j) {
@@ -282,6 +298,7 @@ __global__ void __launch_bounds__(kAttendWarps * 32) k_q4_attend(const __grid_co
 #pragma unroll
       for (int i = 0; i < 8; ++i) o[j][i >> 2][i & 3] = 0.0f;
     }
+    const bool pairs = (a.R & 1) == 0;
     const int* pos_rows = a.c.pos + sg.begin;
     int pos_next = 0;
     if (MASK && from + warp < to) pos_next = pos_rows[min((from + warp) * kTileRows + lane, sg.len - 1)];
@@ -290,7 +307,7 @@ __global__ void __launch_bounds__(kAttendWarps * 32) k_q4_attend(const __grid_co
       const int n = min(kTileRows, sg.len - tile * kTileRows), slot = used % kStages;
       const int pos_here = pos_next;
       if (MASK && tile + kAttendWarps < to) pos_next = pos_rows[min((tile + kAttendWarps) * kTileRows + lane, sg.len - 1)];
-      unsigned char* buf = ring + slot * kStageBytes;
+      const uint32_t buf = ring_at + slot * kStageBytes;
       if (!dead) {                                         // a copy that does not come in a second is not waited for again
         dead = __any_sync(0xffffffffu, !copies_there(bar0 + 8 * slot, (used / kStages) & 1));
         if (dead) {
@@ -302,111 +319,114 @@ __global__ void __launch_bounds__(kAttendWarps * 32) k_q4_attend(const __grid_co
       if (n < kTileRows) {                                 // what lies behind the last row must be finite: scales and zeros
         if (lane >= n) {
 #pragma unroll
-          for (int i = 0; i < RB - HD; i += 16) *reinterpret_cast<uint4*>(buf + lane * RB + HD + i) = make_uint4(0, 0, 0, 0);
+          for (int i = 0; i < RB - HD; i += 16)
+            *reinterpret_cast<uint4*>(ring + slot * kStageBytes + lane * RB + HD + i) = make_uint4(0, 0, 0, 0);
           async_fence();
         }
         __syncwarp();
       }
-      float sc[2][4];
-      // ---- scores: rows key_of(g) and key_of(g + 8) of each half, columns 2 t and 2 t + 1
+#pragma unroll 1
+      for (int k0 = 0; k0 < n; k0 += 16) {
+        // ---- scores: rows key_of(g) and key_of(g + 8), columns 2 t and 2 t + 1
+        const int r0 = k0 + key_of(g), r1 = r0 + 8;
+        const uint32_t rows16 = buf + k0 * RB, p0 = rows16 + key_row, p1 = p0 + 8 * RB;
+        float x[4];
+        {
+          unsigned w0[NG], w1[NG], x0[NG], x1[NG];         // codes; scales and zeros
+          load_words(p0 + HD, x0);
+          load_words(p1 + HD, x1);
+          load_words(p0 + 4 * NG * t, w0);
+          load_words(p1 + 4 * NG * t, w1);
+          mma16816_from_zero(x, x0[NG / 2], x1[NG / 2], NG == 4 ? x0[NG - 1] : 0u, NG == 4 ? x1[NG - 1] : 0u, bz[0], bz[1]);
+          mma16816(x, x0[0], x1[0], NG == 4 ? x0[1] : 0u, NG == 4 ? x1[1] : 0u, bs[0], bs[1]);
 #pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        const int r0 = half * 16 + key_of(g), r1 = r0 + 8;
-        const unsigned char *p0 = buf + r0 * RB, *p1 = buf + r1 * RB;
-        unsigned w0[NG], w1[NG], x0[NG], x1[NG];           // codes; scales and zeros
-        load_words(p0 + 4 * NG * t, w0);
-        load_words(p1 + 4 * NG * t, w1);
-        load_words(p0 + HD, x0);
-        load_words(p1 + HD, x1);
-        float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        mma16816(acc, x0[NG / 2], x1[NG / 2], NG == 4 ? x0[NG - 1] : 0u, NG == 4 ? x1[NG - 1] : 0u, bz[0], bz[1]);
+          for (int j = 0; j < NG; ++j) {
+            float d[4];
+            const unsigned a00 = k_pair<0>(w0[j], one), a01 = k_pair<1>(w0[j], one), a02 = k_pair<2>(w0[j], one), a03 = k_pair<3>(w0[j], one);
+            const unsigned a10 = k_pair<0>(w1[j], one), a11 = k_pair<1>(w1[j], one), a12 = k_pair<2>(w1[j], one), a13 = k_pair<3>(w1[j], one);
 #pragma unroll
-        for (int j = 0; j < NG; ++j) {
-          float d[4] = {init[j][0], init[j][1], init[j][0], init[j][1]};
-          const unsigned a00 = k_pair<0>(w0[j]), a01 = k_pair<1>(w0[j]), a02 = k_pair<2>(w0[j]), a03 = k_pair<3>(w0[j]);
-          const unsigned a10 = k_pair<0>(w1[j]), a11 = k_pair<1>(w1[j]), a12 = k_pair<2>(w1[j]), a13 = k_pair<3>(w1[j]);
-#pragma unroll
-          for (int p = 0; p < PARTS; ++p) {
-            mma16816(d, a00, a10, a01, a11, bq[p][j][0][0], bq[p][j][0][1]);
-            mma16816(d, a02, a12, a03, a13, bq[p][j][1][0], bq[p][j][1][1]);
+            for (int p = 0; p < PARTS; ++p) {
+              if (p == 0) mma16816_from_zero(d, a00, a10, a01, a11, bq[p][j][0][0], bq[p][j][0][1]);
+              else mma16816(d, a00, a10, a01, a11, bq[p][j][0][0], bq[p][j][0][1]);
+              mma16816(d, a02, a12, a03, a13, bq[p][j][1][0], bq[p][j][1][1]);
+            }
+            const float s0 = j & 1 ? hi_f(x0[j >> 1]) : lo_f(x0[j >> 1]), s1 = j & 1 ? hi_f(x1[j >> 1]) : lo_f(x1[j >> 1]);
+            x[0] = fmaf(s0, d[0], x[0]); x[1] = fmaf(s0, d[1], x[1]);
+            x[2] = fmaf(s1, d[2], x[2]); x[3] = fmaf(s1, d[3], x[3]);
           }
-          const float s0 = j & 1 ? hi_f(x0[j >> 1]) : lo_f(x0[j >> 1]), s1 = j & 1 ? hi_f(x1[j >> 1]) : lo_f(x1[j >> 1]);
-          acc[0] = fmaf(s0, d[0], acc[0]); acc[1] = fmaf(s0, d[1], acc[1]);
-          acc[2] = fmaf(s1, d[2], acc[2]); acc[3] = fmaf(s1, d[3], acc[3]);
         }
-        int pos0 = 0, pos1 = 0;
+        if (a.softcap > 0.0f) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x[i] = a.softcap * kLog2e * tanhf(x[i] * cap_in);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x[i] *= to_log2;
+        }
         if (MASK) {
-          pos0 = __shfl_sync(0xffffffffu, pos_here, r0);
-          pos1 = __shfl_sync(0xffffffffu, pos_here, r1);
-        }
+          const int pos0 = __shfl_sync(0xffffffffu, pos_here, r0), pos1 = __shfl_sync(0xffffffffu, pos_here, r1);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float x = a.softcap > 0.0f ? a.softcap * kLog2e * tanhf(acc[i] * cap_in) : acc[i] * to_log2;
-          bool visible = (i < 2 ? r0 : r1) < n;
-          if (MASK) {
+          for (int i = 0; i < 4; ++i) {
             const int pos = i < 2 ? pos0 : pos1;
-            x = fmaf(slope[i & 1], (float)(pos - qp[i & 1]), x);
-            visible = visible && pos <= qp[i & 1];
+            x[i] = pos <= qp[i & 1] ? fmaf(slope[i & 1], (float)(pos - qp[i & 1]), x[i]) : -INFINITY;
           }
-          sc[half][i] = visible ? x : -INFINITY;
+        }
+        if (k0 + 16 > n) {                                 // the last rows of a segment
+          if (r0 >= n) x[0] = x[1] = -INFINITY;
+          if (r1 >= n) x[2] = x[3] = -INFINITY;
         }
         if (a.accumulate) {
           const int col = cb * kCols + 2 * t;
           float* to_row = a.scores + ((long long)sg.begin + tile * kTileRows) * a.R + col;
+          if (pairs) {
+            if (r0 < n && col < a.R) *reinterpret_cast<float2*>(to_row + r0 * a.R) = make_float2(x[0], x[1]);
+            if (r1 < n && col < a.R) *reinterpret_cast<float2*>(to_row + r1 * a.R) = make_float2(x[2], x[3]);
+          } else {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int r = i < 2 ? r0 : r1;
-            if (r < n && col + (i & 1) < a.R) to_row[r * a.R + (i & 1)] = sc[half][i];
+            for (int i = 0; i < 4; ++i) {
+              const int r = i < 2 ? r0 : r1;
+              if (r < n && col + (i & 1) < a.R) to_row[r * a.R + (i & 1)] = x[i];
+            }
           }
         }
-      }
-      // ---- running maximum and sum
-      float p[2][4], up[2];
-      bool grew = false;
+        // ---- running maximum and sum.  The maximum need not be the largest score, only near it: it moves when a score is
+        // over it by a factor of 2^8, and then to the largest, so that most steps exchange nothing between the lanes.
+        const float top0 = fmaxf(x[0], x[2]), top1 = fmaxf(x[1], x[3]);
+        if (__any_sync(0xffffffffu, top0 > m[0] + kSlack || top1 > m[1] + kSlack)) {
+          float up[2];
 #pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        float x = fmaxf(fmaxf(sc[0][c], sc[0][c + 2]), fmaxf(sc[1][c], sc[1][c + 2]));
-        x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
-        x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
-        x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
-        up[c] = 1.0f;
-        if (x > m[c]) {
-          up[c] = ex2(m[c] - x);
-          m[c] = x;
-          grew = true;
+          for (int c = 0; c < 2; ++c) {
+            float y = c ? top1 : top0;
+            y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, 4));
+            y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, 8));
+            y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, 16));
+            y = fmaxf(y, m[c]);
+            up[c] = ex2(m[c] - y);
+            m[c] = y;
+            l[c] *= up[c];
+          }
+#pragma unroll
+          for (int j = 0; j < NG; ++j) {
+            zacc[j][0] *= up[0]; zacc[j][1] *= up[1];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) o[j][i >> 2][i & 3] *= up[i & 1];
+          }
         }
-      }
-      if (__any_sync(0xffffffffu, grew)) {
-#pragma unroll
-        for (int j = 0; j < NG; ++j) {
-          zacc[j][0] *= up[0]; zacc[j][1] *= up[1];
-#pragma unroll
-          for (int i = 0; i < 8; ++i) o[j][i >> 2][i & 3] *= up[i & 1];
-        }
-        l[0] *= up[0]; l[1] *= up[1];
-      }
-      const float base[2] = {m[0] == -INFINITY ? 0.0f : m[0], m[1] == -INFINITY ? 0.0f : m[1]};
-#pragma unroll
-      for (int half = 0; half < 2; ++half)
+        bool seen[4];
+        float p[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          p[half][i] = ex2(sc[half][i] - base[i & 1]);
-          l[i & 1] += p[half][i];
+          seen[i] = !MASK || x[i] != -INFINITY;
+          p[i] = ex2(x[i] - m[i & 1]);
+          l[i & 1] += p[i];
         }
-      // ---- output
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        const int r0 = half * 16 + key_of(g), r1 = r0 + 8;
+        // ---- output
         unsigned x0[NG], x1[NG];
-        load_words(buf + r0 * RB + HD + 4 * NG, x0);
-        load_words(buf + r1 * RB + HD + 4 * NG, x1);
-        const int k0 = half * 16 + key_of(2 * t), k1 = half * 16 + key_of(2 * t + 1);
+        load_words(p0 + HD + 4 * NG, x0);
+        load_words(p1 + HD + 4 * NG, x1);
         unsigned va[4][NG / 2];                            // keys 2 t, 2 t + 1, 2 t + 8, 2 t + 9
 #pragma unroll
-        for (int i = 0; i < 4; ++i) load_words(buf + ((i & 1 ? k1 : k0) + (i & 2 ? 8 : 0)) * RB + HD / 2 + g * (HD / 16), va[i]);
-        bool seen[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) seen[i] = !MASK || sc[half][i] != -INFINITY;
+        for (int i = 0; i < 4; ++i)
+          load_words(rows16 + value_row[i & 1] + (i & 2 ? 8 * RB : 0), va[i]);
 #pragma unroll
         for (int j = 0; j < NG; ++j) {
           const float s0 = j & 1 ? hi_f(x0[j >> 1]) : lo_f(x0[j >> 1]), s1 = j & 1 ? hi_f(x1[j >> 1]) : lo_f(x1[j >> 1]);
@@ -417,13 +437,13 @@ __global__ void __launch_bounds__(kAttendWarps * 32) k_q4_attend(const __grid_co
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const float zz = seen[i] ? (i < 2 ? z0 : z1) : 0.0f;
-            zacc[j][i & 1] = fmaf(p[half][i], zz, zacc[j][i & 1]);
-            y[i] = seen[i] ? p[half][i] * (i < 2 ? s0 : s1) : 0.0f;
+            zacc[j][i & 1] = fmaf(p[i], zz, zacc[j][i & 1]);
+            y[i] = seen[i] ? p[i] * (i < 2 ? s0 : s1) : 0.0f;
           }
           const unsigned t01 = __byte_perm(va[0][j >> 1], va[1][j >> 1], j & 1 ? 0x7632 : 0x5410);
           const unsigned t89 = __byte_perm(va[2][j >> 1], va[3][j >> 1], j & 1 ? 0x7632 : 0x5410);
-          const unsigned f0[4] = {v_pair<0>(t01), v_pair<1>(t01), v_pair<0>(t89), v_pair<1>(t89)};
-          const unsigned f1[4] = {v_pair<2>(t01), v_pair<3>(t01), v_pair<2>(t89), v_pair<3>(t89)};
+          const unsigned f0[4] = {v_pair<0>(t01, h128, h136), v_pair<1>(t01, h128, h136), v_pair<0>(t89, h128, h136), v_pair<1>(t89, h128, h136)};
+          const unsigned f1[4] = {v_pair<2>(t01, h128, h136), v_pair<3>(t01, h128, h136), v_pair<2>(t89, h128, h136), v_pair<3>(t89, h128, h136)};
           if constexpr (PARTS == 1) {
             const unsigned b0 = transpose8(pack2(y[0], y[1])), b1 = transpose8(pack2(y[2], y[3]));
             mma16816(o[j][0], f0[0], f0[1], f0[2], f0[3], b0, b1);
@@ -478,15 +498,14 @@ __global__ void __launch_bounds__(kAttendWarps * 32) k_q4_attend(const __grid_co
     for (int i = tid; i < kCols * HD / 4; i += kAttendWarps * 32) {
       const int c = i / (HD / 4), ch = 4 * (i % (HD / 4)), col = cb * kCols + c;
       if (col >= a.R) continue;
-      float top = merge_m[0][c];
+      float top = merge_m[0][c];                           // kLowest, and a sum of 0, where no row is seen
 #pragma unroll
       for (int w = 1; w < kAttendWarps; ++w) top = fmaxf(top, merge_m[w][c]);
-      const float base = top == -INFINITY ? 0.0f : top;
       float sum_l = 0.0f;
       float4 v = make_float4(0, 0, 0, 0);
 #pragma unroll
       for (int w = 0; w < kAttendWarps; ++w) {
-        const float f = ex2(merge_m[w][c] - base);         // 0 for a warp without rows
+        const float f = ex2(merge_m[w][c] - top);
         const float4 x = *reinterpret_cast<const float4*>(smem + w * (kStages * kStageBytes) + (c * kPitch + ch) * 4);
         sum_l = fmaf(merge_l[w][c], f, sum_l);
         v.x = fmaf(x.x, f, v.x); v.y = fmaf(x.y, f, v.y); v.z = fmaf(x.z, f, v.z); v.w = fmaf(x.w, f, v.w);
@@ -535,18 +554,18 @@ __device__ __forceinline__ long long piece_at(const Q4Pieces& p, int i, int c) {
 }
 // Maximum and sum over a unit's pieces for one column; whole warp.
 __device__ __forceinline__ float2 join_ml(const Q4AttendArgs& a, const Q4Pieces& p, int c, int lane) {
-  float m = -INFINITY, l = 0.0f;
+  float m = kLowest, l = 0.0f;
   for (int i = p.first + lane; i <= p.last; i += 32) {
     const float2 x = a.ml[piece_at(p, i, c)];
-    const float top = fmaxf(m, x.x), base = top == -INFINITY ? 0.0f : top;
-    l = l * ex2(m - base) + x.y * ex2(x.x - base);
+    const float top = fmaxf(m, x.x);
+    l = l * ex2(m - top) + x.y * ex2(x.x - top);
     m = top;
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
     const float om = __shfl_xor_sync(0xffffffffu, m, o), ol = __shfl_xor_sync(0xffffffffu, l, o);
-    const float top = fmaxf(m, om), base = top == -INFINITY ? 0.0f : top;
-    l = l * ex2(m - base) + ol * ex2(om - base);
+    const float top = fmaxf(m, om);
+    l = l * ex2(m - top) + ol * ex2(om - top);
     m = top;
   }
   return make_float2(m, l);
@@ -569,17 +588,16 @@ __global__ void __launch_bounds__(kJoinThreads) k_q4_join(const __grid_constant_
       p = pieces_of(a, seg * a.n_cb + cb, tiles);
       if (p.first == p.last) return;
     }
-    float2 ml = make_float2(-INFINITY, 0.0f);
+    float2 ml = make_float2(kLowest, 0.0f);
     float acc[V];
 #pragma unroll
     for (int e = 0; e < V; ++e) acc[e] = 0.0f;
     if (tiles > 0) {
       ml = join_ml(a, p, c, lane);
-      const float base = ml.x == -INFINITY ? 0.0f : ml.x;
 #pragma unroll 4
       for (int i = p.first + warp; i <= p.last; i += kWarps) {
         const long long at = piece_at(p, i, c);
-        const float f = ex2(a.ml[at].x - base);
+        const float f = ex2(a.ml[at].x - ml.x);
 #pragma unroll
         for (int e = 0; e < V; ++e) acc[e] = fmaf(a.part[at * HD + lane + 32 * e], f, acc[e]);
       }

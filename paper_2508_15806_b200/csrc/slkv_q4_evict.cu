@@ -2,28 +2,35 @@
 // largest accumulated weights.
 //
 // Rows are ranked by 32-bit keys -- the newest rows first, then by weight, NaN last -- and a segment's kept rows are the
-// `kept` largest, ties to the lower slot: a descent over the keys' bits, 11 + 11 + 10 of them, with a histogram each.  The kept
-// rows that lie behind the first `kept` slots then fill the holes before them, in order, so that as few rows move as can, no
-// row is read that another one overwrites, and a cache can be evicted from in place.
-// Two launches: the selection, a CTA per segment, leaves for every kept slot where its row comes from; the moves are spread
-// over the whole device.  What bounds it: for few rows the selection's chain of passes over its keys, for many the rows' bytes.
+// `kept` largest, ties to the lower slot.  The kept-th largest key comes from a histogram of the keys' upper 11 bits, a second
+// and a third one where many keys share them, and as soon as few do from counting, for each of these, how many are above it.
+// The kept rows that lie behind the first `kept` slots then fill the holes before them, in order, so that as few rows move as
+// can, no row is read that another one overwrites, and a cache can be evicted from in place.
+// One launch: a cluster of CTAs per segment (one CTA where there are many segments or few rows), each with a contiguous share
+// of the slots, keys in shared memory; they add up their histograms in the first CTA's and share the moves evenly.
+// What bounds it: for few rows the chain of passes over the keys, for many the rows' bytes.
+#include <cooperative_groups.h>
+
 #include "slkv_q4_device.cuh"
 
 namespace slkv {
 namespace {
 
-constexpr int kEvictBins = 2048;
-constexpr int kMostKeys = 49152;        // that shared memory holds
+namespace cg = cooperative_groups;
+
+constexpr int kEvictThreads = 512, kEvictBins = 2048, kEvictCluster = 8;
+constexpr int kMostKeys = 40960;        // that shared memory holds beside the rest
+constexpr int kFewKeys = 128;           // are ranked by counting, one for each thread: 0.5 us; another histogram takes 1.5
 
 struct Q4EvictArgs {
   Q4CacheView from, to;
   const int32_t *budgets, *newest;
   int32_t* status;
-  int32_t* source;                      // [capacity of from] per kept slot, from its segment's first: the slot its row is in
-  int32_t *holes, *movers;              // likewise
-  int32_t* kept;                        // [n_seg] rows to write
+  int32_t* source;                      // [capacity of from] per kept slot, from its segment's first: the slot its row is in, or
+                                        // ~i: the i-th of `movers`
+  int32_t *holes, *movers;              // likewise: slots whose rows go, slots whose rows move
   int n_kv_heads, window, key_room;     // key_room: keys that the launch's shared memory holds
-  int in_place, splits;
+  int in_place, ctas;                   // ctas: of a cluster
 };
 
 __device__ __forceinline__ unsigned evict_key(float weight, int pos, long long newest_kept) {
@@ -35,7 +42,8 @@ __device__ __forceinline__ unsigned evict_key(float weight, int pos, long long n
 
 // Exclusive prefix sum over the CTA; *total: of all.
 __device__ __forceinline__ unsigned cta_scan(unsigned x, unsigned* warp_sums, unsigned* total) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n_warps = blockDim.x >> 5;
+  constexpr int kWarps = kEvictThreads / 32;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   unsigned inc = x;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
@@ -45,177 +53,304 @@ __device__ __forceinline__ unsigned cta_scan(unsigned x, unsigned* warp_sums, un
   __syncthreads();                                         // the sums of the scan before are read
   if (lane == 31) warp_sums[warp] = inc;
   __syncthreads();
-  unsigned w = lane < n_warps ? warp_sums[lane] : 0u;
+  unsigned w = lane < kWarps ? warp_sums[lane] : 0u;
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
+  for (int o = 1; o < kWarps; o <<= 1) {
     const unsigned y = __shfl_up_sync(0xffffffffu, w, o);
     if (lane >= o) w += y;
   }
-  *total = __shfl_sync(0xffffffffu, w, 31);
-  const unsigned before = __shfl_sync(0xffffffffu, w, warp) - __shfl_sync(0xffffffffu, inc, 31);
-  return before + inc - x;
+  *total = __shfl_sync(0xffffffffu, w, kWarps - 1);
+  const unsigned upto = __shfl_sync(0xffffffffu, w, warp), own = __shfl_sync(0xffffffffu, inc, 31);
+  return upto - own + inc - x;
 }
 
-__global__ void __launch_bounds__(1024) k_q4_evict_select(const __grid_constant__ Q4EvictArgs a) {
+// n <= 32 rows of this warp, lane i the i-th: from slot `src` of one cache to slot `dst` of the other, 16 rows' loads before their
+// stores (more in flight would take registers that a second CTA per SM needs).
+template <int HD>
+__device__ __forceinline__ void move_rows(const Q4EvictArgs& a, int n, int src, int dst, int lane) {
+  constexpr int RB = q4_record_bytes(HD), kPieces = RB / 16, kRound = 5;
+  const int pos = lane < n ? a.from.pos[src] : 0;
+  const float weight = lane < n ? a.from.weight[src] : 0.0f;
+#pragma unroll
+  for (int i0 = 0; i0 < kPieces; i0 += kRound) {
+    uint4 x[kRound];
+#pragma unroll
+    for (int i = 0; i < kRound; ++i) {
+      const int piece = lane + 32 * (i0 + i), row = piece / kPieces, s = __shfl_sync(0xffffffffu, src, row);
+      if (row < n) x[i] = __ldcs(reinterpret_cast<const uint4*>(a.from.records + (long long)s * RB) + (piece - row * kPieces));
+    }
+#pragma unroll
+    for (int i = 0; i < kRound; ++i) {
+      const int piece = lane + 32 * (i0 + i), row = piece / kPieces, d = __shfl_sync(0xffffffffu, dst, row);
+      if (row < n) *(reinterpret_cast<uint4*>(a.to.records + (long long)d * RB) + (piece - row * kPieces)) = x[i];
+    }
+  }
+  if (lane < n) {
+    a.to.pos[dst] = pos;
+    a.to.weight[dst] = weight;
+  }
+}
+
+struct EvictShared {
+  unsigned hist[kEvictBins];            // of the CTA's keys; the cluster's in the first CTA's
+  unsigned few[kFewKeys];               // the first CTA's: the keys that share the prefix
+  unsigned warp_sums[32];
+  unsigned found[3], n_few;
+  unsigned counts[4];
+};
+
+template <int HD, bool CLUSTER>
+__global__ void __launch_bounds__(kEvictThreads, 2) k_q4_evict(const __grid_constant__ Q4EvictArgs a) {
   extern __shared__ unsigned keys[];
-  __shared__ unsigned hist[kEvictBins];
-  __shared__ unsigned warp_sums[32];
-  __shared__ unsigned found[3];
+  __shared__ EvictShared sh;
+  cg::cluster_group cluster = cg::this_cluster();
+  auto sync = [&] {
+    if constexpr (CLUSTER) cluster.sync();
+    else __syncthreads();
+  };
   pdl_launch_dependents();
   pdl_wait();
-  const int tid = threadIdx.x, seg = blockIdx.x, threads = blockDim.x;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int ctas = CLUSTER ? a.ctas : 1, rank = CLUSTER ? (int)cluster.block_rank() : 0, seg = blockIdx.x / ctas;
+  EvictShared* first = CLUSTER ? cluster.map_shared_rank(&sh, 0) : &sh;
   const Q4Segment s = q4_segment(a.from.starts, a.from.lens, seg, a.from.capacity);
   const int sq = seg / a.n_kv_heads, h = seg - sq * a.n_kv_heads;
   const int kept = min(s.len, max(a.budgets[h], a.window));
-  const int room = a.in_place ? s.room : q4_segment(a.to.starts, a.to.starts, seg, a.to.capacity).room;
-  __syncthreads();                                         // the length is read by all before it changes
-  if (tid == 0) {
-    a.to.lens[seg] = min(kept, room);
-    a.kept[seg] = a.in_place && kept == s.len ? 0 : min(kept, room);
-    if (kept > room && a.status) *a.status = SLKV_ERR_CAPACITY;
+  const Q4Segment d = a.in_place ? s : q4_segment(a.to.starts, a.to.starts, seg, a.to.capacity);
+  sync();                                                  // the length is read by all before it changes
+  if (rank == 0 && tid == 0) {
+    a.to.lens[seg] = min(kept, d.room);
+    if (kept > d.room && a.status) *a.status = SLKV_ERR_CAPACITY;
   }
-  int32_t* source = a.source + s.begin;
+  const int per_warp = 32, n_warps = ctas * (kEvictThreads / 32), my_warp = rank * (kEvictThreads / 32) + warp;
   if (kept == s.len) {                                     // everything stays
     if (!a.in_place)
-      for (int i = tid; i < kept; i += threads) source[i] = i;
+      for (int i = my_warp * per_warp; i < min(kept, d.room); i += n_warps * per_warp)
+        move_rows<HD>(a, min(per_warp, min(kept, d.room) - i), s.begin + min(i + lane, kept - 1), d.begin + i + lane, lane);
     return;
   }
   const float* weight = a.from.weight + s.begin;
   const int32_t* pos = a.from.pos + s.begin;
   const long long newest_kept = (long long)a.newest[sq] - a.window;
-  const bool cached = s.len <= a.key_room;
-  auto key_at = [&](int i) { return cached ? keys[i] : evict_key(weight[i], pos[i], newest_kept); };
-  if (cached)
-    for (int i = tid; i < s.len; i += threads) keys[i] = evict_key(weight[i], pos[i], newest_kept);
+  // the CTA's slots [c0, c1)
+  const int share = ((s.len + ctas - 1) / ctas + 3) & ~3, c0 = min(rank * share, s.len), c1 = min(c0 + share, s.len), n = c1 - c0;
+  const bool cached = share <= a.key_room;
+  auto key_at = [&](int i) { return cached ? keys[i] : evict_key(weight[c0 + i], pos[c0 + i], newest_kept); };
 
-  // ---- the kept-th largest key: its bits from the top
+  // ---- the kept-th largest key
   unsigned prefix = 0, need = kept, equal = 0;             // need: of the keys that share the prefix; equal: how many do
-#pragma unroll
+  int known = 0;                                           // bits of the prefix
   for (int level = 0; level < 3; ++level) {
-    const int shift = level == 0 ? 21 : level == 1 ? 10 : 0, bits = level == 2 ? 10 : 11;
-    for (int i = tid; i < kEvictBins; i += threads) hist[i] = 0;
-    __syncthreads();
-    for (int i = tid; i < s.len; i += threads) {
-      const unsigned k = key_at(i);
-      if (level == 0 || (k >> (shift + bits)) == prefix) atomicAdd(&hist[(k >> shift) & ((1u << bits) - 1)], 1u);
-    }
-    __syncthreads();
-    // bins from the top, consecutive ones to a thread
-    const int per = kEvictBins / threads, top = kEvictBins - 1 - tid * per;
-    unsigned mine = 0;
-    for (int i = 0; i < per; ++i) mine += hist[top - i];
-    unsigned total;
-    unsigned above = cta_scan(mine, warp_sums, &total);
-    if (above < need && need <= above + mine) {
-      int i = 0;
-      unsigned c = hist[top];
-      while (above + c < need) {
-        above += c;
-        ++i;
-        c = hist[top - i];
+    const int bits = level == 2 ? 10 : 11, shift = 32 - known - bits;
+    for (int i = tid; i < kEvictBins; i += kEvictThreads) sh.hist[i] = 0;
+    if (tid == 0) sh.n_few = 0;
+    sync();
+    if (level == 0 && cached) {
+      constexpr int kAtOnce = 4;
+      for (int i0 = tid; i0 < n; i0 += kAtOnce * kEvictThreads) {
+        float w[kAtOnce];
+        int p[kAtOnce];
+#pragma unroll
+        for (int e = 0; e < kAtOnce; ++e) {
+          const int i = min(i0 + e * kEvictThreads, n - 1);
+          w[e] = weight[c0 + i];
+          p[e] = pos[c0 + i];
+        }
+#pragma unroll
+        for (int e = 0; e < kAtOnce; ++e) {
+          const int i = i0 + e * kEvictThreads;
+          if (i >= n) break;
+          const unsigned k = evict_key(w[e], p[e], newest_kept);
+          keys[i] = k;
+          atomicAdd(&sh.hist[k >> 21], 1u);
+        }
       }
-      found[0] = top - i;
-      found[1] = need - above;
-      found[2] = c;
+    } else {
+      for (int i = tid; i < n; i += kEvictThreads) {
+        const unsigned k = key_at(i);
+        if (known == 0 || (k >> (32 - known)) == prefix) atomicAdd(&sh.hist[(k >> shift) & ((1u << bits) - 1)], 1u);
+      }
+    }
+    if constexpr (CLUSTER) {
+      __syncthreads();
+      if (rank != 0)
+        for (int i = tid; i < kEvictBins; i += kEvictThreads)
+          if (sh.hist[i]) atomicAdd(&first->hist[i], sh.hist[i]);
+      cluster.sync();
+    } else {
+      __syncthreads();
+    }
+    // bins from the top, consecutive ones to a thread
+    constexpr int kPer = kEvictBins / kEvictThreads;
+    const int top = kEvictBins - 1 - tid * kPer;
+    unsigned bin[kPer], mine = 0, total;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) mine += bin[i] = first->hist[top - i];
+    unsigned above = cta_scan(mine, sh.warp_sums, &total);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      if (above < need && need <= above + bin[i]) {
+        sh.found[0] = top - i;
+        sh.found[1] = need - above;
+        sh.found[2] = bin[i];
+      }
+      above += bin[i];
     }
     __syncthreads();
-    prefix = (prefix << bits) | found[0];
-    need = found[1];
-    equal = found[2];
+    prefix = (prefix << bits) | sh.found[0];
+    known += bits;
+    need = sh.found[1];
+    equal = sh.found[2];
+    if (known == 32 || equal <= kFewKeys) break;
+    sync();                                                  // the first CTA's histogram is read
+  }
+  if (known < 32) {                                          // few keys: which of them has need - 1 others above it?
+    for (int i = tid; i < n; i += kEvictThreads) {
+      const unsigned k = key_at(i);
+      if ((k >> (32 - known)) == prefix) first->few[atomicAdd(&first->n_few, 1u)] = k;
+    }
+    sync();
+    unsigned mine = 0, above = 0, same = 0;
+    if (tid < (int)equal) mine = first->few[tid];
+    const unsigned* few = CLUSTER ? sh.hist : sh.few;
+    if constexpr (CLUSTER) {                                 // a copy nearby: nobody reads a histogram any more
+      if (tid < (int)equal) sh.hist[tid] = mine;
+      __syncthreads();
+    }
+    if (tid < (int)equal) {
+      for (unsigned i = 0; i < equal; ++i) {
+        above += few[i] > mine;
+        same += few[i] == mine;
+      }
+      if (above < need && need <= above + same) {            // the same from every thread that has this key
+        sh.found[0] = mine;
+        sh.found[1] = need - above;
+        sh.found[2] = same;
+      }
+    }
     __syncthreads();
+    prefix = sh.found[0];
+    need = sh.found[1];
+    equal = sh.found[2];
   }
 
-  // ---- kept or not, in the order of the slots: holes among the first `kept`, rows to move behind them
-  int32_t *holes = a.holes + s.begin, *movers = a.movers + s.begin;
+  // ---- kept or not, in the order of the slots: holes among the first `kept`, rows to move behind them.  Where a CTA's begin
+  // follows from how many keys above and at the bound each CTA has on either side of slot `kept`.
   const bool ties = need < equal;
-  unsigned n_equal = 0, n_holes = 0, n_moves = 0;          // so far
+  unsigned n_equal = 0, n_holes = 0, n_moves = 0, all_moves = 0;      // of the CTAs before; then so far
+  if constexpr (CLUSTER) {
+    unsigned c[4] = {0, 0, 0, 0};                            // above / equal, before slot `kept` / behind
+    for (int i = tid; i < n; i += kEvictThreads) {
+      const unsigned k = key_at(i);
+      const int behind = c0 + i >= kept;
+      if (k > prefix) c[behind] += 1;
+      else if (k == prefix) c[2 + behind] += 1;
+    }
+    if (tid < 4) sh.counts[tid] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const unsigned x = __reduce_add_sync(0xffffffffu, c[e]);
+      if (lane == 0 && x) atomicAdd(&sh.counts[e], x);
+    }
+    cluster.sync();
+    unsigned eq = 0;                                         // keys at the bound so far
+    for (int r = 0; r < ctas; ++r) {
+      const unsigned* rc = cluster.map_shared_rank(&sh, r)->counts;
+      const int b = min(r * share, s.len), e = min(b + share, s.len);
+      const unsigned front = max(min(e, kept) - b, 0);       // its slots before `kept`
+      const unsigned eq_front = min(rc[2], need - min(eq, need)), eq_back = min(rc[3], need - min(eq + rc[2], need));
+      if (r == rank) n_equal = eq;
+      if (r < rank) {
+        n_holes += front - rc[0] - eq_front;
+        n_moves += rc[1] + eq_back;
+      }
+      all_moves += rc[1] + eq_back;
+      eq += rc[2] + rc[3];
+    }
+  }
+  int32_t *holes = a.holes + s.begin, *movers = a.movers + s.begin, *source = a.source + s.begin;
   constexpr int kItems = 4;
-  for (int i0 = 0; i0 < s.len; i0 += threads * kItems) {
+  for (int i0 = 0; i0 < n; i0 += kEvictThreads * kItems) {
     const int at = i0 + tid * kItems;
     unsigned k[kItems], eq = 0;
 #pragma unroll
     for (int e = 0; e < kItems; ++e) {
-      k[e] = at + e < s.len ? key_at(at + e) : 0u;
-      if (at + e < s.len && k[e] == prefix) eq |= 1u << e;
+      k[e] = at + e < n ? key_at(at + e) : 0u;
+      if (at + e < n && k[e] == prefix) eq |= 1u << e;
     }
-    unsigned rank = 0, total;
+    unsigned rank_of = 0, total;
     if (ties) {
-      rank = n_equal + cta_scan(__popc(eq), warp_sums, &total);
+      rank_of = n_equal + cta_scan(__popc(eq), sh.warp_sums, &total);
       n_equal += total;
     }
     unsigned hole = 0, mover = 0;
 #pragma unroll
     for (int e = 0; e < kItems; ++e) {
-      if (at + e >= s.len) break;
+      if (at + e >= n) break;
       bool keep = k[e] > prefix;
       if (eq >> e & 1) {
-        keep = !ties || rank < need;
-        ++rank;
+        keep = !ties || rank_of < need;
+        ++rank_of;
       }
-      if (at + e < kept) {
+      if (c0 + at + e < kept) {
         if (!keep) hole |= 1u << e;
-        source[at + e] = at + e;
       } else if (keep) {
         mover |= 1u << e;
       }
     }
-    const unsigned before = cta_scan(__popc(hole) | (__popc(mover) << 16), warp_sums, &total);   // at most 4096 of either
+    const unsigned before = cta_scan(__popc(hole) | (__popc(mover) << 16), sh.warp_sums, &total);      // at most 2048 of either
     unsigned nh = n_holes + (before & 0xffffu), nm = n_moves + (before >> 16);
 #pragma unroll
     for (int e = 0; e < kItems; ++e) {
-      if (hole >> e & 1) holes[nh++] = at + e;
-      if (mover >> e & 1) movers[nm++] = at + e;
+      const int slot = c0 + at + e;
+      if (at + e >= n) break;
+      if (mover >> e & 1) movers[nm++] = slot;
+      if (a.in_place) {
+        if (hole >> e & 1) holes[nh++] = slot;
+      } else if (slot < kept) {
+        source[slot] = hole >> e & 1 ? ~(int)nh++ : slot;
+      }
     }
     n_holes += total & 0xffffu;
     n_moves += total >> 16;
   }
-  __syncthreads();
-  for (unsigned i = tid; i < n_moves; i += threads) source[holes[i]] = movers[i];
-}
+  if (!CLUSTER) all_moves = n_moves;
+  __threadfence();                                           // the lists are read by other CTAs of the cluster
+  sync();
 
-// Kept rows to their places.  A warp looks at 32 slots; those whose row comes from elsewhere are moved together.
-template <int HD>
-__global__ void __launch_bounds__(256) k_q4_evict_move(const __grid_constant__ Q4EvictArgs a) {
-  constexpr int RB = q4_record_bytes(HD), kLanes = RB / 16, kAtOnce = 32 / kLanes;      // lanes per record, records at once
-  pdl_launch_dependents();
-  pdl_wait();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int seg = blockIdx.x / a.splits, split = blockIdx.x - seg * a.splits;
-  const int kept = a.kept[seg];
-  if (kept == 0) return;
-  const int from0 = q4_segment(a.from.starts, a.to.lens, seg, a.from.capacity).begin;
-  const int to0 = a.in_place ? from0 : q4_segment(a.to.starts, a.to.lens, seg, a.to.capacity).begin;
-  const int sub = lane / kLanes, part = lane - sub * kLanes;
-  for (int i0 = (split * 8 + warp) * 32; i0 < kept; i0 += a.splits * 256) {
-    const int i = i0 + lane;
-    const int src = i < kept ? a.source[from0 + i] : 0;
-    const bool moves = i < kept && !(a.in_place && src == i);
-    if (moves) {
-      a.to.pos[to0 + i] = a.from.pos[from0 + src];
-      a.to.weight[to0 + i] = a.from.weight[from0 + src];
+  // ---- the rows
+  if (a.in_place) {
+    for (int i = my_warp * per_warp; i < (int)all_moves; i += n_warps * per_warp) {
+      const int m = min(per_warp, (int)all_moves - i), j = i + min(lane, m - 1);
+      move_rows<HD>(a, m, s.begin + movers[j], s.begin + holes[j], lane);
     }
-    unsigned todo = __ballot_sync(0xffffffffu, moves);
-    while (todo) {
-      unsigned mine = todo;                                // the sub-th of them
-      for (int e = 0; e < sub && mine; ++e) mine &= mine - 1;
-      const int which = mine ? __ffs(mine) - 1 : 0;
-      const int row_src = __shfl_sync(0xffffffffu, src, which);
-      if (mine && sub < kAtOnce)
-        *reinterpret_cast<uint4*>(a.to.records + (long long)(to0 + i0 + which) * RB + part * 16) =
-            *reinterpret_cast<const uint4*>(a.from.records + (long long)(from0 + row_src) * RB + part * 16);
-#pragma unroll
-      for (int e = 0; e < kAtOnce; ++e) todo &= todo - 1;
+  } else {
+    const int rows = min(kept, d.room);
+    for (int i = my_warp * per_warp; i < rows; i += n_warps * per_warp) {
+      const int m = min(per_warp, rows - i), j = i + min(lane, m - 1);
+      int src = source[j];
+      if (src < 0) src = movers[~src];
+      move_rows<HD>(a, m, s.begin + src, d.begin + i + lane, lane);
     }
   }
 }
 
 size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 
+template <int HD>
+cudaError_t launch_evict(const Q4EvictArgs& a, cudaStream_t st) {
+  constexpr int kMostBytes = kMostKeys * (int)sizeof(unsigned);
+  const size_t smem = (size_t)a.key_room * sizeof(unsigned);
+  const dim3 grid((unsigned)(a.from.n_seg * a.ctas)), block(kEvictThreads);
+  auto kernel = a.ctas > 1 ? k_q4_evict<HD, true> : k_q4_evict<HD, false>;
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostBytes);
+  return e == cudaSuccess ? launch_pdl(kernel, grid, block, smem, st, a.ctas, a) : e;
+}
+
 }  // namespace
 
-size_t q4_evict_workspace(int n_seg, long long capacity) {
-  return 3 * up256((size_t)capacity * sizeof(int32_t)) + up256((size_t)n_seg * sizeof(int32_t));
-}
+size_t q4_evict_workspace(int n_seg, long long capacity) { return 3 * up256((size_t)capacity * sizeof(int32_t)); }
 
 cudaError_t launch_q4_evict(const Q4CacheView& from, const Q4CacheView& to, int n_kv_heads, int head_dim, const int32_t* budgets,
                             int window, const int32_t* newest, int32_t* status, void* workspace, cudaStream_t st, int* launches) {
@@ -226,27 +361,17 @@ cudaError_t launch_q4_evict(const Q4CacheView& from, const Q4CacheView& to, int 
   a.source = reinterpret_cast<int32_t*>(ws);
   a.holes = reinterpret_cast<int32_t*>(ws + rows);
   a.movers = reinterpret_cast<int32_t*>(ws + 2 * rows);
-  a.kept = reinterpret_cast<int32_t*>(ws + 3 * rows);
   a.n_kv_heads = n_kv_heads; a.window = window;
   a.in_place = from.records == to.records;
   const long long room = from.capacity / from.n_seg;       // of an average segment
-  const int threads = room <= 2048 ? 256 : room <= 16384 ? 512 : 1024;
-  a.key_room = 2048;
-  while (a.key_room < 2 * room && a.key_room < kMostKeys) a.key_room *= 2;
+  // CTAs per segment: as many as the device holds beside the other segments, but some 2000 slots for each
+  a.ctas = 1;
+  while (a.ctas < kEvictCluster && 2ll * a.ctas * from.n_seg <= 2 * sm_count() && room >= 4096ll * a.ctas) a.ctas *= 2;
+  a.key_room = 2048;                                       // for segments of up to twice the average
+  while (a.key_room < 2 * room / a.ctas && a.key_room < kMostKeys) a.key_room *= 2;
   if (a.key_room > kMostKeys) a.key_room = kMostKeys;
-  cudaError_t e = cudaFuncSetAttribute(k_q4_evict_select, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostKeys * (int)sizeof(unsigned));
-  if (e != cudaSuccess) return e;
-  {
-    LaunchScope scope(KID_Q4_EVICT, st, launches);
-    e = launch_pdl(k_q4_evict_select, dim3((unsigned)from.n_seg), dim3((unsigned)threads), (size_t)a.key_room * sizeof(unsigned), st, 1, a);
-  }
-  if (e != cudaSuccess) return e;
-  const long long want = (room + 255) / 256, most = 65535ll * 16 / from.n_seg;
-  a.splits = (int)(want < 1 ? 1 : want < 256 ? want : 256);
-  if (a.splits > most) a.splits = (int)(most < 1 ? 1 : most);
   LaunchScope scope(KID_Q4_EVICT, st, launches);
-  return launch_pdl(head_dim == 128 ? k_q4_evict_move<128> : k_q4_evict_move<64>, dim3((unsigned)(from.n_seg * a.splits)), dim3(256),
-                    0, st, 1, a);
+  return head_dim == 128 ? launch_evict<128>(a, st) : launch_evict<64>(a, st);
 }
 
 }  // namespace slkv

@@ -34,7 +34,7 @@ def quantise_row(x):
         s = bf16_towards(float(np.float32(span) / np.float32(15.0)), up=True)
         scale[j], zero[j] = s, z
         if s > 0:
-            codes[32 * j:32 * j + 32] = np.clip(np.rint((g - z) / s), 0, 15)
+            codes[32 * j:32 * j + 32] = np.rint((g.astype(np.float32) - np.float32(z)) / np.float32(s))
     return codes, scale, zero
 
 
