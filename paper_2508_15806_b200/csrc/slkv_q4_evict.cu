@@ -2,12 +2,13 @@
 // largest accumulated weights.
 //
 // Rows are ranked by 32-bit keys -- the newest rows first, then by weight, NaN last -- and a segment's kept rows are the
-// `kept` largest, ties to the lower slot.  The kept-th largest key comes from a histogram of the keys' upper 11 bits, a second
-// and a third one where many keys share them, and as soon as few do from counting, for each of these, how many are above it.
+// `kept` largest, ties to the lower slot.  The kept-th largest key comes from a histogram with 64 bins to an octave -- that many, so
+// that few lanes of a warp meet in a bin -- and from counting, for each of the keys in its bin, how many are above it.  Where a
+// bin holds too many for that (weights that are all alike, or far out) their bits are descended, 11 + 11 + 10 of them.
 // The kept rows that lie behind the first `kept` slots then fill the holes before them, in order, so that as few rows move as
 // can, no row is read that another one overwrites, and a cache can be evicted from in place.
 // One launch: a cluster of CTAs per segment (one CTA where there are many segments or few rows), each with a contiguous share
-// of the slots, keys in shared memory; they add up their histograms in the first CTA's and share the moves evenly.
+// of the slots, keys in shared memory; they share the moves evenly.
 // What bounds it: for few rows the chain of passes over the keys, for many the rows' bytes.
 #include <cooperative_groups.h>
 
@@ -38,6 +39,24 @@ __device__ __forceinline__ unsigned evict_key(float weight, int pos, long long n
   if (weight != weight) return 0u;
   const unsigned b = __float_as_uint(weight + 0.0f);       // -0 as 0
   return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+
+// First histogram: bins between 2^-22 and 2^10, the lowest for everything below, the highest for everything above.
+__device__ __forceinline__ unsigned octave_bin(unsigned key) {
+  constexpr unsigned kShift = 17, kFloor = 0x80000000u + ((127u - 22u) << 23) - (1u << kShift);
+  return min((max(key, kFloor) - kFloor) >> kShift, kEvictBins - 1u);
+}
+
+// Adds one to the lanes' bins; all lanes in one bin (rows that nobody looked at) as one.  Whole warp.
+__device__ __forceinline__ void count_bin(unsigned* hist, unsigned bin, bool valid) {
+  const unsigned all = __ballot_sync(0xffffffffu, valid), lead = all ? __ffs(all) - 1 : 0;
+  const unsigned of_lead = __shfl_sync(0xffffffffu, bin, lead);               // by all lanes, valid or not
+  const bool alike = __all_sync(0xffffffffu, !valid || bin == of_lead);
+  if (alike) {
+    if (all && (threadIdx.x & 31) == lead) atomicAdd(&hist[bin], (unsigned)__popc(all));
+  } else if (valid) {
+    atomicAdd(&hist[bin], 1u);
+  }
 }
 
 // Exclusive prefix sum over the CTA; *total: of all.
@@ -92,7 +111,7 @@ __device__ __forceinline__ void move_rows(const Q4EvictArgs& a, int n, int src, 
 }
 
 struct EvictShared {
-  unsigned hist[kEvictBins];            // of the CTA's keys; the cluster's in the first CTA's
+  alignas(16) unsigned hist[kEvictBins];   // of the CTA's keys
   unsigned few[kFewKeys];               // the first CTA's: the keys that share the prefix
   unsigned warp_sums[32];
   unsigned found[3], n_few;
@@ -138,54 +157,55 @@ __global__ void __launch_bounds__(kEvictThreads, 2) k_q4_evict(const __grid_cons
   auto key_at = [&](int i) { return cached ? keys[i] : evict_key(weight[c0 + i], pos[c0 + i], newest_kept); };
 
   // ---- the kept-th largest key
-  unsigned prefix = 0, need = kept, equal = 0;             // need: of the keys that share the prefix; equal: how many do
-  int known = 0;                                           // bits of the prefix
-  for (int level = 0; level < 3; ++level) {
-    const int bits = level == 2 ? 10 : 11, shift = 32 - known - bits;
+  unsigned prefix = 0, need = kept, equal = 0;             // need: of the keys that are looked at; equal: how many there are
+  unsigned octave = 0;                                     // those in this bin of the first histogram
+  int known = 0;                                           // and with this many bits of the prefix
+  for (int level = 0;; ++level) {
+    const int bits = level == 3 ? 10 : 11, shift = 32 - known - bits;
     for (int i = tid; i < kEvictBins; i += kEvictThreads) sh.hist[i] = 0;
     if (tid == 0) sh.n_few = 0;
     sync();
-    if (level == 0 && cached) {
-      constexpr int kAtOnce = 4;
-      for (int i0 = tid; i0 < n; i0 += kAtOnce * kEvictThreads) {
+    constexpr int kAtOnce = 4;
+    for (int i0 = 0; i0 < n; i0 += kAtOnce * kEvictThreads) {
+      unsigned k[kAtOnce];
+      if (level == 0) {
         float w[kAtOnce];
         int p[kAtOnce];
 #pragma unroll
         for (int e = 0; e < kAtOnce; ++e) {
-          const int i = min(i0 + e * kEvictThreads, n - 1);
+          const int i = min(i0 + e * kEvictThreads + tid, n - 1);
           w[e] = weight[c0 + i];
           p[e] = pos[c0 + i];
         }
 #pragma unroll
-        for (int e = 0; e < kAtOnce; ++e) {
-          const int i = i0 + e * kEvictThreads;
-          if (i >= n) break;
-          const unsigned k = evict_key(w[e], p[e], newest_kept);
-          keys[i] = k;
-          atomicAdd(&sh.hist[k >> 21], 1u);
+        for (int e = 0; e < kAtOnce; ++e) k[e] = evict_key(w[e], p[e], newest_kept);
+      }
+#pragma unroll
+      for (int e = 0; e < kAtOnce; ++e) {
+        const int i = i0 + e * kEvictThreads + tid;
+        if (i0 + e * kEvictThreads >= n) break;
+        if (level == 0) {
+          if (cached && i < n) keys[i] = k[e];
+          count_bin(sh.hist, octave_bin(k[e]), i < n);
+        } else {
+          const unsigned x = i < n ? key_at(i) : 0u;
+          const bool in = i < n && octave_bin(x) == octave && (known == 0 || (x >> (32 - known)) == prefix);
+          count_bin(sh.hist, (x >> shift) & ((1u << bits) - 1), in);
         }
       }
-    } else {
-      for (int i = tid; i < n; i += kEvictThreads) {
-        const unsigned k = key_at(i);
-        if (known == 0 || (k >> (32 - known)) == prefix) atomicAdd(&sh.hist[(k >> shift) & ((1u << bits) - 1)], 1u);
-      }
     }
-    if constexpr (CLUSTER) {
-      __syncthreads();
-      if (rank != 0)
-        for (int i = tid; i < kEvictBins; i += kEvictThreads)
-          if (sh.hist[i]) atomicAdd(&first->hist[i], sh.hist[i]);
-      cluster.sync();
-    } else {
-      __syncthreads();
-    }
-    // bins from the top, consecutive ones to a thread
+    sync();
+    // bins from the top, four to a thread: each CTA reads and adds up all CTAs' (adding into the first CTA's instead took 12 us)
     constexpr int kPer = kEvictBins / kEvictThreads;
+    static_assert(kPer == 4, "one 16-byte load");
     const int top = kEvictBins - 1 - tid * kPer;
-    unsigned bin[kPer], mine = 0, total;
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) mine += bin[i] = first->hist[top - i];
+    unsigned bin[kPer] = {0, 0, 0, 0}, total;
+    for (int r = 0; r < ctas; ++r) {
+      const EvictShared* of = CLUSTER ? cluster.map_shared_rank(&sh, r) : &sh;
+      const uint4 x = *reinterpret_cast<const uint4*>(&of->hist[top - 3]);
+      bin[0] += x.w; bin[1] += x.z; bin[2] += x.y; bin[3] += x.x;
+    }
+    const unsigned mine = (bin[0] + bin[1]) + (bin[2] + bin[3]);
     unsigned above = cta_scan(mine, sh.warp_sums, &total);
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
@@ -197,17 +217,21 @@ __global__ void __launch_bounds__(kEvictThreads, 2) k_q4_evict(const __grid_cons
       above += bin[i];
     }
     __syncthreads();
-    prefix = (prefix << bits) | sh.found[0];
-    known += bits;
+    if (level == 0) {
+      octave = sh.found[0];
+    } else {
+      prefix = (prefix << bits) | sh.found[0];
+      known += bits;
+    }
     need = sh.found[1];
     equal = sh.found[2];
     if (known == 32 || equal <= kFewKeys) break;
-    sync();                                                  // the first CTA's histogram is read
+    sync();                                                  // the histograms are read
   }
   if (known < 32) {                                          // few keys: which of them has need - 1 others above it?
     for (int i = tid; i < n; i += kEvictThreads) {
       const unsigned k = key_at(i);
-      if ((k >> (32 - known)) == prefix) first->few[atomicAdd(&first->n_few, 1u)] = k;
+      if (octave_bin(k) == octave && (known == 0 || (k >> (32 - known)) == prefix)) first->few[atomicAdd(&first->n_few, 1u)] = k;
     }
     sync();
     unsigned mine = 0, above = 0, same = 0;
