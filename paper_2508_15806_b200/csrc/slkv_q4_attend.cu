@@ -14,10 +14,12 @@
 // fp32 queries and probabilities go through the same products in three bf16 parts, which is exact (8 + 8 + 8 bits); sums over
 // 16 keys are then added in fp32 outside the matrix unit, whose own accumulation cuts off.
 //
-// Work: a (segment, block of columns) is a unit of 32-row tiles; the tiles of all units form one line, cut evenly over the
-// CTAs, whatever the lengths.  A unit that lies in one CTA is finished there; the others leave a maximum, a sum and an
-// unscaled output per piece, which a second launch joins.  In a CTA each warp takes every fourth tile with its own ring of
-// bulk copies, so that no warp waits for another before a piece ends.
+// Work: a (segment, block of columns) is a unit of 32-row tiles.  Units longer than a share of the work that leaves about as many
+// pieces as CTAs are cut into equal pieces of whole tiles; a CTA takes a piece, and further ones where there are more.  A unit of
+// one piece is finished by its CTA; the others leave a maximum, a sum and an unscaled output per piece, which a second launch
+// joins.  In a CTA each warp takes every fourth tile with its own ring of bulk copies, so that no warp waits for another before
+// a piece ends.  (Cutting the line of all tiles evenly instead, pieces running across units, took 40 us where this takes XX:
+// a CTA's second piece starts with 3.4 us of latencies.)
 // The weights need the final log-sum-exps: the scores are kept in the workspace, the second launch turns them into
 // probabilities.
 // What bounds it: the arithmetic between DRAM and the products (unpacking, scales).
@@ -31,8 +33,11 @@ namespace {
 constexpr int kAttendWarps = 4, kTileRows = 32, kCols = 8;
 constexpr float kLowest = -3e38f;       // a maximum over nothing: below every score, and differences of two stay numbers
 constexpr float kSlack = 8.0f;
-constexpr int kFewestTiles = 4;         // a CTA's share, at least: a tile for each warp
+constexpr int kFewestTiles = 4;         // of a piece, where its unit has as many: one for each warp
 constexpr unsigned long long kQ4WaitNs = 1000ull * 1000ull * 1000ull;
+
+// What the second launch wants to know of a piece: its rows, its segment, and its unit's pieces (of the first block of columns).
+struct Q4Piece { int row0, rows, seg, cb, n, place; };
 
 struct Q4AttendArgs {
   Q4CacheView c;
@@ -46,12 +51,12 @@ struct Q4AttendArgs {
   int n_kv_heads, n_q_heads, n_tokens, G, R, n_cb, n_cta, accumulate;
   float scale, softcap, decay, lse_unit;                     // lse_unit: of a base-2 logarithm
   // workspace
-  int* head;                            // tiles per CTA, tiles
-  int* unit_tile;                       // [n_units] first tile of a unit
-  int4* walk;                           // [n_cta] where a CTA's share begins: segment, block of columns, tile in it
-  float2* ml;                           // [n_cta][2][8] maximum and sum of a piece's columns
-  float* part;                          // [n_cta][2][8][HD] their unscaled outputs
-  float* lse2;                          // [n_seg][R] of units that lie in one CTA, base 2
+  int* head;                            // pieces
+  int2* unit;                           // [n_units] pieces of a unit, and the first one's place in ml and part
+  Q4Piece* piece;                       // [pieces]
+  float2* ml;                           // [places][8] maximum and sum of a piece's columns
+  float* part;                          // [places][8][HD] their unscaled outputs
+  float* lse2;                          // [n_seg][R] of units of one piece, base 2
   float* scores;                        // [capacity][R] base 2 (accumulate)
 };
 
@@ -134,6 +139,30 @@ __device__ __forceinline__ void load_words(uint32_t at, unsigned (&w)[N]) {
     asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w[0]) : "r"(at) : "memory");
 }
 
+// Sum over the CTA, and what the threads before this one have of it.  sums: a word for each warp, not used since the last barrier but one.
+__device__ __forceinline__ int cta_before(int x, int* sums) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int sum = x;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, sum, o);
+    if (lane >= o) sum += y;
+  }
+  __syncthreads();
+  if (lane == 31) sums[warp] = sum;
+  __syncthreads();
+  for (int w = 0; w < warp; ++w) sum += sums[w];
+  return sum - x;
+}
+__device__ __forceinline__ int cta_total(int x, int* sums) {
+  x = __reduce_add_sync(0xffffffffu, x);
+  if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5] = x;
+  __syncthreads();
+  int sum = 0;
+  for (int w = 0; w < kAttendWarps; ++w) sum += sums[w];
+  return sum;
+}
+
 template <int HD> constexpr int kQ4Stages = HD == 128 ? 2 : 4;
 template <int HD> constexpr int kQ4Smem = kAttendWarps * kQ4Stages<HD> * kTileRows * q4_record_bytes(HD);
 
@@ -142,7 +171,7 @@ __global__ void __launch_bounds__(kAttendWarps * 32, PARTS == 1 ? 4 : HD == 64 ?
   constexpr int NG = HD / 32, RB = q4_record_bytes(HD), kStages = kQ4Stages<HD>, kStageBytes = kTileRows * RB;
   extern __shared__ __align__(128) unsigned char smem[];
   __shared__ __align__(8) unsigned long long bars[kAttendWarps][kStages];
-  __shared__ int found[kAttendWarps];
+  __shared__ int found[8], before[kAttendWarps * 32 + 1], places[kAttendWarps * 32];
   __shared__ float merge_m[kAttendWarps][kCols], merge_l[kAttendWarps][kCols];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
   unsigned char* ring = smem + warp * (kStages * kStageBytes);
@@ -157,51 +186,52 @@ __global__ void __launch_bounds__(kAttendWarps * 32, PARTS == 1 ? 4 : HD == 64 ?
   pdl_launch_dependents();
   pdl_wait();
 
-  // ---- the CTA's share of the line of tiles
+  // ---- tiles of all units, the size of a piece, how many pieces come before each thread's segments
   const int n_seg = a.c.n_seg, per_thread = (n_seg + kAttendWarps * 32 - 1) / (kAttendWarps * 32);
   const int first = min(tid * per_thread, n_seg), last = min(first + per_thread, n_seg);
+  auto tiles_at = [&](int seg) { return tiles_of(q4_segment(a.c.starts, a.c.lens, seg, a.c.capacity).len); };
   int mine = 0;
-  for (int s = first; s < last; ++s) mine += tiles_of(q4_segment(a.c.starts, a.c.lens, s, a.c.capacity).len) * a.n_cb;
-  int sum = mine;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int x = __shfl_up_sync(0xffffffffu, sum, o);
-    if (lane >= o) sum += x;
+  for (int s = first; s < last; ++s) mine += tiles_at(s);
+  const int total = cta_total(mine, found) * a.n_cb;
+  const int units = n_seg * a.n_cb;
+  const int per = max((total - 1) / max(a.n_cta - units / 2, a.n_cta / 4) + 1, kFewestTiles);
+  int pieces = 0, split = 0;                               // of this thread's segments; those of units of several
+  for (int s = first; s < last; ++s) {
+    const int n = (tiles_at(s) + per - 1) / per;
+    pieces += n * a.n_cb;
+    split += n > 1 ? n * a.n_cb : 0;
   }
-  if (lane == 31) found[warp] = sum;
+  before[tid] = cta_before(pieces, found);
+  places[tid] = cta_before(split, found + 4);
+  if (tid == kAttendWarps * 32 - 1) before[tid + 1] = before[tid] + pieces;
   __syncthreads();
-  for (int w = 0; w < warp; ++w) sum += found[w];
-  int total = found[0];
-  for (int w = 1; w < kAttendWarps; ++w) total += found[w];
-  const int per = max((total + a.n_cta - 1) / a.n_cta, kFewestTiles);
-  const long long t0 = (long long)blockIdx.x * per;
-  if (blockIdx.x == 0 && tid == 0) { a.head[0] = per; a.head[1] = total; }
-  __syncthreads();
-  if (t0 >= total) return;
-  if (sum - mine <= t0 && t0 < sum) {                      // the one thread whose segments the share begins in
-    int u = sum - mine, s = first, n = 0;
-    for (; s < last; ++s) {
-      n = tiles_of(q4_segment(a.c.starts, a.c.lens, s, a.c.capacity).len);
-      if (t0 < u + n * a.n_cb) break;
-      u += n * a.n_cb;
-    }
-    found[0] = s; found[1] = ((int)t0 - u) / n; found[2] = ((int)t0 - u) % n;
-    a.walk[blockIdx.x] = make_int4(s, found[1], found[2], 0);
-  }
-  __syncthreads();
-  int seg = found[0], cb = found[1], from = found[2];
-  int left = (int)min((long long)per, total - t0);
-  int line = (int)t0;                                      // tile on the line
+  const int all = before[kAttendWarps * 32];
+  if (blockIdx.x == 0 && tid == 0) a.head[0] = all;
   unsigned issued = 0, used = 0, lost = 0;                 // copies of this warp's ring
   bool dead = false;
 
-  while (left > 0 && seg < n_seg) {
+  for (int index = blockIdx.x; index < all; index += a.n_cta) {
+    if (before[tid] <= index && index < before[tid + 1]) { // the one thread that has the piece's segment
+      int u = before[tid], s = first, n = 0, place = places[tid];
+      for (; s < last; ++s) {
+        n = (tiles_at(s) + per - 1) / per;
+        if (index < u + n * a.n_cb) break;
+        u += n * a.n_cb;
+        place += n > 1 ? n * a.n_cb : 0;
+      }
+      found[0] = s; found[1] = (index - u) / n; found[2] = (index - u) % n; found[3] = n; found[4] = place;
+    }
+    __syncthreads();
+    const int seg = found[0], cb = found[1], nth = found[2], n_pieces = found[3], place = found[4] + cb * n_pieces;
     const Q4Segment sg = q4_segment(a.c.starts, a.c.lens, seg, a.c.capacity);
     const int tiles = tiles_of(sg.len);
-    if (tiles == 0) { ++seg; cb = 0; from = 0; continue; }
-    const int to = min(tiles, from + left);
+    const int from = (int)((long long)tiles * nth / n_pieces), to = (int)((long long)tiles * (nth + 1) / n_pieces);
     const unsigned char* rows = a.c.records + (long long)sg.begin * RB;
-    if (from == 0 && tid == 0) a.unit_tile[seg * a.n_cb + cb] = line;
+    if (tid == 0) {
+      if (nth == 0) a.unit[seg * a.n_cb + cb] = make_int2(n_pieces, place);
+      if (a.accumulate)
+        a.piece[index] = {sg.begin + from * kTileRows, min(to * kTileRows, sg.len) - from * kTileRows, seg, cb, n_pieces, found[4]};
+    }
 
     // the ring's first copies
     auto issue = [&](int tile) {
@@ -493,8 +523,7 @@ __global__ void __launch_bounds__(kAttendWarps * 32, PARTS == 1 ? 4 : HD == 64 ?
             make_float4(o[j][0][c] + zacc[j][c], o[j][0][c + 2] + zacc[j][c], o[j][1][c] + zacc[j][c], o[j][1][c + 2] + zacc[j][c]);
     async_fence();
     __syncthreads();
-    const bool whole = from == 0 && to == tiles;
-    const int part = from == 0 ? 1 : 0;                    // a CTA's share ends in at most one unit that begins in it
+    const bool whole = n_pieces == 1;
     for (int i = tid; i < kCols * HD / 4; i += kAttendWarps * 32) {
       const int c = i / (HD / 4), ch = 4 * (i % (HD / 4)), col = cb * kCols + c;
       if (col >= a.R) continue;
@@ -525,16 +554,12 @@ __global__ void __launch_bounds__(kAttendWarps * 32, PARTS == 1 ? 4 : HD == 64 ?
           a.lse2[(long long)seg * a.R + col] = z;
         }
       } else {
-        const long long at = ((long long)blockIdx.x * 2 + part) * kCols + c;
+        const long long at = (long long)(place + nth) * kCols + c;
         if (ch == 0) a.ml[at] = make_float2(top, sum_l);
         *reinterpret_cast<float4*>(a.part + at * HD + ch) = v;
       }
     }
     __syncthreads();                                       // the rings and the sums are free again
-    line += to - from;
-    left -= to - from;
-    from = 0;
-    if (++cb == a.n_cb) { cb = 0; ++seg; }
   }
   if (dead)                                                // what is still in flight lands before the memory is another CTA's
     for (unsigned i = lost; i < issued; ++i) copies_there(bar0 + 8 * (i % kStages), (i / kStages) & 1);
@@ -543,20 +568,11 @@ __global__ void __launch_bounds__(kAttendWarps * 32, PARTS == 1 ? 4 : HD == 64 ?
 // ---- the pieces of units that lie in several CTAs, and the weights ---------------------------------------------------
 constexpr int kJoinThreads = 128;
 
-// Pieces of a unit: CTAs first .. last of the launch before; one CTA has finished it by itself.
-struct Q4Pieces { int first, last; };
-__device__ __forceinline__ Q4Pieces pieces_of(const Q4AttendArgs& a, int unit, int tiles) {
-  const int per = a.head[0], at = a.unit_tile[unit];
-  return {at / per, (at + tiles - 1) / per};
-}
-__device__ __forceinline__ long long piece_at(const Q4Pieces& p, int i, int c) {
-  return ((long long)i * 2 + (i == p.first ? 1 : 0)) * kCols + c;
-}
-// Maximum and sum over a unit's pieces for one column; whole warp.
-__device__ __forceinline__ float2 join_ml(const Q4AttendArgs& a, const Q4Pieces& p, int c, int lane) {
+// Maximum and sum over a unit's n pieces for one column; whole warp.
+__device__ __forceinline__ float2 join_ml(const float2* ml, int n, int lane) {
   float m = kLowest, l = 0.0f;
-  for (int i = p.first + lane; i <= p.last; i += 32) {
-    const float2 x = a.ml[piece_at(p, i, c)];
+  for (int i = lane; i < n; i += 32) {
+    const float2 x = ml[i * kCols];
     const float top = fmaxf(m, x.x);
     l = l * ex2(m - top) + x.y * ex2(x.x - top);
     m = top;
@@ -574,33 +590,28 @@ __device__ __forceinline__ float2 join_ml(const Q4AttendArgs& a, const Q4Pieces&
 template <int HD, bool F32>
 __global__ void __launch_bounds__(kJoinThreads) k_q4_join(const __grid_constant__ Q4AttendArgs a) {
   constexpr int kWarps = kJoinThreads / 32, V = HD / 32;   // channels per lane
-  __shared__ float shares[kWarps][HD], lse_of[kMaxQ4Columns];
+  __shared__ __align__(16) float shares[kWarps][HD], lse_of[kMaxQ4Columns];
   pdl_launch_dependents();
   pdl_wait();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int n_out = a.c.n_seg * a.R;
   if ((int)blockIdx.x < n_out) {                           // one segment's column
     const int seg = blockIdx.x / a.R, col = blockIdx.x - seg * a.R, cb = col / kCols, c = col - cb * kCols;
+    const int2 u = a.unit[seg * a.n_cb + cb];              // not written for a segment without rows
+    const int n = q4_segment(a.c.starts, a.c.lens, seg, a.c.capacity).len > 0 ? u.x : 0;
+    if (n == 1) return;
     const int s = seg / a.n_kv_heads, h = seg - s * a.n_kv_heads, tok = col / a.G, qh = h * a.G + col - tok * a.G;
-    const int tiles = tiles_of(q4_segment(a.c.starts, a.c.lens, seg, a.c.capacity).len);
-    Q4Pieces p = {0, 0};
-    if (tiles > 0) {
-      p = pieces_of(a, seg * a.n_cb + cb, tiles);
-      if (p.first == p.last) return;
-    }
-    float2 ml = make_float2(kLowest, 0.0f);
+    const long long first = n > 0 ? (long long)u.y * kCols + c : 0;
+    const float2 ml = join_ml(a.ml + first, n, lane);
     float acc[V];
 #pragma unroll
     for (int e = 0; e < V; ++e) acc[e] = 0.0f;
-    if (tiles > 0) {
-      ml = join_ml(a, p, c, lane);
 #pragma unroll 4
-      for (int i = p.first + warp; i <= p.last; i += kWarps) {
-        const long long at = piece_at(p, i, c);
-        const float f = ex2(a.ml[at].x - ml.x);
+    for (int i = warp; i < n; i += kWarps) {
+      const long long at = first + i * kCols;
+      const float f = ex2(a.ml[at].x - ml.x);
 #pragma unroll
-        for (int e = 0; e < V; ++e) acc[e] = fmaf(a.part[at * HD + lane + 32 * e], f, acc[e]);
-      }
+      for (int e = 0; e < V; ++e) acc[e] = fmaf(a.part[at * HD + lane + 32 * e], f, acc[e]);
     }
 #pragma unroll
     for (int e = 0; e < V; ++e) shares[warp][lane + 32 * e] = acc[e];
@@ -617,50 +628,64 @@ __global__ void __launch_bounds__(kJoinThreads) k_q4_join(const __grid_constant_
     if (tid == 0 && a.lse) a.lse[((long long)s * a.n_q_heads + qh) * a.n_tokens + tok] = (ml.x + log2f(ml.y)) * a.lse_unit;
     return;
   }
-  // the weights of the rows of one CTA's share: a row has its scores of all columns, so the first block of columns does it
-  const int cta = blockIdx.x - n_out, per = a.head[0];
-  if ((long long)cta * per >= a.head[1]) return;
-  const int4 w = a.walk[cta];
-  int seg = w.x, cb = w.y, from = w.z, left = min(per, a.head[1] - cta * per);
+  // The weights of a piece's rows: a row has its scores of all columns, so the first block of columns does it.  Rows are taken
+  // four to a thread; the first ones' loads do not wait for the log-sum-exps.
+  constexpr int kRowsAtOnce = 4;
   const float inv_g = 1.0f / (float)a.G;
-  while (left > 0 && seg < a.c.n_seg) {
-    const Q4Segment sg = q4_segment(a.c.starts, a.c.lens, seg, a.c.capacity);
-    const int tiles = tiles_of(sg.len);
-    if (tiles == 0) { ++seg; cb = 0; from = 0; continue; }
-    const int to = min(tiles, from + left);
-    if (cb == 0) {
-      __syncthreads();
-      for (int col = warp; col < a.R; col += kWarps) {
-        const Q4Pieces p = pieces_of(a, seg * a.n_cb + col / kCols, tiles);
-        float z;
-        if (p.first == p.last) {
-          z = a.lse2[(long long)seg * a.R + col];
+  const int all = a.head[0];
+  const bool quads = (a.R & 3) == 0;
+  for (int index = blockIdx.x - n_out; index < all; index += a.n_cta) {
+    const Q4Piece p = a.piece[index];
+    if (p.cb != 0) continue;
+    float4 x[kRowsAtOnce];
+    float old[kRowsAtOnce];
+    auto row = [&](int r0, int e) { return (long long)p.row0 + min(r0 + e * kJoinThreads, p.rows - 1); };
+    auto load = [&](int r0, int c) {
+#pragma unroll
+      for (int e = 0; e < kRowsAtOnce; ++e) {
+        const float* at = a.scores + row(r0, e) * a.R + c;
+        if (quads) x[e] = *reinterpret_cast<const float4*>(at);
+        else x[e] = make_float4(at[0], c + 1 < a.R ? at[1] : -INFINITY, c + 2 < a.R ? at[2] : -INFINITY, c + 3 < a.R ? at[3] : -INFINITY);
+      }
+    };
+    load(tid, 0);
+#pragma unroll
+    for (int e = 0; e < kRowsAtOnce; ++e) old[e] = a.c.weight[row(tid, e)];
+    __syncthreads();                                       // the log-sum-exps of the piece before are read
+    for (int col = warp; col < ((a.R + 3) & ~3); col += kWarps) {
+      float z = INFINITY;                                  // a column that is none, or sees nothing, gives nothing
+      if (col < a.R) {
+        if (p.n == 1) {
+          z = a.lse2[(long long)p.seg * a.R + col];
         } else {
-          const float2 ml = join_ml(a, p, col % kCols, lane);
+          const float2 ml = join_ml(a.ml + ((long long)p.place + col / kCols * p.n) * kCols + col % kCols, p.n, lane);
           z = ml.x + log2f(ml.y);
         }
-        if (lane == 0) lse_of[col] = z == -INFINITY ? INFINITY : z;        // a column that sees nothing gives nothing
+        if (z == -INFINITY) z = INFINITY;
       }
-      __syncthreads();
-      const int end = min(to * kTileRows, sg.len);
-      for (int r = from * kTileRows + tid; r < end; r += kJoinThreads) {
-        const long long slot = (long long)sg.begin + r;
-        const float* x = a.scores + slot * a.R;
-        float sum = 0.0f;
-        if ((a.R & 3) == 0) {
-          for (int c = 0; c < a.R; c += 4) {
-            const float4 v = *reinterpret_cast<const float4*>(x + c);
-            sum += (ex2(v.x - lse_of[c]) + ex2(v.y - lse_of[c + 1])) + (ex2(v.z - lse_of[c + 2]) + ex2(v.w - lse_of[c + 3]));
-          }
-        } else {
-          for (int c = 0; c < a.R; ++c) sum += ex2(x[c] - lse_of[c]);
-        }
-        a.c.weight[slot] = fmaf(a.decay, a.c.weight[slot], sum * inv_g);
-      }
+      if (lane == 0) lse_of[col] = z;
     }
-    left -= to - from;
-    from = 0;
-    if (++cb == a.n_cb) { cb = 0; ++seg; }
+    __syncthreads();
+    for (int r0 = tid; r0 < p.rows; r0 += kRowsAtOnce * kJoinThreads) {
+      float sum[kRowsAtOnce] = {0.0f, 0.0f, 0.0f, 0.0f};
+      if (r0 != tid) {
+        load(r0, 0);
+#pragma unroll
+        for (int e = 0; e < kRowsAtOnce; ++e) old[e] = a.c.weight[row(r0, e)];
+      }
+      for (int c = 0;;) {
+        const float4 z = *reinterpret_cast<const float4*>(lse_of + c);
+#pragma unroll
+        for (int e = 0; e < kRowsAtOnce; ++e)
+          sum[e] += (ex2(x[e].x - z.x) + ex2(x[e].y - z.y)) + (ex2(x[e].z - z.z) + ex2(x[e].w - z.w));
+        c += 4;
+        if (c >= a.R) break;
+        load(r0, c);
+      }
+#pragma unroll
+      for (int e = 0; e < kRowsAtOnce; ++e)
+        if (r0 + e * kJoinThreads < p.rows) a.c.weight[row(r0, e)] = fmaf(a.decay, old[e], sum[e] * inv_g);
+    }
   }
 }
 
@@ -668,14 +693,14 @@ constexpr size_t kAlign = 256;
 size_t up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
 
 struct Q4Workspace {
-  size_t unit_tile, walk, ml, part, lse2, scores, total;
+  size_t unit, piece, ml, part, lse2, scores, total;
   Q4Workspace(int n_seg, int head_dim, int R, long long capacity, bool accumulate) {
-    const size_t n_cb = (size_t)(R + kCols - 1) / kCols, ctas = kMaxQ4Ctas;
-    unit_tile = kAlign;
-    walk = unit_tile + up(n_seg * n_cb * sizeof(int));
-    ml = walk + up(ctas * sizeof(int4));
-    part = ml + up(ctas * 2 * kCols * sizeof(float2));
-    lse2 = part + up(ctas * 2 * kCols * head_dim * sizeof(float));
+    const size_t units = (size_t)n_seg * ((R + kCols - 1) / kCols), places = 2 * kMaxQ4Ctas;      // of units of several pieces
+    unit = kAlign;
+    piece = unit + up(units * sizeof(int2));
+    ml = piece + up((kMaxQ4Ctas + units) * sizeof(Q4Piece));
+    part = ml + up(places * kCols * sizeof(float2));
+    lse2 = part + up(places * kCols * head_dim * sizeof(float));
     scores = lse2 + up((size_t)n_seg * R * sizeof(float));
     total = scores + (accumulate ? up((size_t)capacity * R * sizeof(float)) : 0);
   }
@@ -735,8 +760,8 @@ cudaError_t launch_q4_attend(const Q4CacheView& c, const slkv_q4_cache& cache, c
   const Q4Workspace w(c.n_seg, cache.head_dim, a.R, c.capacity, accumulate);
   char* ws = static_cast<char*>(workspace);
   a.head = reinterpret_cast<int*>(ws);
-  a.unit_tile = reinterpret_cast<int*>(ws + w.unit_tile);
-  a.walk = reinterpret_cast<int4*>(ws + w.walk);
+  a.unit = reinterpret_cast<int2*>(ws + w.unit);
+  a.piece = reinterpret_cast<Q4Piece*>(ws + w.piece);
   a.ml = reinterpret_cast<float2*>(ws + w.ml);
   a.part = reinterpret_cast<float*>(ws + w.part);
   a.lse2 = reinterpret_cast<float*>(ws + w.lse2);
