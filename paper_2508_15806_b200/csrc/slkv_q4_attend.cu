@@ -1,13 +1,16 @@
 // Attention of new tokens over the 4-bit cache: out = softmax(f(scale q.k)) v per query head, its log-sum-exp, and the rows'
 // accumulated weights.
 //
-// One pass over the records with a running maximum and sum (base 2, fp32).  Four bits become matrix operands in registers:
-//   scores  a K nibble c, shifted to the top of a bf16 mantissa under the exponent of one, is 1 + c / 16, exactly; the
-//           score is sum over groups of 16 scale * (product - sum of the group's queries) + zero * (sum of the group's queries);
-//           the last two are two more products, of scales and zeros as they lie in the record and the query sums in three
-//           bf16 parts, which is exact.
-//   output  a V nibble under the exponent of 128 is 128 + c; less 136 it is c - 8, exactly.  Probabilities times the group's
-//           scale, rounded to bf16, are the other operand.  zero + 8 scale goes with the unrounded probabilities, in fp32.
+// One pass over the records with a running maximum and sum (base 2, fp32).  Four bits become matrix operands in registers.  The
+// low eight bits of a bf16 with nothing above them are an integer times 2^-133 -- subnormal up to 127, the first normal numbers
+// from there on -- so a nibble needs no more than a mask where it lies in them, the lower one as it is, the upper one as 16 times
+// itself: one shift and four masks make eight operands.
+//   scores  the queries are scaled by a power of two per head that keeps every product a normal fp32 number, and those that
+//           meet upper nibbles by 1/16; both are exact.  A score is the sum over groups of scale * product, plus the sum over
+//           groups of zero * (sum of the group's queries), which is one more product: the zeros as they lie in the record, the
+//           query sums in three bf16 parts.
+//   output  one packed multiply-add makes (c - 8) / 128 of a value nibble, exactly.  Probabilities times the group's scale,
+//           rounded to bf16, are the other operand.  zero + 8 scale goes with the unrounded probabilities, in fp32.
 // Keys are the products' long side (m16), the query heads of a KV head and its tokens the short one (n8): with four heads to a
 // KV head nothing wider would be used.  The scores' accumulators hold keys along the lanes, the second product wants
 // them along the other axis: one 8 x 8 transposition by the matrix unit's own instruction per 8 keys and group.
@@ -18,7 +21,7 @@
 // pieces as CTAs are cut into equal pieces of whole tiles; a CTA takes a piece, and further ones where there are more.  A unit of
 // one piece is finished by its CTA; the others leave a maximum, a sum and an unscaled output per piece, which a second launch
 // joins.  In a CTA each warp takes every fourth tile with its own ring of bulk copies, so that no warp waits for another before
-// a piece ends.  (Cutting the line of all tiles evenly instead, pieces running across units, took 40 us where this takes XX:
+// a piece ends.  (Cutting the line of all tiles evenly instead, pieces running across units, took 40 us where this takes 33:
 // a CTA's second piece starts with 3.4 us of latencies.)
 // The weights need the final log-sum-exps: the scores are kept in the workspace, the second launch turns them into
 // probabilities.
@@ -31,6 +34,7 @@ namespace slkv {
 namespace {
 
 constexpr int kAttendWarps = 4, kTileRows = 32, kCols = 8;
+constexpr unsigned kLower = 0x000f000fu, kUpper = 0x00f000f0u;
 constexpr float kLowest = -3e38f;       // a maximum over nothing: below every score, and differences of two stay numbers
 constexpr float kSlack = 8.0f;
 constexpr int kFewestTiles = 4;         // of a piece, where its unit has as many: one for each warp
@@ -101,29 +105,19 @@ __device__ __forceinline__ unsigned pack2(float lo, float hi) {
 }
 __device__ __forceinline__ float lo_f(unsigned w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float hi_f(unsigned w) { return __uint_as_float(w & 0xffff0000u); }
-// (x & mask) | under
-__device__ __forceinline__ unsigned put_under(unsigned x, unsigned mask, unsigned under) {
-  unsigned y;
-  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(y) : "r"(x), "r"(mask), "r"(under));
-  return y;
-}
 // A constant that stays in a register: the loop has no room for instructions that bring it there again and again.
 __device__ __forceinline__ unsigned held(unsigned x) {
   unsigned y;
   asm volatile("mov.b32 %0, %1;" : "=r"(y) : "r"(x));
   return y;
 }
-// nibbles I and I + 4 of a word as 1 + c / 16
+// Nibble I of both halves of a word as (c - 8) / 128.
+struct Q4Centre { unsigned lower, upper, minus; };         // 2^126, 2^122, -1/16: a nibble c is c 2^-133 or c 2^-129
 template <int I>
-__device__ __forceinline__ unsigned k_pair(unsigned w, unsigned one) {
-  return put_under(I == 0 ? w << 3 : w >> (I == 0 ? 0 : 4 * I - 3), 0x00780078u, one);
-}
-// nibbles I of both halves as c - 8
-template <int I>
-__device__ __forceinline__ unsigned v_pair(unsigned w, unsigned h128, unsigned h136) {
-  const unsigned x = put_under(w >> (4 * I), 0x000f000fu, h128);
-  const __nv_bfloat162 y = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&x), *reinterpret_cast<const __nv_bfloat162*>(&h136));
-  return *reinterpret_cast<const unsigned*>(&y);
+__device__ __forceinline__ unsigned v_pair(unsigned w, const Q4Centre& c) {
+  unsigned y;
+  asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(y) : "r"((I & 2 ? w >> 8 : w) & (I & 1 ? 0x00f000f0u : 0x000f000fu)), "r"(I & 1 ? c.upper : c.lower), "r"(c.minus));
+  return y;
 }
 // Key of a product's row r: neighbours apart, so that the lanes of one shared-memory access meet all banks.
 __device__ __forceinline__ int key_of(int r) { return (r & 8) | ((0x57463120u >> (4 * (r & 7))) & 7); }      // 0 2 1 3 6 4 7 5
@@ -176,7 +170,7 @@ __global__ void __launch_bounds__(kAttendWarps * 32, PARTS == 1 ? 4 : HD == 64 ?
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
   unsigned char* ring = smem + warp * (kStages * kStageBytes);
   const uint32_t bar0 = smem_at(bars[warp]), ring_at = smem_at(ring);
-  const unsigned one = held(0x3f803f80u), h128 = held(0x43004300u), h136 = held(0x43084308u);
+  const Q4Centre centre = {held(0x7e807e80u), held(0x7c807c80u), held(0xbd80bd80u)};
   // where a lane finds its keys in 16 rows: rows key_of(g) and that + 8 of the first product, key_of(2 t), key_of(2 t + 1) and
   // those + 8 of the second
   const uint32_t key_row = key_of(g) * RB, value_row[2] = {uint32_t(key_of(2 * t) * RB + HD / 2 + g * (HD / 16)),
@@ -194,7 +188,8 @@ __global__ void __launch_bounds__(kAttendWarps * 32, PARTS == 1 ? 4 : HD == 64 ?
   for (int s = first; s < last; ++s) mine += tiles_at(s);
   const int total = cta_total(mine, found) * a.n_cb;
   const int units = n_seg * a.n_cb;
-  const int per = max((total - 1) / max(a.n_cta - units / 2, a.n_cta / 4) + 1, kFewestTiles);
+  // a unit's last piece is half full on average; few units get no further wave for a bad average
+  const int per = max((total - 1) / max(a.n_cta - (8 * units <= a.n_cta ? units : units / 2), a.n_cta / 4) + 1, kFewestTiles);
   int pieces = 0, split = 0;                               // of this thread's segments; those of units of several
   for (int s = first; s < last; ++s) {
     const int n = (tiles_at(s) + per - 1) / per;
@@ -251,64 +246,75 @@ __global__ void __launch_bounds__(kAttendWarps * 32, PARTS == 1 ? 4 : HD == 64 ?
 
     // ---- the unit's queries: fragments, and sums per group
     const int s = seg / a.n_kv_heads, h = seg - s * a.n_kv_heads;
-    unsigned bq[PARTS][NG][2][2], bz[2] = {0u, 0u}, bs[2] = {0u, 0u};
+    unsigned bq[PARTS][NG][2][2], bz[2] = {0u, 0u};
+    float to_log2[2];                                      // of columns 2 t and 2 t + 1: from the products' units
     {
       const int col = cb * kCols + g;
       const bool there = col < a.R;
       const int tok = there ? col / a.G : 0, qh = h * a.G + (there ? col - tok * a.G : 0);
       const long long at = s * a.q_seq + tok * a.q_tok + qh * a.q_head + 8 * t;
-      float qs[NG];
+      float x[NG][8], qs[NG], most = 0.0f;
 #pragma unroll
       for (int j = 0; j < NG; ++j) {
-        float x[8];
         if constexpr (PARTS == 1) {
           uint4 w = make_uint4(0, 0, 0, 0);
           if (there) w = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.q) + at + 32 * j);
-          bq[0][j][0][0] = __byte_perm(w.x, w.z, 0x5410); bq[0][j][0][1] = __byte_perm(w.x, w.z, 0x7632);
-          bq[0][j][1][0] = __byte_perm(w.y, w.w, 0x5410); bq[0][j][1][1] = __byte_perm(w.y, w.w, 0x7632);
-          x[0] = lo_f(w.x); x[1] = hi_f(w.x); x[2] = lo_f(w.y); x[3] = hi_f(w.y);
-          x[4] = lo_f(w.z); x[5] = hi_f(w.z); x[6] = lo_f(w.w); x[7] = hi_f(w.w);
+          x[j][0] = lo_f(w.x); x[j][1] = hi_f(w.x); x[j][2] = lo_f(w.y); x[j][3] = hi_f(w.y);
+          x[j][4] = lo_f(w.z); x[j][5] = hi_f(w.z); x[j][6] = lo_f(w.w); x[j][7] = hi_f(w.w);
         } else {
           float4 u = make_float4(0, 0, 0, 0), v = u;
           if (there) {
             const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(a.q) + at + 32 * j);
             u = p[0]; v = p[1];
           }
-          x[0] = u.x; x[1] = u.y; x[2] = u.z; x[3] = u.w; x[4] = v.x; x[5] = v.y; x[6] = v.z; x[7] = v.w;
-          float r[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) r[e] = x[e];
-#pragma unroll
-          for (int p = 0; p < PARTS; ++p)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const unsigned w = pack2(r[e], r[e + 4]);
-              bq[p][j][e >> 1][e & 1] = w;
-              r[e] -= lo_f(w);
-              r[e + 4] -= hi_f(w);
-            }
+          x[j][0] = u.x; x[j][1] = u.y; x[j][2] = u.z; x[j][3] = u.w; x[j][4] = v.x; x[j][5] = v.y; x[j][6] = v.z; x[j][7] = v.w;
         }
-        qs[j] = ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(x[j][e]));
+      }
+      most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
+      most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
+      // The head's largest query to 2^99 .. 2^100 (heads of less than 2^-40 or more than 2^86: as if they were those): products
+      // with a nibble are below 2^-29 and normal down to 2^-97 of the largest.
+      const int up2 = 99 - min(max((int)(__float_as_uint(most) >> 23) - 127, -40), 86);
+      const float f = __int_as_float((127 + up2 / 2) << 23), f2 = __int_as_float((127 + up2 - up2 / 2) << 23);
+#pragma unroll
+      for (int j = 0; j < NG; ++j) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[j][e] = x[j][e] * f * f2;
+        qs[j] = ((x[j][0] + x[j][1]) + (x[j][2] + x[j][3])) + ((x[j][4] + x[j][5]) + (x[j][6] + x[j][7]));
         qs[j] += __shfl_xor_sync(0xffffffffu, qs[j], 1);
         qs[j] += __shfl_xor_sync(0xffffffffu, qs[j], 2);
+#pragma unroll
+        for (int e = 1; e < 8; e += 2) x[j][e] *= 0.0625f;
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const unsigned w = pack2(x[j][e], x[j][e + 4]);
+            bq[p][j][e >> 1][e & 1] = w;
+            x[j][e] -= lo_f(w);
+            x[j][e + 4] -= hi_f(w);
+          }
       }
-      // the query sums in three parts: lane t holds part t of all groups, where the fragments of scales and zeros expect them
+      // the query sums in the products' units, 2^-133, in three parts: lane t holds part t of all groups, where the zeros'
+      // fragment expects them
 #pragma unroll
       for (int jj = 0; jj < NG / 2; ++jj) {
-        float x = -qs[2 * jj], y = -qs[2 * jj + 1];
+        float y0 = qs[2 * jj] * 0x1p-100f * 0x1p-33f, y1 = qs[2 * jj + 1] * 0x1p-100f * 0x1p-33f;
 #pragma unroll
         for (int p = 0; p < 3; ++p) {
-          const unsigned v = pack2(x, y);
-          if (p == t) {                                    // lane t = 3: zeros
-            bs[jj] = v;
-            bz[jj] = pack2(-0.0625f * lo_f(v), -0.0625f * hi_f(v));
-          }
-          x -= lo_f(v);
-          y -= hi_f(v);
+          const unsigned v = pack2(y0, y1);
+          if (p == t) bz[jj] = v;                          // lane t = 3: zeros
+          y0 -= lo_f(v);
+          y1 -= hi_f(v);
         }
       }
+#pragma unroll
+      for (int c = 0; c < 2; ++c)                          // 2^(133 - up2), at most 2^120
+        to_log2[c] = a.scale * kLog2e * __int_as_float((127 + 133 - __shfl_sync(0xffffffffu, up2, 8 * t + 4 * c)) << 23);
     }
-    const float to_log2 = a.scale * (16.0f * kLog2e), cap_in = a.softcap > 0.0f ? 16.0f * a.scale / a.softcap : 0.0f;
+    const float per_cap = a.softcap > 0.0f ? 1.0f / (a.softcap * kLog2e) : 0.0f;
     int qp[2] = {0, 0};
     float slope[2] = {0.0f, 0.0f};
     if (MASK) {
@@ -368,29 +374,26 @@ __global__ void __launch_bounds__(kAttendWarps * 32, PARTS == 1 ? 4 : HD == 64 ?
           load_words(p0 + 4 * NG * t, w0);
           load_words(p1 + 4 * NG * t, w1);
           mma16816_from_zero(x, x0[NG / 2], x1[NG / 2], NG == 4 ? x0[NG - 1] : 0u, NG == 4 ? x1[NG - 1] : 0u, bz[0], bz[1]);
-          mma16816(x, x0[0], x1[0], NG == 4 ? x0[1] : 0u, NG == 4 ? x1[1] : 0u, bs[0], bs[1]);
 #pragma unroll
           for (int j = 0; j < NG; ++j) {
             float d[4];
-            const unsigned a00 = k_pair<0>(w0[j], one), a01 = k_pair<1>(w0[j], one), a02 = k_pair<2>(w0[j], one), a03 = k_pair<3>(w0[j], one);
-            const unsigned a10 = k_pair<0>(w1[j], one), a11 = k_pair<1>(w1[j], one), a12 = k_pair<2>(w1[j], one), a13 = k_pair<3>(w1[j], one);
+            const unsigned u0 = w0[j] >> 8, u1 = w1[j] >> 8;
 #pragma unroll
             for (int p = 0; p < PARTS; ++p) {
-              if (p == 0) mma16816_from_zero(d, a00, a10, a01, a11, bq[p][j][0][0], bq[p][j][0][1]);
-              else mma16816(d, a00, a10, a01, a11, bq[p][j][0][0], bq[p][j][0][1]);
-              mma16816(d, a02, a12, a03, a13, bq[p][j][1][0], bq[p][j][1][1]);
+              if (p == 0) mma16816_from_zero(d, w0[j] & kLower, w1[j] & kLower, w0[j] & kUpper, w1[j] & kUpper, bq[p][j][0][0], bq[p][j][0][1]);
+              else mma16816(d, w0[j] & kLower, w1[j] & kLower, w0[j] & kUpper, w1[j] & kUpper, bq[p][j][0][0], bq[p][j][0][1]);
+              mma16816(d, u0 & kLower, u1 & kLower, u0 & kUpper, u1 & kUpper, bq[p][j][1][0], bq[p][j][1][1]);
             }
             const float s0 = j & 1 ? hi_f(x0[j >> 1]) : lo_f(x0[j >> 1]), s1 = j & 1 ? hi_f(x1[j >> 1]) : lo_f(x1[j >> 1]);
             x[0] = fmaf(s0, d[0], x[0]); x[1] = fmaf(s0, d[1], x[1]);
             x[2] = fmaf(s1, d[2], x[2]); x[3] = fmaf(s1, d[3], x[3]);
           }
         }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] *= to_log2[i & 1];
         if (a.softcap > 0.0f) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) x[i] = a.softcap * kLog2e * tanhf(x[i] * cap_in);
-        } else {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) x[i] *= to_log2;
+          for (int i = 0; i < 4; ++i) x[i] = a.softcap * kLog2e * tanhf(x[i] * per_cap);
         }
         if (MASK) {
           const int pos0 = __shfl_sync(0xffffffffu, pos_here, r0), pos1 = __shfl_sync(0xffffffffu, pos_here, r1);
@@ -472,8 +475,8 @@ __global__ void __launch_bounds__(kAttendWarps * 32, PARTS == 1 ? 4 : HD == 64 ?
           }
           const unsigned t01 = __byte_perm(va[0][j >> 1], va[1][j >> 1], j & 1 ? 0x7632 : 0x5410);
           const unsigned t89 = __byte_perm(va[2][j >> 1], va[3][j >> 1], j & 1 ? 0x7632 : 0x5410);
-          const unsigned f0[4] = {v_pair<0>(t01, h128, h136), v_pair<1>(t01, h128, h136), v_pair<0>(t89, h128, h136), v_pair<1>(t89, h128, h136)};
-          const unsigned f1[4] = {v_pair<2>(t01, h128, h136), v_pair<3>(t01, h128, h136), v_pair<2>(t89, h128, h136), v_pair<3>(t89, h128, h136)};
+          const unsigned f0[4] = {v_pair<0>(t01, centre), v_pair<1>(t01, centre), v_pair<0>(t89, centre), v_pair<1>(t89, centre)};
+          const unsigned f1[4] = {v_pair<2>(t01, centre), v_pair<3>(t01, centre), v_pair<2>(t89, centre), v_pair<3>(t89, centre)};
           if constexpr (PARTS == 1) {
             const unsigned b0 = transpose8(pack2(y[0], y[1])), b1 = transpose8(pack2(y[2], y[3]));
             mma16816(o[j][0], f0[0], f0[1], f0[2], f0[3], b0, b1);
@@ -520,7 +523,8 @@ __global__ void __launch_bounds__(kAttendWarps * 32, PARTS == 1 ? 4 : HD == 64 ?
 #pragma unroll
       for (int c = 0; c < 2; ++c)
         *reinterpret_cast<float4*>(mine_o + (2 * t + c) * kPitch + 32 * j + 4 * g) =
-            make_float4(o[j][0][c] + zacc[j][c], o[j][0][c + 2] + zacc[j][c], o[j][1][c] + zacc[j][c], o[j][1][c + 2] + zacc[j][c]);
+            make_float4(fmaf(128.0f, o[j][0][c], zacc[j][c]), fmaf(128.0f, o[j][0][c + 2], zacc[j][c]),
+                        fmaf(128.0f, o[j][1][c], zacc[j][c]), fmaf(128.0f, o[j][1][c + 2], zacc[j][c]));
     async_fence();
     __syncthreads();
     const bool whole = n_pieces == 1;
