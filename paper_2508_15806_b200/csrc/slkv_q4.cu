@@ -110,24 +110,6 @@ struct Q4PackArgs {
 constexpr int kChunkRows = 32;          // consecutive rows of a warp
 constexpr int kAhead = 4;               // steps whose rows are loaded before the steps before them are done
 
-// Where rows of a packed layer go: the segment of the row looked at last, and how far it reaches.
-struct Q4Places {
-  int seg;
-  long long end, shift, limit;          // rows below end are at slot row + shift, as long as that is below limit
-  __device__ __forceinline__ void at(const Q4PackArgs& a, int s) {
-    seg = s;
-    const Q4Segment t = q4_segment(a.c.starts, a.c.starts, s, a.c.capacity);
-    end = s + 1 < a.c.n_seg ? (long long)a.offsets[s + 1] : (1ll << 40);
-    shift = (long long)t.begin - max(a.offsets[s], 0);
-    limit = (long long)t.begin + t.room;
-  }
-  __device__ __forceinline__ long long of(const Q4PackArgs& a, long long row) {
-    while (row >= end) at(a, seg + 1);
-    const long long slot = row + shift;
-    return slot < limit ? slot : -1;
-  }
-};
-
 template <int HD, bool F32>
 __global__ void __launch_bounds__(kQ4Warps * 32) k_q4_pack(const __grid_constant__ Q4PackArgs a) {
   using Q = Q4Lane<HD>;
@@ -153,8 +135,21 @@ __global__ void __launch_bounds__(kQ4Warps * 32) k_q4_pack(const __grid_constant
     Q4Raw<F32> raw[kAhead];
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) raw[i] = load(min(i, steps - 1));
-    Q4Places to;
-    to.at(a, q4_find(a.offsets, n_seg, (int)r0, lane));
+    // lane i finds row i's slot, and writes what the slot has beside the record
+    int slot = -1;
+    int seg = q4_find(a.offsets, n_seg, (int)r0, lane);
+    if (lane < a.chunk && r0 + lane < rows) {
+      const int r = (int)r0 + lane;
+      const int pos = a.kept_idx[r];
+      while (seg + 1 < n_seg && a.offsets[seg + 1] <= r) ++seg;
+      const Q4Segment s = q4_segment(a.c.starts, a.c.starts, seg, a.c.capacity);
+      const int at = r - max(a.offsets[seg], 0);
+      if (at >= 0 && at < s.room) {
+        slot = s.begin + at;
+        a.c.pos[slot] = pos;
+        if (a.c.weight) a.c.weight[slot] = 0.0f;
+      }
+    }
     for (int i0 = 0; i0 < steps; i0 += kAhead) {
 #pragma unroll
       for (int u = 0; u < kAhead; ++u) {
@@ -163,12 +158,7 @@ __global__ void __launch_bounds__(kQ4Warps * 32) k_q4_pack(const __grid_constant
         float x[8];
         q4_widen(raw[u], x);
         if (i + kAhead < steps) raw[u] = load(i + kAhead);
-        const long long r = r0 + i * Q::kRows + sub, slot = r < rows ? to.of(a, r) : -1;
-        q4_store<HD>(x, slot, a.c.records, lane);
-        if (slot >= 0 && l == 0) {
-          if (lane < 16) a.c.pos[slot] = a.kept_idx[r];
-          else if (a.c.weight) a.c.weight[slot] = 0.0f;
-        }
+        q4_store<HD>(x, __shfl_sync(0xffffffffu, slot, i * Q::kRows + sub), a.c.records, lane);
       }
     }
   }
