@@ -517,34 +517,35 @@ def make_q4_cache(records: torch.Tensor, pos: torch.Tensor, weight: Optional[tor
     c = SlkvQ4Cache(n_seg // n_kv_heads, n_kv_heads, head_dim, 0, rows, records.data_ptr(), pos.data_ptr(),
                     weight.data_ptr() if weight is not None else None, starts.data_ptr(), lens.data_ptr())
     c.tensors, c.device, c.lens_tensor = tensors, records.device, lens
+    c.index = records.get_device() if records.is_cuda else -2           # no tensor is on that one
     return c
 
 
-# The calls of a decode step are issued at the rate the checks below allow: each looks at a tensor's properties once.
-def _q4_here(cache: SlkvQ4Cache, *tensors: torch.Tensor) -> None:
-    """Calls are enqueued on a stream of the current device: that has to be the cache's and the tensors'."""
-    d = torch._C._cuda_getDevice() if cache.device.type == "cuda" else -2
-    if cache.device.index != d or [1 for t in tensors if t.get_device() != d]:
-        raise AssertionError("the cache and the tensors have to be on the current device")
+# The calls of a decode step are issued at the rate that the checks below allow: each looks at a property once.  Calls are enqueued
+# on a stream of the current device: that has to be the cache's and the tensors'.
+_I32, _F32 = torch.int32, torch.float32
+_current_device = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else torch.cuda.current_device
+
+
+def _q4_elsewhere() -> None:
+    raise AssertionError("the cache and the tensors have to be on the current device")
 
 
 def _q4_status(cache: SlkvQ4Cache, status: torch.Tensor) -> None:
-    _q4_here(cache, status)
-    assert status.dtype is torch.int32 and status.numel() >= 1
-
-
-def _q4_int32(t: torch.Tensor, n: int) -> None:
-    assert t.dtype is torch.int32 and t.numel() == n and t.is_contiguous()
+    if status.get_device() != cache.index:
+        _q4_elsewhere()
+    assert status.dtype is _I32 and status.numel() >= 1
 
 
 def slkv_q4_pack(cache: SlkvQ4Cache, k: torch.Tensor, v: torch.Tensor, offsets: torch.Tensor, kept_idx: torch.Tensor,
                  status: Optional[torch.Tensor] = None, stream=None) -> None:
     """k, v [rows, head_dim], offsets, kept_idx: as slkv_compress wrote them."""
-    _q4_here(cache, k, v, offsets, kept_idx)
-    rows, dim = k.shape
-    assert dim == cache.head_dim and v.shape == (rows, dim) and k.dtype is v.dtype and k.is_contiguous() and v.is_contiguous()
-    _q4_int32(offsets, cache.n_seqs * cache.n_kv_heads + 1)
-    assert kept_idx.dtype is torch.int32 and kept_idx.is_contiguous() and kept_idx.numel() >= rows
+    if not cache.index == k.get_device() == v.get_device() == offsets.get_device() == kept_idx.get_device() == _current_device():
+        _q4_elsewhere()
+    shape = rows, dim = k.shape
+    assert dim == cache.head_dim and v.shape == shape and k.dtype is v.dtype and k.is_contiguous() and v.is_contiguous()
+    assert offsets.dtype is _I32 and offsets.is_contiguous() and offsets.numel() == cache.n_seqs * cache.n_kv_heads + 1
+    assert kept_idx.dtype is _I32 and kept_idx.is_contiguous() and kept_idx.numel() >= rows
     if status is not None:
         _q4_status(cache, status)
     rc = _fn["slkv_q4_pack"](stream, cache, _DTYPES[k.dtype], k, v, rows, offsets, kept_idx, status)
@@ -556,10 +557,11 @@ def slkv_q4_append(cache: SlkvQ4Cache, k: torch.Tensor, v: torch.Tensor, pos: to
                    status: Optional[torch.Tensor] = None, stream=None) -> None:
     """k, v [n_seqs, n_tokens, n_kv_heads, head_dim] (any strides over a contiguous last dimension), pos int32 [n_seqs, n_tokens].
     after: the same cache with lengths of its own, which take the new ones."""
-    _q4_here(cache, k, v, pos)
+    if not cache.index == k.get_device() == v.get_device() == pos.get_device() == _current_device():
+        _q4_elsewhere()
     shape = ns, n, hkv, dim = k.shape
-    assert (ns, hkv, dim) == (cache.n_seqs, cache.n_kv_heads, cache.head_dim) and v.shape == shape and k.dtype is v.dtype
-    _q4_int32(pos, ns * n)
+    assert ns == cache.n_seqs and hkv == cache.n_kv_heads and dim == cache.head_dim and v.shape == shape and k.dtype is v.dtype
+    assert pos.dtype is _I32 and pos.is_contiguous() and pos.numel() == ns * n
     ks, kt, kh, k1 = k.stride()
     vs, vt, vh, v1 = v.stride()
     assert k1 == v1 == 1
@@ -578,15 +580,15 @@ def slkv_q4_unpack(cache: SlkvQ4Cache, k_out: torch.Tensor, v_out: torch.Tensor,
                    stream=None) -> None:
     """k_out, v_out [n, head_dim]: the rows of the slots given (int32 [n], entries outside the cache are padding), or of every
     filled slot at its own place (n = slots of the cache)."""
-    _q4_here(cache, k_out, v_out)
+    if not cache.index == k_out.get_device() == v_out.get_device() == _current_device():
+        _q4_elsewhere()
     shape = n, dim = k_out.shape
     assert dim == cache.head_dim and v_out.shape == shape and k_out.dtype is v_out.dtype
     assert k_out.is_contiguous() and v_out.is_contiguous()
     if slots is None:
         assert n == cache.capacity_rows
     else:
-        _q4_here(cache, slots)
-        _q4_int32(slots, n)
+        assert slots.dtype is _I32 and slots.is_contiguous() and slots.numel() == n and slots.get_device() == cache.index
     rc = _fn["slkv_q4_unpack"](stream, cache, _DTYPES[k_out.dtype], slots, n, k_out, v_out)
     if rc != SLKV_OK:
         raise SlkvError(rc, "slkv_q4_unpack")
@@ -619,18 +621,17 @@ def slkv_q4_attend(cache: SlkvQ4Cache, params: SlkvQ4AttendParams, q: torch.Tens
                    accumulate: bool = False, status: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """q, out: the shapes and strides params was made from.  q_pos int32 [n_seqs, n_tokens], slopes float32 [n_q_heads],
     lse float32 [n_seqs, n_q_heads, n_tokens]; accumulate adds to the cache's weights."""
-    _q4_here(cache, q, out, workspace)
+    d = cache.index
+    if not d == q.get_device() == out.get_device() == workspace.get_device() == _current_device():
+        _q4_elsewhere()
     assert (q.shape, q.stride(), q.dtype) == params.q_like and (out.shape, out.stride(), out.dtype) == params.out_like
     ns, nt, hq, _ = params.q_like[0]
     if q_pos is not None:
-        _q4_here(cache, q_pos)
-        _q4_int32(q_pos, ns * nt)
+        assert q_pos.dtype is _I32 and q_pos.is_contiguous() and q_pos.numel() == ns * nt and q_pos.get_device() == d
     if slopes is not None:
-        _q4_here(cache, slopes)
-        assert slopes.dtype is torch.float32 and slopes.numel() == hq and slopes.is_contiguous()
+        assert slopes.dtype is _F32 and slopes.is_contiguous() and slopes.numel() == hq and slopes.get_device() == d
     if lse is not None:
-        _q4_here(cache, lse)
-        assert lse.dtype is torch.float32 and lse.numel() == ns * nt * hq and lse.is_contiguous()
+        assert lse.dtype is _F32 and lse.is_contiguous() and lse.numel() == ns * nt * hq and lse.get_device() == d
     if status is not None:
         _q4_status(cache, status)
     rc = _fn["slkv_q4_attend"](stream, cache, params, q, q_pos, slopes, out, lse, 1 if accumulate else 0, status, workspace,
@@ -655,10 +656,10 @@ def new_q4_evict_workspace(cache: SlkvQ4Cache, to: Optional[SlkvQ4Cache] = None)
 def slkv_q4_evict(cache: SlkvQ4Cache, to: SlkvQ4Cache, budgets: torch.Tensor, window: int, newest: torch.Tensor,
                   workspace: torch.Tensor, status: Optional[torch.Tensor] = None, stream=None) -> None:
     """budgets int32 [n_kv_heads], newest int32 [n_seqs]; to: `cache` itself, or another cache."""
-    _q4_here(cache, budgets, newest, workspace)
-    assert to.device == cache.device
-    _q4_int32(budgets, cache.n_kv_heads)
-    _q4_int32(newest, cache.n_seqs)
+    if not cache.index == to.index == budgets.get_device() == newest.get_device() == workspace.get_device() == _current_device():
+        _q4_elsewhere()
+    assert budgets.dtype is _I32 and budgets.is_contiguous() and budgets.numel() == cache.n_kv_heads
+    assert newest.dtype is _I32 and newest.is_contiguous() and newest.numel() == cache.n_seqs
     if status is not None:
         _q4_status(cache, status)
     rc = _fn["slkv_q4_evict"](stream, cache, to, budgets, int(window), newest, status, workspace, workspace.numel())

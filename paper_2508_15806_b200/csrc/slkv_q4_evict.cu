@@ -10,6 +10,8 @@
 // One launch: a cluster of CTAs per segment (one CTA where there are many segments or few rows), each with a contiguous share
 // of the slots, keys in shared memory; they share the moves evenly.
 // What bounds it: for few rows the chain of passes over the keys, for many the rows' bytes.
+#include <atomic>
+
 #include <cooperative_groups.h>
 
 #include "slkv_q4_device.cuh"
@@ -362,14 +364,19 @@ __global__ void __launch_bounds__(kEvictThreads, 2) k_q4_evict(const __grid_cons
 
 size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 
-template <int HD>
+template <int HD, bool CLUSTER>
 cudaError_t launch_evict(const Q4EvictArgs& a, cudaStream_t st) {
-  constexpr int kMostBytes = kMostKeys * (int)sizeof(unsigned);
-  const size_t smem = (size_t)a.key_room * sizeof(unsigned);
-  const dim3 grid((unsigned)(a.from.n_seg * a.ctas)), block(kEvictThreads);
-  auto kernel = a.ctas > 1 ? k_q4_evict<HD, true> : k_q4_evict<HD, false>;
-  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostBytes);
-  return e == cudaSuccess ? launch_pdl(kernel, grid, block, smem, st, a.ctas, a) : e;
+  auto kernel = k_q4_evict<HD, CLUSTER>;
+  static std::atomic<unsigned> allowed{0};                 // devices on which the kernel may have that much shared memory
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev >= 32 || !(allowed.load(std::memory_order_relaxed) >> dev & 1u)) {
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostKeys * (int)sizeof(unsigned));
+    if (e != cudaSuccess) return e;
+    if (dev < 32) allowed.fetch_or(1u << dev, std::memory_order_relaxed);
+  }
+  return launch_pdl(kernel, dim3((unsigned)(a.from.n_seg * a.ctas)), dim3(kEvictThreads), (size_t)a.key_room * sizeof(unsigned), st, a.ctas, a);
 }
 
 }  // namespace
@@ -395,7 +402,8 @@ cudaError_t launch_q4_evict(const Q4CacheView& from, const Q4CacheView& to, int 
   while (a.key_room < 2 * room / a.ctas && a.key_room < kMostKeys) a.key_room *= 2;
   if (a.key_room > kMostKeys) a.key_room = kMostKeys;
   LaunchScope scope(KID_Q4_EVICT, st, launches);
-  return head_dim == 128 ? launch_evict<128>(a, st) : launch_evict<64>(a, st);
+  if (head_dim == 128) return a.ctas > 1 ? launch_evict<128, true>(a, st) : launch_evict<128, false>(a, st);
+  return a.ctas > 1 ? launch_evict<64, true>(a, st) : launch_evict<64, false>(a, st);
 }
 
 }  // namespace slkv
