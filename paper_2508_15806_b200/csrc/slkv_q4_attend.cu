@@ -23,16 +23,23 @@
 // joins.  In a CTA each warp takes every fourth tile with its own ring of bulk copies, so that no warp waits for another before
 // a piece ends.  (Cutting the line of all tiles evenly instead, pieces running across units, took 40 us where this takes 33:
 // a CTA's second piece starts with 3.4 us of latencies.)
+// Where units are few and short one launch does it all: a cluster of CTAs per unit, equal shares of its tiles, the shares joined
+// through the cluster's shared memory.  (One user, 8 heads of 129 to 1031 rows: 9.3 us with two launches, 7.6 with one.)
 // The weights need the final log-sum-exps: the scores are kept in the workspace, the second launch turns them into
-// probabilities.
+// probabilities (the same CTA, behind the cluster's exchange, where there is one launch).
 // What bounds it: the arithmetic between DRAM and the products (unpacking, scales).
 #include <atomic>
+
+#include <cooperative_groups.h>
 
 #include "slkv_q4_device.cuh"
 
 namespace slkv {
 namespace {
 
+namespace cg = cooperative_groups;
+
+constexpr int kAttendCluster = 8;       // CTAs of a cluster, at most
 constexpr int kAttendWarps = 4, kTileRows = 32, kCols = 8;
 constexpr unsigned kLower = 0x000f000fu, kUpper = 0x00f000f0u;
 constexpr float kLowest = -3e38f;       // a maximum over nothing: below every score, and differences of two stay numbers
@@ -52,7 +59,7 @@ struct Q4AttendArgs {
   const float* slopes;                  // optional
   int32_t* status;
   long long q_seq, q_tok, q_head, o_seq, o_tok, o_head;      // elements
-  int n_kv_heads, n_q_heads, n_tokens, G, R, n_cb, n_cta, accumulate;
+  int n_kv_heads, n_q_heads, n_tokens, G, R, n_cb, n_cta, ctas, accumulate;         // ctas: of a cluster
   float scale, softcap, decay, lse_unit;                     // lse_unit: of a base-2 logarithm
   // workspace
   int* head;                            // pieces
@@ -160,13 +167,22 @@ __device__ __forceinline__ int cta_total(int x, int* sums) {
 template <int HD> constexpr int kQ4Stages = HD == 128 ? 2 : 4;
 template <int HD> constexpr int kQ4Smem = kAttendWarps * kQ4Stages<HD> * kTileRows * q4_record_bytes(HD);
 
-template <int HD, int PARTS, bool MASK>
+// What a CTA of a cluster shows the others: its share's maximum, sum and unscaled output per column.
+template <int HD>
+struct Q4Share {
+  float2 ml[kCols];
+  float out[kCols][HD];
+};
+
+template <int HD, int PARTS, bool MASK, bool CLUSTER>
 __global__ void __launch_bounds__(kAttendWarps * 32, PARTS == 1 ? 4 : HD == 64 ? 3 : 2) k_q4_attend(const __grid_constant__ Q4AttendArgs a) {
   constexpr int NG = HD / 32, RB = q4_record_bytes(HD), kStages = kQ4Stages<HD>, kStageBytes = kTileRows * RB;
   extern __shared__ __align__(128) unsigned char smem[];
   __shared__ __align__(8) unsigned long long bars[kAttendWarps][kStages];
   __shared__ int found[8], before[kAttendWarps * 32 + 1], places[kAttendWarps * 32];
   __shared__ float merge_m[kAttendWarps][kCols], merge_l[kAttendWarps][kCols];
+  __shared__ __align__(16) unsigned char share_room[CLUSTER ? sizeof(Q4Share<HD>) : 16];
+  __shared__ float2 shares_ml[CLUSTER ? kAttendCluster : 1][kCols];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
   unsigned char* ring = smem + warp * (kStages * kStageBytes);
   const uint32_t bar0 = smem_at(bars[warp]), ring_at = smem_at(ring);
@@ -181,15 +197,20 @@ __global__ void __launch_bounds__(kAttendWarps * 32, PARTS == 1 ? 4 : HD == 64 ?
   pdl_wait();
 
   // ---- tiles of all units, the size of a piece, how many pieces come before each thread's segments
-  const int n_seg = a.c.n_seg, per_thread = (n_seg + kAttendWarps * 32 - 1) / (kAttendWarps * 32);
+  const int n_seg = a.c.n_seg;
+  unsigned issued = 0, used = 0, lost = 0;                 // copies of this warp's ring
+  bool dead = false;
+  const int per_thread = CLUSTER ? 0 : (n_seg + kAttendWarps * 32 - 1) / (kAttendWarps * 32);
   const int first = min(tid * per_thread, n_seg), last = min(first + per_thread, n_seg);
   auto tiles_at = [&](int seg) { return tiles_of(q4_segment(a.c.starts, a.c.lens, seg, a.c.capacity).len); };
+  int all = 1, per = 1;
+  if constexpr (!CLUSTER) {
   int mine = 0;
   for (int s = first; s < last; ++s) mine += tiles_at(s);
   const int total = cta_total(mine, found) * a.n_cb;
   const int units = n_seg * a.n_cb;
   // a unit's last piece is half full on average; few units get no further wave for a bad average
-  const int per = max((total - 1) / max(a.n_cta - (8 * units <= a.n_cta ? units : units / 2), a.n_cta / 4) + 1, kFewestTiles);
+  per = max((total - 1) / max(a.n_cta - (8 * units <= a.n_cta ? units : units / 2), a.n_cta / 4) + 1, kFewestTiles);
   int pieces = 0, split = 0;                               // of this thread's segments; those of units of several
   for (int s = first; s < last; ++s) {
     const int n = (tiles_at(s) + per - 1) / per;
@@ -200,29 +221,34 @@ __global__ void __launch_bounds__(kAttendWarps * 32, PARTS == 1 ? 4 : HD == 64 ?
   places[tid] = cta_before(split, found + 4);
   if (tid == kAttendWarps * 32 - 1) before[tid + 1] = before[tid] + pieces;
   __syncthreads();
-  const int all = before[kAttendWarps * 32];
+  all = before[kAttendWarps * 32];
   if (blockIdx.x == 0 && tid == 0) a.head[0] = all;
-  unsigned issued = 0, used = 0, lost = 0;                 // copies of this warp's ring
-  bool dead = false;
+  }
 
-  for (int index = blockIdx.x; index < all; index += a.n_cta) {
-    if (before[tid] <= index && index < before[tid + 1]) { // the one thread that has the piece's segment
-      int u = before[tid], s = first, n = 0, place = places[tid];
-      for (; s < last; ++s) {
-        n = (tiles_at(s) + per - 1) / per;
-        if (index < u + n * a.n_cb) break;
-        u += n * a.n_cb;
-        place += n > 1 ? n * a.n_cb : 0;
+  for (int index = CLUSTER ? 0 : blockIdx.x; index < all; index += a.n_cta) {
+    int seg, cb, nth, n_pieces, place = 0;
+    if constexpr (CLUSTER) {                               // once: all is 1
+      const int unit = blockIdx.x / a.ctas;
+      seg = unit / a.n_cb; cb = unit - seg * a.n_cb; nth = blockIdx.x - unit * a.ctas; n_pieces = a.ctas;
+    } else {
+      if (before[tid] <= index && index < before[tid + 1]) {       // the one thread that has the piece's segment
+        int u = before[tid], s = first, n = 0, at = places[tid];
+        for (; s < last; ++s) {
+          n = (tiles_at(s) + per - 1) / per;
+          if (index < u + n * a.n_cb) break;
+          u += n * a.n_cb;
+          at += n > 1 ? n * a.n_cb : 0;
+        }
+        found[0] = s; found[1] = (index - u) / n; found[2] = (index - u) % n; found[3] = n; found[4] = at;
       }
-      found[0] = s; found[1] = (index - u) / n; found[2] = (index - u) % n; found[3] = n; found[4] = place;
+      __syncthreads();
+      seg = found[0]; cb = found[1]; nth = found[2]; n_pieces = found[3]; place = found[4] + cb * n_pieces;
     }
-    __syncthreads();
-    const int seg = found[0], cb = found[1], nth = found[2], n_pieces = found[3], place = found[4] + cb * n_pieces;
     const Q4Segment sg = q4_segment(a.c.starts, a.c.lens, seg, a.c.capacity);
     const int tiles = tiles_of(sg.len);
     const int from = (int)((long long)tiles * nth / n_pieces), to = (int)((long long)tiles * (nth + 1) / n_pieces);
     const unsigned char* rows = a.c.records + (long long)sg.begin * RB;
-    if (tid == 0) {
+    if (!CLUSTER && tid == 0) {
       if (nth == 0) a.unit[seg * a.n_cb + cb] = make_int2(n_pieces, place);
       if (a.accumulate)
         a.piece[index] = {sg.begin + from * kTileRows, min(to * kTileRows, sg.len) - from * kTileRows, seg, cb, n_pieces, found[4]};
@@ -527,7 +553,8 @@ __global__ void __launch_bounds__(kAttendWarps * 32, PARTS == 1 ? 4 : HD == 64 ?
                         fmaf(128.0f, o[j][1][c], zacc[j][c]), fmaf(128.0f, o[j][1][c + 2], zacc[j][c]));
     async_fence();
     __syncthreads();
-    const bool whole = n_pieces == 1;
+    const bool whole = !CLUSTER && n_pieces == 1;
+    Q4Share<HD>& share = *reinterpret_cast<Q4Share<HD>*>(share_room);
     for (int i = tid; i < kCols * HD / 4; i += kAttendWarps * 32) {
       const int c = i / (HD / 4), ch = 4 * (i % (HD / 4)), col = cb * kCols + c;
       if (col >= a.R) continue;
@@ -557,13 +584,61 @@ __global__ void __launch_bounds__(kAttendWarps * 32, PARTS == 1 ? 4 : HD == 64 ?
           if (a.lse) a.lse[((long long)s * a.n_q_heads + qh) * a.n_tokens + tok] = z * a.lse_unit;
           a.lse2[(long long)seg * a.R + col] = z;
         }
+      } else if constexpr (CLUSTER) {
+        if (ch == 0) share.ml[c] = make_float2(top, sum_l);
+        *reinterpret_cast<float4*>(&share.out[c][ch]) = v;
       } else {
         const long long at = (long long)(place + nth) * kCols + c;
         if (ch == 0) a.ml[at] = make_float2(top, sum_l);
         *reinterpret_cast<float4*>(a.part + at * HD + ch) = v;
       }
     }
-    __syncthreads();                                       // the rings and the sums are free again
+    if constexpr (CLUSTER) {
+      cg::cluster_group cluster = cg::this_cluster();
+      cluster.sync();
+      const int cols = min(kCols, a.R - cb * kCols);       // the block's
+      if (tid < a.ctas * kCols && (tid & (kCols - 1)) < cols)
+        shares_ml[tid / kCols][tid & (kCols - 1)] = cluster.map_shared_rank(&share, tid / kCols)->ml[tid & (kCols - 1)];
+      __syncthreads();
+      float* lse_of = merge_m[0];                          // [8]
+      if (tid < cols) {
+        float top = kLowest, sum_l = 0.0f;
+        for (int r = 0; r < a.ctas; ++r) top = fmaxf(top, shares_ml[r][tid].x);
+        for (int r = 0; r < a.ctas; ++r) sum_l = fmaf(shares_ml[r][tid].y, ex2(shares_ml[r][tid].x - top), sum_l);
+        const float z = top + log2f(sum_l);
+        merge_l[0][tid] = sum_l == 0.0f ? 0.0f : 1.0f / sum_l;             // no visible row: zeros
+        merge_l[1][tid] = top;
+        lse_of[tid] = z == -INFINITY ? INFINITY : z;
+        const int col = cb * kCols + tid, tok = col / a.G;
+        if (a.lse && nth == 0) a.lse[((long long)s * a.n_q_heads + h * a.G + col - tok * a.G) * a.n_tokens + tok] = z * a.lse_unit;
+      }
+      __syncthreads();
+      for (int i = tid; i < cols * HD; i += kAttendWarps * 32) {           // each CTA its share of the columns
+        const int c = i / HD, ch = i - c * HD;
+        if (c % a.ctas != nth) continue;
+        float v = 0.0f;
+#pragma unroll 4
+        for (int r = 0; r < a.ctas; ++r) v = fmaf(cluster.map_shared_rank(&share, r)->out[c][ch], ex2(shares_ml[r][c].x - merge_l[1][c]), v);
+        v *= merge_l[0][c];
+        const int col = cb * kCols + c, tok = col / a.G;
+        const long long at = s * a.o_seq + tok * a.o_tok + (h * a.G + col - tok * a.G) * a.o_head + ch;
+        if constexpr (PARTS == 1) static_cast<__nv_bfloat16*>(a.out)[at] = __float2bfloat16_rn(v);
+        else static_cast<float*>(a.out)[at] = v;
+      }
+      if (a.accumulate) {                                  // one block of columns: the CTA has its rows' scores of all of them
+        const float inv_g = 1.0f / (float)a.G;
+        for (int r = from * kTileRows + tid; r < min(to * kTileRows, sg.len); r += kAttendWarps * 32) {
+          const float* x = a.scores + ((long long)sg.begin + r) * a.R;
+          float sum = 0.0f;
+          for (int c = 0; c < a.R; ++c) sum += ex2(x[c] - lse_of[c]);
+          float* w = a.c.weight + sg.begin + r;
+          *w = fmaf(a.decay, *w, sum * inv_g);
+        }
+      }
+      cluster.sync();                                      // nobody reads this CTA's share any more
+    } else {
+      __syncthreads();                                     // the rings and the sums are free again
+    }
   }
   if (dead)                                                // what is still in flight lands before the memory is another CTA's
     for (unsigned i = lost; i < issued; ++i) copies_there(bar0 + 8 * (i % kStages), (i / kStages) & 1);
@@ -710,26 +785,51 @@ struct Q4Workspace {
   }
 };
 
-template <int HD, int PARTS, bool MASK>
-cudaError_t launch_attend(Q4AttendArgs& a, cudaStream_t st, int* launches) {
-  auto kernel = k_q4_attend<HD, PARTS, MASK>;
-  static std::atomic<int> per_sm[16];                      // of each device; found once
+// CTAs of one SM, and its dynamic shared memory allowed; found once for each device.
+template <int HD, int PARTS, bool MASK, bool CLUSTER>
+cudaError_t attend_ctas(int* per_sm) {
+  auto kernel = k_q4_attend<HD, PARTS, MASK, CLUSTER>;
+  static std::atomic<int> known[16];
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
-  int n = dev < 16 ? per_sm[dev].load(std::memory_order_relaxed) : 0;
+  int n = dev < 16 ? known[dev].load(std::memory_order_relaxed) : 0;
   if (n == 0) {
     e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kQ4Smem<HD>);
     if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, kAttendWarps * 32, kQ4Smem<HD>);
     if (e != cudaSuccess) return e;
     if (n < 1) return cudaErrorLaunchOutOfResources;
-    if (dev < 16) per_sm[dev].store(n, std::memory_order_relaxed);
+    if (dev < 16) known[dev].store(n, std::memory_order_relaxed);
   }
-  const int most = sm_count() * n;
+  *per_sm = n;
+  return cudaSuccess;
+}
+
+template <int HD, int PARTS, bool MASK>
+cudaError_t launch_attend(Q4AttendArgs& a, cudaStream_t st, int* launches) {
+  int per_sm = 0;
+  const dim3 block(kAttendWarps * 32);
+  // One launch: units that fit on the device with four or eight CTAs each, of 64 to 128 slots per CTA on average.  A cluster takes
+  // its whole unit, however long: with more slots the longest unit costs more than the second launch (60 units of 33 to 3001
+  // rows, 171 to a CTA: 13.7 us against 11).
+  const long long units = (long long)a.c.n_seg * a.n_cb, room = a.c.capacity / a.c.n_seg;
+  int ctas = kAttendCluster;
+  while (ctas > 1 && (units * ctas > 3ll * sm_count() || room < 64 * ctas)) ctas /= 2;
+  if (ctas >= 4 && room <= 128 * ctas && (a.n_cb == 1 || !a.accumulate)) {
+    cudaError_t e = attend_ctas<HD, PARTS, MASK, true>(&per_sm);
+    if (e != cudaSuccess) return e;
+    a.ctas = ctas;
+    a.n_cta = 1;
+    LaunchScope scope(KID_Q4_ATTEND, st, launches);
+    return launch_pdl(k_q4_attend<HD, PARTS, MASK, true>, dim3((unsigned)(units * ctas)), block, kQ4Smem<HD>, st, ctas, a);
+  }
+  cudaError_t e = attend_ctas<HD, PARTS, MASK, false>(&per_sm);
+  if (e != cudaSuccess) return e;
+  const int most = sm_count() * per_sm;
   a.n_cta = most < kMaxQ4Ctas ? most : kMaxQ4Ctas;
   {
     LaunchScope scope(KID_Q4_ATTEND, st, launches);
-    e = launch_pdl(kernel, dim3((unsigned)a.n_cta), dim3(kAttendWarps * 32), kQ4Smem<HD>, st, 1, a);
+    e = launch_pdl(k_q4_attend<HD, PARTS, MASK, false>, dim3((unsigned)a.n_cta), block, kQ4Smem<HD>, st, 1, a);
   }
   if (e != cudaSuccess) return e;
   LaunchScope scope(KID_Q4_JOIN, st, launches);

@@ -231,6 +231,23 @@ def test_caps_biases_and_masks_by_position(d, dtype, kw):
     assert torch.all(out[1, :, :G] == 0)                    # an empty segment
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("lens,hkv,short", [([700, 1, 0, 1300], 2, True), ([2000, 1500, 3000, 0], 4, False), ([5, 6000], 1, False),
+                                            ([511, 520, 530, 0, 1023, 1], 3, True), ([900, 1200, 40, 1700], 2, True)])
+@pytest.mark.parametrize("G,nt", [(4, 1), (1, 1), (8, 1), (2, 3), (3, 4)])
+def test_few_short_units_and_their_clusters(d, dtype, lens, hkv, short, G, nt):
+    t = R.random_cache(sum(lens) + d + G, lens, d, hkv, device=DEV)
+    q = queries(d + G, len(lens) // hkv, nt, hkv * G, d, dtype)
+    check(t, hkv, q, accumulate=True)
+    assert B.slkv_last_launch_count() == (1 if short and G * nt <= 8 else 2)      # several blocks of columns: weights need a second one
+    q_pos = (torch.arange(len(lens) // hkv * nt, device=DEV, dtype=torch.int32).view(-1, nt) * 397 + 100).contiguous()
+    slopes = torch.exp2(-torch.arange(hkv * G, device=DEV, dtype=torch.float32))
+    check(t, hkv, q, accumulate=True, q_pos=q_pos, slopes=slopes, softcap=10.0)
+    check(t, hkv, q, q_pos=q_pos)
+    assert B.slkv_last_launch_count() == (1 if short else 2)
+
+
 @pytest.mark.parametrize("d,dtype", [(128, torch.bfloat16), (64, torch.float32)])
 def test_long_segments_in_many_pieces(d, dtype):
     lens = [40001, 12, 0, 33000]
