@@ -496,7 +496,8 @@ int slkv_q4_unpack(const slkv_q4_cache* c, int32_t dtype, const int32_t* slots_o
  *   accumulate 1: weight[r] = weight_decay * weight[r] + (1/G) sum over the G query heads of h and over the tokens of p[r], for every
  *              filled slot (the reduction slkv_score uses over window rows and heads)
  *   status     dev, optional: SLKV_ERR_DEVICE_TIMEOUT if a bounded wait inside the kernel ran out
- * Limits: n_q_heads / n_kv_heads * n_tokens <= 256.  Positions are >= 0.  fp32 accumulation throughout; with bf16 rows, probabilities
+ * Limits: n_q_heads / n_kv_heads * n_tokens <= 256.  Positions are >= 0.  Queries are below 2^67 in magnitude (a head with a larger
+ * one, or a NaN, gets NaN).  fp32 accumulation throughout; with bf16 rows, probabilities
  * times scales are rounded to bf16 for the product with V, with fp32 rows they keep 24 bits.
  */
 typedef struct slkv_q4_attend_params {

@@ -5,10 +5,10 @@
 // low eight bits of a bf16 with nothing above them are an integer times 2^-133 -- subnormal up to 127, the first normal numbers
 // from there on -- so a nibble needs no more than a mask where it lies in them, the lower one as it is, the upper one as 16 times
 // itself: one shift and four masks make eight operands.
-//   scores  the queries are scaled by a power of two per head that keeps every product a normal fp32 number, and those that
-//           meet upper nibbles by 1/16; both are exact.  A score is the sum over groups of scale * product, plus the sum over
-//           groups of zero * (sum of the group's queries), which is one more product: the zeros as they lie in the record, the
-//           query sums in three bf16 parts.
+//   scores  the queries are scaled by 2^60, those that meet upper nibbles by 2^56: exact, and every product of one of 2^-50 or more
+//           is a normal fp32 number.  A score is the sum over groups of scale * product, plus the sum over groups of zero *
+//           (sum of the group's queries), which is one more product: the zeros as they lie in the record, the query sums in three
+//           bf16 parts.
 //   output  one packed multiply-add makes (c - 8) / 128 of a value nibble, exactly.  Probabilities times the group's scale,
 //           rounded to bf16, are the other operand.  zero + 8 scale goes with the unrounded probabilities, in fp32.
 // Keys are the products' long side (m16), the query heads of a KV head and its tokens the short one (n8): with four heads to a
@@ -42,6 +42,7 @@ namespace cg = cooperative_groups;
 constexpr int kAttendCluster = 8;       // CTAs of a cluster, at most
 constexpr int kAttendWarps = 4, kTileRows = 32, kCols = 8;
 constexpr unsigned kLower = 0x000f000fu, kUpper = 0x00f000f0u;
+constexpr unsigned kQueryScales = 0x5b805d80u;            // bf16: 2^60 for even channels, which meet lower nibbles, 2^56 for odd ones
 constexpr float kLowest = -3e38f;       // a maximum over nothing: below every score, and differences of two stay numbers
 constexpr float kSlack = 8.0f;
 constexpr int kFewestTiles = 4;         // of a piece, where its unit has as many: one for each warp
@@ -109,6 +110,10 @@ __device__ __forceinline__ unsigned transpose8(unsigned x) {
 __device__ __forceinline__ unsigned pack2(float lo, float hi) {
   const __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<const unsigned*>(&b);
+}
+__device__ __forceinline__ unsigned times2(unsigned a, unsigned b) {
+  const __nv_bfloat162 y = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
+  return *reinterpret_cast<const unsigned*>(&y);
 }
 __device__ __forceinline__ float lo_f(unsigned w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float hi_f(unsigned w) { return __uint_as_float(w & 0xffff0000u); }
@@ -273,57 +278,44 @@ __global__ void __launch_bounds__(kAttendWarps * 32, PARTS == 1 ? 4 : HD == 64 ?
     // ---- the unit's queries: fragments, and sums per group
     const int s = seg / a.n_kv_heads, h = seg - s * a.n_kv_heads;
     unsigned bq[PARTS][NG][2][2], bz[2] = {0u, 0u};
-    float to_log2[2];                                      // of columns 2 t and 2 t + 1: from the products' units
     {
       const int col = cb * kCols + g;
       const bool there = col < a.R;
       const int tok = there ? col / a.G : 0, qh = h * a.G + (there ? col - tok * a.G : 0);
       const long long at = s * a.q_seq + tok * a.q_tok + qh * a.q_head + 8 * t;
-      float x[NG][8], qs[NG], most = 0.0f;
+      float qs[NG];                                        // 2^60 times a group's sum
 #pragma unroll
       for (int j = 0; j < NG; ++j) {
         if constexpr (PARTS == 1) {
           uint4 w = make_uint4(0, 0, 0, 0);
           if (there) w = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.q) + at + 32 * j);
-          x[j][0] = lo_f(w.x); x[j][1] = hi_f(w.x); x[j][2] = lo_f(w.y); x[j][3] = hi_f(w.y);
-          x[j][4] = lo_f(w.z); x[j][5] = hi_f(w.z); x[j][6] = lo_f(w.w); x[j][7] = hi_f(w.w);
+          w.x = times2(w.x, kQueryScales); w.y = times2(w.y, kQueryScales);
+          w.z = times2(w.z, kQueryScales); w.w = times2(w.w, kQueryScales);
+          bq[0][j][0][0] = __byte_perm(w.x, w.z, 0x5410); bq[0][j][0][1] = __byte_perm(w.x, w.z, 0x7632);
+          bq[0][j][1][0] = __byte_perm(w.y, w.w, 0x5410); bq[0][j][1][1] = __byte_perm(w.y, w.w, 0x7632);
+          qs[j] = fmaf(16.0f, (hi_f(w.x) + hi_f(w.y)) + (hi_f(w.z) + hi_f(w.w)), (lo_f(w.x) + lo_f(w.y)) + (lo_f(w.z) + lo_f(w.w)));
         } else {
           float4 u = make_float4(0, 0, 0, 0), v = u;
           if (there) {
             const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(a.q) + at + 32 * j);
             u = p[0]; v = p[1];
           }
-          x[j][0] = u.x; x[j][1] = u.y; x[j][2] = u.z; x[j][3] = u.w; x[j][4] = v.x; x[j][5] = v.y; x[j][6] = v.z; x[j][7] = v.w;
+          qs[j] = 0x1p60f * (((u.x + u.y) + (u.z + u.w)) + ((v.x + v.y) + (v.z + v.w)));
+          float x[8] = {u.x * 0x1p60f, u.y * 0x1p56f, u.z * 0x1p60f, u.w * 0x1p56f, v.x * 0x1p60f, v.y * 0x1p56f, v.z * 0x1p60f, v.w * 0x1p56f};
+#pragma unroll
+          for (int p = 0; p < PARTS; ++p)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const unsigned w = pack2(x[e], x[e + 4]);
+              bq[p][j][e >> 1][e & 1] = w;
+              x[e] -= lo_f(w);
+              x[e + 4] -= hi_f(w);
+            }
         }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(x[j][e]));
-      }
-      most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
-      most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
-      // The head's largest query to 2^99 .. 2^100 (heads of less than 2^-40 or more than 2^86: as if they were those): products
-      // with a nibble are below 2^-29 and normal down to 2^-97 of the largest.
-      const int up2 = 99 - min(max((int)(__float_as_uint(most) >> 23) - 127, -40), 86);
-      const float f = __int_as_float((127 + up2 / 2) << 23), f2 = __int_as_float((127 + up2 - up2 / 2) << 23);
-#pragma unroll
-      for (int j = 0; j < NG; ++j) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[j][e] = x[j][e] * f * f2;
-        qs[j] = ((x[j][0] + x[j][1]) + (x[j][2] + x[j][3])) + ((x[j][4] + x[j][5]) + (x[j][6] + x[j][7]));
         qs[j] += __shfl_xor_sync(0xffffffffu, qs[j], 1);
         qs[j] += __shfl_xor_sync(0xffffffffu, qs[j], 2);
-#pragma unroll
-        for (int e = 1; e < 8; e += 2) x[j][e] *= 0.0625f;
-#pragma unroll
-        for (int p = 0; p < PARTS; ++p)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const unsigned w = pack2(x[j][e], x[j][e + 4]);
-            bq[p][j][e >> 1][e & 1] = w;
-            x[j][e] -= lo_f(w);
-            x[j][e + 4] -= hi_f(w);
-          }
       }
-      // the query sums in the products' units, 2^-133, in three parts: lane t holds part t of all groups, where the zeros'
+      // the query sums in the products' units, 2^(60 - 133), in three parts: lane t holds part t of all groups, where the zeros'
       // fragment expects them
 #pragma unroll
       for (int jj = 0; jj < NG / 2; ++jj) {
@@ -336,10 +328,8 @@ __global__ void __launch_bounds__(kAttendWarps * 32, PARTS == 1 ? 4 : HD == 64 ?
           y1 -= hi_f(v);
         }
       }
-#pragma unroll
-      for (int c = 0; c < 2; ++c)                          // 2^(133 - up2), at most 2^120
-        to_log2[c] = a.scale * kLog2e * __int_as_float((127 + 133 - __shfl_sync(0xffffffffu, up2, 8 * t + 4 * c)) << 23);
     }
+    const float to_log2 = a.scale * kLog2e * 0x1p73f;      // from the products' units
     const float per_cap = a.softcap > 0.0f ? 1.0f / (a.softcap * kLog2e) : 0.0f;
     int qp[2] = {0, 0};
     float slope[2] = {0.0f, 0.0f};
@@ -416,7 +406,7 @@ __global__ void __launch_bounds__(kAttendWarps * 32, PARTS == 1 ? 4 : HD == 64 ?
           }
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] *= to_log2[i & 1];
+        for (int i = 0; i < 4; ++i) x[i] *= to_log2;
         if (a.softcap > 0.0f) {
 #pragma unroll
           for (int i = 0; i < 4; ++i) x[i] = a.softcap * kLog2e * tanhf(x[i] * per_cap);
