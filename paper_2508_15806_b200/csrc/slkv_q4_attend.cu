@@ -145,20 +145,24 @@ __device__ __forceinline__ void load_words(uint32_t at, unsigned (&w)[N]) {
     asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w[0]) : "r"(at) : "memory");
 }
 
-// Sum over the CTA, and what the threads before this one have of it.  sums: a word for each warp, not used since the last barrier but one.
-__device__ __forceinline__ int cta_before(int x, int* sums) {
+// Pieces of a unit, by the reciprocal of their size: to the nearest rounding up, at least one for a unit that has a tile, no more
+// than tiles.  Every thread of the launch gets the same.
+__device__ __forceinline__ int pieces_of(int tiles, float inverse) { return tiles > 0 ? 1 + (int)((float)(tiles - 1) * inverse) : 0; }
+// What the threads before this one have of x and of y.  sums: 2 words for each warp.
+__device__ __forceinline__ void cta_before2(int x, int y, int* x_before, int* y_before, int* sums) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  int sum = x;
+  int sx = x, sy = y;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const int y = __shfl_up_sync(0xffffffffu, sum, o);
-    if (lane >= o) sum += y;
+    const int ux = __shfl_up_sync(0xffffffffu, sx, o), uy = __shfl_up_sync(0xffffffffu, sy, o);
+    if (lane >= o) { sx += ux; sy += uy; }
   }
   __syncthreads();
-  if (lane == 31) sums[warp] = sum;
+  if (lane == 31) { sums[2 * warp] = sx; sums[2 * warp + 1] = sy; }
   __syncthreads();
-  for (int w = 0; w < warp; ++w) sum += sums[w];
-  return sum - x;
+  for (int w = 0; w < warp; ++w) { sx += sums[2 * w]; sy += sums[2 * w + 1]; }
+  *x_before = sx - x;
+  *y_before = sy - y;
 }
 __device__ __forceinline__ int cta_total(int x, int* sums) {
   x = __reduce_add_sync(0xffffffffu, x);
@@ -205,29 +209,73 @@ __global__ void __launch_bounds__(kAttendWarps * 32, PARTS == 1 ? 4 : HD == 64 ?
   const int n_seg = a.c.n_seg;
   unsigned issued = 0, used = 0, lost = 0;                 // copies of this warp's ring
   bool dead = false;
+  constexpr int kHeld = 4;                                 // segments whose tiles a thread keeps; it looks at others again
   const int per_thread = CLUSTER ? 0 : (n_seg + kAttendWarps * 32 - 1) / (kAttendWarps * 32);
   const int first = min(tid * per_thread, n_seg), last = min(first + per_thread, n_seg);
-  auto tiles_at = [&](int seg) { return tiles_of(q4_segment(a.c.starts, a.c.lens, seg, a.c.capacity).len); };
-  int all = 1, per = 1;
+  int held[kHeld], all = 1;
+  float inverse_per = 1.0f;
+  auto each = [&](auto f) {                                // f(segment, its tiles) until it says false
+    for (int i = 0; first + i < last; ++i) {
+      int n = 0;
+      if (i < kHeld) {
+#pragma unroll
+        for (int k = 0; k < kHeld; ++k) n = i == k ? held[k] : n;
+      } else {
+        n = tiles_of(q4_segment(a.c.starts, a.c.lens, first + i, a.c.capacity).len);
+      }
+      if (!f(first + i, n)) break;
+    }
+  };
   if constexpr (!CLUSTER) {
-  int mine = 0;
-  for (int s = first; s < last; ++s) mine += tiles_at(s);
-  const int total = cta_total(mine, found) * a.n_cb;
-  const int units = n_seg * a.n_cb;
-  // a unit's last piece is half full on average; few units get no further wave for a bad average
-  per = max((total - 1) / max(a.n_cta - (8 * units <= a.n_cta ? units : units / 2), a.n_cta / 4) + 1, kFewestTiles);
-  int pieces = 0, split = 0;                               // of this thread's segments; those of units of several
-  for (int s = first; s < last; ++s) {
-    const int n = (tiles_at(s) + per - 1) / per;
-    pieces += n * a.n_cb;
-    split += n > 1 ? n * a.n_cb : 0;
-  }
-  before[tid] = cta_before(pieces, found);
-  places[tid] = cta_before(split, found + 4);
-  if (tid == kAttendWarps * 32 - 1) before[tid + 1] = before[tid] + pieces;
-  __syncthreads();
-  all = before[kAttendWarps * 32];
-  if (blockIdx.x == 0 && tid == 0) a.head[0] = all;
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k) held[k] = first + k < last ? tiles_of(q4_segment(a.c.starts, a.c.lens, first + k, a.c.capacity).len) : 0;
+    int mine = 0;
+    each([&](int, int n) { mine += n; return true; });
+    const int total = cta_total(mine, found) * a.n_cb, units = n_seg * a.n_cb;
+    // The size of a piece: the smallest of five between an even share and what leaves a CTA to each unit's odd rest that makes no
+    // more pieces than CTAs (a further wave of a few would take as long as the first).
+    const int least = max((total - 1) / a.n_cta + 1, kFewestTiles);
+    const int most = max((total - 1) / max(a.n_cta - units, a.n_cta / 4) + 1, kFewestTiles);
+    int per = most;
+    int sums[4] = {0, 0, 0, 0};
+    if (most > least) {
+      float inverse[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) inverse[k] = 1.0f / (float)(least + (most - least) * k / 4);
+      each([&](int, int n) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) sums[k] += pieces_of(n, inverse[k]);
+        return true;
+      });
+      __syncthreads();                                     // the total's words are read
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        sums[k] = __reduce_add_sync(0xffffffffu, sums[k]);
+        if (lane == 0) places[warp * 4 + k] = sums[k];
+      }
+      __syncthreads();
+#pragma unroll
+      for (int k = 3; k >= 0; --k) {
+        int n = 0;
+#pragma unroll
+        for (int w = 0; w < kAttendWarps; ++w) n += places[w * 4 + k];
+        if (n * a.n_cb <= a.n_cta) per = least + (most - least) * k / 4;
+      }
+      __syncthreads();
+    }
+    inverse_per = 1.0f / (float)per;
+    int pieces = 0, split = 0;                             // of this thread's segments; those of units of several
+    each([&](int, int t) {
+      const int n = pieces_of(t, inverse_per);
+      pieces += n * a.n_cb;
+      split += n > 1 ? n * a.n_cb : 0;
+      return true;
+    });
+    cta_before2(pieces, split, &before[tid], &places[tid], found);
+    if (tid == kAttendWarps * 32 - 1) before[tid + 1] = before[tid] + pieces;
+    __syncthreads();
+    all = before[kAttendWarps * 32];
+    if (blockIdx.x == 0 && tid == 0) a.head[0] = all;
   }
 
   for (int index = CLUSTER ? 0 : blockIdx.x; index < all; index += a.n_cta) {
@@ -237,13 +285,15 @@ __global__ void __launch_bounds__(kAttendWarps * 32, PARTS == 1 ? 4 : HD == 64 ?
       seg = unit / a.n_cb; cb = unit - seg * a.n_cb; nth = blockIdx.x - unit * a.ctas; n_pieces = a.ctas;
     } else {
       if (before[tid] <= index && index < before[tid + 1]) {       // the one thread that has the piece's segment
-        int u = before[tid], s = first, n = 0, at = places[tid];
-        for (; s < last; ++s) {
-          n = (tiles_at(s) + per - 1) / per;
-          if (index < u + n * a.n_cb) break;
+        int u = before[tid], s = first, n = 1, at = places[tid];
+        each([&](int segment, int t) {
+          s = segment;
+          n = pieces_of(t, inverse_per);
+          if (index < u + n * a.n_cb) return false;
           u += n * a.n_cb;
           at += n > 1 ? n * a.n_cb : 0;
-        }
+          return true;
+        });
         found[0] = s; found[1] = (index - u) / n; found[2] = (index - u) % n; found[3] = n; found[4] = at;
       }
       __syncthreads();
@@ -251,7 +301,8 @@ __global__ void __launch_bounds__(kAttendWarps * 32, PARTS == 1 ? 4 : HD == 64 ?
     }
     const Q4Segment sg = q4_segment(a.c.starts, a.c.lens, seg, a.c.capacity);
     const int tiles = tiles_of(sg.len);
-    const int from = (int)((long long)tiles * nth / n_pieces), to = (int)((long long)tiles * (nth + 1) / n_pieces);
+    const int even = tiles / n_pieces, odd = tiles - even * n_pieces;        // the first `odd` pieces have a tile more
+    const int from = even * nth + min(nth, odd), to = from + even + (nth < odd);
     const unsigned char* rows = a.c.records + (long long)sg.begin * RB;
     if (!CLUSTER && tid == 0) {
       if (nth == 0) a.unit[seg * a.n_cb + cb] = make_int2(n_pieces, place);
