@@ -437,8 +437,9 @@ int slkv_noalloc_last_cuda_error(void);
  *   pos      the token's position in its sequence (kept_idx).  Slots need not be in the order of their positions.
  *   weight   the attention the row has received: 0 when it comes in, added to by slkv_q4_attend, read by slkv_q4_evict.  May be NULL
  *            for callers that never evict.
- * Everything is enqueued on `stream`, nothing is allocated, every call can be captured.  Results are the same bit for bit from call
- * to call.  n_seqs * n_kv_heads <= 16384, 1 <= capacity_rows < 2^31; records, rows and workspaces 16-byte aligned.
+ * Everything is enqueued on `stream`, nothing is allocated, every call can be captured.  A cache and a workspace belong to one call at a
+ * time: calls on several streams, and graphs that are replayed beside each other, need their own or an order between them.  Results are
+ * the same bit for bit from call to call.  n_seqs * n_kv_heads <= 16384, 1 <= capacity_rows < 2^31; records, rows and workspaces 16-byte aligned.
  */
 typedef struct slkv_q4_cache {
   int32_t n_seqs, n_kv_heads, head_dim;   /* head_dim 64 or 128 */
@@ -506,7 +507,7 @@ typedef struct slkv_q4_attend_params {
   int32_t dtype;            /* SLKV_F32 | SLKV_BF16: q and out */
   int32_t lse_units;        /* SLKV_LSE_LN | SLKV_LSE_LOG2 */
   float scale;              /* 1 / sqrt(head_dim), usually */
-  float softcap;            /* 0: none */
+  float softcap;            /* 0: none; else >= 1e-20 */
   float weight_decay;       /* 1: a plain sum */
   int32_t reserved;
   int64_t q_stride_seq, q_stride_tok, q_stride_head;

@@ -261,6 +261,59 @@ def test_many_short_segments():
     check(t, 6, queries(2, 500, 1, 6, 64, torch.bfloat16), accumulate=True)
 
 
+def test_as_many_columns_as_are_taken():
+    t = R.random_cache(61, [40, 300], 64, 1, device=DEV)
+    q_pos = torch.arange(32, dtype=torch.int32, device=DEV).view(2, 16) * 40
+    check(t, 1, queries(62, 2, 16, 16, 64, torch.bfloat16), accumulate=True, q_pos=q_pos)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_as_many_segments_as_are_taken(d):
+    # one row each: the output is that row's values
+    n, hkv = 16384, 8
+    t = R.random_cache(63, [1] * n, d, hkv, slack=1, device=DEV)
+    q = queries(64, n // hkv, 1, hkv, d, torch.float32).to(DEV)
+    t["weight"].zero_()
+    out, lse = attend(t, hkv, q, accumulate=True)
+    K, V, _ = R.decode(t["records"][t["starts"][:-1].long()], d)
+    x = (K * q.view(n, d).double().cpu().numpy()).sum(1) * d ** -0.5
+    size = (np.abs(K) * np.abs(q.view(n, d).double().cpu().numpy())).sum(1) * d ** -0.5
+    assert np.all(np.abs(lse.view(n).double().cpu().numpy() - x) <= 2.0 ** -19 * (1 + size))
+    # one probability of 1: three parts of bf16, a sum of two fp32 products
+    assert np.all(np.abs(out.view(n, d).double().cpu().numpy() - V) <= 2.0 ** -20 * (np.abs(V) + 16 * np.abs(V).max(1, keepdims=True)))
+    assert torch.all((t["weight"][t["starts"][:-1].long()] - 1).abs() <= 2.0 ** -21)
+
+
+def test_a_cache_beyond_32_bits():
+    d, rows_ = 128, 14_000_100                            # 2.24e9 bytes of records; 160 columns: 2.24e9 scores
+    small = R.random_cache(65, [100, 33], d, 1, slack=0, device=DEV)
+    big = dict(records=torch.zeros(rows_, 160, dtype=torch.uint8, device=DEV), pos=torch.zeros(rows_, dtype=torch.int32, device=DEV),
+               weight=torch.zeros(rows_, device=DEV), starts=torch.tensor([0, 100, rows_], dtype=torch.int32, device=DEV),
+               lens=torch.tensor([100, 0], dtype=torch.int32, device=DEV))
+    far = dict(big, starts=torch.tensor([0, rows_ - 100, rows_], dtype=torch.int32, device=DEV), lens=torch.tensor([0, 100], dtype=torch.int32, device=DEV))
+    here = dict(small, starts=small["starts"].clone(), lens=torch.tensor([100, 0], dtype=torch.int32, device=DEV))
+    for x in ("records", "pos", "weight"):
+        far[x][-100:] = small[x][:100]
+    q = queries(66, 2, 10, 16, d, torch.bfloat16)
+    want, lse = attend(here, 1, q, accumulate=True)
+    got, lse2 = attend(far, 1, torch.flip(q, [0]), accumulate=True)
+    assert torch.equal(got[1], want[0]) and torch.equal(lse2[1], lse[0]) and torch.equal(far["weight"][-100:], small["weight"][:100])
+    c = cache_of(far, 1)
+    k, v = rows(67, 2, d, torch.bfloat16)
+    far["lens"][1] = 99
+    B.slkv_q4_append(c, k.view(2, 1, 1, d).to(DEV), v.view(2, 1, 1, d).to(DEV), torch.full((2, 1), 7, dtype=torch.int32, device=DEV))
+    want_rec = expected_record(k.double().numpy(), v.double().numpy())
+    assert np.array_equal(far["records"][-1].cpu().numpy(), want_rec[1]) and far["lens"].tolist() == [1, 100]
+    ko, vo = (torch.zeros(1, d, device=DEV) for _ in range(2))
+    B.slkv_q4_unpack(c, ko, vo, slots=torch.tensor([rows_ - 1], dtype=torch.int32, device=DEV))
+    assert torch.equal(ko.cpu(), torch.from_numpy(R.decode(far["records"][-1:], d)[0]).float())
+    before = {x: far[x][-100:].cpu().clone() for x in ("records", "pos", "weight")}
+    before["starts"] = torch.tensor([0, 100])
+    assert run_evict(far, 1, [60], 1, [-1, -1]) == 0
+    src = R.evict_order(before["weight"].tolist(), before["pos"].tolist(), -1, 1, 60)
+    assert torch.equal(far["records"][-100:-40].cpu(), before["records"][src])
+
+
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_scores_far_apart_and_large_queries(dtype):
     t = R.random_cache(8, [500, 90], 128, 1, device=DEV)
@@ -406,6 +459,38 @@ def test_eviction_keeps_what_the_definition_says(d, lens, hkv, budgets, window, 
             assert torch.all(after["records"][b:e] == 0xAB) and torch.all(after["pos"][b:e] == -7)
 
 
+@pytest.mark.parametrize("kind", ["equal", "zero", "narrow", "huge", "tiny", "negative", "inf", "nan", "two values"])
+@pytest.mark.parametrize("lens,hkv", [([900, 3000], 1), ([20000, 9000, 30001], 3)])
+def test_eviction_by_weights_of_any_size(kind, lens, hkv):
+    t = R.random_cache(71, lens, 64, hkv, device=DEV)
+    n = t["weight"].numel()
+    g = torch.Generator().manual_seed(72)
+    u = torch.rand(n, generator=g)
+    w = {"equal": torch.full((n,), 1.25), "zero": torch.zeros(n), "narrow": 1 + u * 1e-4, "huge": u * 1e38, "tiny": u * 1e-38, "negative": -u * 1e3,
+         "inf": torch.where(u < 0.6, float("inf"), u), "nan": torch.where(u < 0.6, float("nan"), u),
+         "two values": torch.where(u < 0.4, 0.5, 0.25)}[kind]
+    t["weight"].copy_(w)
+    before = {k: v.cpu().clone() for k, v in t.items()}
+    budgets, newest = [len_ // 2 for len_ in lens[:hkv]], [-10 ** 6] * (len(lens) // hkv)          # no row is among the newest
+    assert run_evict(t, hkv, budgets, 1, newest) == 0
+    kept = [min(n_, budgets[s % hkv]) for s, n_ in enumerate(lens)]
+    assert t["lens"].tolist() == kept
+    expect_evicted(before, lens, hkv, budgets, 1, newest, before["starts"].tolist(), kept, {k: v.cpu() for k, v in t.items()})
+
+
+@pytest.mark.parametrize("lens", [[60000] + [10] * 23, [200001, 5, 0, 77]])
+@pytest.mark.parametrize("in_place", [True, False])
+def test_eviction_where_one_segment_is_far_longer_than_the_others(lens, in_place):
+    t = R.random_cache(73, lens, 64, 1, device=DEV)
+    before = {k: v.cpu().clone() for k, v in t.items()}
+    budgets, newest = [31000], [10 ** 6] * len(lens)
+    kept = [min(n, 31000) for n in lens]
+    to = None if in_place else empty_cache([x + 1 for x in kept], 64, 1)[0]
+    assert run_evict(t, 1, budgets, 16, newest, to=to) == 0
+    after = {k: v.cpu() for k, v in (to or t).items()}
+    expect_evicted(before, lens, 1, budgets, 16, newest, after["starts"].tolist(), kept, after)
+
+
 def test_eviction_into_a_cache_that_is_too_small():
     lens = [50, 60]
     t = R.random_cache(3, lens, 128, 1, device=DEV)
@@ -507,3 +592,53 @@ def test_the_same_bits_every_time_on_two_streams_and_in_a_graph():
         for x in ("lens", "records", "pos"):
             assert torch.equal(r[0][x], one[0][x]), x
         assert torch.equal(r[0]["weight"].view(torch.int32), one[0]["weight"].view(torch.int32))
+
+
+def test_the_first_calls_of_a_process_can_be_captured():
+    import os
+    import subprocess
+    import sys
+    program = """
+import sys
+sys.path[:0] = [%r, %r]
+import torch
+import q4_reference as R
+import test_gpu_q4_cache as T
+from paper_2508_15806_b200 import binding as B
+B.lib()
+lens = [3000, 5000, 100, 4100]
+t = R.random_cache(5, lens, 128, 2, device=T.DEV)
+few = R.random_cache(6, [300, 700], 64, 1, device=T.DEV)
+q = T.queries(1, 2, 1, 8, 128, torch.bfloat16).to(T.DEV)
+qf = T.queries(2, 2, 1, 4, 64, torch.float32).to(T.DEV)
+k, v = (T.queries(3 + i, 2, 1, 2, 128, torch.bfloat16).to(T.DEV) for i in range(2))
+newest = torch.full((2,), 50000, dtype=torch.int32, device=T.DEV)
+budgets = torch.tensor([700, 1500], dtype=torch.int32, device=T.DEV)
+ko, vo = (torch.zeros(t["records"].size(0), 128, device=T.DEV) for _ in range(2))
+c, cf = T.cache_of(t, 2), T.cache_of(few, 1)
+out, outf = torch.empty_like(q), torch.empty_like(qf)
+p, pf = B.make_q4_attend(c, q, out), B.make_q4_attend(cf, qf, outf)
+ws, wsf, ews = B.new_q4_workspace(c, p, True), B.new_q4_workspace(cf, pf), B.new_q4_evict_workspace(c)
+def step():
+    B.slkv_q4_append(c, k, v, newest.view(2, 1))
+    B.slkv_q4_attend(c, p, q, out, ws, accumulate=True)
+    B.slkv_q4_attend(cf, pf, qf, outf, wsf)
+    B.slkv_q4_evict(c, c, budgets, 8, newest, ews)
+    B.slkv_q4_unpack(c, ko, vo)
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    step()
+start = {x: y.clone() for x, y in t.items()}
+g.replay()
+torch.cuda.synchronize()
+first = [x.clone() for x in (out, outf, ko, vo, t["lens"], t["records"])]
+for x, y in start.items():
+    t[x].copy_(y)
+step()
+torch.cuda.synchronize()
+assert all(torch.equal(x, y) for x, y in zip(first, (out, outf, ko, vo, t["lens"], t["records"])))
+print("captured")
+""" % (os.path.dirname(os.path.dirname(os.path.abspath(__file__))), os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", program], capture_output=True, text=True, timeout=120)
+    assert r.returncode == 0 and "captured" in r.stdout, r.stdout + r.stderr

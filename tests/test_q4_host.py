@@ -77,7 +77,7 @@ def test_attention_arguments(L):
     E, c = B.ERR, C.byref(cache())
     for kw, code in [(dict(dtype=2), "BAD_DTYPE"), (dict(lse_units=5), "BAD_DTYPE"), (dict(n_tokens=0), "BAD_SHAPE"), (dict(n_q_heads=2), "BAD_SHAPE"),
                      (dict(n_q_heads=18), "BAD_SHAPE"), (dict(n_tokens=65), "BAD_SHAPE"), (dict(scale=float("nan")), "BAD_SHAPE"),
-                     (dict(softcap=-1.0), "BAD_SHAPE"), (dict(softcap=float("inf")), "BAD_SHAPE"), (dict(weight_decay=float("inf")), "BAD_SHAPE"),
+                     (dict(softcap=-1.0), "BAD_SHAPE"), (dict(softcap=1e-30), "BAD_SHAPE"), (dict(softcap=float("inf")), "BAD_SHAPE"), (dict(weight_decay=float("inf")), "BAD_SHAPE"),
                      (dict(q_stride_head=64), "BAD_SHAPE"), (dict(o_stride_tok=2052), "BAD_ALIGN")]:
         p = C.byref(attend_params(**kw))
         assert L.slkv_q4_attend(c, p, f, None, None, f, None, 0, None, f, 1 << 40, None) == E[code], kw
