@@ -23,7 +23,9 @@ namespace cg = cooperative_groups;
 
 constexpr int kEvictThreads = 512, kEvictBins = 2048, kEvictCluster = 8;
 constexpr int kMostKeys = 40960;        // that shared memory holds beside the rest
-constexpr int kFewKeys = 128;           // are ranked by counting, one for each thread: 0.5 us; another histogram takes 1.5
+// Keys that are ranked by counting, one for each thread: 128 of them take 0.5 us, 512 2 us; another histogram takes 1.5 us, and 8
+// in a cluster.
+template <bool CLUSTER> constexpr unsigned kFewKeys = CLUSTER ? kEvictThreads : 128;
 
 struct Q4EvictArgs {
   Q4CacheView from, to;
@@ -114,7 +116,7 @@ __device__ __forceinline__ void move_rows(const Q4EvictArgs& a, int n, int src, 
 
 struct EvictShared {
   alignas(16) unsigned hist[kEvictBins];   // of the CTA's keys
-  unsigned few[kFewKeys];               // the first CTA's: the keys that share the prefix
+  unsigned few[kEvictThreads];               // the first CTA's: the keys that share the prefix
   unsigned warp_sums[32];
   unsigned found[3], n_few;
   unsigned counts[4];
@@ -227,7 +229,7 @@ __global__ void __launch_bounds__(kEvictThreads, 2) k_q4_evict(const __grid_cons
     }
     need = sh.found[1];
     equal = sh.found[2];
-    if (known == 32 || equal <= kFewKeys) break;
+    if (known == 32 || equal <= kFewKeys<CLUSTER>) break;
     sync();                                                  // the histograms are read
   }
   if (known < 32) {                                          // few keys: which of them has need - 1 others above it?
