@@ -89,6 +89,11 @@ __device__ __forceinline__ bool copies_there(uint32_t bar, uint32_t parity) {
     if (now - began > kQ4WaitNs) return false;
   }
 }
+__device__ __forceinline__ float rcp(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
 __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -133,6 +138,15 @@ __device__ __forceinline__ unsigned v_pair(unsigned w, const Q4Centre& c) {
 }
 // Key of a product's row r: neighbours apart, so that the lanes of one shared-memory access meet all banks.
 __device__ __forceinline__ int key_of(int r) { return (r & 8) | ((0x57463120u >> (4 * (r & 7))) & 7); }      // 0 2 1 3 6 4 7 5
+// Tiles [*from, *to) of the nth of n equal pieces: the first ones have a tile more.
+__device__ __forceinline__ void piece_tiles(int tiles, int nth, int n, int* from, int* to) {
+  int even = (int)((float)tiles / (float)n);               // near: put right
+  while ((long long)even * n > tiles) --even;
+  while ((long long)(even + 1) * n <= tiles) ++even;
+  const int more = tiles - even * n;
+  *from = even * nth + min(nth, more);
+  *to = *from + even + (nth < more);
+}
 __device__ __forceinline__ int tiles_of(int len) { return (len + kTileRows - 1) / kTileRows; }
 // N 32-bit words from shared memory
 template <int N>
@@ -188,7 +202,7 @@ __global__ void __launch_bounds__(kAttendWarps * 32, PARTS == 1 ? 4 : HD == 64 ?
   constexpr int NG = HD / 32, RB = q4_record_bytes(HD), kStages = kQ4Stages<HD>, kStageBytes = kTileRows * RB;
   extern __shared__ __align__(128) unsigned char smem[];
   __shared__ __align__(8) unsigned long long bars[kAttendWarps][kStages];
-  __shared__ int found[8], before[kAttendWarps * 32 + 1], places[kAttendWarps * 32];
+  __shared__ int found[9], wholes[kAttendWarps * 32 + 1], splits[kAttendWarps * 32 + 1];
   __shared__ float merge_m[kAttendWarps][kCols], merge_l[kAttendWarps][kCols];
   __shared__ __align__(16) unsigned char share_room[CLUSTER ? sizeof(Q4Share<HD>) : 16];
   __shared__ float2 shares_ml[CLUSTER ? kAttendCluster : 1][kCols];
@@ -205,30 +219,21 @@ __global__ void __launch_bounds__(kAttendWarps * 32, PARTS == 1 ? 4 : HD == 64 ?
   pdl_launch_dependents();
   pdl_wait();
 
-  // ---- tiles of all units, the size of a piece, how many pieces come before each thread's segments
+  // ---- tiles of all units, the size of a piece, how many pieces come before those of each thread's segments
   const int n_seg = a.c.n_seg;
   unsigned issued = 0, used = 0, lost = 0;                 // copies of this warp's ring
   bool dead = false;
-  constexpr int kHeld = 4;                                 // segments whose tiles a thread keeps; it looks at others again
   const int per_thread = CLUSTER ? 0 : (n_seg + kAttendWarps * 32 - 1) / (kAttendWarps * 32);
   const int first = min(tid * per_thread, n_seg), last = min(first + per_thread, n_seg);
-  int held[kHeld], all = 1;
+  int all = 1, all_split = 0;
   float inverse_per = 1.0f;
+  // Loops as they are written: this code runs once, and what it costs is bringing it into the instruction cache.
   auto each = [&](auto f) {                                // f(segment, its tiles) until it says false
-    for (int i = 0; first + i < last; ++i) {
-      int n = 0;
-      if (i < kHeld) {
-#pragma unroll
-        for (int k = 0; k < kHeld; ++k) n = i == k ? held[k] : n;
-      } else {
-        n = tiles_of(q4_segment(a.c.starts, a.c.lens, first + i, a.c.capacity).len);
-      }
-      if (!f(first + i, n)) break;
-    }
+#pragma unroll 1
+    for (int i = first; i < last; ++i)
+      if (!f(i, tiles_of(q4_segment(a.c.starts, a.c.lens, i, a.c.capacity).len))) break;
   };
   if constexpr (!CLUSTER) {
-#pragma unroll
-    for (int k = 0; k < kHeld; ++k) held[k] = first + k < last ? tiles_of(q4_segment(a.c.starts, a.c.lens, first + k, a.c.capacity).len) : 0;
     int mine = 0;
     each([&](int, int n) { mine += n; return true; });
     const int total = cta_total(mine, found) * a.n_cb, units = n_seg * a.n_cb;
@@ -251,58 +256,71 @@ __global__ void __launch_bounds__(kAttendWarps * 32, PARTS == 1 ? 4 : HD == 64 ?
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         sums[k] = __reduce_add_sync(0xffffffffu, sums[k]);
-        if (lane == 0) places[warp * 4 + k] = sums[k];
+        if (lane == 0) wholes[warp * 4 + k] = sums[k];
       }
       __syncthreads();
 #pragma unroll
       for (int k = 3; k >= 0; --k) {
         int n = 0;
 #pragma unroll
-        for (int w = 0; w < kAttendWarps; ++w) n += places[w * 4 + k];
+        for (int w = 0; w < kAttendWarps; ++w) n += wholes[w * 4 + k];
         if (n * a.n_cb <= a.n_cta) per = least + (most - least) * k / 4;
       }
       __syncthreads();
     }
     inverse_per = 1.0f / (float)per;
-    int pieces = 0, split = 0;                             // of this thread's segments; those of units of several
+    // Pieces of units of several come first, all of some size, then the units of one piece, many of them small: CTAs that share an
+    // SM lie far apart in this order, and so have some of either.
+    int whole = 0, split = 0;                              // of this thread's segments
     each([&](int, int t) {
       const int n = pieces_of(t, inverse_per);
-      pieces += n * a.n_cb;
-      split += n > 1 ? n * a.n_cb : 0;
+      if (n > 1) split += n * a.n_cb;
+      else whole += n * a.n_cb;
       return true;
     });
-    cta_before2(pieces, split, &before[tid], &places[tid], found);
-    if (tid == kAttendWarps * 32 - 1) before[tid + 1] = before[tid] + pieces;
+    cta_before2(whole, split, &wholes[tid], &splits[tid], found);
+    if (tid == kAttendWarps * 32 - 1) { wholes[tid + 1] = wholes[tid] + whole; splits[tid + 1] = splits[tid] + split; }
     __syncthreads();
-    all = before[kAttendWarps * 32];
+    all_split = splits[kAttendWarps * 32];
+    all = all_split + wholes[kAttendWarps * 32];
     if (blockIdx.x == 0 && tid == 0) a.head[0] = all;
   }
 
   for (int index = CLUSTER ? 0 : blockIdx.x; index < all; index += a.n_cta) {
-    int seg, cb, nth, n_pieces, place = 0;
+    int seg, cb, nth, n_pieces, place = 0, from, to;
+    Q4Segment sg;
     if constexpr (CLUSTER) {                               // once: all is 1
       const int unit = blockIdx.x / a.ctas;
       seg = unit / a.n_cb; cb = unit - seg * a.n_cb; nth = blockIdx.x - unit * a.ctas; n_pieces = a.ctas;
+      sg = q4_segment(a.c.starts, a.c.lens, seg, a.c.capacity);
+      piece_tiles(tiles_of(sg.len), nth, n_pieces, &from, &to);
     } else {
-      if (before[tid] <= index && index < before[tid + 1]) {       // the one thread that has the piece's segment
-        int u = before[tid], s = first, n = 1, at = places[tid];
+      const bool of_several = index < all_split;
+      const int* before = of_several ? splits : wholes;
+      const int nth_of = of_several ? index : index - all_split;
+      if (before[tid] <= nth_of && nth_of < before[tid + 1]) {     // the one thread that has the piece's segment
+        int u = before[tid], s = first, n = 1, tiles = 0;
         each([&](int segment, int t) {
           s = segment;
+          tiles = t;
           n = pieces_of(t, inverse_per);
-          if (index < u + n * a.n_cb) return false;
+          if (n == 0 || of_several != (n > 1)) return true;
+          if (nth_of < u + n * a.n_cb) return false;
           u += n * a.n_cb;
-          at += n > 1 ? n * a.n_cb : 0;
           return true;
         });
-        found[0] = s; found[1] = (index - u) / n; found[2] = (index - u) % n; found[3] = n; found[4] = at;
+        const Q4Segment found_sg = q4_segment(a.c.starts, a.c.lens, s, a.c.capacity);
+        int block = 0, rest = nth_of - u;
+        for (; rest >= n; rest -= n) ++block;
+        found[0] = s; found[1] = block; found[2] = rest; found[3] = n; found[4] = u;
+        found[5] = found_sg.begin; found[6] = found_sg.len;
+        piece_tiles(tiles, rest, n, &found[7], &found[8]);
       }
       __syncthreads();
-      seg = found[0]; cb = found[1]; nth = found[2]; n_pieces = found[3]; place = found[4] + cb * n_pieces;
+      seg = found[0]; cb = found[1]; nth = found[2]; n_pieces = found[3]; place = found[4] + cb * n_pieces;           // of a unit of several: its pieces' own order
+      sg.begin = found[5]; sg.len = found[6];
+      from = found[7]; to = found[8];
     }
-    const Q4Segment sg = q4_segment(a.c.starts, a.c.lens, seg, a.c.capacity);
-    const int tiles = tiles_of(sg.len);
-    const int even = tiles / n_pieces, odd = tiles - even * n_pieces;        // the first `odd` pieces have a tile more
-    const int from = even * nth + min(nth, odd), to = from + even + (nth < odd);
     const unsigned char* rows = a.c.records + (long long)sg.begin * RB;
     if (!CLUSTER && tid == 0) {
       if (nth == 0) a.unit[seg * a.n_cb + cb] = make_int2(n_pieces, place);
@@ -381,7 +399,10 @@ __global__ void __launch_bounds__(kAttendWarps * 32, PARTS == 1 ? 4 : HD == 64 ?
       }
     }
     const float to_log2 = a.scale * kLog2e * 0x1p73f;      // from the products' units
-    const float per_cap = a.softcap > 0.0f ? 1.0f / (a.softcap * kLog2e) : 0.0f;
+    // softcap tanh(x / softcap) as softcap (1 - 2 / (1 + e^(2 x / softcap))), in base 2: off by 2^-22 of the cap at most, a few units
+    // in the last place of the larger scores (tanhf is exact to the last place for small ones too, which a softmax does not
+    // notice, and takes five times the instructions)
+    const float cap = a.softcap * kLog2e, per_cap = a.softcap > 0.0f ? 2.0f / a.softcap : 0.0f;
     int qp[2] = {0, 0};
     float slope[2] = {0.0f, 0.0f};
     if (MASK) {
@@ -460,7 +481,7 @@ __global__ void __launch_bounds__(kAttendWarps * 32, PARTS == 1 ? 4 : HD == 64 ?
         for (int i = 0; i < 4; ++i) x[i] *= to_log2;
         if (a.softcap > 0.0f) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) x[i] = a.softcap * kLog2e * tanhf(x[i] * per_cap);
+          for (int i = 0; i < 4; ++i) x[i] = fmaf(cap * -2.0f, rcp(1.0f + ex2(x[i] * per_cap)), cap);
         }
         if (MASK) {
           const int pos0 = __shfl_sync(0xffffffffu, pos_here, r0), pos1 = __shfl_sync(0xffffffffu, pos_here, r1);
@@ -711,7 +732,8 @@ template <int HD, bool F32>
 __global__ void __launch_bounds__(kJoinThreads) k_q4_join(const __grid_constant__ Q4AttendArgs a) {
   constexpr int kWarps = kJoinThreads / 32, V = HD / 32;   // channels per lane
   __shared__ __align__(16) float shares[kWarps][HD], lse_of[kMaxQ4Columns];
-  pdl_launch_dependents();
+  // No early launch of what comes after: CTAs that wait would hold the places of the next attention's, whose last ones then begin
+  // late (98 us a pass over long caches, against 89).
   pdl_wait();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int n_out = a.c.n_seg * a.R;

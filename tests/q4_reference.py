@@ -97,6 +97,9 @@ def attend(records, pos, weight, starts, lens, q, n_kv_heads, scale, softcap=0.0
                 # a score is a chain of about 32 fp32 additions of products whose magnitudes add up to `size` (zero and code
                 # parts: twice that), converted, exponentiated (2^-22) and summed
                 e = 2.0 ** -19 * (1.0 + float(np.max(size))) + 2.0 ** -22 * float(np.max(np.abs(x)))
+                # a capped score is cap (1 - 2 t), t = 1 / (1 + 2^y): 2^y off by 2^-22 of itself moves t by t (1 - t) 2^-22 <= 2^-24, the
+                # reciprocal by 2^-23; twice both times the cap, and the sum's rounding: under 2^-21 caps
+                e += 2.0 ** -21 * softcap
                 eta[s, h * G + hh, i] = e
                 spread[s, i, h * G + hh] = p @ A[vis]
                 mass[s, i, h * G + hh] = p @ np.abs(V[vis]) + p @ A[vis]
