@@ -21,10 +21,10 @@
 // pieces as CTAs are cut into equal pieces of whole tiles; a CTA takes a piece, and further ones where there are more.  A unit of
 // one piece is finished by its CTA; the others leave a maximum, a sum and an unscaled output per piece, which a second launch
 // joins.  In a CTA each warp takes every fourth tile with its own ring of bulk copies, so that no warp waits for another before
-// a piece ends.  (Cutting the line of all tiles evenly instead, pieces running across units, took 40 us where this takes 33:
-// a CTA's second piece starts with 3.4 us of latencies.)
+// a piece ends.  (Cutting the line of all tiles evenly instead, pieces running across units, took 40 us for 256 segments of 256 to 4096 rows
+// where this takes 32: a CTA's second piece starts with 3.4 us of latencies.)
 // Where units are few and short one launch does it all: a cluster of CTAs per unit, equal shares of its tiles, the shares joined
-// through the cluster's shared memory.  (One user, 8 heads of 129 to 1031 rows: 9.3 us with two launches, 7.6 with one.)
+// through the cluster's shared memory.  (One user, 8 heads of 129 to 1031 rows: 9.3 us with two launches, 7.4 with one.)
 // The weights need the final log-sum-exps: the scores are kept in the workspace, the second launch turns them into
 // probabilities (the same CTA, behind the cluster's exchange, where there is one launch).
 // What bounds it: the arithmetic between DRAM and the products (unpacking, scales).
