@@ -250,6 +250,16 @@ struct Q4UnpackArgs {
 
 constexpr int kUnpackRows = 8;          // of a warp at once
 
+__device__ __forceinline__ unsigned sub2(unsigned a, unsigned b) {
+  const __nv_bfloat162 y = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
+  return *reinterpret_cast<const unsigned*>(&y);
+}
+__device__ __forceinline__ unsigned fma2(unsigned a, unsigned b, unsigned c) {
+  unsigned y;
+  asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(y) : "r"(a), "r"(b), "r"(c));
+  return y;
+}
+
 template <int HD, bool F32>
 __global__ void __launch_bounds__(kQ4Warps * 32, 4) k_q4_unpack(const __grid_constant__ Q4UnpackArgs a) {
   // K in lanes 0 .. 15, V in 16 .. 31, eight channels to a lane
@@ -297,21 +307,23 @@ __global__ void __launch_bounds__(kQ4Warps * 32, 4) k_q4_unpack(const __grid_con
       const unsigned other = __shfl_xor_sync(0xffffffffu, j & 1 ? codes[i] & 0xffffu : codes[i] >> 16, 4);
       const unsigned mine = !is_v ? codes[i] : j & 1 ? (other | (codes[i] & 0xffff0000u)) : ((codes[i] & 0xffffu) | (other << 16));
       if (__shfl_sync(0xffffffffu, slot, i * kRows + sub) < 0) continue;
-      const float s = __uint_as_float(scale[i] << 16), z = __uint_as_float(zero[i] << 16);
-      float x[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e)                          // a nibble under the exponent of 2^23 is 2^23 + c
-        x[e] = __fmaf_rn(__uint_as_float(((mine >> (4 * e)) & 15u) | 0x4b000000u) - 8388608.0f, s, z);
       char* o = dst + (r0 + i * kRows + sub) * (HD * (F32 ? 4 : 2));
-      if (F32) {
+      if constexpr (F32) {
+        const float s = __uint_as_float(scale[i] << 16), z = __uint_as_float(zero[i] << 16);
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e)                        // a nibble under the exponent of 2^23 is 2^23 + c
+          x[e] = __fmaf_rn(__uint_as_float(((mine >> (4 * e)) & 15u) | 0x4b000000u) - 8388608.0f, s, z);
         __stcs(reinterpret_cast<float4*>(o), make_float4(x[0], x[1], x[2], x[3]));
         __stcs(reinterpret_cast<float4*>(o) + 1, make_float4(x[4], x[5], x[6], x[7]));
       } else {
+        // two channels at a time: under the exponent of 128 a nibble is 128 + c; one packed multiply-add, rounded once
+        const unsigned s = scale[i] * 0x10001u, z = zero[i] * 0x10001u, odd = mine >> 4;
         unsigned w[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const __nv_bfloat162 b = __floats2bfloat162_rn(x[2 * e], x[2 * e + 1]);
-          w[e] = *reinterpret_cast<const unsigned*>(&b);
+          const unsigned u = (__byte_perm(mine, odd, e | (4 + e) << 8) & 0x000f000fu) | 0x43004300u;
+          w[e] = fma2(sub2(u, 0x43004300u), s, z);
         }
         __stcs(reinterpret_cast<uint4*>(o), make_uint4(w[0], w[1], w[2], w[3]));
       }

@@ -216,6 +216,7 @@ __global__ void __launch_bounds__(kAttendWarps * 32, PARTS == 1 ? 4 : HD == 64 ?
                                                           uint32_t(key_of(2 * t + 1) * RB + HD / 2 + g * (HD / 16))};
   if (lane < kStages) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bar0 + 8 * lane) : "memory");
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  __syncthreads();
   pdl_launch_dependents();
   pdl_wait();
 
@@ -441,7 +442,7 @@ __global__ void __launch_bounds__(kAttendWarps * 32, PARTS == 1 ? 4 : HD == 64 ?
       }
       ++used;
       if (n < kTileRows) {                                 // what lies behind the last row must be finite: scales and zeros
-        if (lane >= n) {
+        if (lane >= n && lane < kTileRows) {
 #pragma unroll
           for (int i = 0; i < RB - HD; i += 16)
             *reinterpret_cast<uint4*>(ring + slot * kStageBytes + lane * RB + HD + i) = make_uint4(0, 0, 0, 0);
@@ -488,7 +489,8 @@ __global__ void __launch_bounds__(kAttendWarps * 32, PARTS == 1 ? 4 : HD == 64 ?
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const int pos = i < 2 ? pos0 : pos1;
-            x[i] = pos <= qp[i & 1] ? fmaf(slope[i & 1], (float)(pos - qp[i & 1]), x[i]) : -INFINITY;
+            if (a.slopes) x[i] = fmaf(slope[i & 1], (float)(pos - qp[i & 1]), x[i]);
+            if (pos > qp[i & 1]) x[i] = -INFINITY;
           }
         }
         if (k0 + 16 > n) {                                 // the last rows of a segment
