@@ -178,12 +178,13 @@ __device__ __forceinline__ void cta_before2(int x, int y, int* x_before, int* y_
   *x_before = sx - x;
   *y_before = sy - y;
 }
-__device__ __forceinline__ int cta_total(int x, int* sums) {
-  x = __reduce_add_sync(0xffffffffu, x);
-  if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5] = x;
+__device__ __forceinline__ float cta_total(float x, int* sums) {
+#pragma unroll
+  for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+  if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5] = __float_as_int(x);
   __syncthreads();
-  int sum = 0;
-  for (int w = 0; w < kAttendWarps; ++w) sum += sums[w];
+  float sum = 0.0f;
+  for (int w = 0; w < kAttendWarps; ++w) sum += __int_as_float(sums[w]);
   return sum;
 }
 
@@ -235,50 +236,51 @@ __global__ void __launch_bounds__(kAttendWarps * 32, PARTS == 1 ? 4 : HD == 64 ?
       if (!f(i, tiles_of(q4_segment(a.c.starts, a.c.lens, i, a.c.capacity).len))) break;
   };
   if constexpr (!CLUSTER) {
-    int mine = 0;
-    each([&](int, int n) { mine += n; return true; });
-    const int total = cta_total(mine, found) * a.n_cb, units = n_seg * a.n_cb;
+    float mine = 0.0f;                                     // near enough, and whatever starts holds it does not wrap around
+    each([&](int, int n) { mine += (float)n; return true; });
+    const float total = cta_total(mine, found) * (float)a.n_cb;
+    const int units = n_seg * a.n_cb;
     // The size of a piece: the smallest of five between an even share and what leaves a CTA to each unit's odd rest that makes no
-    // more pieces than CTAs (a further wave of a few would take as long as the first).
-    const int least = max((total - 1) / a.n_cta + 1, kFewestTiles);
-    const int most = max((total - 1) / max(a.n_cta - units, a.n_cta / 4) + 1, kFewestTiles);
-    int per = most;
-    int sums[4] = {0, 0, 0, 0};
-    if (most > least) {
-      float inverse[4];
+    // more pieces than CTAs (a further wave of a few would take as long as the first).  Reciprocals are near enough, too: they are
+    // the same in every thread of the launch.
+    auto share = [&](int n) { return max((int)fminf(total * rcp((float)n), 1e8f) + 1, kFewestTiles); };   // no unit has 1e8 tiles
+    const int least = share(a.n_cta), most = share(max(a.n_cta - units, a.n_cta / 4));
+    constexpr int kSizes = 5;
+    float inverse[kSizes];
+    int pieces[kSizes], several[kSizes];                   // of this thread's segments; of those cut into several
 #pragma unroll
-      for (int k = 0; k < 4; ++k) inverse[k] = 1.0f / (float)(least + (most - least) * k / 4);
-      each([&](int, int n) {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) sums[k] += pieces_of(n, inverse[k]);
-        return true;
-      });
-      __syncthreads();                                     // the total's words are read
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        sums[k] = __reduce_add_sync(0xffffffffu, sums[k]);
-        if (lane == 0) wholes[warp * 4 + k] = sums[k];
-      }
-      __syncthreads();
-#pragma unroll
-      for (int k = 3; k >= 0; --k) {
-        int n = 0;
-#pragma unroll
-        for (int w = 0; w < kAttendWarps; ++w) n += wholes[w * 4 + k];
-        if (n * a.n_cb <= a.n_cta) per = least + (most - least) * k / 4;
-      }
-      __syncthreads();
+    for (int k = 0; k < kSizes; ++k) {
+      inverse[k] = rcp((float)(least + ((most - least) * k >> 2)));
+      pieces[k] = several[k] = 0;
     }
-    inverse_per = 1.0f / (float)per;
-    // Pieces of units of several come first, all of some size, then the units of one piece, many of them small: CTAs that share an
-    // SM lie far apart in this order, and so have some of either.
-    int whole = 0, split = 0;                              // of this thread's segments
     each([&](int, int t) {
-      const int n = pieces_of(t, inverse_per);
-      if (n > 1) split += n * a.n_cb;
-      else whole += n * a.n_cb;
+#pragma unroll
+      for (int k = 0; k < kSizes; ++k) {
+        const int n = pieces_of(t, inverse[k]);
+        pieces[k] += n;
+        several[k] += n > 1 ? n : 0;
+      }
       return true;
     });
+#pragma unroll
+    for (int k = 0; k < kSizes - 1; ++k) {
+      const int n = __reduce_add_sync(0xffffffffu, pieces[k]);
+      if (lane == 0) wholes[warp * 4 + k] = n;
+    }
+    __syncthreads();
+    inverse_per = inverse[kSizes - 1];
+    int whole = pieces[kSizes - 1], split = several[kSizes - 1];
+#pragma unroll
+    for (int k = kSizes - 2; k >= 0; --k) {
+      int n = 0;
+#pragma unroll
+      for (int w = 0; w < kAttendWarps; ++w) n += wholes[w * 4 + k];
+      if (n * a.n_cb <= a.n_cta) { inverse_per = inverse[k]; whole = pieces[k]; split = several[k]; }
+    }
+    // Pieces of units of several come first, all of some size, then the units of one piece, many of them small: CTAs that share an
+    // SM lie far apart in this order, and so have some of either.
+    whole = (whole - split) * a.n_cb;
+    split *= a.n_cb;
     cta_before2(whole, split, &wholes[tid], &splits[tid], found);
     if (tid == kAttendWarps * 32 - 1) { wholes[tid + 1] = wholes[tid] + whole; splits[tid + 1] = splits[tid] + split; }
     __syncthreads();
