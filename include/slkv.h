@@ -430,7 +430,7 @@ int slkv_noalloc_last_cuda_error(void);
  *              zero = the minimum of the group rounded down to bf16, scale = (maximum - zero) / 15 rounded up to bf16,
  *              code = (x - zero) / scale in fp32, rounded to the nearest integer, ties to even: 0 .. 15
  *            so that |x - value| <= scale / 2 up to fp32 rounding.  A group with a NaN or an infinity, or with a range that fp32 does
- *            not hold, stands for NaN throughout.
+ *            not hold or a zero that bf16 does not, stands for NaN throughout.
  *            Layout: head_dim/2 bytes K codes, head_dim/2 bytes V codes, then head_dim/32 bf16 each of K scales, K zeros, V scales and
  *            V zeros.  K codes: 32-bit word t * head_dim/32 + j has channels 32 j + 8 t + e in its nibbles e = 0 .. 7, lowest first; V
  *            codes: 16-bit unit g * head_dim/32 + j has channels 32 j + 4 g + e in its nibbles e = 0 .. 3.

@@ -568,6 +568,7 @@ def slkv_q4_append(cache: SlkvQ4Cache, k: torch.Tensor, v: torch.Tensor, pos: to
     lens_out = None
     if after is not None:
         assert after.records == cache.records and after.starts == cache.starts and after.pos == cache.pos
+        assert after.n_seqs == ns and after.n_kv_heads == hkv
         lens_out = after.lens_tensor
     if status is not None:
         _q4_status(cache, status)
@@ -625,7 +626,8 @@ def slkv_q4_attend(cache: SlkvQ4Cache, params: SlkvQ4AttendParams, q: torch.Tens
     if not d == q.get_device() == out.get_device() == workspace.get_device() == _current_device():
         _q4_elsewhere()
     assert (q.shape, q.stride(), q.dtype) == params.q_like and (out.shape, out.stride(), out.dtype) == params.out_like
-    ns, nt, hq, _ = params.q_like[0]
+    ns, nt, hq, dim = params.q_like[0]
+    assert ns == cache.n_seqs and dim == cache.head_dim
     if q_pos is not None:
         assert q_pos.dtype is _I32 and q_pos.is_contiguous() and q_pos.numel() == ns * nt and q_pos.get_device() == d
     if slopes is not None:

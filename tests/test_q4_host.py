@@ -143,3 +143,32 @@ def test_python_layer_refuses_what_the_library_cannot_see(L):
         B.make_q4_attend(c, q[:1], q[:1])
     with pytest.raises(AssertionError):                              # not on a GPU
         B.slkv_q4_attend(c, B.make_q4_attend(c, q, q), q, q, rec)
+
+
+def test_python_layer_refuses_arguments_made_for_another_cache(monkeypatch):
+    # the library and the device taken away: a call that is not refused is seen
+    calls = []
+    monkeypatch.setattr(B, "_current_device", lambda: -1)
+    monkeypatch.setattr(B, "_fn", {n: lambda *a: calls.append(a) or B.SLKV_OK for n in ("slkv_q4_attend", "slkv_q4_append")})
+    t = lambda *s, dt=torch.int32: torch.zeros(*s, dtype=dt)        # noqa: E731
+    rec, pos, w, starts, lens = t(10, 160, dt=torch.uint8), t(10), t(10, dt=torch.float32), t(9), t(8)
+
+    def make(rec, n_seg, n_kv_heads):
+        c = B.make_q4_cache(rec, pos, w, starts[:n_seg + 1], lens[:n_seg], n_kv_heads)
+        c.index = -1
+        return c
+    c = make(rec, 8, 4)
+    q, new, at = torch.zeros(2, 1, 16, 128), torch.zeros(2, 1, 4, 128), t(2, 1)
+    p = B.make_q4_attend(c, q, q)
+    B.slkv_q4_attend(c, p, q, q, rec)
+    B.slkv_q4_append(c, new, new, at, c)
+    assert len(calls) == 2
+    for other in (make(rec, 4, 4), make(rec, 4, 2), make(t(10, 80, dt=torch.uint8), 8, 4)):
+        if (other.n_seqs, other.head_dim) != (2, 128):               # else: 16 query heads go with two KV heads as well
+            with pytest.raises(AssertionError):
+                B.slkv_q4_attend(other, p, q, q, rec)
+        with pytest.raises(AssertionError):                          # lengths for fewer segments than are written
+            B.slkv_q4_append(c, new, new, at, other)
+    with pytest.raises(AssertionError):
+        B.slkv_q4_append(c, new, new, at, make(rec, 8, 2))
+    assert len(calls) == 2
