@@ -402,9 +402,10 @@ __global__ void __launch_bounds__(kAttendWarps * 32, PARTS == 1 ? 4 : HD == 64 ?
       }
     }
     const float to_log2 = a.scale * kLog2e * 0x1p73f;      // from the products' units
-    // softcap tanh(x / softcap) as softcap (1 - 2 / (1 + e^(2 x / softcap))), in base 2: off by 2^-22 of the cap at most, a few units
-    // in the last place of the larger scores (tanhf is exact to the last place for small ones too, which a softmax does not
-    // notice, and takes five times the instructions)
+    // softcap tanh(x / softcap) as softcap (1 - 2 / (1 + e^(2 x / softcap))), in base 2: off by 2^-22 of the cap at most.  Under a
+    // quarter of the cap that could be more than the score itself: there x (1 - y^2 / 3 + 2 y^4 / 15 - 17 y^6 / 315 + 62 y^8 / 2835),
+    // y = x / softcap, tanh's Taylor series, whose next term is below 2^-26.  (tanhf is exact to the last place, which a softmax
+    // does not notice, and takes several times the instructions.)
     const float cap = a.softcap * kLog2e, per_cap = a.softcap > 0.0f ? 2.0f / a.softcap : 0.0f;
     int qp[2] = {0, 0};
     float slope[2] = {0.0f, 0.0f};
@@ -484,7 +485,13 @@ __global__ void __launch_bounds__(kAttendWarps * 32, PARTS == 1 ? 4 : HD == 64 ?
         for (int i = 0; i < 4; ++i) x[i] *= to_log2;
         if (a.softcap > 0.0f) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) x[i] = fmaf(cap * -2.0f, rcp(1.0f + ex2(x[i] * per_cap)), cap);
+          for (int i = 0; i < 4; ++i) {
+            constexpr float kUnit = 0.34657359027997265f * 0.34657359027997265f;         // (ln 2 / 2)^2: from u^2 to y^2
+            const float u = x[i] * per_cap, z = u * u * kUnit;
+            const float near = fmaf(x[i] * z, fmaf(z, fmaf(z, fmaf(z, 62.0f / 2835.0f, -17.0f / 315.0f), 2.0f / 15.0f), -1.0f / 3.0f), x[i]);
+            const float far = fmaf(cap * -2.0f, rcp(1.0f + ex2(u)), cap);
+            x[i] = fabsf(u) < 0.72f ? near : far;
+          }
         }
         if (MASK) {
           const int pos0 = __shfl_sync(0xffffffffu, pos_here, r0), pos1 = __shfl_sync(0xffffffffu, pos_here, r1);

@@ -86,6 +86,7 @@ def attend(records, pos, weight, starts, lens, q, n_kv_heads, scale, softcap=0.0
                 size = abs(scale) * (np.abs(K[vis]) @ np.abs(qq))
                 if softcap:
                     x = softcap * np.tanh(x / softcap)
+                capped = float(np.max(np.abs(x)))
                 if slopes is not None:
                     x = x + float(slopes[h * G + hh]) * (pos[b:b + n][vis] - int(q_pos[s, i]))
                 m = x.max()
@@ -98,8 +99,10 @@ def attend(records, pos, weight, starts, lens, q, n_kv_heads, scale, softcap=0.0
                 # parts: twice that), converted, exponentiated (2^-22) and summed
                 e = 2.0 ** -19 * (1.0 + float(np.max(size))) + 2.0 ** -22 * float(np.max(np.abs(x)))
                 # a capped score is cap (1 - 2 t), t = 1 / (1 + 2^y): 2^y off by 2^-22 of itself moves t by t (1 - t) 2^-22 <= 2^-24, the
-                # reciprocal by 2^-23; twice both times the cap, and the sum's rounding: under 2^-21 caps
-                e += 2.0 ** -21 * softcap
+                # reciprocal by 2^-23; twice both times the cap, and the sum's rounding: under 2^-21 caps.  Scores under a quarter of
+                # the cap (x = cap tanh y, |y| < 0.25) come from a series of eight roundings at most, of which all but the last
+                # are of terms of y^2 / 3 < 2^-5: under 2^-22 |x|; those above have a cap of under 4.1 |x|: under 2^-18 |x|
+                e += min(2.0 ** -21 * softcap, 2.0 ** -18 * capped)
                 eta[s, h * G + hh, i] = e
                 spread[s, i, h * G + hh] = p @ A[vis]
                 mass[s, i, h * G + hh] = p @ np.abs(V[vis]) + p @ A[vis]

@@ -217,7 +217,8 @@ def test_attention_over_any_lengths_and_columns(d, dtype, lens, hkv, G, nt):
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("kw", [dict(softcap=5.0), dict(softcap=30.0, weight_decay=0.9, scale=0.3), dict(slopes=True), dict(slopes=True, softcap=20.0),
-                                dict(units=B.SLKV_LSE_LOG2, weight_decay=0.0), dict(scale=-0.05)])
+                                dict(units=B.SLKV_LSE_LOG2, weight_decay=0.0), dict(scale=-0.05), dict(softcap=1e6), dict(softcap=3e38), dict(softcap=0.25),
+                                dict(slopes=True, softcap=1000.0)])
 def test_caps_biases_and_masks_by_position(d, dtype, kw):
     kw = dict(kw)
     hkv, G, nt = 2, 4, 3
