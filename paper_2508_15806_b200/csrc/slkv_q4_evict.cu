@@ -7,9 +7,10 @@
 // bin holds too many for that (weights that are all alike, or far out) their bits are descended, 11 + 11 + 10 of them.
 // The kept rows that lie behind the first `kept` slots then fill the holes before them, in order, so that as few rows move as
 // can, no row is read that another one overwrites, and a cache can be evicted from in place.
-// One launch: a cluster of CTAs per segment (one CTA where there are many segments or few rows), each with a contiguous share
-// of the slots, keys in shared memory; they share the moves evenly.
+// A cluster of CTAs per segment (one CTA where there are many segments or few rows), each with a contiguous share of the slots, keys in
+// shared memory; they share the moves evenly.  Where that is a handful of CTAs, a second launch moves the rows.
 // What bounds it: for few rows the chain of passes over the keys, for many the rows' bytes.
+#include <algorithm>
 #include <atomic>
 
 #include <cooperative_groups.h>
@@ -35,7 +36,7 @@ struct Q4EvictArgs {
                                         // ~i: the i-th of `movers`
   int32_t *holes, *movers;              // likewise: slots whose rows go, slots whose rows move
   int n_kv_heads, window, key_room;     // key_room: keys that the launch's shared memory holds
-  int in_place, ctas;                   // ctas: of a cluster
+  int in_place, apart, ctas;            // apart: a second launch moves the rows; ctas: of a cluster
 };
 
 __device__ __forceinline__ unsigned evict_key(float weight, int pos, long long newest_kept) {
@@ -87,39 +88,43 @@ __device__ __forceinline__ unsigned cta_scan(unsigned x, unsigned* warp_sums, un
   return upto - own + inc - x;
 }
 
-// n <= 32 rows of this warp, lane i the i-th: from slot `src` of one cache to slot `dst` of the other, 16 rows' loads before their
-// stores (more in flight would take registers that a second CTA per SM needs).
-template <int HD>
-__device__ __forceinline__ void move_rows(const Q4EvictArgs& a, int n, int src, int dst, int lane) {
-  constexpr int RB = q4_record_bytes(HD), kPieces = RB / 16, kRound = 5;
-  const int pos = lane < n ? a.from.pos[src] : 0;
-  const float weight = lane < n ? a.from.weight[src] : 0.0f;
+// A row of each lane: from slot `src` of one cache to slot `dst` of the other, if that is not < 0.  The loads of ROUND 16-byte pieces
+// to a lane come before their stores, and what `meanwhile` does in between; lanes without a row of their own read another's, since
+// loads under a condition were not issued together (256 segments of 600 to 2400 rows: 27 us, 24 so).  Whole warp.
+template <int HD, int ROUND, class F>
+__device__ __forceinline__ void move_rows(const Q4EvictArgs& a, int src, int dst, int lane, F meanwhile) {
+  constexpr int RB = q4_record_bytes(HD), kPieces = RB / 16;
+  static_assert(kPieces % ROUND == 0, "whole rounds");
+  const int pos = a.from.pos[src];
+  const float weight = a.from.weight[src];
 #pragma unroll
-  for (int i0 = 0; i0 < kPieces; i0 += kRound) {
-    uint4 x[kRound];
+  for (int i0 = 0; i0 < kPieces; i0 += ROUND) {
+    uint4 x[ROUND];
 #pragma unroll
-    for (int i = 0; i < kRound; ++i) {
+    for (int i = 0; i < ROUND; ++i) {
       const int piece = lane + 32 * (i0 + i), row = piece / kPieces, s = __shfl_sync(0xffffffffu, src, row);
-      if (row < n) x[i] = __ldcs(reinterpret_cast<const uint4*>(a.from.records + (long long)s * RB) + (piece - row * kPieces));
+      x[i] = __ldcs(reinterpret_cast<const uint4*>(a.from.records + (long long)s * RB) + (piece - row * kPieces));
     }
+    meanwhile();
 #pragma unroll
-    for (int i = 0; i < kRound; ++i) {
+    for (int i = 0; i < ROUND; ++i) {
       const int piece = lane + 32 * (i0 + i), row = piece / kPieces, d = __shfl_sync(0xffffffffu, dst, row);
-      if (row < n) *(reinterpret_cast<uint4*>(a.to.records + (long long)d * RB) + (piece - row * kPieces)) = x[i];
+      if (d >= 0) *(reinterpret_cast<uint4*>(a.to.records + (long long)d * RB) + (piece - row * kPieces)) = x[i];
     }
   }
-  if (lane < n) {
+  if (dst >= 0) {
     a.to.pos[dst] = pos;
     a.to.weight[dst] = weight;
   }
 }
+constexpr int kRound = 5;               // of the evicting kernel: more would take registers that a second CTA per SM needs
 
 struct EvictShared {
   alignas(16) unsigned hist[kEvictBins];   // of the CTA's keys
   unsigned few[kEvictThreads];               // the first CTA's: the keys that share the prefix
   unsigned warp_sums[32];
   unsigned found[3], n_few;
-  unsigned counts[4];
+  alignas(16) unsigned counts[4];
 };
 
 template <int HD, bool CLUSTER>
@@ -148,8 +153,11 @@ __global__ void __launch_bounds__(kEvictThreads, 2) k_q4_evict(const __grid_cons
   const int per_warp = 32, n_warps = ctas * (kEvictThreads / 32), my_warp = rank * (kEvictThreads / 32) + warp;
   if (kept == s.len) {                                     // everything stays
     if (!a.in_place)
-      for (int i = my_warp * per_warp; i < min(kept, d.room); i += n_warps * per_warp)
-        move_rows<HD>(a, min(per_warp, min(kept, d.room) - i), s.begin + min(i + lane, kept - 1), d.begin + i + lane, lane);
+      for (int i = my_warp * per_warp; i < min(kept, d.room); i += n_warps * per_warp) {
+        const bool mine = i + lane < min(kept, d.room);
+        if (!a.apart) move_rows<HD, kRound>(a, s.begin + min(i + lane, kept - 1), mine ? d.begin + i + lane : -1, lane, [] {});
+        else if (mine) a.source[s.begin + i + lane] = i + lane;
+      }
     return;
   }
   const float* weight = a.from.weight + s.begin;
@@ -169,7 +177,7 @@ __global__ void __launch_bounds__(kEvictThreads, 2) k_q4_evict(const __grid_cons
     for (int i = tid; i < kEvictBins; i += kEvictThreads) sh.hist[i] = 0;
     if (tid == 0) sh.n_few = 0;
     sync();
-    constexpr int kAtOnce = 4;
+    constexpr int kAtOnce = CLUSTER ? 8 : 4;                 // loads on their way before the first is counted
     for (int i0 = 0; i0 < n; i0 += kAtOnce * kEvictThreads) {
       unsigned k[kAtOnce];
       if (level == 0) {
@@ -204,10 +212,16 @@ __global__ void __launch_bounds__(kEvictThreads, 2) k_q4_evict(const __grid_cons
     static_assert(kPer == 4, "one 16-byte load");
     const int top = kEvictBins - 1 - tid * kPer;
     unsigned bin[kPer] = {0, 0, 0, 0}, total;
-    for (int r = 0; r < ctas; ++r) {
-      const EvictShared* of = CLUSTER ? cluster.map_shared_rank(&sh, r) : &sh;
-      const uint4 x = *reinterpret_cast<const uint4*>(&of->hist[top - 3]);
-      bin[0] += x.w; bin[1] += x.z; bin[2] += x.y; bin[3] += x.x;
+#pragma unroll
+    for (int r0 = 0; r0 < (CLUSTER ? kEvictCluster : 1); r0 += 4) {          // four loads under way at once
+      uint4 x[4];
+#pragma unroll
+      for (int r = r0; r < r0 + 4; ++r) {
+        x[r - r0] = make_uint4(0, 0, 0, 0);
+        if (r < ctas) x[r - r0] = *reinterpret_cast<const uint4*>(&(CLUSTER ? cluster.map_shared_rank(&sh, r) : &sh)->hist[top - 3]);
+      }
+#pragma unroll
+      for (int r = 0; r < 4; ++r) { bin[0] += x[r].w; bin[1] += x[r].z; bin[2] += x[r].y; bin[3] += x[r].x; }
     }
     const unsigned mine = (bin[0] + bin[1]) + (bin[2] + bin[3]);
     unsigned above = cta_scan(mine, sh.warp_sums, &total);
@@ -283,8 +297,11 @@ __global__ void __launch_bounds__(kEvictThreads, 2) k_q4_evict(const __grid_cons
     }
     cluster.sync();
     unsigned eq = 0;                                         // keys at the bound so far
+    uint4 of_cta = make_uint4(0, 0, 0, 0);                   // lane r: CTA r's
+    if (lane < ctas) of_cta = *reinterpret_cast<const uint4*>(cluster.map_shared_rank(&sh, lane)->counts);
     for (int r = 0; r < ctas; ++r) {
-      const unsigned* rc = cluster.map_shared_rank(&sh, r)->counts;
+      const unsigned rc[4] = {__shfl_sync(0xffffffffu, of_cta.x, r), __shfl_sync(0xffffffffu, of_cta.y, r),
+                              __shfl_sync(0xffffffffu, of_cta.z, r), __shfl_sync(0xffffffffu, of_cta.w, r)};
       const int b = min(r * share, s.len), e = min(b + share, s.len);
       const unsigned front = max(min(e, kept) - b, 0);       // its slots before `kept`
       const unsigned eq_front = min(rc[2], need - min(eq, need)), eq_back = min(rc[3], need - min(eq + rc[2], need));
@@ -346,20 +363,62 @@ __global__ void __launch_bounds__(kEvictThreads, 2) k_q4_evict(const __grid_cons
   if (!CLUSTER) all_moves = n_moves;
   __threadfence();                                           // the lists are read by other CTAs of the cluster
   sync();
+  if (a.apart) return;
 
   // ---- the rows
   if (a.in_place) {
     for (int i = my_warp * per_warp; i < (int)all_moves; i += n_warps * per_warp) {
-      const int m = min(per_warp, (int)all_moves - i), j = i + min(lane, m - 1);
-      move_rows<HD>(a, m, s.begin + movers[j], s.begin + holes[j], lane);
+      const int j = min(i + lane, (int)all_moves - 1);
+      move_rows<HD, kRound>(a, s.begin + movers[j], i + lane == j ? s.begin + holes[j] : -1, lane, [] {});
     }
   } else {
     const int rows = min(kept, d.room);
     for (int i = my_warp * per_warp; i < rows; i += n_warps * per_warp) {
-      const int m = min(per_warp, rows - i), j = i + min(lane, m - 1);
+      const int j = min(i + lane, rows - 1);
       int src = source[j];
       if (src < 0) src = movers[~src];
-      move_rows<HD>(a, m, s.begin + src, d.begin + i + lane, lane);
+      move_rows<HD, kRound>(a, s.begin + src, i + lane == j ? d.begin + j : -1, lane, [] {});
+    }
+  }
+}
+
+// The rows of an eviction into another cache, over that one's slots.
+constexpr int kMoveWarps = 8;
+template <int HD>
+__global__ void __launch_bounds__(kMoveWarps * 32) k_q4_move(const __grid_constant__ Q4EvictArgs a) {
+  pdl_launch_dependents();
+  pdl_wait();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n_seg = a.to.n_seg;
+  // where the row of slot r0 + lane comes from; < 0: from nowhere
+  auto source_of = [&](long long r0) {
+    const long long r = r0 + lane;
+    int src = -1;
+    if (r0 >= a.to.capacity) return src;
+    int seg = q4_find(a.to.starts, n_seg, (int)r0, lane);
+    if (r < a.to.capacity) {
+      while (seg + 1 < n_seg && a.to.starts[seg + 1] <= r) ++seg;
+      const Q4Segment d = q4_segment(a.to.starts, a.to.lens, seg, a.to.capacity);
+      if (r >= d.begin && r < (long long)d.begin + d.len) {
+        const int begin = q4_segment(a.from.starts, a.from.starts, seg, a.from.capacity).begin;
+        src = a.source[begin + (int)(r - d.begin)];
+        if (src < 0) src = a.movers[begin + ~src];
+        src += begin;
+      }
+    }
+    return src;
+  };
+  const long long step = (long long)gridDim.x * kMoveWarps * 32;
+  long long r0 = ((long long)blockIdx.x * kMoveWarps + warp) * 32;
+  int next = source_of(r0);
+  for (; r0 < a.to.capacity; r0 += step) {
+    const int src = next;
+    const unsigned some = __ballot_sync(0xffffffffu, src >= 0);
+    if (some) {
+      const int any = __shfl_sync(0xffffffffu, src, __ffs(some) - 1);      // for lanes that have none to read, too
+      move_rows<HD, q4_record_bytes(HD) / 16>(a, src >= 0 ? src : any, src >= 0 ? (int)(r0 + lane) : -1, lane,
+                                              [&] { next = source_of(r0 + step); });
+    } else {
+      next = source_of(r0 + step);
     }
   }
 }
@@ -403,9 +462,20 @@ cudaError_t launch_q4_evict(const Q4CacheView& from, const Q4CacheView& to, int 
   a.key_room = 2048;                                       // for segments of up to twice the average
   while (a.key_room < 2 * room / a.ctas && a.key_room < kMostKeys) a.key_room *= 2;
   if (a.key_room > kMostKeys) a.key_room = kMostKeys;
-  LaunchScope scope(KID_Q4_EVICT, st, launches);
-  if (head_dim == 128) return a.ctas > 1 ? launch_evict<128, true>(a, st) : launch_evict<128, false>(a, st);
-  return a.ctas > 1 ? launch_evict<64, true>(a, st) : launch_evict<64, false>(a, st);
+  // A second launch for the rows where the clusters have only a few SMs to move them with (into another cache, half of the rows kept
+  // where nothing else is said): 1 segment of 300000 rows 106 us against 185, 2 of 65536 42 against 50, 8 of 8192 with four CTAs
+  // each 17 either way, 16 against 20 with 95 % kept; 8 of 32768 with eight CTAs each 37 against 35, 64 of 8192 36 against 27.
+  a.apart = !a.in_place && a.ctas > 1 && (long long)from.n_seg * a.ctas <= sm_count() / 4;
+  {
+    LaunchScope scope(KID_Q4_EVICT, st, launches);
+    const cudaError_t e = head_dim == 128 ? (a.ctas > 1 ? launch_evict<128, true>(a, st) : launch_evict<128, false>(a, st))
+                                          : (a.ctas > 1 ? launch_evict<64, true>(a, st) : launch_evict<64, false>(a, st));
+    if (e != cudaSuccess || !a.apart) return e;
+  }
+  LaunchScope scope(KID_Q4_MOVE, st, launches);
+  const long long chunks = (to.capacity + kMoveWarps * 32 - 1) / (kMoveWarps * 32);
+  const dim3 grid((unsigned)std::min(chunks, 6ll * sm_count())), block(kMoveWarps * 32);
+  return head_dim == 128 ? launch_pdl(k_q4_move<128>, grid, block, 0, st, 1, a) : launch_pdl(k_q4_move<64>, grid, block, 0, st, 1, a);
 }
 
 }  // namespace slkv

@@ -492,6 +492,26 @@ def test_eviction_where_one_segment_is_far_longer_than_the_others(lens, in_place
     expect_evicted(before, lens, 1, budgets, 16, newest, after["starts"].tolist(), kept, after)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("lens,launches", [([9000, 4000, 12001], 2), ([33000], 2), ([5000, 30, 9001, 8192] * 6, 1)])
+def test_eviction_of_long_segments_into_another_cache(d, lens, launches):
+    t = R.random_cache(74, lens, d, 1, device=DEV)
+    before = {k: v.cpu().clone() for k, v in t.items()}
+    newest = [10 ** 6] * len(lens)
+    kept = [min(n, 4444) for n in lens]                     # some stay whole
+    rooms = [k + (7 * s) % 100 if s % 3 else k - 5 for s, k in enumerate(kept)]          # some too small, some with slack
+    to, _ = empty_cache(rooms, d, 1)
+    assert run_evict(t, 1, [4444], 16, newest, to=to) == B.ERR["CAPACITY"]
+    assert B.slkv_last_launch_count() == launches
+    n = [min(k, r) for k, r in zip(kept, rooms)]
+    assert to["lens"].tolist() == n and torch.equal(t["records"].cpu(), before["records"])
+    after = {k: v.cpu() for k, v in to.items()}
+    expect_evicted(before, lens, 1, [4444], 16, newest, after["starts"].tolist(), rooms, after)
+    for seg in range(len(lens)):
+        b, e = int(after["starts"][seg]) + n[seg], int(after["starts"][seg + 1])
+        assert torch.all(after["records"][b:e] == 0xAB) and torch.all(after["pos"][b:e] == -7) and torch.all(after["weight"][b:e] == 5.0)
+
+
 def test_eviction_into_a_cache_that_is_too_small():
     lens = [50, 60]
     t = R.random_cache(3, lens, 128, 1, device=DEV)
