@@ -294,13 +294,11 @@ __global__ void __launch_bounds__(kQ4Warps * 32, 4) k_q4_unpack(const __grid_con
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {
       const int from = __shfl_sync(0xffffffffu, slot, i * kRows + sub);
-      codes[i] = scale[i] = zero[i] = 0;
-      if (from >= 0) {
-        const unsigned char* rec = a.c.records + (long long)from * q4_record_bytes(HD);
-        codes[i] = reinterpret_cast<const unsigned*>(rec)[word];
-        scale[i] = *reinterpret_cast<const unsigned short*>(rec + scale_at);
-        zero[i] = *reinterpret_cast<const unsigned short*>(rec + scale_at + 2 * kGroups);
-      }
+      // a lane without a slot reads the first one's: loads under a condition are not issued together
+      const unsigned char* rec = a.c.records + (long long)max(from, 0) * q4_record_bytes(HD);
+      codes[i] = reinterpret_cast<const unsigned*>(rec)[word];
+      scale[i] = *reinterpret_cast<const unsigned short*>(rec + scale_at);
+      zero[i] = *reinterpret_cast<const unsigned short*>(rec + scale_at + 2 * kGroups);
     }
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {

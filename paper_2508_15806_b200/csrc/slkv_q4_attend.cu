@@ -359,8 +359,8 @@ __global__ void __launch_bounds__(kAttendWarps * 32, PARTS == 1 ? 4 : HD == 64 ?
 #pragma unroll
       for (int j = 0; j < NG; ++j) {
         if constexpr (PARTS == 1) {
-          uint4 w = make_uint4(0, 0, 0, 0);
-          if (there) w = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.q) + at + 32 * j);
+          uint4 w = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.q) + at + 32 * j);
+          if (!there) w = make_uint4(0, 0, 0, 0);
           w.x = times2(w.x, kQueryScales); w.y = times2(w.y, kQueryScales);
           w.z = times2(w.z, kQueryScales); w.w = times2(w.w, kQueryScales);
           bq[0][j][0][0] = __byte_perm(w.x, w.z, 0x5410); bq[0][j][0][1] = __byte_perm(w.x, w.z, 0x7632);
