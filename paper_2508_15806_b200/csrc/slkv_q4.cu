@@ -157,7 +157,6 @@ template <int HD, bool F32>
 __global__ void __launch_bounds__(kQ4Warps * 32) k_q4_pack(const __grid_constant__ Q4PackArgs a) {
   using Q = Q4Lane<HD>;
   constexpr int elem = F32 ? 4 : 2;
-  pdl_launch_dependents();
   pdl_wait();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int n_seg = a.c.n_seg;
@@ -213,7 +212,6 @@ struct Q4AppendArgs {
 template <int HD, bool F32>
 __global__ void __launch_bounds__(kQ4Warps * 32) k_q4_append(const __grid_constant__ Q4AppendArgs a) {
   using Q = Q4Lane<HD>;
-  pdl_launch_dependents();
   pdl_wait();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n_warps = blockDim.x >> 5;
   const int seg = blockIdx.x, s = seg / a.n_kv_heads, h = seg - s * a.n_kv_heads;
@@ -264,7 +262,6 @@ template <int HD, bool F32>
 __global__ void __launch_bounds__(kQ4Warps * 32, 4) k_q4_unpack(const __grid_constant__ Q4UnpackArgs a) {
   // K in lanes 0 .. 15, V in 16 .. 31, eight channels to a lane
   constexpr int kGroups = HD / 32, kLanes = HD / 8, kRows = 16 / kLanes, kSteps = kUnpackRows / kRows;
-  pdl_launch_dependents();
   pdl_wait();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const bool is_v = lane >= 16;

@@ -218,7 +218,6 @@ __global__ void __launch_bounds__(kAttendWarps * 32, PARTS == 1 ? 4 : HD == 64 ?
   if (lane < kStages) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bar0 + 8 * lane) : "memory");
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   __syncthreads();
-  pdl_launch_dependents();
   pdl_wait();
 
   // ---- tiles of all units, the size of a piece, how many pieces come before those of each thread's segments
@@ -743,8 +742,6 @@ template <int HD, bool F32>
 __global__ void __launch_bounds__(kJoinThreads) k_q4_join(const __grid_constant__ Q4AttendArgs a) {
   constexpr int kWarps = kJoinThreads / 32, V = HD / 32;   // channels per lane
   __shared__ __align__(16) float shares[kWarps][HD], lse_of[kMaxQ4Columns];
-  // No early launch of what comes after: CTAs that wait would hold the places of the next attention's, whose last ones then begin
-  // late (98 us a pass over long caches, against 89).
   pdl_wait();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int n_out = a.c.n_seg * a.R;

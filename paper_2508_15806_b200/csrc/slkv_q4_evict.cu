@@ -136,7 +136,6 @@ __global__ void __launch_bounds__(kEvictThreads, 2) k_q4_evict(const __grid_cons
     if constexpr (CLUSTER) cluster.sync();
     else __syncthreads();
   };
-  pdl_launch_dependents();
   pdl_wait();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int ctas = CLUSTER ? a.ctas : 1, rank = CLUSTER ? (int)cluster.block_rank() : 0, seg = blockIdx.x / ctas;
@@ -386,7 +385,6 @@ __global__ void __launch_bounds__(kEvictThreads, 2) k_q4_evict(const __grid_cons
 constexpr int kMoveWarps = 8;
 template <int HD>
 __global__ void __launch_bounds__(kMoveWarps * 32) k_q4_move(const __grid_constant__ Q4EvictArgs a) {
-  pdl_launch_dependents();
   pdl_wait();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n_seg = a.to.n_seg;
   // where the row of slot r0 + lane comes from; < 0: from nowhere
@@ -463,7 +461,7 @@ cudaError_t launch_q4_evict(const Q4CacheView& from, const Q4CacheView& to, int 
   while (a.key_room < 2 * room / a.ctas && a.key_room < kMostKeys) a.key_room *= 2;
   if (a.key_room > kMostKeys) a.key_room = kMostKeys;
   // A second launch for the rows where the clusters have only a few SMs to move them with (into another cache, half of the rows kept
-  // where nothing else is said): 1 segment of 300000 rows 106 us against 185, 2 of 65536 42 against 50, 8 of 8192 with four CTAs
+  // where nothing else is said): 1 segment of 300000 rows 102 us against 185, 2 of 65536 35 against 50, 8 of 8192 with four CTAs
   // each 17 either way, 16 against 20 with 95 % kept; 8 of 32768 with eight CTAs each 37 against 35, 64 of 8192 36 against 27.
   a.apart = !a.in_place && a.ctas > 1 && (long long)from.n_seg * a.ctas <= sm_count() / 4;
   {
