@@ -354,24 +354,24 @@ __global__ void __launch_bounds__(kAttendWarps * 32, PARTS == 1 ? 4 : HD == 64 ?
       const bool there = col < a.R;
       const int tok = there ? col / a.G : 0, qh = h * a.G + (there ? col - tok * a.G : 0);
       const long long at = s * a.q_seq + tok * a.q_tok + qh * a.q_head + 8 * t;
-      float qs[NG];                                        // 2^60 times a group's sum
+      float qs[NG];                                        // a group's sum, before the scaling: that leaves no room for 32 of them
 #pragma unroll
       for (int j = 0; j < NG; ++j) {
         if constexpr (PARTS == 1) {
           uint4 w = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.q) + at + 32 * j);
           if (!there) w = make_uint4(0, 0, 0, 0);
+          qs[j] = ((hi_f(w.x) + hi_f(w.y)) + (hi_f(w.z) + hi_f(w.w))) + ((lo_f(w.x) + lo_f(w.y)) + (lo_f(w.z) + lo_f(w.w)));
           w.x = times2(w.x, kQueryScales); w.y = times2(w.y, kQueryScales);
           w.z = times2(w.z, kQueryScales); w.w = times2(w.w, kQueryScales);
           bq[0][j][0][0] = __byte_perm(w.x, w.z, 0x5410); bq[0][j][0][1] = __byte_perm(w.x, w.z, 0x7632);
           bq[0][j][1][0] = __byte_perm(w.y, w.w, 0x5410); bq[0][j][1][1] = __byte_perm(w.y, w.w, 0x7632);
-          qs[j] = fmaf(16.0f, (hi_f(w.x) + hi_f(w.y)) + (hi_f(w.z) + hi_f(w.w)), (lo_f(w.x) + lo_f(w.y)) + (lo_f(w.z) + lo_f(w.w)));
         } else {
           float4 u = make_float4(0, 0, 0, 0), v = u;
           if (there) {
             const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(a.q) + at + 32 * j);
             u = p[0]; v = p[1];
           }
-          qs[j] = 0x1p60f * (((u.x + u.y) + (u.z + u.w)) + ((v.x + v.y) + (v.z + v.w)));
+          qs[j] = ((u.x + u.y) + (u.z + u.w)) + ((v.x + v.y) + (v.z + v.w));
           float x[8] = {u.x * 0x1p60f, u.y * 0x1p56f, u.z * 0x1p60f, u.w * 0x1p56f, v.x * 0x1p60f, v.y * 0x1p56f, v.z * 0x1p60f, v.w * 0x1p56f};
 #pragma unroll
           for (int p = 0; p < PARTS; ++p)
@@ -390,7 +390,7 @@ __global__ void __launch_bounds__(kAttendWarps * 32, PARTS == 1 ? 4 : HD == 64 ?
       // fragment expects them
 #pragma unroll
       for (int jj = 0; jj < NG / 2; ++jj) {
-        float y0 = qs[2 * jj] * 0x1p-100f * 0x1p-33f, y1 = qs[2 * jj + 1] * 0x1p-100f * 0x1p-33f;
+        float y0 = qs[2 * jj] * 0x1p-73f, y1 = qs[2 * jj + 1] * 0x1p-73f;
 #pragma unroll
         for (int p = 0; p < 3; ++p) {
           const unsigned v = pack2(y0, y1);
