@@ -256,7 +256,9 @@ int slkv_compress(const slkv_params* p, const void* q_win, const void* k, const 
  *     queued and makes `stream` wait for every overlapped call made so far on the current device (no host wait);
  *     consume outputs, or free / overwrite any input, output or workspace buffer -- q_win, k, v, cu_seqlens_dev
  *     and budgets included -- only behind it.  cu_seqlens_host is read during the call only.  Any other slkv_*
- *     call that uses a workspace joins by itself first, except the slkv_q4_* calls: join before packing.
+ *     call that uses a workspace joins by itself first.  Of the slkv_q4_* calls, slkv_q4_pack sends out what is queued on its
+ *     own stream, so that it finds the rows of calls made there before it; the others do not look at queued layers, and no
+ *     slkv_q4_* call waits for another stream: a cache that is filled on one and read on another needs an order from the caller.
  *   - Streams and host threads: the calls made on one stream form one sequence (queue, workspace);
  *     calls made on another stream -- by another host thread or the same one -- form another, and the two do not
  *     disturb each other as long as each has its own workspace (calls on two streams that share a workspace are
@@ -460,6 +462,8 @@ size_t slkv_q4_record_bytes(int32_t head_dim);   /* 0 for a head_dim that is not
  *   k, v       dev, [n_rows, head_dim] elements of dtype (SLKV_F32 | SLKV_BF16), contiguous; n_rows: rows that may be read
  *   offsets    dev, int32[n_seqs*n_kv_heads + 1];  kept_idx dev, int32[n_rows]
  *   status     dev, optional: SLKV_ERR_CAPACITY if a segment has more rows than slots, or offsets run past n_rows (the rest is dropped)
+ * Behind slkv_compress_overlapped calls on the same stream no slkv_join is needed (what is queued goes out, so pack behind the last
+ * layer, not between the layers); behind those of another stream it is.
  */
 int slkv_q4_pack(const slkv_q4_cache* c, int32_t dtype, const void* k, const void* v, int64_t n_rows, const int32_t* offsets,
                  const int32_t* kept_idx, int32_t* status, void* stream);

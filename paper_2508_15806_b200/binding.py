@@ -539,7 +539,8 @@ def _q4_status(cache: SlkvQ4Cache, status: torch.Tensor) -> None:
 
 def slkv_q4_pack(cache: SlkvQ4Cache, k: torch.Tensor, v: torch.Tensor, offsets: torch.Tensor, kept_idx: torch.Tensor,
                  status: Optional[torch.Tensor] = None, stream=None) -> None:
-    """k, v [rows, head_dim], offsets, kept_idx: as slkv_compress wrote them."""
+    """k, v [rows, head_dim], offsets, kept_idx: as slkv_compress wrote them, or slkv_compress_overlapped on the same stream (what is
+    queued there goes out first; rows from another stream need a slkv_join)."""
     if not cache.index == k.get_device() == v.get_device() == offsets.get_device() == kept_idx.get_device() == _current_device():
         _q4_elsewhere()
     shape = rows, dim = k.shape

@@ -559,6 +559,18 @@ unsigned long long next_launch_tag() {
   return n * 0x9E3779B97F4A7C15ull;
 }
 
+// Sends out what overlapped calls on `st` have queued: `st` then has it in front of what follows.  Nothing waits for other streams.
+cudaError_t send_queued_layers(cudaStream_t st, int* launches) {
+  std::lock_guard<std::mutex> lock(g_lists_mu);
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess || dev < 0 || dev >= kMaxDevices || !g_lists[dev]) return e;
+  DeviceStates* d = g_lists[dev];
+  for (int i = 0; i < kStatesPerDevice && e == cudaSuccess; ++i)
+    if (d->used[i] && d->owner[i] == st) e = flush_list(&d->st[i], st, launches);
+  return e;
+}
+
 int report(cudaError_t e, int launches) {
   g_last_launches = launches;
   return e == cudaSuccess ? SLKV_OK : cuda_fail(e);

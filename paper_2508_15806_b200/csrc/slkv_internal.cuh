@@ -336,6 +336,8 @@ cudaError_t launch_q4_attend(const Q4CacheView& c, const slkv_q4_cache& cache, c
 size_t q4_evict_workspace(int n_seg, long long capacity);
 cudaError_t launch_q4_evict(const Q4CacheView& from, const Q4CacheView& to, int n_kv_heads, int head_dim, const int32_t* budgets, int window,
                             const int32_t* newest, int32_t* status, void* workspace, cudaStream_t st, int* launches);
+// What slkv_compress_overlapped has queued on this stream goes out (slkv_api.cu).
+cudaError_t send_queued_layers(cudaStream_t st, int* launches);
 // A call's status for the caller, its CUDA error and its launches kept for this thread.
 int report(cudaError_t e, int launches);
 

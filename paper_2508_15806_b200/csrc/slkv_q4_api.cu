@@ -76,9 +76,10 @@ int slkv_q4_pack(const slkv_q4_cache* c, int32_t dtype, const void* k, const voi
   if (n_rows < 0 || n_rows >= (1ll << 31)) return SLKV_ERR_BAD_SHAPE;
   if (n_rows > 0 && (!k || !v || !kept_idx)) return SLKV_ERR_NULL_PTR;
   if (!aligned16(k) || !aligned16(v)) return SLKV_ERR_BAD_ALIGN;
+  // the rows may be those of a layer that is still queued
   int launches = 0;
-  const cudaError_t e = launch_q4_pack(view, c->head_dim, dtype == SLKV_F32, k, v, n_rows, offsets, kept_idx, status,
-                                       (cudaStream_t)stream, &launches);
+  cudaError_t e = send_queued_layers((cudaStream_t)stream, &launches);
+  if (e == cudaSuccess) e = launch_q4_pack(view, c->head_dim, dtype == SLKV_F32, k, v, n_rows, offsets, kept_idx, status, (cudaStream_t)stream, &launches);
   return report(e, launches);
 }
 
