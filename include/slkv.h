@@ -500,7 +500,8 @@ int slkv_q4_unpack(const slkv_q4_cache* c, int32_t dtype, const int32_t* slots_o
  *   lse_opt    dev, optional out, float[n_seqs][n_q_heads][n_tokens] in lse_units
  *   accumulate 1: weight[r] = weight_decay * weight[r] + (1/G) sum over the G query heads of h and over the tokens of p[r], for every
  *              filled slot (the reduction slkv_score uses over window rows and heads)
- *   status     dev, optional: SLKV_ERR_DEVICE_TIMEOUT if a bounded wait inside the kernel ran out
+ *   status     dev, optional: SLKV_ERR_DEVICE_TIMEOUT if a wait inside the kernel ran out (a copy that takes a second).  out and lse of
+ *              the query heads concerned are then NaN, and with accumulate the weights of their segments too; the rest is as ever
  * Limits: n_q_heads / n_kv_heads * n_tokens <= 256.  Positions are >= 0.  Queries are below 2^67 in magnitude (a head with a larger
  * one, or a NaN, gets NaN).  fp32 accumulation throughout; with bf16 rows, probabilities
  * times scales are rounded to bf16 for the product with V, with fp32 rows they keep 24 bits.
@@ -569,10 +570,11 @@ int slkv_trace_set_buffer(void* dev_buf, size_t bytes);
 /*
  * Test hook for the bounded waits (no counterpart in the paper).  Where the CTAs of a launch wait for one another
  * (the counters between the two passes of the score kernel; row sums and votes between the CTAs of a segment where one launch does
- * a short layer), every wait gives up after one second, sets SLKV_ERR_DEVICE_TIMEOUT in the call's status word, releases what the CTA
- * holds and returns.  With the hook armed (on != 0) the next such launch made by the calling thread waits for one arrival more than
- * there are -- on = 1: where the CTAs of a score launch wait for the statistics, 2: for their clearing, 3: where those of a
- * one-launch layer wait for the row sums, 4: for the votes -- so that exactly this path runs: the call's results are then incomplete
+ * a short layer), and where a warp of slkv_q4_attend waits for its own copies, every wait gives up after one second, sets
+ * SLKV_ERR_DEVICE_TIMEOUT in the call's status word, releases what the CTA holds and returns.  With the hook armed (on != 0) the next
+ * such launch made by the calling thread waits for one arrival more than there are -- on = 1: where the CTAs of a score launch wait for
+ * the statistics, 2: for their clearing, 3: where those of a one-launch layer wait for the row sums, 4: for the votes, 5: where the first
+ * warp of slkv_q4_attend waits for rows -- so that exactly this path runs: the call's results are then incomplete
  * and its status word says so; the calls after it are unaffected.  While it is armed with 1 or 2, short layers go the way of the
  * others; a list that goes with one product with every key (slkv_debug_list_way) waits for statistics only where some head needs all
  * its votes.  One-shot: the launch that takes it disarms it.

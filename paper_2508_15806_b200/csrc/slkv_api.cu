@@ -13,6 +13,7 @@ namespace {
 thread_local int g_last_cuda_error = 0;
 thread_local int g_last_launches = 0;
 thread_local int g_expire_next_layer_wait = 0;
+thread_local int g_expire_next_copy_wait = 0;
 
 // ---- per-kernel timing (off by default) -----------------------------------------------------------
 struct TimedLaunch { int kid; cudaEvent_t a, b; };
@@ -583,6 +584,12 @@ int take_expire_next_layer_wait(bool sums) {
   g_expire_next_layer_wait = 0;
   return v;
 }
+void expire_next_copy_wait(int on) { g_expire_next_copy_wait = on; }
+int take_expire_next_copy_wait() {
+  const int v = g_expire_next_copy_wait;
+  g_expire_next_copy_wait = 0;
+  return v;
+}
 
 LaunchScope::LaunchScope(int kid, cudaStream_t st, int* launches) : kid_(kid), st_(st), slot_(-1) {
   ++*launches;
@@ -674,7 +681,8 @@ int slkv_debug_list_way(int way) {
 int slkv_debug_expire_next_wait(int on) {
   const int layer = on == 3 || on == 4 ? on - 2 : 0;
   expire_next_layer_wait(layer);
-  expire_next_wait(layer ? 0 : on == 2 ? 2 : on != 0);
+  expire_next_copy_wait(on == 5);
+  expire_next_wait(layer || on == 5 ? 0 : on == 2 ? 2 : on != 0);
   return SLKV_OK;
 }
 

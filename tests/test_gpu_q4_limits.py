@@ -69,3 +69,47 @@ def test_packing_sends_out_what_its_stream_has_queued():
         for name in ("lens", "pos", "records", "weight"):
             assert torch.equal(t[name], t2[name]), name
         assert t["lens"].tolist() == (w["off"][1:] - w["off"][:-1]).tolist()
+
+
+# ---- a wait that runs out ----------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype,d", [(torch.bfloat16, 128), (torch.float32, 64)])
+@pytest.mark.parametrize("lens,hkv,launches", [([700, 1, 0, 1300], 2, 1), ([5000, 90, 9000, 1], 4, 2), ([300] * 600, 8, 2)])
+def test_a_wait_that_runs_out_is_told_by_the_status_and_by_nan(dtype, d, lens, hkv, launches):
+    base = R.random_cache(83, lens, d, hkv, device=DEV)
+    q = T.queries(84, len(lens) // hkv, 1, 4 * hkv, d, dtype).to(DEV)
+    c0 = T.cache_of(base, hkv)
+    out, lse = torch.full_like(q, 9.0), torch.full((q.size(0), q.size(2), 1), 9.0, device=DEV)
+    p = B.make_q4_attend(c0, q, out)
+    ws, status = B.new_q4_workspace(c0, p, True).fill_(0xFF), torch.zeros(1, dtype=torch.int32, device=DEV)
+
+    def call():
+        t = {x: y.clone() for x, y in base.items()}
+        status.zero_()
+        B.slkv_q4_attend(T.cache_of(t, hkv), p, q, out, ws, lse=lse, accumulate=True, status=status)
+        assert B.slkv_last_launch_count() == launches
+        torch.cuda.synchronize()
+        return int(status), out.clone(), lse.clone(), t
+    ok, want, want_lse, want_t = call()
+    assert ok == 0
+    B.slkv_debug_expire_next_wait(5)
+    try:
+        lost, got, got_lse, got_t = call()
+    finally:
+        B.slkv_debug_expire_next_wait(0)
+    assert lost == B.ERR["DEVICE_TIMEOUT"]
+    # the segments whose rows were not waited for are NaN throughout, the others as ever
+    gone = torch.isnan(got_lse).view(len(lens), 4)
+    assert torch.equal(gone.any(1), gone.all(1)) and 0 < int(gone[:, 0].sum()) < len(lens)
+    for seg in range(len(lens)):
+        s, h = divmod(seg, hkv)
+        b, n = int(base["starts"][seg]), lens[seg]
+        mine, w = got[s, 0, 4 * h:4 * h + 4], got_t["weight"][b:b + n]
+        if bool(gone[seg, 0]):
+            assert n > 0 and torch.isnan(mine).all() and torch.isnan(w).all()
+        else:
+            assert torch.equal(mine, want[s, 0, 4 * h:4 * h + 4]) and torch.equal(got_lse[s, 4 * h:4 * h + 4], want_lse[s, 4 * h:4 * h + 4])
+            assert torch.equal(w, want_t["weight"][b:b + n])
+    for name in ("records", "pos", "lens"):
+        assert torch.equal(got_t[name], base[name])
+    ok, again, again_lse, again_t = call()
+    assert ok == 0 and torch.equal(again, want) and torch.equal(again_lse, want_lse) and torch.equal(again_t["weight"], want_t["weight"])
