@@ -511,7 +511,7 @@ typedef struct slkv_q4_attend_params {
   int32_t n_tokens;         /* per sequence, >= 1 */
   int32_t dtype;            /* SLKV_F32 | SLKV_BF16: q and out */
   int32_t lse_units;        /* SLKV_LSE_LN | SLKV_LSE_LOG2 */
-  float scale;              /* 1 / sqrt(head_dim), usually */
+  float scale;              /* 1 / sqrt(head_dim), usually; at most 2^54 in magnitude */
   float softcap;            /* 0: none; else >= 1e-20 */
   float weight_decay;       /* 1: a plain sum */
   int32_t reserved;

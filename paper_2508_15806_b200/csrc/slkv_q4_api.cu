@@ -45,7 +45,8 @@ int check_attend(const slkv_q4_cache* c, const slkv_q4_attend_params* p, Q4Cache
   if (columns > kMaxQ4Columns) return SLKV_ERR_BAD_SHAPE;
   // the tiles of all units are counted in 32 bits
   if ((c->capacity_rows / 32 + view->n_seg) * ((columns + 7) / 8) >= (1ll << 31)) return SLKV_ERR_BAD_SHAPE;
-  if (!std::isfinite(p->scale) || !std::isfinite(p->softcap) || (p->softcap != 0.0f && p->softcap < 1e-20f) ||
+  // the kernel multiplies with 2^73 log2(e) scale
+  if (!(std::fabs(p->scale) <= 0x1p54f) || !std::isfinite(p->softcap) || (p->softcap != 0.0f && p->softcap < 1e-20f) ||
       !std::isfinite(p->weight_decay))
     return SLKV_ERR_BAD_SHAPE;
   const int64_t strides[] = {p->q_stride_seq, p->q_stride_tok, p->q_stride_head, p->o_stride_seq, p->o_stride_tok, p->o_stride_head};
