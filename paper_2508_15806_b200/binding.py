@@ -591,6 +591,8 @@ def slkv_q4_unpack(cache: SlkvQ4Cache, k_out: torch.Tensor, v_out: torch.Tensor,
         assert n == cache.capacity_rows
     else:
         assert slots.dtype is _I32 and slots.is_contiguous() and slots.numel() == n and slots.get_device() == cache.index
+        if n == 0:                                         # an empty tensor's address is null, which asks for every slot
+            return
     rc = _fn["slkv_q4_unpack"](stream, cache, _DTYPES[k_out.dtype], slots, n, k_out, v_out)
     if rc != SLKV_OK:
         raise SlkvError(rc, "slkv_q4_unpack")

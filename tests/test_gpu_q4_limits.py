@@ -113,3 +113,23 @@ def test_a_wait_that_runs_out_is_told_by_the_status_and_by_nan(dtype, d, lens, h
         assert torch.equal(got_t[name], base[name])
     ok, again, again_lse, again_t = call()
     assert ok == 0 and torch.equal(again, want) and torch.equal(again_lse, want_lse) and torch.equal(again_t["weight"], want_t["weight"])
+
+
+# ---- nothing asked for ------------------------------------------------------------------------------------------------
+def test_an_empty_list_of_slots_unpacks_nothing():
+    t = R.random_cache(89, [40], 128, 1, device=DEV)
+    c = T.cache_of(t, 1)
+    ko, vo = (torch.full((50, 128), 77.0, device=DEV) for _ in range(2))
+    none = torch.empty(0, dtype=torch.int32, device=DEV)
+    B.slkv_q4_unpack(c, ko[:0], vo[:0], slots=none)
+    B.slkv_q4_unpack(c, torch.empty(0, 128, device=DEV), torch.empty(0, 128, device=DEV), slots=none)
+    torch.cuda.synchronize()
+    assert torch.all(ko == 77.0) and torch.all(vo == 77.0)
+
+
+def test_a_layer_without_rows_empties_the_segments():
+    t, c = T.empty_cache([3, 0, 5], 64, 1)
+    none = torch.empty(0, 64, dtype=torch.bfloat16, device=DEV)
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    B.slkv_q4_pack(c, none, none, torch.zeros(4, dtype=torch.int32, device=DEV), torch.empty(0, dtype=torch.int32, device=DEV), status)
+    assert status.item() == 0 and t["lens"].tolist() == [0, 0, 0] and torch.all(t["records"] == 0xAB)
