@@ -574,7 +574,7 @@ int slkv_trace_set_buffer(void* dev_buf, size_t bytes);
  * SLKV_ERR_DEVICE_TIMEOUT in the call's status word, releases what the CTA holds and returns.  With the hook armed (on != 0) the next
  * such launch made by the calling thread waits for one arrival more than there are -- on = 1: where the CTAs of a score launch wait for
  * the statistics, 2: for their clearing, 3: where those of a one-launch layer wait for the row sums, 4: for the votes, 5: where the first
- * warp of slkv_q4_attend waits for rows -- so that exactly this path runs: the call's results are then incomplete
+ * CTA of slkv_q4_attend waits for rows -- so that exactly this path runs: the call's results are then incomplete
  * and its status word says so; the calls after it are unaffected.  While it is armed with 1 or 2, short layers go the way of the
  * others; a list that goes with one product with every key (slkv_debug_list_way) waits for statistics only where some head needs all
  * its votes.  One-shot: the launch that takes it disarms it.

@@ -345,7 +345,7 @@ int report(cudaError_t e, int launches);
 unsigned long long* tensor_trace_buffer(int n_cta);
 // Diagnostics: arm / consume the one-shot switches that make an inter-CTA wait of this thread's next launch run out: a wait for words
 // in memory (slkv_score_pipe.cu, slkv_score_simt.cu; 1, 2), one of the kernels that do a whole layer (1 for the row sums, where the
-// launch forms them, 2 for the votes), a warp's wait for its copies in the attention over the 4-bit cache.
+// launch forms them, 2 for the votes), the first CTA's waits for its copies in the attention over the 4-bit cache.
 void expire_next_wait(int on);
 int take_expire_next_wait();
 bool next_wait_expires();                        // armed

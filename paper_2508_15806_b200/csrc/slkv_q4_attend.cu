@@ -61,7 +61,7 @@ struct Q4AttendArgs {
   int32_t* status;
   long long q_seq, q_tok, q_head, o_seq, o_tok, o_head;      // elements
   int n_kv_heads, n_q_heads, n_tokens, G, R, n_cb, n_cta, ctas, accumulate;         // ctas: of a cluster
-  int expire;                           // diagnostics: the first warp's wait for its copies runs out
+  int arrivals;                         // of a phase of the first CTA's barriers: 1; diagnostics: 2, and its waits run out
   float scale, softcap, decay, lse_unit;                     // lse_unit: of a base-2 logarithm
   // workspace
   int* head;                            // pieces
@@ -217,7 +217,7 @@ __global__ void __launch_bounds__(kAttendWarps * 32, PARTS == 1 ? 4 : HD == 64 ?
   const uint32_t key_row = key_of(g) * RB, value_row[2] = {uint32_t(key_of(2 * t) * RB + HD / 2 + g * (HD / 16)),
                                                           uint32_t(key_of(2 * t + 1) * RB + HD / 2 + g * (HD / 16))};
   if (lane < kStages)
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar0 + 8 * lane), "r"(1 + (a.expire && blockIdx.x == 0 && warp == 0)) : "memory");
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar0 + 8 * lane), "r"(blockIdx.x ? 1 : a.arrivals) : "memory");
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   __syncthreads();
   pdl_wait();
@@ -602,7 +602,6 @@ __global__ void __launch_bounds__(kAttendWarps * 32, PARTS == 1 ? 4 : HD == 64 ?
         next += kAttendWarps;
       }
     }
-    if (dead) l[0] = l[1] = __int_as_float(0x7fffffff);    // rows that did not come: the unit's outputs, sums and weights are NaN
     // ---- the piece's end: the warps' shares together.  A warp's ring is empty now and takes its output.
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
@@ -614,7 +613,7 @@ __global__ void __launch_bounds__(kAttendWarps * 32, PARTS == 1 ? 4 : HD == 64 ?
       }
       if (g == 0) {
         merge_m[warp][2 * t + c] = m[c];
-        merge_l[warp][2 * t + c] = l[c];
+        merge_l[warp][2 * t + c] = dead ? __int_as_float(0x7fffffff) : l[c];       // rows that did not come: their unit is NaN throughout
       }
     }
     float* mine_o = reinterpret_cast<float*>(ring);        // [column][HD + 4]
@@ -716,7 +715,7 @@ __global__ void __launch_bounds__(kAttendWarps * 32, PARTS == 1 ? 4 : HD == 64 ?
     }
   }
   if (dead)                                                // what is still in flight lands before the memory is another CTA's
-    for (unsigned i = lost; i < issued && copies_there(bar0 + 8 * (i % kStages), (i / kStages) & 1); ++i) {}
+    for (unsigned i = lost; i < issued; ++i) copies_there(bar0 + 8 * (i % kStages), (i / kStages) & 1);
 }
 
 // ---- the pieces of units that lie in several CTAs, and the weights ---------------------------------------------------
@@ -933,7 +932,7 @@ cudaError_t launch_q4_attend(const Q4CacheView& c, const slkv_q4_cache& cache, c
   a.n_kv_heads = cache.n_kv_heads; a.n_q_heads = p.n_q_heads; a.n_tokens = p.n_tokens;
   a.G = p.n_q_heads / cache.n_kv_heads; a.R = a.G * p.n_tokens; a.n_cb = (a.R + kCols - 1) / kCols;
   a.accumulate = accumulate;
-  a.expire = take_expire_next_copy_wait();
+  a.arrivals = take_expire_next_copy_wait() ? 2 : 1;
   a.scale = p.scale; a.softcap = p.softcap; a.decay = p.weight_decay;
   a.lse_unit = p.lse_units == SLKV_LSE_LOG2 ? 1.0f : 0.69314718055994531f;
   const Q4Workspace w(c.n_seg, cache.head_dim, a.R, c.capacity, accumulate);
