@@ -482,9 +482,9 @@ int slkv_q4_append(const slkv_q4_cache* c, int32_t dtype, const void* k, const v
 
 /*
  * The values that records stand for, as rows of dtype (rounded to nearest for bf16).
- *   slots_opt    dev, optional, int32[n]: row i of k_out, v_out [n, head_dim] is slot slots_opt[i]'s; entries outside the cache are
- *                padding.  NULL: row i is slot i's, for the filled slots (n is capacity_rows whatever is passed).
- * Rows of padding and of slots that are not filled are left as they are.
+ *   slots_opt    dev, optional, int32[n]: row i of k_out, v_out [n, head_dim] is slot slots_opt[i]'s, filled or not (tokens that were
+ *                drafted lie behind the filled ones); entries outside the cache are padding, whose rows are left as they are.
+ *                NULL: row i is slot i's, for the filled slots (n is capacity_rows whatever is passed); the other rows are left as they are.
  */
 int slkv_q4_unpack(const slkv_q4_cache* c, int32_t dtype, const int32_t* slots_opt, int64_t n, void* k_out, void* v_out, void* stream);
 
@@ -503,8 +503,13 @@ int slkv_q4_unpack(const slkv_q4_cache* c, int32_t dtype, const int32_t* slots_o
  *   status     dev, optional: SLKV_ERR_DEVICE_TIMEOUT if a wait inside the kernel ran out (a copy that takes a second).  out and lse of
  *              the query heads concerned are then NaN, and with accumulate the weights of their segments too; the rest is as ever
  * Limits: n_q_heads / n_kv_heads * n_tokens <= 256.  Positions are >= 0.  Queries are below 2^67 in magnitude (a head with a larger
- * one, or a NaN, gets NaN).  fp32 accumulation throughout; with bf16 rows, probabilities
- * times scales are rounded to bf16 for the product with V, with fp32 rows they keep 24 bits.
+ * one, or a NaN, gets NaN), sums of products q . K below 2^200, scores below 2^124, values below 2^119 over the number of a segment's
+ * rows (outputs are summed before they are divided by the softmax's sum); beyond these a head may get NaN.  A score is off by up to
+ * |scale| * |K| * 2^-58 beside its roundings, which shows only for queries far below 2^-40.
+ * fp32 accumulation throughout; with bf16 rows, probabilities times scales are rounded to bf16 for the product with V: up to 2^-8 of
+ * each term p * scale * |code - 8|.  With fp32 rows, over the same cache, they keep 24 bits.
+ * The workspace is some 64 bytes per segment and block of 8 columns, 8 MB at most for outputs of pieces, and with accumulate a float
+ * per slot of the cache (filled or not) and column (query head of a KV head, and token): 16 bytes a slot for 4 heads and one token.
  */
 typedef struct slkv_q4_attend_params {
   int32_t n_q_heads;        /* multiple of the cache's n_kv_heads */

@@ -10,7 +10,10 @@
 //           (sum of the group's queries), which is one more product: the zeros as they lie in the record, the query sums in three
 //           bf16 parts.
 //   output  one packed multiply-add makes (c - 8) / 128 of a value nibble, exactly.  Probabilities times the group's scale,
-//           rounded to bf16, are the other operand.  zero + 8 scale goes with the unrounded probabilities, in fp32.
+//           rounded to bf16, are the other operand.  zero + 8 scale goes with the unrounded probabilities, in fp32.  With a second
+//           bf16 part of the operand, a relative error of 0.0023 over 64 long segments became the 0.0017 of the bf16 output itself, at
+//           105 us instead of 93 (256 segments of 256 to 4096 rows: 0.0020, 0.0017, 32.8 us instead of 30.5); one part it is, as fp32
+//           rows are there for those who want more.  (A branch round the second part where no row of 16 has much weight: 110 us.)
 // Keys are the products' long side (m16), the query heads of a KV head and its tokens the short one (n8): with four heads to a
 // KV head nothing wider would be used.  The scores' accumulators hold keys along the lanes, the second product wants
 // them along the other axis: one 8 x 8 transposition by the matrix unit's own instruction per 8 keys and group.
@@ -21,13 +24,18 @@
 // pieces as CTAs are cut into equal pieces of whole tiles; a CTA takes a piece, and further ones where there are more.  A unit of
 // one piece is finished by its CTA; the others leave a maximum, a sum and an unscaled output per piece, which a second launch
 // joins.  In a CTA each warp takes every fourth tile with its own ring of bulk copies, so that no warp waits for another before
-// a piece ends.  (Cutting the line of all tiles evenly instead, pieces running across units, took 40 us for 256 segments of 256 to 4096 rows
-// where this takes 32: a CTA's second piece starts with 3.4 us of latencies.)
+// a piece ends.  (Cutting the line of all tiles evenly instead, pieces running across units, took 8 us more for 256 segments of 256 to
+// 4096 rows: a CTA's second piece starts with 3.4 us of latencies.)
 // Where units are few and short one launch does it all: a cluster of CTAs per unit, equal shares of its tiles, the shares joined
-// through the cluster's shared memory.  (One user, 8 heads of 129 to 1031 rows: 9.3 us with two launches, 7.4 with one.)
+// through the cluster's shared memory.  (One user, 8 heads of 129 to 1031 rows: 8.4 us with two launches, 7.4 with one.)  The rule goes by
+// the room of an average segment, since the host does not know lengths: the same rows with four times the room take two launches.
+// A block of columns reads and unpacks the cache for itself: 256 segments of 256 to 4096 rows take 26 us with 4 columns, 56 with
+// 16, 208 with 64 (masked).
 // The weights need the final log-sum-exps: the scores are kept in the workspace, the second launch turns them into
 // probabilities (the same CTA, behind the cluster's exchange, where there is one launch).
-// What bounds it: the arithmetic between DRAM and the products (unpacking, scales).
+// What bounds it: instructions, 400 of them per 16 rows, from few warps -- their registers leave four CTAs to an SM, 3.5 warps to a
+// scheduler, and those find an instruction to issue in 59 % of the cycles (64 long segments; ALU pipe 49 %, matrix pipe 20 %, DRAM 44 %).
+// The masked forms for head_dim 128 spill 24 to 36 bytes around the loop at these 128 registers.
 #include <atomic>
 
 #include <cooperative_groups.h>

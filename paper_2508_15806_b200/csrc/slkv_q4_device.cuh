@@ -6,7 +6,7 @@
 //   V  16-bit unit g * (d/32) + j: channels 32 j + 4 g + e in its nibbles e = 0 .. 3                (lane g of eight)
 // None of the kernels lets the next launch begin early, which would only wait: its CTAs take the places that come free first, so
 // that their SMs have an uneven share of it (packing and unpacking 4636 rows 7.5 us against 5.8, one row in and one out for 128
-// segments 12.0 against 10.6, attention to 8 short segments 7.7 against 7.4 and to 64 long ones, two launches, 98 against 92).
+// segments 12.0 against 10.2, attention to 8 short segments 7.7 against 7.4 and to 64 long ones, two launches, 98 against 92).
 #pragma once
 #include "slkv_internal.cuh"
 
