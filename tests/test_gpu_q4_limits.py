@@ -1,5 +1,7 @@
 """The 4-bit cache at its documented limits, against the same definitions: large queries, rows in numbers that make the kernels go round
 their loops, evictions in which the weights decide."""
+import math
+
 import numpy as np
 import pytest
 import torch
@@ -27,6 +29,57 @@ def test_queries_of_one_sign_up_to_the_documented_bound(d, dtype, sign):
     for kw in (dict(), dict(q_pos=q_pos), dict(q_pos=q_pos, softcap=5.0)):
         out, lse = T.check(t, hkv, q, accumulate=True, scale=2.0 ** -66 / d, **kw)
         assert torch.isfinite(out).all()
+
+
+# ---- large keys, values and scores --------------------------------------------------------------------------------------
+def times_power(t, d, parts, power):
+    """The cache with the scales and zeros of K (parts 0, 1) or V (2, 3) times 2^power."""
+    s = t["records"][:, d:].contiguous().view(torch.bfloat16).view(-1, 4, d // 32).float()
+    s[:, parts] *= 2.0 ** power
+    return dict(t, records=torch.cat([t["records"][:, :d], s.bfloat16().view(t["records"].size(0), -1).view(torch.uint8)], 1).contiguous())
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("k_power,q_power,v_power", [(0, 0, 105), (100, 60, 0), (100, 20, 0), (120, 0, -60), (-60, 60, 0), (60, -30, 40)])
+def test_keys_and_values_within_the_documented_bounds(d, dtype, k_power, q_power, v_power):
+    lens, hkv, G = [300, 40, 5, 1000], 2, 4
+    t = R.random_cache(91 + d, lens, d, hkv, device=DEV)
+    t = times_power(times_power(t, d, slice(0, 2), k_power), d, slice(2, 4), v_power)
+    q = T.queries(92, 2, 2, hkv * G, d, torch.float32, 2.0 ** q_power).to(dtype)
+    scale = float(np.float32(2.0 ** -(k_power + q_power) * 0.125))          # as it is passed: 2^-163 is 0 in fp32
+    q_pos = torch.tensor([[100, 400], [3, 5000]], dtype=torch.int32, device=DEV)
+    for kw in (dict(), dict(q_pos=q_pos), dict(q_pos=q_pos, softcap=3.0)):
+        out, lse = T.check(t, hkv, q, accumulate=True, scale=scale, **kw)
+        assert torch.isfinite(out).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("softcap", [0.0, 2.0 ** 110, 2.0 ** 124, 3e38])
+def test_scores_up_to_the_documented_bound(dtype, softcap):
+    # powers of two apart, so that one row takes everything whatever is rounded: its values come out, its score is the log-sum-exp
+    d, n = 64, 40
+    t = R.random_cache(93, [n], d, 1, slack=2, device=DEV)
+    s = t["records"][:, d:].contiguous().view(torch.bfloat16).view(-1, 4, 2)
+    s[:, 0], s[:, 1] = 0.0, (2.0 ** torch.arange(s.size(0), device=DEV).remainder(n).float())[:, None].bfloat16()      # K row r: 2^r throughout
+    t["records"][:, d:] = s.view(s.size(0), -1).view(torch.uint8)
+    q = torch.ones(1, 1, 2, d, dtype=dtype, device=DEV)
+    q[0, 0, 1] = -1.0
+    scale = 2.0 ** 50                                         # 64 channels: the largest score is 2^(50 + 6 + 39)
+    q = q * 2.0 ** 28                                         # .. now 2^123
+    out, lse = T.attend(t, 1, q, scale=scale, softcap=softcap)
+    _, V, _ = R.decode(t["records"][:n], d)
+    for head, row in ((0, n - 1), (1, 0)):
+        x = 2.0 ** (84 + row) * (1 if head == 0 else -1)
+        if softcap:
+            x = softcap * math.tanh(x / softcap)
+        if softcap == 2.0 ** 110 and head == 0:              # several scores at the cap: some mixture of those rows
+            assert torch.isfinite(out[0, 0, head]).all()
+        else:
+            # three parts of bf16 at least hold the value; the bf16 way rounds p * scale, then the output
+            tol = 2.0 ** -19 * np.abs(V).max() if dtype == torch.float32 else 2.0 ** -6 * np.abs(V).max()
+            assert np.all(np.abs(out[0, 0, head].double().cpu().numpy() - V[row]) <= tol)
+        assert abs(float(lse[0, head, 0]) - x) <= 2.0 ** -17 * abs(x)
 
 
 # ---- packing behind overlapped compressions ----------------------------------------------------------------------------
