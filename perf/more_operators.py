@@ -397,7 +397,7 @@ def _own(st):
     if h is None:
         h = st["handles"] = {}
         if c["kind"] == "prompt":
-            h["params"] = B.make_prompt(st["q"], st["k"], st["v"], st["out"], window=c["window"])
+            h["params"] = B.make_prompt(st["q"], st["k"], st["v"], st["out"], c["n_seqs"], window=c["window"])
             h["workspace"] = B.new_prompt_workspace(h["params"], st["cu_q"], st["cu_k"])
         else:
             for name, lens, n_free in (("cache", "lens", "n_free"), ("after", "lens_out", "n_free_out")):
@@ -406,7 +406,7 @@ def _own(st):
         if c["kind"] == "step":
             h["slots"] = st["slots"][:st["n_layer_seg"]]
         if c["kind"] == "tree":
-            h["params"] = B.make_paged_attend(h["cache"], st["q"], st["out"])
+            h["params"] = B.make_paged_attend(h["cache"], st["q"], st["out"], st["k"], st["v"])
             h["workspace"] = B.new_paged_workspace(h["cache"], h["params"])
     if c["kind"] == "prompt":
         B.slkv_prompt_attend(h["params"], st["q"], st["k"], st["v"], st["cu_q_dev"], st["cu_q"], st["out"], h["workspace"],
