@@ -11,6 +11,8 @@
  *   slkv_cp_*            the same for one sequence whose keys are split over ranks (context parallel)
  *   slkv_row_lse         the window rows' log-sum-exp over their softmax domain       (Eq. 3-4, Eq. 7)
  *   slkv_q4_*            the compressed cache in decoding: held in 4 bits, attended to, evicted from
+ *   slkv_prompt_attend   the prompt's own attention, which leaves the window rows' log-sum-exp for the compression
+ *   slkv_paged_*         the compressed cache in pages: planned, written, attended to by trees of drafted tokens
  *
  * Conventions
  *   - "dev" pointers are device memory of the current CUDA device, "host" pointers are host memory.
@@ -543,7 +545,131 @@ size_t slkv_q4_evict_workspace_bytes(const slkv_q4_cache* from);     /* 0: bad a
 int slkv_q4_evict(const slkv_q4_cache* from, const slkv_q4_cache* to, const int32_t* budgets, int32_t window, const int32_t* newest,
                   int32_t* status, void* workspace, size_t workspace_bytes, void* stream);
 
-/* Number of kernels the most recent slkv_score / slkv_compress / slkv_compress_host / slkv_q4_* call on
+/*
+ * Attention of whole prompts, causal (Eq. 1-5; the attention whose keys slkv_compress then selects from).  Sequence s has nq = cu_q[s+1] -
+ * cu_q[s] queries and nk = cu_k[s+1] - cu_k[s] keys, the queries being its last tokens (nk > nq: what lies before them was there
+ * already, a prompt in chunks).  For token i < nq, query head qh of KV head h, over the keys j <= i + nk - nq:
+ *     out = sum p V[j],  p = softmax of scale * q . K[j];   lse = log sum exp(scale * q . K[j])
+ * A query that sees no key (nk < nq) gets zeros and -infinity.  A key that a query does not see gives it nothing, whatever K and V hold
+ * there; sequences do not see one another.
+ *   q, out        dev, elements of dtype: element (t, qh, p) at t*stride_tok + qh*stride_head + p, t in [0, cu_q[n_seqs])
+ *   k, v          dev, likewise by KV head, t in [0, cu_k[n_seqs])
+ *   cu_q_dev      dev, int32[n_seqs+1], cu_q[0] = 0;  cu_q_host: the same values on the host (they size the launch)
+ *   cu_k_*_opt    both or neither; NULL: the keys are the queries' own tokens
+ *   lse_opt       dev, optional out, float[n_seqs][n_q_heads][window] in lse_units: row i of a sequence is its token nq - window + i; rows
+ *                 before its first query are left as they are.  With the window of slkv_params this is the lse_opt of slkv_score and
+ *                 slkv_compress (SLKV_ALL_CAUSAL), which spares them their pass over K for it.
+ *   status        dev, optional: SLKV_ERR_DEVICE_TIMEOUT if a wait inside a kernel ran out; rows concerned are then left as they were or NaN
+ * Limits: n_q_heads / n_kv_heads <= 64, fewer than 2^31 - 512 tokens.  Scores below fp32's range in magnitude.
+ * fp32 accumulation throughout; with bf16, probabilities are rounded to bf16 for the product with V (2^-8 of each term).  Results are the
+ * same bit for bit from call to call.  A workspace belongs to one call at a time.
+ */
+typedef struct slkv_prompt_params {
+  int32_t n_seqs;
+  int32_t n_q_heads;        /* multiple of n_kv_heads */
+  int32_t n_kv_heads;
+  int32_t head_dim;         /* 64 or 128 */
+  int32_t window;           /* >= 1: rows of lse_opt */
+  int32_t dtype;            /* SLKV_F32 | SLKV_BF16 */
+  int32_t lse_units;        /* SLKV_LSE_LN | SLKV_LSE_LOG2 */
+  float scale;              /* 1 / sqrt(head_dim), usually; 2^-54 .. 2^54 */
+  int64_t q_stride_tok, q_stride_head, k_stride_tok, k_stride_head, v_stride_tok, v_stride_head, o_stride_tok, o_stride_head;
+} slkv_prompt_params;
+size_t slkv_prompt_attend_workspace_bytes(const slkv_prompt_params* p, const int32_t* cu_q_host, const int32_t* cu_k_host_opt);   /* 0: bad arguments */
+int slkv_prompt_attend(const slkv_prompt_params* p, const void* q, const void* k, const void* v, const int32_t* cu_q_dev,
+                       const int32_t* cu_q_host, const int32_t* cu_k_dev_opt, const int32_t* cu_k_host_opt, void* out, float* lse_opt,
+                       int32_t* status, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The compressed cache in pages (no counterpart in the paper): rows as slkv_compress packs them, with room to grow.  Budgets differ per
+ * head, so every segment has a length of its own: a page belongs to one segment of one layer, and all layers share the pool.
+ *
+ * Segment seg = (layer * n_seqs + s) * n_kv_heads + h has lens[seg] rows; row r is row r % page_rows of page tables[seg][r / page_rows].
+ * A slot is page * page_rows + row.  free_pages[0 .. n_free) is a stack of the pages that no segment has.  Tables, lengths and stack are
+ * device arrays that the host never reads: lengths beyond max_pages pages are cut to them, entries of tables outside the pool are read as
+ * pages of zeros (status: SLKV_ERR_BAD_SHAPE).
+ * Everything is enqueued on `stream`, nothing is allocated, every call can be captured.  A cache and a workspace belong to one call at a
+ * time.  n_seqs * n_kv_heads <= 16384, n_layers times that <= 2^20, n_pages and max_pages times page_rows <= 2^31 - 512; pages, rows and workspaces
+ * 16-byte aligned.
+ */
+typedef struct slkv_paged_cache {
+  int32_t n_layers, n_seqs, n_kv_heads;
+  int32_t head_dim;         /* 64 or 128 */
+  int32_t dtype;            /* SLKV_F32 | SLKV_BF16 */
+  int32_t page_rows;        /* 16, 32, 64 or 128 */
+  int32_t n_pages;          /* of the pool */
+  int32_t max_pages;        /* entries of a segment's table */
+  void *k_pages, *v_pages;  /* dev, [n_pages][page_rows][head_dim] */
+  int32_t* tables;          /* dev, [n_layers*n_seqs*n_kv_heads][max_pages] */
+  int32_t* lens;            /* dev, [n_layers*n_seqs*n_kv_heads] */
+  int32_t* free_pages;      /* dev, [n_pages] */
+  int32_t* n_free;          /* dev, [1] */
+} slkv_paged_cache;
+
+/*
+ * New lengths for all segments: pages that are no longer needed go back to the stack, pages that are come from it, and new rows get
+ * their slots.  Wanted lengths, by mode:
+ *   SLKV_PAGED_LENGTHS  want[n_segments]: the length itself (0: the sequence is done; less than it has: drafted rows go again)
+ *   SLKV_PAGED_OFFSETS  want[n_layers][n_seqs*n_kv_heads + 1]: offsets as slkv_compress writes them, a segment's rows being its length
+ *   SLKV_PAGED_ADD      want[n_seqs]: rows that every segment of the sequence gets in addition (below 0 counts as 0)
+ * First all pages are returned, so that the first segment's first returned page ends up on top of the stack, the next ones below it; then
+ * the segments take theirs from the top, in order.  Taking and returning are each other's inverse: going back to the old lengths leaves
+ * stack and tables as they were.  Where the pages run out (or a table is full) a segment gets what there is, the ones behind it nothing,
+ * and lengths are cut to the pages: status is SLKV_ERR_CAPACITY.
+ *   slots_opt        dev, optional out, int32[n_slots]: the slots of the rows that come in (old length .. new length - 1).
+ *                    slot_width = 0: one segment's behind the other's, from slot_offsets[seg] on (slot_offsets_opt: int32[n_segments+1],
+ *                    required); -1 behind the last one.  A fresh cache's slots so lie in the order of slkv_compress' packed rows.
+ *                    slot_width > 0: segment seg's from seg * slot_width on, -1 behind them.
+ *                    Rows beyond n_slots or slot_width get none (status: SLKV_ERR_CAPACITY).
+ *   lens_out, n_free_out   dev, optional, both or neither: take the new values in place of c->lens and c->n_free, which then keep the old
+ *                    ones: c still describes the cache as it was (tokens that are drafted), until a plan from there takes the pages again.
+ * OFFSETS behind slkv_compress_overlapped calls on the same stream needs no slkv_join: what is queued there goes out first.
+ */
+enum { SLKV_PAGED_LENGTHS = 0, SLKV_PAGED_OFFSETS = 1, SLKV_PAGED_ADD = 2 };
+int slkv_paged_plan(const slkv_paged_cache* c, int32_t mode, const int32_t* want, int32_t* slots_opt, int64_t n_slots, int32_t slot_width,
+                    int32_t* slot_offsets_opt, int32_t* lens_out, int32_t* n_free_out, int32_t* status, void* stream);
+
+/*
+ * Rows into slots: for every sequence s, head h and r < n_slots with a slot inside the pool, token t = take_opt[s][r] (NULL: r) of k and v,
+ * bit for bit.  Slots outside the pool are padding, and so are tokens outside 0 .. n_tokens - 1.  A slot is to be named once.
+ *   k, v       dev, elements of the cache's dtype: element (s, t, h, p) at s*stride_seq + t*stride_tok + h*stride_head + p
+ *   slots      dev, int32[n_seqs][n_heads][n_slots]: a layer's part of what slkv_paged_plan wrote
+ *   take_opt   dev, optional, int32[n_seqs][n_slots]: which tokens (of a tree, the accepted ones)
+ * A packed layer (k_out, v_out of slkv_compress) is one sequence and one head of n_tokens = its rows.  Behind slkv_compress_overlapped
+ * calls on the same stream no slkv_join is needed.
+ */
+int slkv_paged_write(const slkv_paged_cache* c, const void* k, const void* v, int32_t n_seqs, int32_t n_heads, int32_t n_tokens,
+                     int64_t k_stride_seq, int64_t k_stride_tok, int64_t k_stride_head, int64_t v_stride_seq, int64_t v_stride_tok,
+                     int64_t v_stride_head, const int32_t* slots, int32_t n_slots, const int32_t* take_opt, void* stream);
+
+/*
+ * Attention of n_tokens <= 64 tokens per sequence over one layer of the cache and over each other.  Token i of sequence s sees all rows of
+ * the segment (s, h) and, with has_new, those tokens j whose bit is set in tree[s][i]; their K and V rows are k_new and v_new, which are
+ * not in the cache (tokens that are refused leave no trace; the accepted ones go in by slkv_paged_plan and slkv_paged_write).
+ * out and lse as slkv_prompt_attend; a token that sees nothing gets zeros and -infinity, what it does not see gives it nothing.
+ *   q, out         dev: element (s, i, qh, p) at s*stride_seq + i*stride_tok + qh*stride_head + p
+ *   k_new, v_new   dev, with has_new: element (s, i, h, p) likewise
+ *   tree_opt       dev, optional, uint64[n_seqs][n_tokens]; NULL: token i sees the tokens 0 .. i
+ *   n_new_opt      dev, optional, int32[n_seqs]: tokens of each sequence; the rows behind them are padding: not read by others, outputs left as they are
+ *   lse_opt        dev, optional out, float[n_seqs][n_q_heads][n_tokens] in lse_units
+ * Limits, precision, status and workspace as slkv_prompt_attend.
+ */
+typedef struct slkv_paged_attend_params {
+  int32_t n_q_heads;        /* multiple of the cache's n_kv_heads */
+  int32_t n_tokens;         /* per sequence, 1 .. 64 */
+  int32_t layer;            /* of the cache */
+  int32_t has_new;          /* 1: the tokens' own rows are in k_new, v_new; 0: only the cache is seen */
+  int32_t lse_units;        /* SLKV_LSE_LN | SLKV_LSE_LOG2 */
+  float scale;
+  int64_t q_stride_seq, q_stride_tok, q_stride_head, o_stride_seq, o_stride_tok, o_stride_head;
+  int64_t k_stride_seq, k_stride_tok, k_stride_head, v_stride_seq, v_stride_tok, v_stride_head;
+} slkv_paged_attend_params;
+size_t slkv_paged_attend_workspace_bytes(const slkv_paged_cache* c, const slkv_paged_attend_params* p);   /* 0: bad arguments */
+int slkv_paged_attend(const slkv_paged_cache* c, const slkv_paged_attend_params* p, const void* q, const void* k_new, const void* v_new,
+                      const uint64_t* tree_opt, const int32_t* n_new_opt, void* out, float* lse_opt, int32_t* status, void* workspace,
+                      size_t workspace_bytes, void* stream);
+
+/* Number of kernels the most recent slkv_score / slkv_compress / slkv_compress_host / slkv_q4_* / slkv_prompt_* / slkv_paged_* call on
  * this thread enqueued (launch accounting for benchmarks). */
 int slkv_last_launch_count(void);
 
@@ -575,11 +701,11 @@ int slkv_trace_set_buffer(void* dev_buf, size_t bytes);
 /*
  * Test hook for the bounded waits (no counterpart in the paper).  Where the CTAs of a launch wait for one another
  * (the counters between the two passes of the score kernel; row sums and votes between the CTAs of a segment where one launch does
- * a short layer), and where a warp of slkv_q4_attend waits for its own copies, every wait gives up after one second, sets
+ * a short layer), and where warps of slkv_q4_attend, slkv_prompt_attend or slkv_paged_attend wait for copies and products, every wait gives up after one second, sets
  * SLKV_ERR_DEVICE_TIMEOUT in the call's status word, releases what the CTA holds and returns.  With the hook armed (on != 0) the next
  * such launch made by the calling thread waits for one arrival more than there are -- on = 1: where the CTAs of a score launch wait for
  * the statistics, 2: for their clearing, 3: where those of a one-launch layer wait for the row sums, 4: for the votes, 5: where the first
- * CTA of slkv_q4_attend waits for rows -- so that exactly this path runs: the call's results are then incomplete
+ * CTA of slkv_q4_attend waits for rows, or that of a bf16 slkv_prompt_attend or slkv_paged_attend for probabilities -- so that exactly this path runs: the call's results are then incomplete
  * and its status word says so; the calls after it are unaffected.  While it is armed with 1 or 2, short layers go the way of the
  * others; a list that goes with one product with every key (slkv_debug_list_way) waits for statistics only where some head needs all
  * its votes.  One-shot: the launch that takes it disarms it.

@@ -52,7 +52,26 @@ class SlkvQ4AttendParams(C.Structure):
                                          "o_stride_head")]
 
 
+class SlkvPromptParams(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_seqs", "n_q_heads", "n_kv_heads", "head_dim", "window", "dtype", "lse_units")] + \
+               [("scale", C.c_float)] + \
+               [(n, C.c_int64) for n in ("q_stride_tok", "q_stride_head", "k_stride_tok", "k_stride_head", "v_stride_tok",
+                                         "v_stride_head", "o_stride_tok", "o_stride_head")]
+
+
+class SlkvPagedCache(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_layers", "n_seqs", "n_kv_heads", "head_dim", "dtype", "page_rows", "n_pages",
+                                         "max_pages")] + \
+               [(n, C.c_void_p) for n in ("k_pages", "v_pages", "tables", "lens", "free_pages", "n_free")]
+
+
+class SlkvPagedAttendParams(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_q_heads", "n_tokens", "layer", "has_new", "lse_units")] + [("scale", C.c_float)] + \
+               [(f"{x}_stride_{y}", C.c_int64) for x in "qokv" for y in ("seq", "tok", "head")]
+
+
 SLKV_NORM_GLOBAL, SLKV_NORM_WITHIN_LAYER = 0, 1
+SLKV_PAGED_LENGTHS, SLKV_PAGED_OFFSETS, SLKV_PAGED_ADD = 0, 1, 2
 SLKV_ROUND_SUM_EXACT, SLKV_ROUND_PAPER = 0, 1
 
 
@@ -162,6 +181,19 @@ def lib() -> C.CDLL:
         L.slkv_q4_evict_workspace_bytes.argtypes = [cp]
         L.slkv_q4_evict.restype = C.c_int
         L.slkv_q4_evict.argtypes = [cp, cp, vp, i32, vp, vp, vp, sz, vp]
+        rp, gp, tp = C.POINTER(SlkvPromptParams), C.POINTER(SlkvPagedCache), C.POINTER(SlkvPagedAttendParams)
+        L.slkv_prompt_attend_workspace_bytes.restype = sz
+        L.slkv_prompt_attend_workspace_bytes.argtypes = [rp, i32p, i32p]
+        L.slkv_prompt_attend.restype = C.c_int
+        L.slkv_prompt_attend.argtypes = [rp, vp, vp, vp, vp, i32p, vp, i32p, vp, vp, vp, vp, sz, vp]
+        L.slkv_paged_plan.restype = C.c_int
+        L.slkv_paged_plan.argtypes = [gp, i32, vp, vp, i64, i32, vp, vp, vp, vp, vp]
+        L.slkv_paged_write.restype = C.c_int
+        L.slkv_paged_write.argtypes = [gp, vp, vp, i32, i32, i32, i64, i64, i64, i64, i64, i64, vp, i32, vp, vp]
+        L.slkv_paged_attend_workspace_bytes.restype = sz
+        L.slkv_paged_attend_workspace_bytes.argtypes = [gp, tp]
+        L.slkv_paged_attend.restype = C.c_int
+        L.slkv_paged_attend.argtypes = [gp, tp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         _lib = L
     return _lib
 
@@ -670,3 +702,207 @@ def slkv_q4_evict(cache: SlkvQ4Cache, to: SlkvQ4Cache, budgets: torch.Tensor, wi
     rc = _fn["slkv_q4_evict"](stream, cache, to, budgets, int(window), newest, status, workspace, workspace.numel())
     if rc != SLKV_OK:
         raise SlkvError(rc, "slkv_q4_evict")
+
+
+# ---- prompts and the paged cache: thin wrappers, see include/slkv.h ----------------------------------------------------------
+def make_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor, n_seqs: int, window: int = 1,
+                scale: Optional[float] = None, lse_units: int = SLKV_LSE_LN) -> SlkvPromptParams:
+    """Shapes and strides from the tensors: q, out [tokens, n_q_heads, head_dim], k, v [keys, n_kv_heads, head_dim] (last dim
+    contiguous).  window: rows of lse."""
+    assert q.dim() == k.dim() == 3 and q.shape == out.shape and k.shape == v.shape and q.size(2) == k.size(2)
+    assert q.dtype == k.dtype == v.dtype == out.dtype and q.stride(2) == k.stride(2) == v.stride(2) == out.stride(2) == 1
+    p = SlkvPromptParams(n_seqs, q.size(1), k.size(1), q.size(2), window, _DTYPES[q.dtype], lse_units,
+                         q.size(2) ** -0.5 if scale is None else scale, *q.stride()[:2], *k.stride()[:2], *v.stride()[:2],
+                         *out.stride()[:2])
+    p.q_like, p.out_like = (q.shape, q.stride(), q.dtype), (out.shape, out.stride(), out.dtype)
+    p.k_like, p.v_like, p.device = (k.shape, k.stride(), k.dtype), (v.shape, v.stride(), v.dtype), q.device
+    return p
+
+
+def _like(t: torch.Tensor):
+    return t.shape, t.stride(), t.dtype
+
+
+def slkv_prompt_attend_workspace_bytes(params: SlkvPromptParams, cu_q: Sequence[int], cu_k: Optional[Sequence[int]] = None) -> int:
+    assert len(cu_q) == params.n_seqs + 1 and (cu_k is None or len(cu_k) == len(cu_q))
+    return int(lib().slkv_prompt_attend_workspace_bytes(C.byref(params), _cu_host(cu_q), None if cu_k is None else _cu_host(cu_k)))
+
+
+def new_prompt_workspace(params: SlkvPromptParams, cu_q: Sequence[int], cu_k: Optional[Sequence[int]] = None) -> torch.Tensor:
+    n = slkv_prompt_attend_workspace_bytes(params, cu_q, cu_k)
+    if n == 0:
+        raise SlkvError(ERR["BAD_SHAPE"], "slkv_prompt_attend_workspace_bytes")
+    return torch.empty(n, dtype=torch.uint8, device=params.device)
+
+
+def slkv_prompt_attend(params: SlkvPromptParams, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.Tensor,
+                       cu_q_host: Sequence[int], out: torch.Tensor, workspace: torch.Tensor, cu_k: Optional[torch.Tensor] = None,
+                       cu_k_host: Optional[Sequence[int]] = None, lse: Optional[torch.Tensor] = None,
+                       status: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """q, k, v, out: the shapes and strides params was made from; cu_q, cu_k int32 [n_seqs + 1] on the device, the same on the host.
+    lse float32 [n_seqs, n_q_heads, window]."""
+    d = q.get_device()
+    if not d == k.get_device() == v.get_device() == cu_q.get_device() == out.get_device() == workspace.get_device() == _current_device():
+        _q4_elsewhere()
+    assert _like(q) == params.q_like and _like(out) == params.out_like and _like(k) == params.k_like and _like(v) == params.v_like
+    n = params.n_seqs
+    assert len(cu_q_host) == n + 1 and cu_q.dtype is _I32 and cu_q.is_contiguous() and cu_q.numel() == n + 1
+    assert (cu_k is None) == (cu_k_host is None)
+    if cu_k is not None:
+        assert len(cu_k_host) == n + 1 and cu_k.dtype is _I32 and cu_k.is_contiguous() and cu_k.numel() == n + 1 and cu_k.get_device() == d
+    assert cu_q_host[n] <= q.size(0) and (cu_q_host if cu_k is None else cu_k_host)[n] <= k.size(0)
+    if lse is not None:
+        assert lse.dtype is _F32 and lse.is_contiguous() and lse.get_device() == d
+        assert lse.numel() == n * params.n_q_heads * params.window
+    if status is not None:
+        assert status.dtype is _I32 and status.numel() >= 1 and status.get_device() == d
+    rc = _fn["slkv_prompt_attend"](stream, params, q, k, v, cu_q, _cu_list(cu_q_host), cu_k,
+                                   None if cu_k is None else _cu_list(cu_k_host), out, lse, status, workspace, workspace.numel())
+    if rc != SLKV_OK:
+        raise SlkvError(rc, "slkv_prompt_attend")
+    return out
+
+
+def make_paged_cache(k_pages: torch.Tensor, v_pages: torch.Tensor, tables: torch.Tensor, lens: torch.Tensor, free_pages: torch.Tensor,
+                     n_free: torch.Tensor, n_seqs: int, n_kv_heads: int) -> SlkvPagedCache:
+    """k_pages, v_pages [n_pages, page_rows, head_dim], tables int32 [n_segments, max_pages], lens int32 [n_segments], free_pages
+    int32 [n_pages], n_free int32 [1], all contiguous; n_segments = layers * n_seqs * n_kv_heads.  The structure keeps the tensors alive
+    and belongs to their device."""
+    tensors = (k_pages, v_pages, tables, lens, free_pages, n_free)
+    assert k_pages.dim() == 3 and k_pages.shape == v_pages.shape and k_pages.dtype == v_pages.dtype
+    for t in tensors:
+        assert t.is_contiguous() and t.device == k_pages.device
+    for t in tensors[2:]:
+        assert t.dtype == torch.int32
+    n_pages, page_rows, dim = k_pages.shape
+    assert tables.dim() == 2 and lens.numel() == tables.size(0) and free_pages.numel() == n_pages and n_free.numel() == 1
+    assert n_seqs >= 1 and n_kv_heads >= 1 and lens.numel() % (n_seqs * n_kv_heads) == 0
+    c = SlkvPagedCache(lens.numel() // (n_seqs * n_kv_heads), n_seqs, n_kv_heads, dim, _DTYPES[k_pages.dtype], page_rows, n_pages,
+                       tables.size(1), *(t.data_ptr() for t in tensors))
+    c.tensors, c.device, c.element = tensors, k_pages.device, k_pages.dtype
+    c.index = k_pages.get_device() if k_pages.is_cuda else -2
+    return c
+
+
+def slkv_paged_plan(cache: SlkvPagedCache, mode: int, want: torch.Tensor, slots: Optional[torch.Tensor] = None,
+                    slot_offsets: Optional[torch.Tensor] = None, after: Optional[SlkvPagedCache] = None,
+                    status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """want int32: [n_segments] (SLKV_PAGED_LENGTHS), [n_layers, n_seqs * n_kv_heads + 1] (SLKV_PAGED_OFFSETS) or [n_seqs]
+    (SLKV_PAGED_ADD).  slots int32: [n] with slot_offsets int32 [n_segments + 1], or [n_segments, width] without.  after: the same cache
+    with lengths and a count of free pages of its own, which take the new ones."""
+    d = cache.index
+    if not d == want.get_device() == _current_device():
+        _q4_elsewhere()
+    per = cache.n_seqs * cache.n_kv_heads
+    n_seg = cache.n_layers * per
+    assert want.dtype is _I32 and want.is_contiguous()
+    assert want.numel() == {SLKV_PAGED_LENGTHS: n_seg, SLKV_PAGED_OFFSETS: n_seg + cache.n_layers, SLKV_PAGED_ADD: cache.n_seqs}[mode]
+    width = n_slots = 0
+    if slots is not None:
+        assert slots.dtype is _I32 and slots.is_contiguous() and slots.get_device() == d
+        n_slots = slots.numel()
+        if slot_offsets is None:
+            assert slots.dim() == 2 and slots.size(0) == n_seg
+            width = slots.size(1)
+            if width == 0:
+                slots = None
+        else:
+            assert slot_offsets.dtype is _I32 and slot_offsets.is_contiguous() and slot_offsets.numel() == n_seg + 1
+            assert slot_offsets.get_device() == d
+    lens_out = n_free_out = None
+    if after is not None:
+        assert after.tables == cache.tables and after.free_pages == cache.free_pages and after.n_layers == cache.n_layers
+        assert after.n_seqs == cache.n_seqs and after.n_kv_heads == cache.n_kv_heads and after.max_pages == cache.max_pages
+        lens_out, n_free_out = after.tensors[3], after.tensors[5]
+    if status is not None:
+        _q4_status(cache, status)
+    rc = _fn["slkv_paged_plan"](stream, cache, mode, want, slots, n_slots, width, slot_offsets, lens_out, n_free_out, status)
+    if rc != SLKV_OK:
+        raise SlkvError(rc, "slkv_paged_plan")
+
+
+def slkv_paged_write(cache: SlkvPagedCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, take: Optional[torch.Tensor] = None,
+                     stream=None) -> None:
+    """k, v [n_seqs, n_tokens, n_heads, head_dim] (any strides over a contiguous last dimension) with slots int32 of n_seqs * n_heads *
+    width entries and take int32 [n_seqs, width], or [rows, head_dim] with slots int32 [n]."""
+    d = cache.index
+    if not d == k.get_device() == v.get_device() == slots.get_device() == _current_device():
+        _q4_elsewhere()
+    assert k.shape == v.shape and k.dtype is v.dtype is cache.element and slots.dtype is _I32 and slots.is_contiguous()
+    if k.dim() == 2:
+        (nt, dim), ns, hkv = k.shape, 1, 1
+        (kt, k1), (vt, v1) = k.stride(), v.stride()
+        ks = kh = vs = vh = dim
+    else:
+        ns, nt, hkv, dim = k.shape
+        ks, kt, kh, k1 = k.stride()
+        vs, vt, vh, v1 = v.stride()
+    assert k1 == v1 == 1 and dim == cache.head_dim and ns * hkv > 0 and slots.numel() % (ns * hkv) == 0
+    width = slots.numel() // (ns * hkv)
+    if take is not None:
+        assert take.dtype is _I32 and take.is_contiguous() and take.numel() == ns * width and take.get_device() == d
+    rc = _fn["slkv_paged_write"](stream, cache, k, v, ns, hkv, nt, ks, kt, kh, vs, vt, vh, slots, width, take)
+    if rc != SLKV_OK:
+        raise SlkvError(rc, "slkv_paged_write")
+
+
+def make_paged_attend(cache: SlkvPagedCache, q: torch.Tensor, out: torch.Tensor, k_new: Optional[torch.Tensor] = None,
+                      v_new: Optional[torch.Tensor] = None, layer: int = 0, scale: Optional[float] = None,
+                      lse_units: int = SLKV_LSE_LN) -> SlkvPagedAttendParams:
+    """Shapes and strides from the tensors: q, out [n_seqs, n_tokens, n_q_heads, head_dim], k_new, v_new [n_seqs, n_tokens, n_kv_heads,
+    head_dim] (last dim contiguous)."""
+    assert q.shape == out.shape and q.dim() == 4 and q.dtype == out.dtype == cache.element and q.stride(3) == 1 and out.stride(3) == 1
+    assert q.size(0) == cache.n_seqs and q.size(3) == cache.head_dim and (k_new is None) == (v_new is None)
+    kv = [(0, 0, 0)] * 2
+    if k_new is not None:
+        for t in (k_new, v_new):
+            assert t.shape == (cache.n_seqs, q.size(1), cache.n_kv_heads, cache.head_dim) and t.dtype == q.dtype and t.stride(3) == 1
+        kv = [k_new.stride()[:3], v_new.stride()[:3]]
+    p = SlkvPagedAttendParams(q.size(2), q.size(1), layer, int(k_new is not None), lse_units,
+                              cache.head_dim ** -0.5 if scale is None else scale, *q.stride()[:3], *out.stride()[:3], *kv[0], *kv[1])
+    p.q_like, p.out_like = _like(q), _like(out)
+    p.k_like, p.v_like = (None, None) if k_new is None else (_like(k_new), _like(v_new))
+    return p
+
+
+def slkv_paged_attend_workspace_bytes(cache: SlkvPagedCache, params: SlkvPagedAttendParams) -> int:
+    return int(lib().slkv_paged_attend_workspace_bytes(C.byref(cache), C.byref(params)))
+
+
+def new_paged_workspace(cache: SlkvPagedCache, params: SlkvPagedAttendParams) -> torch.Tensor:
+    n = slkv_paged_attend_workspace_bytes(cache, params)
+    if n == 0:
+        raise SlkvError(ERR["BAD_SHAPE"], "slkv_paged_attend_workspace_bytes")
+    return torch.empty(n, dtype=torch.uint8, device=cache.device)
+
+
+def slkv_paged_attend(cache: SlkvPagedCache, params: SlkvPagedAttendParams, q: torch.Tensor, out: torch.Tensor, workspace: torch.Tensor,
+                      k_new: Optional[torch.Tensor] = None, v_new: Optional[torch.Tensor] = None, tree: Optional[torch.Tensor] = None,
+                      n_new: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None,
+                      stream=None) -> torch.Tensor:
+    """q, out, k_new, v_new: the shapes and strides params was made from.  tree int64 (or uint64) [n_seqs, n_tokens], n_new int32 [n_seqs],
+    lse float32 [n_seqs, n_q_heads, n_tokens]."""
+    d = cache.index
+    if not d == q.get_device() == out.get_device() == workspace.get_device() == _current_device():
+        _q4_elsewhere()
+    assert _like(q) == params.q_like and _like(out) == params.out_like
+    ns, nt, hq, dim = params.q_like[0]
+    assert ns == cache.n_seqs and dim == cache.head_dim and q.dtype is cache.element
+    if params.k_like is None:
+        assert k_new is None and v_new is None
+    else:
+        assert _like(k_new) == params.k_like and _like(v_new) == params.v_like
+        assert k_new.get_device() == v_new.get_device() == d and params.k_like[0][2] == cache.n_kv_heads
+    if tree is not None:
+        assert tree.element_size() == 8 and not tree.is_floating_point() and tree.is_contiguous() and tree.numel() == ns * nt
+        assert tree.get_device() == d
+    if n_new is not None:
+        assert n_new.dtype is _I32 and n_new.is_contiguous() and n_new.numel() == ns and n_new.get_device() == d
+    if lse is not None:
+        assert lse.dtype is _F32 and lse.is_contiguous() and lse.numel() == ns * nt * hq and lse.get_device() == d
+    if status is not None:
+        _q4_status(cache, status)
+    rc = _fn["slkv_paged_attend"](stream, cache, params, q, k_new, v_new, tree, n_new, out, lse, status, workspace, workspace.numel())
+    if rc != SLKV_OK:
+        raise SlkvError(rc, "slkv_paged_attend")
+    return out

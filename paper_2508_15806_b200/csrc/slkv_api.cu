@@ -658,7 +658,8 @@ const char* slkv_kernel_name(int kernel_id) {
   static const char* names[KID_COUNT] = {"k_setup", "k_score_lse", "k_score_vote", "k_pool", "k_select",
                                          "k_gather", "k_alloc", "k_score_fused", "k_score_list", "k_window_stats",
                                          "k_merge_lse", "k_behavior", "k_cp", "k_layer", "k_score_bound",
-                                         "k_q4_rows", "k_q4_attend", "k_q4_join", "k_q4_evict", "k_q4_move"};
+                                         "k_q4_rows", "k_q4_attend", "k_q4_join", "k_q4_evict", "k_q4_move", "k_attend", "k_attend_join", "k_paged_plan",
+                                         "k_paged_write"};
   return (kernel_id >= 0 && kernel_id < KID_COUNT) ? names[kernel_id] : "";
 }
 

@@ -1,0 +1,296 @@
+// What the attention kernels of prompts and of paged caches share (slkv_attend_tc.cu, slkv_attend_fma.cu, slkv_attend_api.cu).
+//
+// Both are one problem: a unit is a block of query rows of one KV head -- some tokens times the G query heads that share its keys --
+// against tiles of 128 keys.  What differs is where a tile lies and which of its keys a row sees:
+//   prompt  keys are rows of the packed sequence; token i of nq sees the first i + 1 + nk - nq
+//   paged   the segment's rows lie in pages and all tokens see them; one more tile holds the drafted tokens' own rows, of which
+//           token i sees those whose bit is set in its mask
+#pragma once
+
+#include "slkv_internal.cuh"
+
+namespace slkv {
+
+constexpr int kAttendTile = 128;                 // keys of a tile, query rows of a block
+constexpr int kMaxDrafted = 64;                  // drafted tokens of a sequence: the bits of a mask
+constexpr int kMaxGroup = 64;                    // query heads of a KV head
+
+// What the kernels need to know of a call.
+struct AttendShape {
+  int n_seqs, n_kv_heads, n_q_heads, G, head_dim;
+  int block_tokens, unit_tokens, tile_keys;      // tokens of a block of query rows and of a unit (one or two blocks); keys of a tile
+  int paged;
+  // prompt
+  const int32_t *cu_q, *cu_k;
+  int window;                                    // rows of lse
+  // paged
+  const int32_t *tables, *lens;                  // of the layer
+  int page_rows, max_pages, n_pages;
+  int n_tokens;
+  int has_new;
+  const int32_t* n_new;                          // may be null: n_tokens
+  const unsigned long long* tree;                // may be null: token i sees 0 .. i
+  // tensors: q, out, drafted rows by (sequence, token, head); a prompt's sequence stride is not used
+  const void *q, *k, *v, *k_new, *v_new;         // paged: k, v are the pools
+  long long q_seq, q_tok, q_head, o_seq, o_tok, o_head, k_tok, k_head, v_tok, v_head, kn_seq, kn_tok, kn_head, vn_seq, vn_tok, vn_head;
+  long long rows_q, rows_k;                      // that exist: of all sequences; paged: of the pool
+  void* out;
+  float* lse;                                    // may be null
+  int32_t* status;                               // may be null
+  float scale, lse_unit;                         // lse_unit: log2 units -> the caller's
+  // how the units are shared out
+  int spread;                                    // 1: whole units in turn, the longest first; 0: every CTA as many tiles as the others
+  int n_cta;
+  int levels;                                    // spread: blocks of the longest sequence
+  long long tiles;                               // prompt, not spread: tiles of all units (a unit without any counts one)
+  // partial results of units that several CTAs share
+  float* part;                                   // [n_cta][2][rows][head_dim]
+  float2* ml;                                    // [n_cta][2][rows]
+  int4* desc;                                    // [n_cta][2]
+  int part_rows, used_rows;                      // rows of a unit there is room for, and at most in use
+  int q_head_inner, box_tokens;                  // how a block's rows lie: see attend_row; tokens of a block in shared memory
+};
+
+size_t attend_workspace(int n_cta, int part_rows, int head_dim);
+void attend_bind(AttendShape* a, void* workspace);
+int attend_fma_ctas();
+cudaError_t launch_attend_tensor(const AttendShape& a, cudaStream_t st, int* launches);
+cudaError_t launch_attend_fma(const AttendShape& a, cudaStream_t st, int* launches);
+cudaError_t launch_attend_join(const AttendShape& a, bool f32, cudaStream_t st, int* launches);
+
+#ifdef __CUDACC__
+// A piece of a unit: its tiles tile0 .. tile0 + n - 1 of n_all.
+struct AttendPiece {
+  int s, h;
+  int tok0, n_tok;               // the unit's tokens, of the sequence
+  int n_seq_tok;                 // tokens of the sequence
+  int nk;                        // keys: prompt: of the sequence, paged: rows of the segment
+  int shift;                     // prompt: token i sees keys below i + 1 + shift
+  int q_row, k_row;              // prompt: first rows of the sequence
+  int tile0, n, n_all;
+  int part;                      // -1: the unit's only piece; 0: one that does not begin it; 1: its first
+  int stop;
+};
+
+// Row r of a unit: its token of the unit and its query head of the group; false: no row.  Rows come in blocks of 128 (the FMA kernel: one
+// block); in a block the query heads of a token lie next to each other, or the tokens of a query head (q_head_inner = 0).
+__device__ __forceinline__ bool attend_row(const AttendShape& a, int r, int* tok, int* head) {
+  const int b = r >> 7, i = r & 127;
+  int rt, rh;
+  if (a.q_head_inner) { rt = i / a.G; rh = i - rt * a.G; }
+  else { rh = i / a.box_tokens; rt = i - rh * a.box_tokens; }
+  *tok = b * a.block_tokens + rt;
+  *head = rh;
+  return rt < a.block_tokens && rh < a.G;
+}
+// The row's log-sum-exp m + log2(l), where the caller wants it.
+__device__ __forceinline__ void attend_lse(const AttendShape& a, int s, int qh, int tok, int n_seq_tok, float m, float l) {
+  if (!a.lse) return;
+  const float lse = (l > 0.f || l != l ? m + log2f(l) : -INFINITY) * a.lse_unit;
+  const long long row = (long long)s * a.n_q_heads + qh;
+  if (a.paged) a.lse[row * a.n_tokens + tok] = lse;
+  else if (tok >= n_seq_tok - a.window) a.lse[row * a.window + tok - (n_seq_tok - a.window)] = lse;
+}
+
+// Deals out the pieces of a launch; one warp runs it, every lane with the same results.
+//   spread       whole units, to the CTAs in turn and back (0 .. n - 1, n - 1 .. 0, ..), the ones with the most tiles of their
+//                sequence first: shares differ by about the last units, which are short, and CTAs that run beside each other read the
+//                same keys
+//   not spread   the tiles of all units in one row, cut into n_cta equal shares: for few units.  A unit without tiles counts one.
+class AttendSchedule {
+ public:
+  __device__ AttendSchedule(const AttendShape& a, int cta) : a_(a), cta_(cta), lane_(threadIdx.x & 31) {
+    if (a_.spread) {
+      item_ = cta;
+      round_ = 0;
+      level_ = a_.levels - 1;
+      base_ = 0;
+      count_ = level_count(level_);
+    } else {
+      long long total = a_.tiles;
+      if (a_.paged) total = paged_total();
+      pos_ = total * cta / a_.n_cta;
+      end_ = total * (cta + 1) / a_.n_cta;
+      if (pos_ < end_) find(pos_);
+    }
+  }
+  __device__ bool next(AttendPiece* p) { return a_.spread ? next_spread(p) : next_share(p); }
+
+ private:
+  const AttendShape& a_;
+  int cta_, lane_;
+  // spread
+  long long item_, base_, count_;
+  int level_, round_;
+  // shares: the group of units with the same tiles (prompt: a block of tokens, all KV heads; paged: a segment, all blocks)
+  long long pos_, end_, group_;  // group_: first position of the group
+  int s_, x_;                    // sequence; prompt: block of tokens, paged: KV head
+  int inner_, each_;             // units of the group, tiles counted for each
+
+  __device__ int seq_tokens(int s) const {
+    if (!a_.paged) return max(__ldg(a_.cu_q + s + 1) - __ldg(a_.cu_q + s), 0);
+    return a_.n_new ? min(max(a_.n_new[s], 0), a_.n_tokens) : a_.n_tokens;
+  }
+  __device__ int seq_keys(int s) const { return max(__ldg(a_.cu_k + s + 1) - __ldg(a_.cu_k + s), 0); }
+  __device__ int blocks(int tokens) const { return (tokens + a_.unit_tokens - 1) / a_.unit_tokens; }
+  __device__ int rows_of(int seg) const { return (int)min((long long)max(a_.lens[seg], 0), (long long)a_.max_pages * a_.page_rows); }
+  // Tiles of a unit.
+  __device__ int prompt_tiles(int nq, int nk, int t) const {
+    const int seen = min(nq, (t + 1) * a_.unit_tokens) + nk - nq;
+    return seen <= 0 ? 0 : (seen + a_.tile_keys - 1) / a_.tile_keys;
+  }
+  __device__ int paged_tiles(int rows) const { return (rows + a_.tile_keys - 1) / a_.tile_keys + a_.has_new; }
+
+  // ---- spread
+  __device__ long long level_count(int t) const {
+    int n = 0;
+    for (int s0 = 0; s0 < a_.n_seqs; s0 += 32) {
+      const int s = s0 + lane_;
+      n += __popc(__ballot_sync(0xffffffffu, s < a_.n_seqs && blocks(seq_tokens(s)) > t));
+    }
+    return (long long)n * a_.n_kv_heads;
+  }
+  __device__ bool next_spread(AttendPiece* p) {
+    while (level_ >= 0 && item_ >= base_ + count_) {
+      base_ += count_;
+      if (--level_ >= 0) count_ = level_count(level_);
+    }
+    if (level_ < 0) return false;
+    int nth = (int)((item_ - base_) / a_.n_kv_heads);
+    const int h = (int)((item_ - base_) - (long long)nth * a_.n_kv_heads);
+    int s = 0;
+    for (int s0 = 0; s0 < a_.n_seqs; s0 += 32) {
+      unsigned m = __ballot_sync(0xffffffffu, s0 + lane_ < a_.n_seqs && blocks(seq_tokens(s0 + lane_)) > level_);
+      const int n = __popc(m);
+      if (nth < n) {
+        for (; nth > 0; --nth) m &= m - 1;
+        s = s0 + __ffs(m) - 1;
+        break;
+      }
+      nth -= n;
+    }
+    fill(p, s, h, level_);
+    p->tile0 = 0;
+    p->n = p->n_all;
+    p->part = -1;
+    ++round_;
+    item_ = (long long)round_ * a_.n_cta + (round_ & 1 ? a_.n_cta - 1 - cta_ : cta_);
+    return true;
+  }
+
+  // ---- equal shares
+  __device__ long long paged_total() const {
+    const int n_seg = a_.n_seqs * a_.n_kv_heads;
+    long long sum = 0;
+#pragma unroll 4
+    for (int seg = lane_; seg < n_seg; seg += 32)
+      sum += (long long)blocks(seq_tokens(seg / a_.n_kv_heads)) * max(paged_tiles(rows_of(seg)), 1);
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+    return sum;
+  }
+  __device__ void load_group() {
+    if (a_.paged) {
+      inner_ = blocks(seq_tokens(s_));
+      each_ = max(paged_tiles(rows_of(s_ * a_.n_kv_heads + x_)), 1);
+    } else {
+      const int nq = seq_tokens(s_);
+      inner_ = x_ < blocks(nq) ? a_.n_kv_heads : 0;
+      each_ = max(prompt_tiles(nq, seq_keys(s_), x_), 1);
+    }
+  }
+  __device__ void advance() {
+    const int last = a_.paged ? a_.n_kv_heads : blocks(seq_tokens(s_));
+    if (++x_ >= last) { x_ = 0; ++s_; }
+  }
+  // The group that holds position pos, which exists: 32 groups at a time.
+  __device__ void find(long long pos) {
+    long long before = 0;
+    s_ = x_ = 0;
+    if (a_.paged) {
+      const int n_seg = a_.n_seqs * a_.n_kv_heads;
+      for (int g0 = 0; g0 < n_seg; g0 += 32) {
+        const int g = g0 + lane_;
+        long long w = 0;
+        if (g < n_seg) w = (long long)blocks(seq_tokens(g / a_.n_kv_heads)) * max(paged_tiles(rows_of(g)), 1);
+        if (locate(pos, w, &before, g0)) {
+          s_ = found_ / a_.n_kv_heads;
+          x_ = found_ - s_ * a_.n_kv_heads;
+          break;
+        }
+      }
+    } else {
+      bool found = false;
+      for (int s = 0; s < a_.n_seqs && !found; ++s) {
+        const int nq = seq_tokens(s), nk = seq_keys(s), n = blocks(nq);
+        for (int t0 = 0; t0 < n && !found; t0 += 32) {
+          const int t = t0 + lane_;
+          const long long w = t < n ? (long long)a_.n_kv_heads * max(prompt_tiles(nq, nk, t), 1) : 0;
+          if (locate(pos, w, &before, t0)) { s_ = s; x_ = found_; found = true; }
+        }
+      }
+    }
+    group_ = before;
+    load_group();
+  }
+  int found_;
+  // Of 32 weights: is pos behind `before` inside them?  If so found_ is the index, and before what lies in front of it.
+  __device__ bool locate(long long pos, long long w, long long* before, int first) {
+    long long incl = w;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const long long o = __shfl_up_sync(0xffffffffu, incl, d);
+      if (lane_ >= d) incl += o;
+    }
+    const unsigned m = __ballot_sync(0xffffffffu, *before + incl > pos);
+    if (m == 0) {
+      *before += __shfl_sync(0xffffffffu, incl, 31);
+      return false;
+    }
+    const int at = __ffs(m) - 1;
+    *before += __shfl_sync(0xffffffffu, incl - w, at);
+    found_ = first + at;
+    return true;
+  }
+  __device__ bool next_share(AttendPiece* p) {
+    if (pos_ >= end_) return false;
+    while (pos_ >= group_ + (long long)inner_ * each_) {
+      group_ += (long long)inner_ * each_;
+      advance();
+      if (s_ >= a_.n_seqs) return false;                       // lengths on the device that are not the host's
+      load_group();
+    }
+    const int rel = (int)(pos_ - group_), unit = rel / each_, tile0 = rel - unit * each_;
+    const int take = (int)min((long long)(each_ - tile0), end_ - pos_);
+    if (a_.paged) fill(p, s_, x_, unit);
+    else fill(p, s_, unit, x_);
+    p->tile0 = tile0;
+    p->n = p->n_all == 0 ? 0 : take;
+    p->part = take == each_ ? -1 : (tile0 == 0 ? 1 : 0);
+    pos_ += take;
+    return true;
+  }
+  __device__ void fill(AttendPiece* p, int s, int h, int t) const {
+    p->s = s;
+    p->h = h;
+    const int nq = seq_tokens(s);
+    p->n_seq_tok = nq;
+    p->tok0 = t * a_.unit_tokens;
+    p->n_tok = min(a_.unit_tokens, nq - p->tok0);
+    if (a_.paged) {
+      p->nk = rows_of(s * a_.n_kv_heads + h);
+      p->shift = p->q_row = p->k_row = 0;
+      p->n_all = paged_tiles(p->nk);
+    } else {
+      p->nk = seq_keys(s);
+      p->shift = p->nk - nq;
+      p->q_row = __ldg(a_.cu_q + s);
+      p->k_row = __ldg(a_.cu_k + s);
+      p->n_all = prompt_tiles(nq, p->nk, t);
+    }
+    p->stop = 0;
+  }
+};
+#endif
+
+}  // namespace slkv

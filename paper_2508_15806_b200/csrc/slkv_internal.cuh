@@ -131,7 +131,7 @@ struct Problem {
 };
 
 // kernel ids for launch accounting / per-kernel timing
-enum KernelId { KID_SETUP = 0, KID_SCORE_LSE, KID_SCORE_VOTE, KID_POOL, KID_SELECT, KID_GATHER, KID_ALLOC, KID_SCORE_FUSED, KID_SCORE_LIST, KID_WINDOW_STATS, KID_MERGE_LSE, KID_BEHAVIOR, KID_CP, KID_LAYER, KID_SCORE_BOUND, KID_Q4_ROWS, KID_Q4_ATTEND, KID_Q4_JOIN, KID_Q4_EVICT, KID_Q4_MOVE, KID_COUNT };
+enum KernelId { KID_SETUP = 0, KID_SCORE_LSE, KID_SCORE_VOTE, KID_POOL, KID_SELECT, KID_GATHER, KID_ALLOC, KID_SCORE_FUSED, KID_SCORE_LIST, KID_WINDOW_STATS, KID_MERGE_LSE, KID_BEHAVIOR, KID_CP, KID_LAYER, KID_SCORE_BOUND, KID_Q4_ROWS, KID_Q4_ATTEND, KID_Q4_JOIN, KID_Q4_EVICT, KID_Q4_MOVE, KID_ATTEND, KID_ATTEND_JOIN, KID_PAGED_PLAN, KID_PAGED_ROWS, KID_COUNT };
 
 // Brackets one kernel launch: counts it and, when per-kernel timing is on for this thread, records a
 // CUDA event pair around it on the launch stream.
@@ -270,6 +270,9 @@ struct ScorePlan {
   ScoreShape sh;
   ScoreLayer lay;
 };
+// A tensor map of bf16 elements over 128-byte-swizzled boxes 64 elements wide; false where the driver refuses it.
+bool encode_tiled_bf16(CUtensorMap* m, const void* base, int rank, const cuuint64_t* dims, const cuuint64_t* strides,
+                       const cuuint32_t* box);
 // Fills a plan for a problem whose workspace is bound; sh.n_cta = 0 when there is no history to score.
 // cudaErrorNotSupported when the driver has no tensor-map encoder.
 cudaError_t plan_score_tensor(const Problem& pb, const int32_t* cu_host, int32_t* status, ScorePlan* plan);
