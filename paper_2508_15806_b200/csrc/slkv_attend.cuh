@@ -46,7 +46,8 @@ struct AttendShape {
   // partial results of units that several CTAs share
   float* part;                                   // [n_cta][2][rows][head_dim]
   float2* ml;                                    // [n_cta][2][rows]
-  int4* desc;                                    // [n_cta][2]
+  float ml_unit;                                 // times a reference in ml: log2 units
+  int4* desc;                                    // [n_cta][2]: 1 a piece, 2 one that ends its unit, -1 one that failed; sequence, KV head, first token
   int part_rows, used_rows;                      // rows of a unit there is room for, and at most in use
   int q_head_inner, box_tokens;                  // how a block's rows lie: see attend_row; tokens of a block in shared memory
 };
@@ -109,8 +110,9 @@ class AttendSchedule {
     } else {
       long long total = a_.tiles;
       if (a_.paged) total = paged_total();
-      pos_ = total * cta / a_.n_cta;
-      end_ = total * (cta + 1) / a_.n_cta;
+      const long long n = min(total, (long long)a_.n_cta);     // the last CTAs have nothing to do, so that pieces are neighbours
+      pos_ = cta < n ? total * cta / n : 0;
+      end_ = cta < n ? total * (cta + 1) / n : 0;
       if (pos_ < end_) find(pos_);
     }
   }

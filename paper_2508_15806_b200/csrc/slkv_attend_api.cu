@@ -38,6 +38,7 @@ int check_heads(int n_q_heads, int n_kv_heads, int head_dim, int dtype, int lse_
 
 // What follows from the types and shapes for both kernels: blocks, units, tiles.  max_tokens: of a sequence.
 void set_blocks(AttendShape* a, int dtype, long long max_tokens) {
+  a->ml_unit = dtype == SLKV_F32 ? 1.0f : a->scale * kLog2e;
   if (dtype == SLKV_F32) {
     // few rows: a block of 16, for which a thread has a quarter of the work
     a->part_rows = max_tokens * a->G <= kFmaFewRows ? kFmaFewRows : kFmaRows;
@@ -83,9 +84,9 @@ int check_prompt(const slkv_prompt_params* p, const int32_t* cu_q, const int32_t
                        {&a->k_tok, a->rows_k}, {&a->k_head, a->n_kv_heads}, {&a->v_tok, a->rows_k}, {&a->v_head, a->n_kv_heads}};
   rc = check_axes(axes, 8, p->head_dim, p->dtype);
   if (rc != SLKV_OK) return rc;
+  a->scale = p->scale;
   set_blocks(a, p->dtype, longest);
   if (p->dtype == SLKV_BF16) a->q_head_inner = a->q_head <= a->q_tok;
-  a->scale = p->scale;
   a->lse_unit = p->lse_units == SLKV_LSE_LOG2 ? 1.0f : 0.69314718055994531f;
   // Three units or more for each CTA: whole ones, dealt out; fewer: all tiles in equal shares, pieces joined by another launch.
   long long units = 0;
@@ -155,9 +156,9 @@ int check_paged_attend(const slkv_paged_cache* c, const slkv_paged_attend_params
   rc = check_axes(axes, p->has_new ? 12 : 6, c->head_dim, c->dtype);
   if (rc != SLKV_OK) return rc;
   a->has_new = p->has_new != 0;
+  a->scale = p->scale;
   set_blocks(a, c->dtype, a->n_tokens);
   if (c->dtype == SLKV_BF16) a->q_head_inner = a->q_head <= a->q_tok;
-  a->scale = p->scale;
   a->lse_unit = p->lse_units == SLKV_LSE_LOG2 ? 1.0f : 0.69314718055994531f;
   const long long blocks = (a->n_tokens + a->unit_tokens - 1) / a->unit_tokens, longest = (long long)c->max_pages * c->page_rows;
   const long long most = blocks * a->n_seqs * a->n_kv_heads * ((longest + a->tile_keys - 1) / a->tile_keys + a->has_new);

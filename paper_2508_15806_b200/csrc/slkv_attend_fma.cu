@@ -265,8 +265,8 @@ __global__ void __launch_bounds__(kJoinWarps * 32) k_attend_join(const __grid_co
 #pragma unroll 4
     for (int i = 0; i < n; ++i) {
       const float2 x = a.ml[place(i)];
-      if (x.x == -INFINITY) continue;            // sees nothing there; its outputs may not have been computed
-      const float f = exp2_of(x.x - m);
+      if (x.y == 0.f) continue;                  // sees nothing there; its outputs may not have been computed
+      const float f = exp2_of((x.x - m) * a.ml_unit);
       l = fmaf(x.y, f, l);
       const float* o = a.part + place(i) * D + V * lane;
 #pragma unroll
@@ -281,7 +281,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) k_attend_join(const __grid_co
       if (F32) *reinterpret_cast<float2*>(static_cast<float*>(a.out) + at + e) = make_float2(acc[e] * inv, acc[e + 1] * inv);
       else *reinterpret_cast<__nv_bfloat162*>(static_cast<__nv_bfloat16*>(a.out) + at + e) = __floats2bfloat162_rn(acc[e] * inv, acc[e + 1] * inv);
     }
-    if (lane == 0) attend_lse(a, s, qh, tok, nq, m, l);
+    if (lane == 0) attend_lse(a, s, qh, tok, nq, m * a.ml_unit, l);
   }
 }
 

@@ -1,10 +1,11 @@
 // Attention of prompts and of tokens over a paged cache on the tensor cores, bf16.
 //
-//   out_i = sum_j p_ij v_j,  p_ij = 2^(x_ij - m_i) / sum_j 2^(x_ij - m_i),  x_ij = scale log2(e) q_i . k_j over the keys row i sees
+//   out_i = sum_j p_ij v_j,  p_ij = 2^(sc (x_ij - m_i)) / sum_j 2^(sc (x_ij - m_i)),  x_ij = q_i . k_j over the keys row i sees,
+//   sc = scale log2(e)
 //
 // One pass over the keys with a running reference m and sum per row.  A CTA takes pieces of units (AttendSchedule): two blocks of 128
 // query rows, tokens times the query heads of one KV head, against tiles of 128 keys.  S = Q K^T of a block goes to TMEM (128
-// columns), a warpgroup turns its 128 rows, a row per thread, into P = 2^(x - m) in bf16 over the same columns, and O += P V takes P from
+// columns), a warpgroup turns its 128 rows, a row per thread, into P = 2^(sc (x - m)) in bf16 over the same columns, and O += P V takes P from
 // TMEM as its left operand; while one block's rows are exponentiated the tensor cores work on the other block.  m is raised, and O
 // rescaled in TMEM, only where a tile's maximum lies 2^8 above it.  A unit of one block (few tokens) has its tiles shared by the two
 // warpgroups in turn, each with sums of its own, which are merged in the end.
@@ -400,14 +401,14 @@ __device__ __forceinline__ void softmax_role(const AttendTc& t, Smem<D>& sm, int
           for (int e = 1; e < 31; e += 2) mx[q] = fmaxf(fmaxf(mx[q], __uint_as_float(r[q][e])), __uint_as_float(r[q][e + 1]));
           mx[q] = fmaxf(mx[q], __uint_as_float(r[q][31]));
         }
-        const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * t.sc;
+        const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
         if (i == 0) {
           m = top;
         } else {
-          const bool lift = top > m + kLift;     // m = -infinity: any score lifts it
+          const bool lift = (top - m) * t.sc > kLift;      // m = -infinity: any score lifts it
           if (__any_sync(0xffffffffu, lift)) {
             // the product before this one is done: its commit lies in front of this tile's
-            const float f = lift ? ex2(m - top) : 1.0f;
+            const float f = lift ? ex2((m - top) * t.sc) : 1.0f;
             if (lift) { m = top; l *= f; }
 #pragma unroll 1
             for (int ch = 0; ch < D; ch += 32) {
@@ -420,8 +421,17 @@ __device__ __forceinline__ void softmax_role(const AttendTc& t, Smem<D>& sm, int
             }
           }
         }
-        const float base = m == -INFINITY ? 0.0f : m;
-        const f32x2 nm2 = pack2(-base, -base);
+        // 2^(x - m sc) with one rounding of the difference, which is as large as m sc 2^-24: where that is much, differences first
+        float base = m == -INFINITY ? 0.0f : m;
+        if (__any_sync(0xffffffffu, fabsf(base) * t.sc > 0x1p20f)) {
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+#pragma unroll
+            for (int e = 0; e < 32; ++e) r[q][e] = __float_as_uint(__uint_as_float(r[q][e]) - base);
+          base = 0.0f;
+        }
+        const float nm = -base * t.sc;
+        const f32x2 nm2 = pack2(nm, nm);
         f32x2 s0 = 0, s1 = 0;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
@@ -473,8 +483,8 @@ __device__ __forceinline__ void softmax_role(const AttendTc& t, Smem<D>& sm, int
       tc_fence_after();
       const float2 x = sm.ml[0][tid], y = sm.ml[1][tid];
       m = fmaxf(x.x, y.x);
-      f0 = x.x == -INFINITY ? 0.0f : ex2(x.x - m);
-      f1 = y.x == -INFINITY ? 0.0f : ex2(y.x - m);
+      f0 = x.y == 0.0f ? 0.0f : ex2((x.x - m) * t.sc);
+      f1 = y.y == 0.0f ? 0.0f : ex2((y.x - m) * t.sc);
       l = x.y * f0 + y.y * f1;
       o_at = lanes + kTmemO;
       ch0 = g * (D / 2);
@@ -533,7 +543,7 @@ __device__ __forceinline__ void softmax_role(const AttendTc& t, Smem<D>& sm, int
         if (!whole) {
           a.ml[place] = make_float2(m, l);
         } else {
-          attend_lse(a, p.s, p.h * a.G + rh, tok, p.n_seq_tok, m, l);
+          attend_lse(a, p.s, p.h * a.G + rh, tok, p.n_seq_tok, m * t.sc, l);
         }
       }
     }
@@ -674,7 +684,7 @@ cudaError_t launch_attend_tensor(const AttendShape& a, cudaStream_t st, int* lau
   AttendTc t = {};
   AttendMaps m = {};
   t.a = a;
-  t.sc = a.scale * kLog2e;
+  t.sc = a.ml_unit;
   t.arrivals = take_expire_next_copy_wait() ? 5 : 4;
   t.a.box_tokens = a.paged && a.n_tokens < a.block_tokens ? a.n_tokens : a.block_tokens;
   cudaError_t e = encode_rows(&m.q, a.q, a.head_dim, a.n_q_heads, a.paged ? a.n_tokens : a.rows_q, a.paged ? a.n_seqs : 1, a.q_head,

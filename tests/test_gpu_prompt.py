@@ -57,3 +57,205 @@ def run(nq, nk=None, hkv=2, G=4, d=128, dtype="bf16", window=32, scale=None, log
 @pytest.mark.parametrize("nq", [[1], [5], [32], [33], [64], [65], [129], [300], [1, 0, 64, 129, 0, 31]])
 def test_lengths(nq, d, dtype):
     run(nq, d=d, dtype=dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("G", [1, 2, 3, 5, 8, 16, 48, 64])
+def test_groups(G, dtype):
+    run([70, 3, 140], hkv=2, G=G, dtype=dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("nq,nk", [([1], [1000]), ([1, 40, 100], [700, 41, 100]), ([200], [1500]), ([7, 64], [2500, 65])])
+def test_chunks(nq, nk, dtype):
+    """Queries behind keys that were there already; few units, whose tiles several CTAs share."""
+    run(nq, nk, dtype=dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("nq,nk", [([50], [0]), ([50], [20]), ([300, 10, 300], [150, 0, 5])])
+def test_queries_that_see_nothing(nq, nk, dtype):
+    run(nq, nk, dtype=dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_many_units(dtype):
+    """Whole units dealt out, the longest first, several of one CTA."""
+    run([1500, 1, 700, 0, 2300, 64], hkv=8, G=8 if dtype == "bf16" else 4, d=64, dtype=dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_many_sequences(dtype):
+    run([1 + 7 * i % 90 for i in range(150)], hkv=2, G=2, dtype=dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_heads_before_tokens(dtype):
+    """[heads, tokens, head_dim] in memory: strides in the other order."""
+    run([130, 33], dtype=dtype, heads_first=True)
+    run([9], [600], dtype=dtype, heads_first=True)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_inside_wider_ones(dtype):
+    """q, k, v are parts of one projection's output, out of a wider buffer."""
+    g = torch.Generator(device="cuda").manual_seed(3)
+    n, hkv, G, d = 77, 2, 3, 64
+    qkv = torch.randn(n, hkv * (G + 2), d, device="cuda", generator=g).to(DT[dtype])
+    q, k, v = qkv[:, :hkv * G], qkv[:, hkv * G:hkv * (G + 1)], qkv[:, hkv * (G + 1):]
+    wide = torch.full((n, hkv * G, 2 * d), 7.0, dtype=q.dtype, device="cuda")
+    out, lse, before = attend(q, k, v, [n], out=wide[:, :, :d])
+    R.check_prompt(q, k, v, [0, n], [0, n], out, lse, 32, d ** -0.5, before, torch.full_like(lse, 5.0))
+    assert (wide[:, :, d:] == 7.0).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+def test_values_that_are_not_finite(bad, dtype):
+    """K and V at a position reach the queries from there on and no other, in every sequence; what lies behind the last sequence
+    reaches nobody."""
+    nq = [200, 70, 333]
+    q, k, v = inputs(nq, nq, 2, 4, 128, dtype, seed=5)
+    for pos in (0 + 150, 200 + 69, 270 + 40, 270 + 41, 270 + 300):
+        v[pos, 0, 5] = bad
+        v[pos, 1, 100] = -bad
+    k[sum(nq):], v[sum(nq):] = bad, bad
+    k[270 + 332, 1] = float("nan")                                # the last key of a sequence: only its last query sees it
+    out, lse, before = attend(q, k, v, nq)
+    kk = k.clone()
+    kk[270 + 332, 1] = 0.0
+    for s, (a, n) in enumerate(zip(cu(nq), nq)):
+        for h in range(8):
+            upto = n - 1 if s == 2 and h >= 4 else n
+            ref = R.rows(q[a:a + n, h], kk[a:a + n, h // 4], v[a:a + n, h // 4], R.causal(n, n, "cuda"), 128 ** -0.5)
+            R.check(out[a:a + upto, h], None, tuple(x[:upto] for x in ref), dtype == "bf16", 128)
+            assert upto == n or torch.isnan(out[a + upto, h]).all()
+    assert torch.equal(out[sum(nq):], before[sum(nq):])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_values_that_are_not_finite_in_shared_units(dtype):
+    """The same where several CTAs share a unit, and where two warpgroups share its tiles."""
+    for nq, nk in (([60], [1400]), ([20], [900]), ([3], [700])):
+        q, k, v = inputs(nq, nk, 1, 4, 128, dtype, seed=6)
+        for back in (1, 3, 19):
+            if back <= nq[0]:
+                v[nk[0] - back, 0, 7] = float("inf")
+        v[100, 0, 9] = float("nan")
+        out, lse, before = attend(q, k, v, nq, nk)
+        R.check_prompt(q, k, v, cu(nq), cu(nk), out, lse, 32, 128 ** -0.5, before, torch.full_like(lse, 5.0))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_scores_that_rise_and_fall(dtype):
+    """Maxima that come late, early and far apart: the running reference is raised again and again, or never."""
+    for order in (1, -1):
+        nq = [700]
+        q, k, v = inputs(nq, nq, 1, 4, 64, dtype, seed=7)
+        q.copy_(torch.ones_like(q))
+        ramp = torch.linspace(-3.0, 3.0, k.shape[0], device="cuda") * order
+        k.copy_(ramp[:, None, None].expand(k.shape).to(k.dtype))
+        out, lse, before = attend(q, k, v, nq, scale=1.0)
+        R.check_prompt(q, k, v, cu(nq), cu(nq), out, lse, 32, 1.0, before, torch.full_like(lse, 5.0))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_scores_at_the_limits(dtype):
+    """Scores of 2^120 and differences that leave one key per row; scale at its ends."""
+    nq = [150]
+    for factor, scale in ((2.0 ** 60, 1.0), (2.0 ** 40, 2.0 ** 40), (1.0, 2.0 ** -54), (2.0 ** 30, 2.0 ** -54), (2.0 ** 10, 2.0 ** 54)):
+        q, k, v = inputs(nq, nq, 1, 2, 64, dtype, seed=8)
+        q.zero_(), k.zero_()
+        i = torch.arange(k.shape[0], device="cuda")
+        q[:, :, 0] = factor
+        k[:, 0, 0] = (factor * (1 + (i * 37) % 101)).to(k.dtype) if factor < 2.0 ** 50 else factor * (2.0 ** (i % 4).float()).to(k.dtype)
+        out, lse, before = attend(q, k, v, nq, scale=scale)
+        R.check_prompt(q, k, v, cu(nq), cu(nq), out, lse, 32, scale, before, torch.full_like(lse, 5.0))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_window_and_units(dtype):
+    for window in (1, 33, 200):
+        run([150, 20], window=window, dtype=dtype, log2=window == 33)
+
+
+def test_the_same_again_and_without_lse():
+    nq, nk = [33, 500], [1200, 500]
+    q, k, v = inputs(nq, nk, 2, 4, 128, "bf16", seed=9)
+    first = attend(q, k, v, nq, nk)
+    for _ in range(3):
+        again = attend(q, k, v, nq, nk)
+        assert torch.equal(again[0], first[0]) and torch.equal(again[1], first[1])
+    p = B.make_prompt(q, k, v, first[0], 2)
+    c_q, c_k = cu(nq), cu(nk)
+    out = torch.zeros_like(q)
+    ws = B.new_prompt_workspace(p, c_q, c_k)
+    B.slkv_prompt_attend(p, q, k, v, torch.tensor(c_q, dtype=torch.int32, device="cuda"), tuple(c_q), out, ws,
+                         cu_k=torch.tensor(c_k, dtype=torch.int32, device="cuda"), cu_k_host=tuple(c_k))
+    assert torch.equal(out[:sum(nq)], first[0][:sum(nq)])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_captured_and_on_another_stream(dtype):
+    nq, nk = [40, 100], [900, 100]
+    q, k, v = inputs(nq, nk, 2, 4, 128, dtype, seed=10)
+    want = attend(q, k, v, nq, nk)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        got = attend(q, k, v, nq, nk)
+    torch.cuda.synchronize()
+    got_too = attend(q, k, v, nq, nk, stream=torch.cuda.current_stream())
+    assert torch.equal(got_too[0], want[0])
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    c_q, c_k = cu(nq), cu(nk)
+    dq, dk = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in (c_q, c_k))
+    out, lse = torch.zeros_like(q), torch.full_like(want[1], 5.0)
+    p = B.make_prompt(q, k, v, out, 2, window=32)
+    ws = B.new_prompt_workspace(p, c_q, c_k)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        B.slkv_prompt_attend(p, q, k, v, dq, c_q, out, ws, cu_k=dk, cu_k_host=c_k, lse=lse)
+    for _ in range(2):
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out[:sum(nq)], want[0][:sum(nq)]) and torch.equal(lse, want[1])
+
+
+def test_compression_takes_the_log_sum_exp():
+    """prompt -> its window rows' log-sum-exp -> slkv_score: the scores that slkv_score computes by itself over the same softmax."""
+    nq, hkv, G, d, w = [900, 1300], 4, 4, 128, 32
+    q, k, v = inputs(nq, nq, hkv, G, d, "bf16", seed=11, behind=0)
+    out, lse, _ = attend(q, k, v, nq, window=w)
+    c = cu(nq)
+    q_win = torch.stack([q[e - w:e] for e in c[1:]])
+    params = B.make_params(q_win, k, v, w, 7, softmax_domain=B.SLKV_ALL_CAUSAL)
+    dev = torch.tensor(c, dtype=torch.int32, device="cuda")
+    pooled = []
+    for given in (None, lse):
+        x = torch.zeros(B.slkv_pooled_elems(params, c), device="cuda")
+        ws = torch.empty(B.slkv_workspace_bytes(params, c), dtype=torch.uint8, device="cuda")
+        B.slkv_score(params, q_win, k, dev, c, x, ws, lse=given)
+        pooled.append(x)
+    # slkv_score's own bound (10^-3 of the value), and the log-sum-exp's 2^-20
+    assert ((pooled[0] - pooled[1]).abs() <= 2e-3 * pooled[0].abs() + 1e-30).all()
+
+
+def test_a_wait_that_runs_out():
+    q, k, v = inputs([300], [300], 1, 4, 128, "bf16", seed=12)
+    p = B.make_prompt(q, k, v, torch.zeros_like(q), 1)
+    out, status = torch.full_like(q, 7.0), torch.zeros(1, dtype=torch.int32, device="cuda")
+    c = torch.tensor([0, 300], dtype=torch.int32, device="cuda")
+    ws = B.new_prompt_workspace(p, [0, 300])
+    B.slkv_debug_expire_next_wait(5)
+    B.slkv_prompt_attend(p, q, k, v, c, [0, 300], out, ws, status=status)
+    torch.cuda.synchronize()
+    assert int(status) == B.ERR["DEVICE_TIMEOUT"]
+    good, _, _ = attend(q, k, v, [300])
+    got = out[:300]
+    fine = (got == good[:300]) | (got == 7.0) | torch.isnan(got)      # computed, left as it was, or NaN
+    assert fine.all() and not torch.equal(got, good[:300])
+    status.zero_()
+    B.slkv_prompt_attend(p, q, k, v, c, [0, 300], out, ws, status=status)
+    torch.cuda.synchronize()
+    assert int(status) == 0 and torch.equal(out[:300], good[:300])
