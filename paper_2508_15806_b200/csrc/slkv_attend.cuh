@@ -42,12 +42,11 @@ struct AttendShape {
   int spread;                                    // 1: whole units in turn, the longest first; 0: every CTA as many tiles as the others
   int n_cta;
   int levels;                                    // spread: blocks of the longest sequence
-  long long tiles;                               // prompt, not spread: tiles of all units (a unit without any counts one)
   // partial results of units that several CTAs share
   float* part;                                   // [n_cta][2][rows][head_dim]
   float2* ml;                                    // [n_cta][2][rows]
   float ml_unit;                                 // times a reference in ml: log2 units
-  int4* desc;                                    // [n_cta][2]: 1 a piece, 2 one that ends its unit, -1 one that failed; sequence, KV head, first token
+  struct AttendPart* desc;                       // [n_cta][2]
   int part_rows, used_rows;                      // rows of a unit there is room for, and at most in use
   int q_head_inner, box_tokens;                  // how a block's rows lie: see attend_row; tokens of a block in shared memory
 };
@@ -97,26 +96,68 @@ __device__ __forceinline__ void attend_lse(const AttendShape& a, int s, int qh, 
 //   spread       whole units, to the CTAs in turn and back (0 .. n - 1, n - 1 .. 0, ..), the ones with the most tiles of their
 //                sequence first: shares differ by about the last units, which are short, and CTAs that run beside each other read the
 //                same keys
-//   not spread   the tiles of all units in one row, cut into n_cta equal shares: for few units.  A unit without tiles counts one.
+//   not spread   the tiles of all units in one row, cut into equal shares: for few units.  A unit without tiles counts one.
+// The first piece is what a launch waits for, so the search for it is short: 32-bit arithmetic, a run of groups per lane, two scans.
 class AttendSchedule {
  public:
-  __device__ AttendSchedule(const AttendShape& a, int cta) : a_(a), cta_(cta), lane_(threadIdx.x & 31) {
+  __device__ __forceinline__ AttendSchedule(const AttendShape& a, int cta) : a_(a), cta_(cta), lane_(threadIdx.x & 31) {
     if (a_.spread) {
       item_ = cta;
       round_ = 0;
       level_ = a_.levels - 1;
       base_ = 0;
       count_ = level_count(level_);
+      return;
+    }
+    // runs of segments (paged) or sequences (prompt), one per lane
+    const int n = a_.paged ? a_.n_seqs * a_.n_kv_heads : a_.n_seqs, per = (n + 31) / 32;
+    int sum = 0;
+#pragma unroll 4
+    for (int i = 0; i < per; ++i) sum += weight(lane_ * per + i, n);
+    int incl = scan(sum);
+    const int total = __shfl_sync(0xffffffffu, incl, 31);
+    // the first `more` CTAs have each + 1 tiles, the others each; where there are fewer tiles than CTAs the last ones have none
+    const int each = total / a_.n_cta, more = total - each * a_.n_cta;
+    pos_ = each * cta + min(cta, more);
+    end_ = pos_ + each + (cta < more);
+    if (pos_ >= end_) return;
+    share_ = each;
+    more_ = more;
+    int at = __ffs(__ballot_sync(0xffffffffu, incl > pos_)) - 1;
+    int before = __shfl_sync(0xffffffffu, incl - sum, at), first = at * per;
+    const int stop = min(first + per, n);
+    for (;; first += 32) {                       // the run's groups
+      const int w = first + lane_ < stop ? weight(first + lane_, n) : 0;
+      incl = scan(w);
+      const unsigned m = __ballot_sync(0xffffffffu, before + incl > pos_);
+      if (m) {
+        at = __ffs(m) - 1;
+        before += __shfl_sync(0xffffffffu, incl - w, at);
+        first += at;
+        break;
+      }
+      before += __shfl_sync(0xffffffffu, incl, 31);
+      if (first + 32 >= stop) { pos_ = end_; return; }         // lengths on the device that are not the host's
+    }
+    group_ = before;
+    if (a_.paged) {
+      s_ = first / a_.n_kv_heads;
+      x_ = first - s_ * a_.n_kv_heads;
+      load_group();
     } else {
-      long long total = a_.tiles;
-      if (a_.paged) total = paged_total();
-      const long long n = min(total, (long long)a_.n_cta);     // the last CTAs have nothing to do, so that pieces are neighbours
-      pos_ = cta < n ? total * cta / n : 0;
-      end_ = cta < n ? total * (cta + 1) / n : 0;
-      if (pos_ < end_) find(pos_);
+      s_ = first;
+      x_ = 0;
+      load_group();
+      while (pos_ >= group_ + inner_ * each_) {
+        group_ += inner_ * each_;
+        ++x_;
+        load_group();
+      }
     }
   }
-  __device__ bool next(AttendPiece* p) { return a_.spread ? next_spread(p) : next_share(p); }
+  __device__ __forceinline__ bool next(AttendPiece* p) { return a_.spread ? next_spread(p) : next_share(p); }
+  // Of the piece at hand, one of several: how many pieces its unit has.
+  __device__ __forceinline__ int pieces() const { return cta_of(unit_ + each_ - 1) - cta_of(unit_) + 1; }
 
  private:
   const AttendShape& a_;
@@ -125,26 +166,51 @@ class AttendSchedule {
   long long item_, base_, count_;
   int level_, round_;
   // shares: the group of units with the same tiles (prompt: a block of tokens, all KV heads; paged: a segment, all blocks)
-  long long pos_, end_, group_;  // group_: first position of the group
+  int pos_, end_, group_;        // group_: first position of the group
   int s_, x_;                    // sequence; prompt: block of tokens, paged: KV head
   int inner_, each_;             // units of the group, tiles counted for each
+  int unit_;                     // first position of the unit at hand
+  int share_, more_;
 
-  __device__ int seq_tokens(int s) const {
-    if (!a_.paged) return max(__ldg(a_.cu_q + s + 1) - __ldg(a_.cu_q + s), 0);
+  __device__ __forceinline__ int cta_of(int pos) const {
+    const int big = more_ * (share_ + 1);
+    return pos < big ? pos / (share_ + 1) : more_ + (pos - big) / max(share_, 1);
+  }
+  __device__ __forceinline__ int scan(int v) const {
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int o = __shfl_up_sync(0xffffffffu, v, d);
+      if (lane_ >= d) v += o;
+    }
+    return v;
+  }
+  __device__ __forceinline__ int seq_tokens(int s) const {
+    if (!a_.paged) return max(a_.cu_q[s + 1] - a_.cu_q[s], 0);
     return a_.n_new ? min(max(a_.n_new[s], 0), a_.n_tokens) : a_.n_tokens;
   }
-  __device__ int seq_keys(int s) const { return max(__ldg(a_.cu_k + s + 1) - __ldg(a_.cu_k + s), 0); }
-  __device__ int blocks(int tokens) const { return (tokens + a_.unit_tokens - 1) / a_.unit_tokens; }
-  __device__ int rows_of(int seg) const { return (int)min((long long)max(a_.lens[seg], 0), (long long)a_.max_pages * a_.page_rows); }
+  __device__ __forceinline__ int seq_keys(int s) const { return max(a_.cu_k[s + 1] - a_.cu_k[s], 0); }
+  __device__ __forceinline__ int blocks(int tokens) const {
+    return tokens <= a_.unit_tokens ? tokens > 0 : (tokens + a_.unit_tokens - 1) / a_.unit_tokens;
+  }
+  __device__ __forceinline__ int rows_of(int seg) const { return min(max(a_.lens[seg], 0), a_.max_pages * a_.page_rows); }
   // Tiles of a unit.
-  __device__ int prompt_tiles(int nq, int nk, int t) const {
+  __device__ __forceinline__ int prompt_tiles(int nq, int nk, int t) const {
     const int seen = min(nq, (t + 1) * a_.unit_tokens) + nk - nq;
     return seen <= 0 ? 0 : (seen + a_.tile_keys - 1) / a_.tile_keys;
   }
-  __device__ int paged_tiles(int rows) const { return (rows + a_.tile_keys - 1) / a_.tile_keys + a_.has_new; }
+  __device__ __forceinline__ int paged_tiles(int rows) const { return (rows + a_.tile_keys - 1) / a_.tile_keys + a_.has_new; }
+  // Tiles of a segment's or a sequence's units.
+  __device__ __forceinline__ int weight(int i, int n) const {
+    if (i >= n) return 0;
+    if (a_.paged) return blocks(seq_tokens(i / a_.n_kv_heads)) * max(paged_tiles(rows_of(i)), 1);
+    const int nq = seq_tokens(i), nk = seq_keys(i), nb = blocks(nq);
+    int sum = 0;
+    for (int t = 0; t < nb; ++t) sum += max(prompt_tiles(nq, nk, t), 1);
+    return sum * a_.n_kv_heads;
+  }
 
   // ---- spread
-  __device__ long long level_count(int t) const {
+  __device__ __forceinline__ long long level_count(int t) const {
     int n = 0;
     for (int s0 = 0; s0 < a_.n_seqs; s0 += 32) {
       const int s = s0 + lane_;
@@ -152,14 +218,15 @@ class AttendSchedule {
     }
     return (long long)n * a_.n_kv_heads;
   }
-  __device__ bool next_spread(AttendPiece* p) {
+  __device__ __forceinline__ bool next_spread(AttendPiece* p) {
     while (level_ >= 0 && item_ >= base_ + count_) {
       base_ += count_;
       if (--level_ >= 0) count_ = level_count(level_);
     }
     if (level_ < 0) return false;
-    int nth = (int)((item_ - base_) / a_.n_kv_heads);
-    const int h = (int)((item_ - base_) - (long long)nth * a_.n_kv_heads);
+    const unsigned rel = (unsigned)(item_ - base_);            // fewer than 2^31 sequences times heads
+    int nth = (int)(rel / (unsigned)a_.n_kv_heads);
+    const int h = (int)(rel - (unsigned)nth * (unsigned)a_.n_kv_heads);
     int s = 0;
     for (int s0 = 0; s0 < a_.n_seqs; s0 += 32) {
       unsigned m = __ballot_sync(0xffffffffu, s0 + lane_ < a_.n_seqs && blocks(seq_tokens(s0 + lane_)) > level_);
@@ -181,17 +248,7 @@ class AttendSchedule {
   }
 
   // ---- equal shares
-  __device__ long long paged_total() const {
-    const int n_seg = a_.n_seqs * a_.n_kv_heads;
-    long long sum = 0;
-#pragma unroll 4
-    for (int seg = lane_; seg < n_seg; seg += 32)
-      sum += (long long)blocks(seq_tokens(seg / a_.n_kv_heads)) * max(paged_tiles(rows_of(seg)), 1);
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-    return sum;
-  }
-  __device__ void load_group() {
+  __device__ __forceinline__ void load_group() {
     if (a_.paged) {
       inner_ = blocks(seq_tokens(s_));
       each_ = max(paged_tiles(rows_of(s_ * a_.n_kv_heads + x_)), 1);
@@ -201,69 +258,17 @@ class AttendSchedule {
       each_ = max(prompt_tiles(nq, seq_keys(s_), x_), 1);
     }
   }
-  __device__ void advance() {
-    const int last = a_.paged ? a_.n_kv_heads : blocks(seq_tokens(s_));
-    if (++x_ >= last) { x_ = 0; ++s_; }
-  }
-  // The group that holds position pos, which exists: 32 groups at a time.
-  __device__ void find(long long pos) {
-    long long before = 0;
-    s_ = x_ = 0;
-    if (a_.paged) {
-      const int n_seg = a_.n_seqs * a_.n_kv_heads;
-      for (int g0 = 0; g0 < n_seg; g0 += 32) {
-        const int g = g0 + lane_;
-        long long w = 0;
-        if (g < n_seg) w = (long long)blocks(seq_tokens(g / a_.n_kv_heads)) * max(paged_tiles(rows_of(g)), 1);
-        if (locate(pos, w, &before, g0)) {
-          s_ = found_ / a_.n_kv_heads;
-          x_ = found_ - s_ * a_.n_kv_heads;
-          break;
-        }
-      }
-    } else {
-      bool found = false;
-      for (int s = 0; s < a_.n_seqs && !found; ++s) {
-        const int nq = seq_tokens(s), nk = seq_keys(s), n = blocks(nq);
-        for (int t0 = 0; t0 < n && !found; t0 += 32) {
-          const int t = t0 + lane_;
-          const long long w = t < n ? (long long)a_.n_kv_heads * max(prompt_tiles(nq, nk, t), 1) : 0;
-          if (locate(pos, w, &before, t0)) { s_ = s; x_ = found_; found = true; }
-        }
-      }
-    }
-    group_ = before;
-    load_group();
-  }
-  int found_;
-  // Of 32 weights: is pos behind `before` inside them?  If so found_ is the index, and before what lies in front of it.
-  __device__ bool locate(long long pos, long long w, long long* before, int first) {
-    long long incl = w;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-      const long long o = __shfl_up_sync(0xffffffffu, incl, d);
-      if (lane_ >= d) incl += o;
-    }
-    const unsigned m = __ballot_sync(0xffffffffu, *before + incl > pos);
-    if (m == 0) {
-      *before += __shfl_sync(0xffffffffu, incl, 31);
-      return false;
-    }
-    const int at = __ffs(m) - 1;
-    *before += __shfl_sync(0xffffffffu, incl - w, at);
-    found_ = first + at;
-    return true;
-  }
-  __device__ bool next_share(AttendPiece* p) {
+  __device__ __forceinline__ bool next_share(AttendPiece* p) {
     if (pos_ >= end_) return false;
-    while (pos_ >= group_ + (long long)inner_ * each_) {
-      group_ += (long long)inner_ * each_;
-      advance();
+    while (pos_ >= group_ + inner_ * each_) {
+      group_ += inner_ * each_;
+      if (++x_ >= (a_.paged ? a_.n_kv_heads : blocks(seq_tokens(s_)))) { x_ = 0; ++s_; }
       if (s_ >= a_.n_seqs) return false;                       // lengths on the device that are not the host's
       load_group();
     }
-    const int rel = (int)(pos_ - group_), unit = rel / each_, tile0 = rel - unit * each_;
-    const int take = (int)min((long long)(each_ - tile0), end_ - pos_);
+    const int rel = pos_ - group_, unit = rel / each_, tile0 = rel - unit * each_;
+    const int take = min(each_ - tile0, end_ - pos_);
+    unit_ = pos_ - tile0;
     if (a_.paged) fill(p, s_, x_, unit);
     else fill(p, s_, unit, x_);
     p->tile0 = tile0;
@@ -272,7 +277,7 @@ class AttendSchedule {
     pos_ += take;
     return true;
   }
-  __device__ void fill(AttendPiece* p, int s, int h, int t) const {
+  __device__ __forceinline__ void fill(AttendPiece* p, int s, int h, int t) const {
     p->s = s;
     p->h = h;
     const int nq = seq_tokens(s);
@@ -286,13 +291,23 @@ class AttendSchedule {
     } else {
       p->nk = seq_keys(s);
       p->shift = p->nk - nq;
-      p->q_row = __ldg(a_.cu_q + s);
-      p->k_row = __ldg(a_.cu_k + s);
+      p->q_row = a_.cu_q[s];
+      p->k_row = a_.cu_k[s];
       p->n_all = prompt_tiles(nq, p->nk, t);
     }
     p->stop = 0;
   }
 };
+// What the joining launch needs to know of a CTA's pieces: state 0: none, 1: a piece, -1: one that failed; of a unit's first piece
+// all the rest.
+struct AttendPart {
+  int state, pieces, s, h, tok0, n_tok, n_seq_tok, q_row;
+};
+__device__ __forceinline__ void attend_note(const AttendShape& a, int slot, const AttendPiece& p, int pieces) {
+  int4* to = reinterpret_cast<int4*>(a.desc + 2 * blockIdx.x + slot);
+  to[0] = make_int4(1, pieces, p.s, p.h);
+  to[1] = make_int4(p.tok0, p.n_tok, p.n_seq_tok, p.q_row);
+}
 #endif
 
 }  // namespace slkv

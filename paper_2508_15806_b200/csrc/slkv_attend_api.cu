@@ -95,19 +95,19 @@ int check_prompt(const slkv_prompt_params* p, const int32_t* cu_q, const int32_t
   a->levels = (int)((longest + a->unit_tokens - 1) / a->unit_tokens);
   a->spread = units >= 3ll * a->n_cta;
   if (!a->spread) {
-    long long most = 0;
+    long long most = 0, tiles = 0;
     for (int s = 0; s < p->n_seqs; ++s) {
       const int nq = cu_q[s + 1] - cu_q[s], nk = cu_k[s + 1] - cu_k[s];
       for (int t = 0; t * a->unit_tokens < nq; ++t) {
         const int end = (t + 1) * a->unit_tokens < nq ? (t + 1) * a->unit_tokens : nq, seen = end + nk - nq;
         const long long n = seen > 0 ? (seen + a->tile_keys - 1) / a->tile_keys : 1;
-        a->tiles += n * p->n_kv_heads;
+        tiles += n * p->n_kv_heads;
         if (n > most) most = n;
       }
     }
     // units that are short all the same
-    if (units > 0 && most <= 2) a->spread = 1;
-    if (!a->spread && a->tiles < a->n_cta) a->n_cta = (int)a->tiles;
+    if (units > 0 && (most <= 2 || tiles >= (1ll << 31))) a->spread = 1;
+    if (!a->spread && tiles < a->n_cta) a->n_cta = (int)tiles;
   }
   if (a->spread && units < a->n_cta) a->n_cta = (int)(units > 0 ? units : 1);
   return SLKV_OK;
@@ -162,6 +162,7 @@ int check_paged_attend(const slkv_paged_cache* c, const slkv_paged_attend_params
   a->lse_unit = p->lse_units == SLKV_LSE_LOG2 ? 1.0f : 0.69314718055994531f;
   const long long blocks = (a->n_tokens + a->unit_tokens - 1) / a->unit_tokens, longest = (long long)c->max_pages * c->page_rows;
   const long long most = blocks * a->n_seqs * a->n_kv_heads * ((longest + a->tile_keys - 1) / a->tile_keys + a->has_new);
+  if (most >= (1ll << 31)) return SLKV_ERR_BAD_SHAPE;      // tiles are counted in 32 bits
   if (most < a->n_cta) a->n_cta = (int)most;
   return SLKV_OK;
 }

@@ -42,14 +42,13 @@ k_attend_fma(const __grid_constant__ AttendShape a) {
   const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
   pdl_launch_dependents();
   pdl_wait();
-  if (tid == 0 && !a.spread) a.desc[2 * blockIdx.x] = a.desc[2 * blockIdx.x + 1] = make_int4(0, 0, 0, 0);
+  if (tid == 0 && !a.spread) a.desc[2 * blockIdx.x].state = a.desc[2 * blockIdx.x + 1].state = 0;
   AttendSchedule plan(a, blockIdx.x);            // every warp runs it
   const float sc = a.scale * kLog2e;
   for (;;) {
     AttendPiece p = {};
     if (!plan.next(&p)) break;
-    if (tid == 0 && p.part >= 0)
-      a.desc[2 * blockIdx.x + p.part] = make_int4(p.tile0 + max(p.n, 1) == max(p.n_all, 1) ? 2 : 1, p.s, p.h, p.tok0);
+    if (tid == 0 && p.part >= 0) attend_note(a, p.part, p, p.part == 1 ? plan.pieces() : 0);
     // row r: token r / G of the unit, query head r % G of the group
     const int rows = p.n_tok * a.G;
     const float* qb = static_cast<const float*>(a.q) + (a.paged ? p.s * a.q_seq : p.q_row * a.q_tok);
@@ -224,53 +223,47 @@ k_attend_fma(const __grid_constant__ AttendShape a) {
   }
 }
 
-// One CTA's unit that goes on in the next ones: the pieces' outputs by their references, a warp a row.
-constexpr int kJoinWarps = 8, kJoinRows = 32;    // rows of a block
+// One CTA's unit that goes on in the next ones: the pieces' outputs by their references, a warp a row.  What bounds it is latency: what
+// the pieces are, then their references and outputs, all at once.
+constexpr int kJoinWarps = 8, kJoinRows = 16;    // rows of a block
 template <int D, bool F32>
 __global__ void __launch_bounds__(kJoinWarps * 32) k_attend_join(const __grid_constant__ AttendShape a) {
   pdl_launch_dependents();
   pdl_wait();
   const int cta = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int4 first = a.desc[2 * cta + 1];
-  if (first.x != 1) return;
-  const int s = first.y, h = first.z, tok0 = first.w;
-  int n = 1;
-  bool failed = true;                            // until the piece that ends the unit is found
-  for (; cta + n < a.n_cta; ++n) {
-    const int x = a.desc[2 * (cta + n)].x;
-    if (x == 2) { failed = false; ++n; break; }
-    if (x != 1) break;
-  }
-  int nq, q_row = 0;
-  if (a.paged) {
-    nq = a.n_new ? min(max(a.n_new[s], 0), a.n_tokens) : a.n_tokens;
-  } else {
-    q_row = a.cu_q[s];
-    nq = a.cu_q[s + 1] - q_row;
-  }
-  const int n_tok = min(a.unit_tokens, nq - tok0);
+  const int4* note = reinterpret_cast<const int4*>(a.desc + 2 * cta + 1);
+  const int4 x0 = note[0], x1 = note[1];
+  if (x0.x != 1) return;
+  const int n = x0.y, s = x0.z, h = x0.w, tok0 = x1.x, n_tok = x1.y, n_seq_tok = x1.z, q_row = x1.w;
+  constexpr int V = D / 32;
   for (int r = blockIdx.y * kJoinRows + warp; r < (blockIdx.y + 1) * kJoinRows && r < a.part_rows; r += kJoinWarps) {
     int tok, hh;
     if (!attend_row(a, r, &tok, &hh) || tok >= n_tok) continue;
     tok += tok0;
     auto place = [&](int i) { return (long long)(i == 0 ? 2 * cta + 1 : 2 * (cta + i)) * a.part_rows + r; };
     float m = -INFINITY;
-    for (int i = lane; i < n; i += 32) m = fmaxf(m, a.ml[place(i)].x);
+    bool failed = false;
+    for (int i = lane; i < n; i += 32) {
+      m = fmaxf(m, a.ml[place(i)].x);
+      failed |= i > 0 && a.desc[2 * (cta + i)].state != 1;
+    }
+    failed = __any_sync(0xffffffffu, failed);
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-    constexpr int V = D / 32;
     float acc[V], l = 0.f;
 #pragma unroll
     for (int e = 0; e < V; ++e) acc[e] = 0.f;
-#pragma unroll 4
+#pragma unroll 8
     for (int i = 0; i < n; ++i) {
       const float2 x = a.ml[place(i)];
-      if (x.y == 0.f) continue;                  // sees nothing there; its outputs may not have been computed
-      const float f = exp2_of((x.x - m) * a.ml_unit);
-      l = fmaf(x.y, f, l);
-      const float* o = a.part + place(i) * D + V * lane;
+      float o[V];
 #pragma unroll
-      for (int e = 0; e < V; ++e) acc[e] = fmaf(o[e], f, acc[e]);
+      for (int e = 0; e < V; e += 2) *reinterpret_cast<float2*>(o + e) = *reinterpret_cast<const float2*>(a.part + place(i) * D + V * lane + e);
+      const bool some = x.y != 0.f;              // else nothing is seen there, and outputs may not have been computed
+      const float f = some ? exp2_of((x.x - m) * a.ml_unit) : 0.f;
+      l = fmaf(x.y, f, l);
+#pragma unroll
+      for (int e = 0; e < V; ++e) acc[e] = some ? fmaf(o[e], f, acc[e]) : acc[e];
     }
     float inv = l > 0.f || l != l ? 1.f / l : 0.f;
     if (failed) inv = l = __int_as_float(0x7fffffff);
@@ -281,7 +274,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) k_attend_join(const __grid_co
       if (F32) *reinterpret_cast<float2*>(static_cast<float*>(a.out) + at + e) = make_float2(acc[e] * inv, acc[e + 1] * inv);
       else *reinterpret_cast<__nv_bfloat162*>(static_cast<__nv_bfloat16*>(a.out) + at + e) = __floats2bfloat162_rn(acc[e] * inv, acc[e + 1] * inv);
     }
-    if (lane == 0) attend_lse(a, s, qh, tok, nq, m * a.ml_unit, l);
+    if (lane == 0) attend_lse(a, s, qh, tok, n_seq_tok, m * a.ml_unit, l);
   }
 }
 
@@ -321,7 +314,7 @@ int attend_fma_ctas() { return kFmaPerSm * sm_count(); }
 static size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 size_t attend_workspace(int n_cta, int part_rows, int head_dim) {
   const size_t places = 2 * (size_t)n_cta * part_rows;
-  return up256(places * head_dim * sizeof(float)) + up256(places * sizeof(float2)) + up256(2 * n_cta * sizeof(int4));
+  return up256(places * head_dim * sizeof(float)) + up256(places * sizeof(float2)) + up256(2 * n_cta * sizeof(AttendPart));
 }
 void attend_bind(AttendShape* a, void* workspace) {
   const size_t places = 2 * (size_t)a->n_cta * a->part_rows;
@@ -330,7 +323,7 @@ void attend_bind(AttendShape* a, void* workspace) {
   w += up256(places * a->head_dim * sizeof(float));
   a->ml = reinterpret_cast<float2*>(w);
   w += up256(places * sizeof(float2));
-  a->desc = reinterpret_cast<int4*>(w);
+  a->desc = reinterpret_cast<AttendPart*>(w);
 }
 
 }  // namespace slkv

@@ -9,7 +9,8 @@
 // TMEM as its left operand; while one block's rows are exponentiated the tensor cores work on the other block.  m is raised, and O
 // rescaled in TMEM, only where a tile's maximum lies 2^8 above it.  A unit of one block (few tokens) has its tiles shared by the two
 // warpgroups in turn, each with sums of its own, which are merged in the end.
-//   warps 0-3, 4-7  softmax of the two blocks, results      warp 8  TMA loads of Q, K, V      warp 9  MMAs      warp 10  schedule
+//   warps 0-3, 4-7  softmax of the two blocks, results
+//   warp 8  TMA loads of K, V      warp 9  MMAs      warp 10  schedule      warp 11  TMA loads of Q
 // P is rounded to bf16 for the product (2^-8 of each term); the sum of a row is taken of what is not rounded, in fp32.
 //
 // A key that a row does not see gives it nothing, whatever K and V hold there: scores are replaced, not biased, and since 0 times an
@@ -23,7 +24,7 @@ namespace slkv {
 namespace {
 
 constexpr int kThreads = 384;
-constexpr int kLoadWarp = 8, kMmaWarp = 9, kPlanWarp = 10;
+constexpr int kLoadWarp = 8, kMmaWarp = 9, kPlanWarp = 10, kQueryWarp = 11;
 constexpr int kUnits = 4;                        // pieces the schedule is ahead by
 constexpr float kLift = 8.0f;                    // log2 of how far P may exceed 1 before the reference is raised
 constexpr int kTmemS = 0, kTmemO = 256;          // columns: S of block b at 128 b, O at 256 + 128 b
@@ -37,7 +38,7 @@ struct Smem {
   alignas(1024) unsigned char kv[kStages][kTileBytes];
   float2 ml[2][128];
   AttendPiece piece[kUnits];
-  unsigned long long unit_full[kUnits], unit_empty[kUnits], q_full, q_empty, kv_full[kStages], kv_empty[kStages], s_full[2],
+  unsigned long long unit_full[kUnits], unit_empty[kUnits], q_full[2], q_empty[2], kv_full[kStages], kv_empty[kStages], s_full[2],
       p_ready[2], o_full[2], merge_full, merge_done, drain;
   int odd[2];                                    // number + 1 of the piece that found V values that are not finite, by its parity
   int abort;
@@ -51,6 +52,7 @@ struct AttendTc {
   AttendShape a;
   int k_head_inner, v_head_inner, kn_head_inner, vn_head_inner;
   float sc;                                      // scale * log2(e)
+  int wide;                                      // rows of out begin at 32-byte boundaries
   int arrivals;                                  // at p_ready: 4, or 5 where a test makes the wait for them run out
 };
 
@@ -99,7 +101,7 @@ __device__ __forceinline__ void load_role(const AttendTc& t, const AttendMaps& m
   using S = Smem<D>;
   const AttendShape& a = t.a;
   const int lane = threadIdx.x & 31;
-  unsigned loads = 0, n_q = 0, issued = 0;       // loads, n_q: of earlier pieces
+  unsigned loads = 0, issued = 0;                // loads: of earlier pieces
   bool ok = true;
   for (unsigned nth = 0;; ++nth) {
     ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sm.unit_full[nth % kUnits]), (nth / kUnits) & 1, &sm.abort));
@@ -110,23 +112,6 @@ __device__ __forceinline__ void load_role(const AttendTc& t, const AttendMaps& m
     if (p.stop) break;
     if (p.n == 0) continue;
     const Blocks b(t, p);
-    if (n_q > 0) {
-      ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sm.q_empty), (n_q - 1) & 1, &sm.abort));
-      if (!ok) break;
-    }
-    ++n_q;
-    if (lane == 0) {
-      const uint32_t bar = smem_u32(&sm.q_full);
-      const int blocks = b.alt ? 1 : 2;
-      mbar_expect_tx(bar, (uint32_t)(blocks * S::kHalves * t.a.box_tokens * a.G * 128));
-      for (int g = 0; g < blocks; ++g)
-        for (int hf = 0; hf < S::kHalves; ++hf) {
-          const uint32_t dst = smem_u32(sm.q[g]) + hf * kHalfBytes;
-          const int tok = p.tok0 + g * a.block_tokens, head = p.h * a.G;
-          const int y = t.a.q_head_inner ? head : (a.paged ? tok : p.q_row + tok), z = t.a.q_head_inner ? (a.paged ? tok : p.q_row + tok) : head;
-          tma_load_4d(dst, &m.q, hf * 64, y, z, a.paged ? p.s : 0, bar);
-        }
-    }
     const int total = 2 * p.n;
     int ids = 0, ids_first = -1;                 // lane l: page ids_first + l of the segment
     for (int i = 0; i < total; ++i) {
@@ -196,67 +181,131 @@ __device__ __forceinline__ void load_role(const AttendTc& t, const AttendMaps& m
   if (ok) return;
   // a wait ran out: the copies in flight end before the CTA does
   volatile int never = 0;
-  if (n_q > 0) mbar_wait(smem_u32(&sm.q_full), (n_q - 1) & 1, &never);
   for (unsigned no = issued > (unsigned)S::kStages ? issued - S::kStages : 0; no < issued; ++no)
     mbar_wait(smem_u32(&sm.kv_full[no % S::kStages]), (no / S::kStages) & 1, &never);
 }
 
+// Blocks of query rows, ahead of the products with them as far as two buffers allow.
+template <int D>
+__device__ __forceinline__ void query_role(const AttendTc& t, const AttendMaps& m, Smem<D>& sm) {
+  using S = Smem<D>;
+  const AttendShape& a = t.a;
+  unsigned n_q = 0;                              // blocks
+  bool ok = true;
+  for (unsigned nth = 0;; ++nth) {
+    ok = mbar_wait(smem_u32(&sm.unit_full[nth % kUnits]), (nth / kUnits) & 1, &sm.abort);
+    if (!ok) break;
+    const AttendPiece p = sm.piece[nth % kUnits];
+    mbar_arrive(smem_u32(&sm.unit_empty[nth % kUnits]));
+    if (p.stop) break;
+    if (p.n == 0) continue;
+    const int blocks = p.n_tok <= a.block_tokens ? 1 : 2;
+    for (int g = 0; g < blocks && ok; ++g) {
+      const unsigned slot = n_q & 1;
+      if (n_q >= 2) ok = mbar_wait(smem_u32(&sm.q_empty[slot]), ((n_q >> 1) - 1) & 1, &sm.abort);
+      if (!ok) break;
+      ++n_q;
+      const uint32_t bar = smem_u32(&sm.q_full[slot]), dst = smem_u32(sm.q[slot]);
+      mbar_expect_tx(bar, (uint32_t)(S::kHalves * a.box_tokens * a.G * 128));
+      const int tok = (a.paged ? 0 : p.q_row) + p.tok0 + g * a.block_tokens, head = p.h * a.G;
+      for (int hf = 0; hf < S::kHalves; ++hf)
+        tma_load_4d(dst + hf * kHalfBytes, &m.q, hf * 64, a.q_head_inner ? head : tok, a.q_head_inner ? tok : head, a.paged ? p.s : 0, bar);
+    }
+    if (!ok) break;
+  }
+  if (ok) return;
+  volatile int never = 0;                        // a wait ran out: the copies in flight end before the CTA does
+  for (unsigned no = n_q > 2 ? n_q - 2 : 0; no < n_q; ++no) mbar_wait(smem_u32(&sm.q_full[no & 1]), (no >> 1) & 1, &never);
+}
+
+// The whole warp waits, one lane issues.  What a step needs beside P is waited for before P is.
 template <int D>
 __device__ __forceinline__ bool mma_role(const AttendTc& t, Smem<D>& sm) {
   using S = Smem<D>;
   const AttendShape& a = t.a;
   const uint32_t tmem = sm.tmem;
-  const uint32_t id_s = instr_desc(128, kAttendTile), id_o = instr_desc(128, D) | kRowsB;
+  const bool issuer = (threadIdx.x & 31) == 0;
+  constexpr uint32_t kIdS = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kAttendTile >> 3) << 17) | (8u << 24);
+  constexpr uint32_t kIdO = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(D >> 3) << 17) | (8u << 24) | kRowsB;
   unsigned loads = 0, n_q = 0, n_p[2] = {0, 0};
+  auto wait = [&](unsigned long long* bar, unsigned phase) {
+    return __all_sync(0xffffffffu, mbar_poll(smem_u32(bar), phase & 1, &sm.abort)) != 0;
+  };
   for (unsigned nth = 0;; ++nth) {
-    if (!mbar_wait(smem_u32(&sm.unit_full[nth % kUnits]), (nth / kUnits) & 1, &sm.abort)) return false;
+    if (!wait(&sm.unit_full[nth % kUnits], nth / kUnits)) return false;
     const AttendPiece p = sm.piece[nth % kUnits];
-    mbar_arrive(smem_u32(&sm.unit_empty[nth % kUnits]));
+    __syncwarp();
+    if (issuer) mbar_arrive(smem_u32(&sm.unit_empty[nth % kUnits]));
     if (p.stop) return true;
     if (p.n == 0) continue;
     const Blocks b(t, p);
-    if (!mbar_wait(smem_u32(&sm.q_full), n_q++ & 1, &sm.abort)) return false;
-    int left = b.n[0] + b.n[1];                  // products with K
-    auto qk = [&](int g, int i) {
-      const int tl = b.tile(g, i);
-      const unsigned no = loads + b.k_load(tl), slot = no % S::kStages;
-      if (!mbar_wait(smem_u32(&sm.kv_full[slot]), (no / S::kStages) & 1, &sm.abort)) return false;
-      tc_fence_after();
-      const uint32_t qa = smem_u32(sm.q[b.alt ? 0 : g]), ka = smem_u32(sm.kv[slot]);
+    auto k_there = [&](int g, int i) {
+      const unsigned no = loads + b.k_load(b.tile(g, i));
+      return wait(&sm.kv_full[no % S::kStages], no / S::kStages);
+    };
+    auto v_there = [&](int g, int i) {
+      const unsigned no = loads + b.v_load(b.tile(g, i), p.n);
+      return wait(&sm.kv_full[no % S::kStages], no / S::kStages);
+    };
+    auto qk = [&](int g, int i) {                // by the issuer
+      const unsigned slot = (loads + b.k_load(b.tile(g, i))) % S::kStages, block = (n_q + (b.alt ? 0 : g)) & 1;
+      const uint32_t qa = desc_lo(smem_u32(sm.q[block])), ka = desc_lo(smem_u32(sm.kv[slot])), d = tmem + kTmemS + 128 * g;
+      tc_mma_ss<false>(d, qa, ka, kIdS);
 #pragma unroll
-      for (int k = 0; k < D / 16; ++k) {
-        const uint32_t off = (k >> 2) * kHalfBytes + (k & 3) * 32;
-        tc_mma(tmem + kTmemS + 128 * g, smem_desc(qa + off), smem_desc(ka + off), id_s, k > 0);
+      for (int k = 1; k < D / 16; ++k) {
+        const uint32_t off = ((k >> 2) * kHalfBytes + (k & 3) * 32) >> 4;
+        tc_mma_ss<true>(d, qa + off, ka + off, kIdS);
       }
       tc_commit(smem_u32(&sm.s_full[g]));
       if (b.alt || g == 1) tc_commit(smem_u32(&sm.kv_empty[slot]));
-      if (--left == 0) tc_commit(smem_u32(&sm.q_empty));
-      return true;
+      if (b.alt ? 2 * i + g + 1 == p.n : i + 1 == b.n[g]) tc_commit(smem_u32(&sm.q_empty[block]));
     };
-    for (int g = 0; g < 2; ++g)
-      if (b.n[g] > 0 && !qk(g, 0)) return false;
+    for (int g = 0; g < 2; ++g) {
+      if (!b.alt || g == 0) {
+        const unsigned block = n_q + g;
+        if (!wait(&sm.q_full[block & 1], block >> 1)) return false;
+        // a block that sees none of the tiles
+        if (b.n[g] == 0 && issuer) mbar_arrive(smem_u32(&sm.q_empty[block & 1]));
+      }
+      if (b.n[g] == 0) continue;
+      if (!k_there(g, 0)) return false;
+      tc_fence_after();
+      if (issuer) qk(g, 0);
+      __syncwarp();
+    }
     const int steps = max(b.n[0], b.n[1]);
     for (int i = 0; i < steps; ++i)
       for (int g = 0; g < 2; ++g) {
         if (i >= b.n[g]) continue;
-        const int tl = b.tile(g, i);
-        const unsigned no = loads + b.v_load(tl, p.n), slot = no % S::kStages;
-        if (!mbar_wait(smem_u32(&sm.p_ready[g]), n_p[g]++ & 1, &sm.abort)) return false;
-        if (!mbar_wait(smem_u32(&sm.kv_full[slot]), (no / S::kStages) & 1, &sm.abort)) return false;
-        tc_fence_after();
-        const int tok = p.tok0 + (b.alt ? 0 : g * a.block_tokens);
-        const int used = columns(t, p, p.tile0 + tl, tok, min(a.block_tokens, p.n_seq_tok - tok)).used;
-        const uint32_t va = smem_u32(sm.kv[slot]);
-        for (int k = 0; k < used / 16; ++k)
-          tc_mma_ts(tmem + kTmemO + 128 * g, tmem + kTmemS + 128 * g + 8 * k, smem_desc_rows(va + k * 2048), id_o, i > 0 || k > 0);
-        if (b.alt || g == 1) tc_commit(smem_u32(&sm.kv_empty[slot]));
-        if (i + 1 < b.n[g]) {
-          if (!qk(g, i + 1)) return false;
-        } else {
-          tc_commit(smem_u32(&sm.o_full[g]));
+        const bool more = i + 1 < b.n[g];
+        if (b.alt || g == 0 || i >= b.n[0]) {
+          if (!v_there(g, i)) return false;
         }
+        if (more && (b.alt || g == 0 || i + 1 >= b.n[0])) {
+          if (!k_there(g, i + 1)) return false;
+        }
+        const int tok = p.tok0 + (b.alt ? 0 : g * a.block_tokens);
+        const int used = columns(t, p, p.tile0 + b.tile(g, i), tok, min(a.block_tokens, p.n_seq_tok - tok)).used;
+        const unsigned slot = (loads + b.v_load(b.tile(g, i), p.n)) % S::kStages;
+        const uint32_t va = desc_lo(smem_u32(sm.kv[slot])), d = tmem + kTmemO + 128 * g, pa = tmem + kTmemS + 128 * g;
+        if (!wait(&sm.p_ready[g], n_p[g]++)) return false;
+        tc_fence_after();
+        if (issuer) {
+          if (used == kAttendTile) {
+#pragma unroll
+            for (int k = 0; k < kAttendTile / 16; ++k) tc_mma_ts(d, pa + 8 * k, va + k * 128, kIdO, k > 0 ? 1 : i > 0);
+          } else {
+#pragma unroll 1
+            for (int k = 0; k < used / 16; ++k) tc_mma_ts(d, pa + 8 * k, va + k * 128, kIdO, k > 0 || i > 0);
+          }
+          if (b.alt || g == 1) tc_commit(smem_u32(&sm.kv_empty[slot]));
+          if (more) qk(g, i + 1);
+          else tc_commit(smem_u32(&sm.o_full[g]));
+        }
+        __syncwarp();
       }
     loads += 2 * p.n;
+    n_q += b.alt ? 1 : 2;
   }
 }
 
@@ -308,9 +357,10 @@ struct Rows {                                    // of a softmax thread, for the
   unsigned long long mask;                       // paged: drafted tokens that it sees
 };
 
-// Values of V that are not finite and were taken out, in the channels ch .. ch + 31: rows that see them get them back.
-template <int D>
-__device__ __noinline__ void put_back(const AttendTc& t, const AttendPiece& p, int bound, unsigned long long mask, int ch, float (&o)[32]) {
+// Values of V that are not finite and were taken out, in the channels ch0 .. ch1 - 1: rows that see them get them back, in the results
+// that the thread has written.
+template <bool WHOLE>
+__device__ __noinline__ void put_back(const AttendTc& t, const AttendPiece& p, int bound, unsigned long long mask, int ch0, int ch1, void* out) {
   const AttendShape& a = t.a;
   int j0, j1;
   const __nv_bfloat16* base;
@@ -329,13 +379,23 @@ __device__ __noinline__ void put_back(const AttendTc& t, const AttendPiece& p, i
   }
   for (int j = j0; j < j1; ++j) {
     if (a.paged && !(mask >> j & 1)) continue;
-    const __nv_bfloat16* v = base + j * stride + ch;
-#pragma unroll
-    for (int e = 0; e < 32; ++e) {
-      const float x = __bfloat162float(v[e]);
-      if (!(fabsf(x) < INFINITY)) o[e] += x;
+    for (int ch = ch0; ch < ch1; ++ch) {
+      const float x = __bfloat162float(base[j * stride + ch]);
+      if (fabsf(x) < INFINITY) continue;
+      if (WHOLE) {
+        __nv_bfloat16* o = static_cast<__nv_bfloat16*>(out) + ch;
+        *o = __float2bfloat16_rn(__bfloat162float(*o) + x);
+      } else {
+        static_cast<float*>(out)[ch] += x;
+      }
     }
   }
+}
+
+// 32 bytes, from a 32-byte boundary.
+__device__ __forceinline__ void store32(void* to, const uint32_t* w) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]),
+               "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
 }
 
 template <int D>
@@ -491,61 +551,57 @@ __device__ __forceinline__ void softmax_role(const AttendTc& t, Smem<D>& sm, int
       ch1 = ch0 + D / 2;
     }
     if (work && !(b.alt && g == 1 && !merge)) {
-      const bool odd = *(volatile int*)&sm.odd[nth & 1] == (int)nth + 1;
-      const int blk = b.alt ? 0 : g;
       const bool whole = p.part < 0;
-      const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
-      const long long place = whole ? 0 : ((long long)(blockIdx.x * 2 + p.part) * a.part_rows + blk * 128 + tid);
+      const float inv = !whole ? 1.0f : l > 0.0f || l != l ? 1.0f / l : 0.0f;
+      const long long place = (long long)(blockIdx.x * 2 + p.part) * a.part_rows + (b.alt ? 0 : g * 128) + tid;
+      char* const dst = whole ? reinterpret_cast<char*>(static_cast<__nv_bfloat16*>(a.out) + (a.paged ? p.s * a.o_seq : p.q_row * a.o_tok) +
+                                                        tok * a.o_tok + (p.h * a.G + rh) * a.o_head)
+                              : reinterpret_cast<char*>(a.part + place * D);
 #pragma unroll 1
       for (int ch = ch0; ch < ch1; ch += 32) {
-        float o[32];
-        {
+        uint32_t o[32];
+        if (n > 0 || merge) {
+          tc_ld32(o_at + ch, o);
+          tc_wait_ld(o);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 32; ++e) o[e] = 0;
+        }
+        if (merge) {
           uint32_t r[32];
-          if (n > 0 || merge) {
-            tc_ld32(o_at + ch, r);
-            tc_wait_ld(r);
+          tc_ld32(o_at + 128 + ch, r);
+          tc_wait_ld(r);
 #pragma unroll
-            for (int e = 0; e < 32; ++e) o[e] = __uint_as_float(r[e]);
-          } else {
-#pragma unroll
-            for (int e = 0; e < 32; ++e) o[e] = 0.0f;
-          }
-          if (merge) {
-            tc_ld32(o_at + 128 + ch, r);
-            tc_wait_ld(r);
-#pragma unroll
-            for (int e = 0; e < 32; ++e) o[e] = o[e] * f0 + __uint_as_float(r[e]) * f1;
-          }
+          for (int e = 0; e < 32; ++e) o[e] = __float_as_uint((__uint_as_float(o[e]) * f0 + __uint_as_float(r[e]) * f1));
         }
         if (there) {
-          if (odd) put_back<D>(t, p, bound, mask, ch, o);
           if (whole) {
-            __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(a.out) + (a.paged ? p.s * a.o_seq : p.q_row * a.o_tok) + tok * a.o_tok +
-                                 (p.h * a.G + rh) * a.o_head + ch;
+            uint32_t w[16];
 #pragma unroll
-            for (int e = 0; e < 32; e += 8) {
-              uint4 w;
-              w.x = bf16_pair(pack2(o[e] * inv, o[e + 1] * inv));
-              w.y = bf16_pair(pack2(o[e + 2] * inv, o[e + 3] * inv));
-              w.z = bf16_pair(pack2(o[e + 4] * inv, o[e + 5] * inv));
-              w.w = bf16_pair(pack2(o[e + 6] * inv, o[e + 7] * inv));
-              *reinterpret_cast<uint4*>(dst + e) = w;
+            for (int e = 0; e < 16; ++e) w[e] = bf16_pair(pack2(__uint_as_float(o[2 * e]) * inv, __uint_as_float(o[2 * e + 1]) * inv));
+            if (t.wide) {
+              store32(dst + 2 * ch, w);
+              store32(dst + 2 * ch + 32, w + 8);
+            } else {
+#pragma unroll
+              for (int e = 0; e < 16; e += 4) *reinterpret_cast<uint4*>(dst + 2 * ch + 2 * e * 2) = make_uint4(w[e], w[e + 1], w[e + 2], w[e + 3]);
             }
           } else {
-            float* dst = a.part + place * D + ch;
 #pragma unroll
-            for (int e = 0; e < 32; e += 4) *reinterpret_cast<float4*>(dst + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+            for (int e = 0; e < 32; e += 8) store32(dst + 4 * (ch + e), o + e);
           }
         }
         __syncwarp();                            // the next load is the whole warp's
       }
-      if (there && ch0 == 0) {
-        if (!whole) {
-          a.ml[place] = make_float2(m, l);
-        } else {
-          attend_lse(a, p.s, p.h * a.G + rh, tok, p.n_seq_tok, m * t.sc, l);
-        }
+      if (there && *(volatile int*)&sm.odd[nth & 1] == (int)nth + 1) {
+        if (whole) put_back<true>(t, p, bound, mask, ch0, ch1, dst);
+        else put_back<false>(t, p, bound, mask, ch0, ch1, dst);
       }
+      if (there && ch0 == 0) {
+        if (whole) attend_lse(a, p.s, p.h * a.G + rh, tok, p.n_seq_tok, m * t.sc, l);
+        else a.ml[place] = make_float2(m, l);
+      }
+      __syncwarp();
     }
     if (merge) {                                 // the other warpgroup's accumulator is read
       tc_fence_before();
@@ -567,15 +623,15 @@ k_attend_tc(const __grid_constant__ AttendTc t, const __grid_constant__ AttendMa
   if (threadIdx.x == 0) {
     for (int i = 0; i < kUnits; ++i) {
       mbar_init(smem_u32(&sm.unit_full[i]), 1);
-      mbar_init(smem_u32(&sm.unit_empty[i]), 10);
+      mbar_init(smem_u32(&sm.unit_empty[i]), 11);
     }
-    mbar_init(smem_u32(&sm.q_full), 1);
-    mbar_init(smem_u32(&sm.q_empty), 1);
     for (int i = 0; i < S::kStages; ++i) {
       mbar_init(smem_u32(&sm.kv_full[i]), 1);
       mbar_init(smem_u32(&sm.kv_empty[i]), 1);
     }
     for (int g = 0; g < 2; ++g) {
+      mbar_init(smem_u32(&sm.q_full[g]), 1);
+      mbar_init(smem_u32(&sm.q_empty[g]), 1);
       mbar_init(smem_u32(&sm.s_full[g]), 1);
       mbar_init(smem_u32(&sm.p_ready[g]), blockIdx.x == 0 ? t.arrivals : 4);
       mbar_init(smem_u32(&sm.o_full[g]), 1);
@@ -601,13 +657,15 @@ k_attend_tc(const __grid_constant__ AttendTc t, const __grid_constant__ AttendMa
     if (warp == kLoadWarp) {
       load_role<D>(t, maps, sm);
     } else if (warp == kMmaWarp) {
-      if (lane == 0 && !mma_role<D>(t, sm)) {    // a wait ran out: what is under way ends first
+      if (!mma_role<D>(t, sm) && lane == 0) {    // a wait ran out: what is under way ends first
         volatile int never = 0;
         tc_commit(smem_u32(&sm.drain));
         mbar_wait(smem_u32(&sm.drain), 0, &never);
       }
+    } else if (warp == kQueryWarp) {
+      if (lane == 0) query_role<D>(t, maps, sm);
     } else if (warp == kPlanWarp) {
-      if (lane == 0 && !t.a.spread) t.a.desc[2 * blockIdx.x] = t.a.desc[2 * blockIdx.x + 1] = make_int4(0, 0, 0, 0);
+      if (lane == 0 && !t.a.spread) t.a.desc[2 * blockIdx.x].state = t.a.desc[2 * blockIdx.x + 1].state = 0;
       AttendSchedule plan(t.a, blockIdx.x);
       for (unsigned nth = 0;; ++nth) {
         AttendPiece p = {};
@@ -620,8 +678,7 @@ k_attend_tc(const __grid_constant__ AttendTc t, const __grid_constant__ AttendMa
         if (lane == 0) {
           sm.piece[nth % kUnits] = p;
           mbar_arrive(smem_u32(&sm.unit_full[nth % kUnits]));
-          if (more && p.part >= 0)
-            t.a.desc[2 * blockIdx.x + p.part] = make_int4(p.tile0 + max(p.n, 1) == max(p.n_all, 1) ? 2 : 1, p.s, p.h, p.tok0);
+          if (more && p.part >= 0) attend_note(t.a, p.part, p, p.part == 1 ? plan.pieces() : 0);
         }
         if (!more) break;
       }
@@ -636,7 +693,7 @@ k_attend_tc(const __grid_constant__ AttendTc t, const __grid_constant__ AttendMa
   tc_fence_after();
   if (sm.abort && threadIdx.x == 0) {
     if (t.a.status) *t.a.status = SLKV_ERR_DEVICE_TIMEOUT;
-    if (!t.a.spread) t.a.desc[2 * blockIdx.x] = t.a.desc[2 * blockIdx.x + 1] = make_int4(-1, 0, 0, 0);
+    if (!t.a.spread) t.a.desc[2 * blockIdx.x].state = t.a.desc[2 * blockIdx.x + 1].state = -1;
   }
   if (warp == kMmaWarp)
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(sm.tmem) : "memory");
@@ -685,10 +742,11 @@ cudaError_t launch_attend_tensor(const AttendShape& a, cudaStream_t st, int* lau
   AttendMaps m = {};
   t.a = a;
   t.sc = a.ml_unit;
+  t.wide = reinterpret_cast<uintptr_t>(a.out) % 32 == 0 && a.o_tok % 16 == 0 && a.o_head % 16 == 0 && (!a.paged || a.o_seq % 16 == 0);
   t.arrivals = take_expire_next_copy_wait() ? 5 : 4;
   t.a.box_tokens = a.paged && a.n_tokens < a.block_tokens ? a.n_tokens : a.block_tokens;
   cudaError_t e = encode_rows(&m.q, a.q, a.head_dim, a.n_q_heads, a.paged ? a.n_tokens : a.rows_q, a.paged ? a.n_seqs : 1, a.q_head,
-                              a.q_tok, a.paged ? a.q_seq : a.q_tok, a.G, t.a.box_tokens, &t.a.q_head_inner);
+                              a.q_tok, a.paged ? a.q_seq : a.q_tok, a.G, a.box_tokens, &t.a.q_head_inner);
   if (e != cudaSuccess) return e;
   if (a.paged) {
     const cuuint64_t dims[3] = {(cuuint64_t)a.head_dim, (cuuint64_t)a.rows_k, 1}, strides[2] = {(cuuint64_t)a.head_dim * 2, 16};
