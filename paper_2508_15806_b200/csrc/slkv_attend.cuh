@@ -11,14 +11,14 @@
 
 namespace slkv {
 
-constexpr int kAttendTile = 128;                 // keys of a tile, query rows of a block
+constexpr int kAttendTileBits = 7, kAttendTile = 1 << kAttendTileBits;                 // keys of a tile, query rows of a block
 constexpr int kMaxDrafted = 64;                  // drafted tokens of a sequence: the bits of a mask
 constexpr int kMaxGroup = 64;                    // query heads of a KV head
 
 // What the kernels need to know of a call.
 struct AttendShape {
   int n_seqs, n_kv_heads, n_q_heads, G, head_dim;
-  int block_tokens, unit_tokens, tile_keys;      // tokens of a block of query rows and of a unit (one or two blocks); keys of a tile
+  int block_tokens, unit_tokens, tile_bits;      // tokens of a block of query rows and of a unit (one or two blocks); log2 of a tile's keys
   int paged;
   // prompt
   const int32_t *cu_q, *cu_k;
@@ -97,10 +97,86 @@ __device__ __forceinline__ void attend_lse(const AttendShape& a, int s, int qh, 
 //                sequence first: shares differ by about the last units, which are short, and CTAs that run beside each other read the
 //                same keys
 //   not spread   the tiles of all units in one row, cut into equal shares: for few units.  A unit without tiles counts one.
-// The first piece is what a launch waits for, so the search for it is short: 32-bit arithmetic, a run of groups per lane, two scans.
+// The first piece is what a launch waits for, and most of that is instructions that come in for the first time: the threads of the CTA
+// look for it together (attend_start), a few segments each, in little code.
+__device__ __forceinline__ int attend_tokens(const AttendShape& a, int s) {
+  if (!a.paged) return max(a.cu_q[s + 1] - a.cu_q[s], 0);
+  return a.n_new ? min(max(a.n_new[s], 0), a.n_tokens) : a.n_tokens;
+}
+__device__ __forceinline__ int attend_blocks(const AttendShape& a, int tokens) {
+  return tokens <= a.unit_tokens ? tokens > 0 : (int)((unsigned)(tokens + a.unit_tokens - 1) / (unsigned)a.unit_tokens);
+}
+__device__ __forceinline__ int attend_rows(const AttendShape& a, int seg) { return min(max(a.lens[seg], 0), a.max_pages * a.page_rows); }
+// Tiles of a unit.
+__device__ __forceinline__ int attend_prompt_tiles(const AttendShape& a, int nq, int nk, int t) {
+  const int seen = min(nq, (t + 1) * a.unit_tokens) + nk - nq;
+  return seen <= 0 ? 0 : (seen + (1 << a.tile_bits) - 1) >> a.tile_bits;
+}
+__device__ __forceinline__ int attend_paged_tiles(const AttendShape& a, int rows) {
+  return ((rows + (1 << a.tile_bits) - 1) >> a.tile_bits) + a.has_new;
+}
+// Tiles of all units of a segment (paged) or a sequence (prompt); a unit without any counts one.
+__device__ __forceinline__ int attend_weight(const AttendShape& a, int i) {
+  if (a.paged) return attend_blocks(a, attend_tokens(a, (unsigned)i / (unsigned)a.n_kv_heads)) * max(attend_paged_tiles(a, attend_rows(a, i)), 1);
+  const int nq = attend_tokens(a, i), nk = max(a.cu_k[i + 1] - a.cu_k[i], 0);
+  int sum = 0;
+  for (int t = 0; t * a.unit_tokens < nq; ++t) sum += max(attend_prompt_tiles(a, nq, nk, t), 1);
+  return sum * a.n_kv_heads;
+}
+// Where a CTA's share of the tiles begins.
+struct AttendStart {
+  int warp_sum[32];
+  int total;
+  int group, before;             // segment or sequence that the share begins in, tiles in front of it
+};
+// By all threads of a CTA, 32 times n_warps; two barriers inside, one left to the caller.
+__device__ __forceinline__ void attend_start(const AttendShape& a, int cta, AttendStart* st) {
+  if (a.spread) return;
+  const int n = a.paged ? a.n_seqs * a.n_kv_heads : a.n_seqs;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n_warps = blockDim.x >> 5;
+  const int per = (unsigned)n <= blockDim.x ? 1 : (int)((unsigned)(n + blockDim.x - 1) / blockDim.x);
+  const int first = threadIdx.x * per, last = min(first + per, n);
+  int sum = 0;
+  for (int i = first; i < last; ++i) sum += attend_weight(a, i);
+  int incl = sum;
+#pragma unroll 1
+  for (int d = 1; d < 32; d <<= 1) {
+    const int o = __shfl_up_sync(0xffffffffu, incl, d);
+    if (lane >= d) incl += o;
+  }
+  if (lane == 31) st->warp_sum[warp] = incl;
+  __syncthreads();
+  int before = incl - sum, total = 0;
+#pragma unroll 1
+  for (int w = 0; w < n_warps; ++w) {
+    const int x = st->warp_sum[w];
+    if (w < warp) before += x;
+    total += x;
+  }
+  if (threadIdx.x == 0) st->total = total;
+  const int each = (unsigned)total / (unsigned)a.n_cta, more = total - each * a.n_cta, pos = each * cta + min(cta, more);
+  if (pos >= before && pos < before + sum) {
+    int i = first;
+    for (;; ++i) {
+      const int w = attend_weight(a, i);
+      if (pos < before + w || i + 1 >= last) break;
+      before += w;
+    }
+    st->group = i;
+    st->before = before;
+  }
+}
+
 class AttendSchedule {
  public:
-  __device__ __forceinline__ AttendSchedule(const AttendShape& a, int cta) : a_(a), cta_(cta), lane_(threadIdx.x & 31) {
+  __device__ __forceinline__ AttendSchedule(const AttendShape& a, int cta, const AttendStart* st) : a_(a), cta_(cta), lane_(threadIdx.x & 31) {
+    cached_ = !a_.paged && a_.n_seqs <= 32;
+    if (cached_ && lane_ < a_.n_seqs) {
+      q0_ = a_.cu_q[lane_];
+      q1_ = a_.cu_q[lane_ + 1];
+      k0_ = a_.cu_k[lane_];
+      k1_ = a_.cu_k[lane_ + 1];
+    }
     if (a_.spread) {
       item_ = cta;
       round_ = 0;
@@ -109,51 +185,22 @@ class AttendSchedule {
       count_ = level_count(level_);
       return;
     }
-    // runs of segments (paged) or sequences (prompt), one per lane
-    const int n = a_.paged ? a_.n_seqs * a_.n_kv_heads : a_.n_seqs, per = (n + 31) / 32;
-    int sum = 0;
-#pragma unroll 4
-    for (int i = 0; i < per; ++i) sum += weight(lane_ * per + i, n);
-    int incl = scan(sum);
-    const int total = __shfl_sync(0xffffffffu, incl, 31);
     // the first `more` CTAs have each + 1 tiles, the others each; where there are fewer tiles than CTAs the last ones have none
-    const int each = total / a_.n_cta, more = total - each * a_.n_cta;
-    pos_ = each * cta + min(cta, more);
-    end_ = pos_ + each + (cta < more);
+    const int total = st->total;
+    share_ = (unsigned)total / (unsigned)a_.n_cta;
+    more_ = total - share_ * a_.n_cta;
+    pos_ = share_ * cta + min(cta, more_);
+    end_ = pos_ + share_ + (cta < more_);
     if (pos_ >= end_) return;
-    share_ = each;
-    more_ = more;
-    int at = __ffs(__ballot_sync(0xffffffffu, incl > pos_)) - 1;
-    int before = __shfl_sync(0xffffffffu, incl - sum, at), first = at * per;
-    const int stop = min(first + per, n);
-    for (;; first += 32) {                       // the run's groups
-      const int w = first + lane_ < stop ? weight(first + lane_, n) : 0;
-      incl = scan(w);
-      const unsigned m = __ballot_sync(0xffffffffu, before + incl > pos_);
-      if (m) {
-        at = __ffs(m) - 1;
-        before += __shfl_sync(0xffffffffu, incl - w, at);
-        first += at;
-        break;
-      }
-      before += __shfl_sync(0xffffffffu, incl, 31);
-      if (first + 32 >= stop) { pos_ = end_; return; }         // lengths on the device that are not the host's
-    }
-    group_ = before;
+    group_ = st->before;
+    s_ = st->group;
+    x_ = 0;
     if (a_.paged) {
-      s_ = first / a_.n_kv_heads;
-      x_ = first - s_ * a_.n_kv_heads;
-      load_group();
-    } else {
-      s_ = first;
-      x_ = 0;
-      load_group();
-      while (pos_ >= group_ + inner_ * each_) {
-        group_ += inner_ * each_;
-        ++x_;
-        load_group();
-      }
+      const int seg = s_;
+      s_ = (unsigned)seg / (unsigned)a_.n_kv_heads;
+      x_ = seg - s_ * a_.n_kv_heads;
     }
+    load_group();
   }
   __device__ __forceinline__ bool next(AttendPiece* p) { return a_.spread ? next_spread(p) : next_share(p); }
   // Of the piece at hand, one of several: how many pieces its unit has.
@@ -162,13 +209,15 @@ class AttendSchedule {
  private:
   const AttendShape& a_;
   int cta_, lane_;
+  bool cached_ = false;          // prompts of up to 32 sequences: lane s has where sequence s lies
+  int q0_ = 0, q1_ = 0, k0_ = 0, k1_ = 0;
   // spread
   long long item_, base_, count_;
   int level_, round_;
   // shares: the group of units with the same tiles (prompt: a block of tokens, all KV heads; paged: a segment, all blocks)
   int pos_, end_, group_;        // group_: first position of the group
   int s_, x_;                    // sequence; prompt: block of tokens, paged: KV head
-  int inner_, each_;             // units of the group, tiles counted for each
+  int inner_, each_, blocks_;    // units of the group, tiles counted for each; blocks of the sequence
   int unit_;                     // first position of the unit at hand
   int share_, more_;
 
@@ -176,45 +225,26 @@ class AttendSchedule {
     const int big = more_ * (share_ + 1);
     return pos < big ? pos / (share_ + 1) : more_ + (pos - big) / max(share_, 1);
   }
-  __device__ __forceinline__ int scan(int v) const {
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-      const int o = __shfl_up_sync(0xffffffffu, v, d);
-      if (lane_ >= d) v += o;
-    }
-    return v;
-  }
+  // Of sequence s, the same in all lanes.
+  __device__ __forceinline__ int first_query(int s) const { return cached_ ? __shfl_sync(0xffffffffu, q0_, s) : a_.cu_q[s]; }
+  __device__ __forceinline__ int first_key(int s) const { return cached_ ? __shfl_sync(0xffffffffu, k0_, s) : a_.cu_k[s]; }
   __device__ __forceinline__ int seq_tokens(int s) const {
-    if (!a_.paged) return max(a_.cu_q[s + 1] - a_.cu_q[s], 0);
-    return a_.n_new ? min(max(a_.n_new[s], 0), a_.n_tokens) : a_.n_tokens;
+    return cached_ ? __shfl_sync(0xffffffffu, max(q1_ - q0_, 0), s) : attend_tokens(a_, s);
   }
-  __device__ __forceinline__ int seq_keys(int s) const { return max(a_.cu_k[s + 1] - a_.cu_k[s], 0); }
-  __device__ __forceinline__ int blocks(int tokens) const {
-    return tokens <= a_.unit_tokens ? tokens > 0 : (tokens + a_.unit_tokens - 1) / a_.unit_tokens;
+  __device__ __forceinline__ int seq_keys(int s) const {
+    return cached_ ? __shfl_sync(0xffffffffu, max(k1_ - k0_, 0), s) : max(a_.cu_k[s + 1] - a_.cu_k[s], 0);
   }
-  __device__ __forceinline__ int rows_of(int seg) const { return min(max(a_.lens[seg], 0), a_.max_pages * a_.page_rows); }
-  // Tiles of a unit.
-  __device__ __forceinline__ int prompt_tiles(int nq, int nk, int t) const {
-    const int seen = min(nq, (t + 1) * a_.unit_tokens) + nk - nq;
-    return seen <= 0 ? 0 : (seen + a_.tile_keys - 1) / a_.tile_keys;
-  }
-  __device__ __forceinline__ int paged_tiles(int rows) const { return (rows + a_.tile_keys - 1) / a_.tile_keys + a_.has_new; }
-  // Tiles of a segment's or a sequence's units.
-  __device__ __forceinline__ int weight(int i, int n) const {
-    if (i >= n) return 0;
-    if (a_.paged) return blocks(seq_tokens(i / a_.n_kv_heads)) * max(paged_tiles(rows_of(i)), 1);
-    const int nq = seq_tokens(i), nk = seq_keys(i), nb = blocks(nq);
-    int sum = 0;
-    for (int t = 0; t < nb; ++t) sum += max(prompt_tiles(nq, nk, t), 1);
-    return sum * a_.n_kv_heads;
+  // Of the sequence s0 + lane: its blocks.
+  __device__ __forceinline__ int lane_blocks(int s0) const {
+    if (s0 + lane_ >= a_.n_seqs) return 0;
+    return attend_blocks(a_, cached_ ? max(q1_ - q0_, 0) : attend_tokens(a_, s0 + lane_));
   }
 
   // ---- spread
   __device__ __forceinline__ long long level_count(int t) const {
     int n = 0;
     for (int s0 = 0; s0 < a_.n_seqs; s0 += 32) {
-      const int s = s0 + lane_;
-      n += __popc(__ballot_sync(0xffffffffu, s < a_.n_seqs && blocks(seq_tokens(s)) > t));
+      n += __popc(__ballot_sync(0xffffffffu, lane_blocks(s0) > t));
     }
     return (long long)n * a_.n_kv_heads;
   }
@@ -229,7 +259,7 @@ class AttendSchedule {
     const int h = (int)(rel - (unsigned)nth * (unsigned)a_.n_kv_heads);
     int s = 0;
     for (int s0 = 0; s0 < a_.n_seqs; s0 += 32) {
-      unsigned m = __ballot_sync(0xffffffffu, s0 + lane_ < a_.n_seqs && blocks(seq_tokens(s0 + lane_)) > level_);
+      unsigned m = __ballot_sync(0xffffffffu, lane_blocks(s0) > level_);
       const int n = __popc(m);
       if (nth < n) {
         for (; nth > 0; --nth) m &= m - 1;
@@ -249,24 +279,25 @@ class AttendSchedule {
 
   // ---- equal shares
   __device__ __forceinline__ void load_group() {
+    const int nq = seq_tokens(s_);
+    blocks_ = attend_blocks(a_, nq);
     if (a_.paged) {
-      inner_ = blocks(seq_tokens(s_));
-      each_ = max(paged_tiles(rows_of(s_ * a_.n_kv_heads + x_)), 1);
+      inner_ = blocks_;
+      each_ = max(attend_paged_tiles(a_, attend_rows(a_, s_ * a_.n_kv_heads + x_)), 1);
     } else {
-      const int nq = seq_tokens(s_);
-      inner_ = x_ < blocks(nq) ? a_.n_kv_heads : 0;
-      each_ = max(prompt_tiles(nq, seq_keys(s_), x_), 1);
+      inner_ = x_ < blocks_ ? a_.n_kv_heads : 0;
+      each_ = max(attend_prompt_tiles(a_, nq, seq_keys(s_), x_), 1);
     }
   }
   __device__ __forceinline__ bool next_share(AttendPiece* p) {
     if (pos_ >= end_) return false;
     while (pos_ >= group_ + inner_ * each_) {
       group_ += inner_ * each_;
-      if (++x_ >= (a_.paged ? a_.n_kv_heads : blocks(seq_tokens(s_)))) { x_ = 0; ++s_; }
+      if (++x_ >= (a_.paged ? a_.n_kv_heads : blocks_)) { x_ = 0; ++s_; }
       if (s_ >= a_.n_seqs) return false;                       // lengths on the device that are not the host's
       load_group();
     }
-    const int rel = pos_ - group_, unit = rel / each_, tile0 = rel - unit * each_;
+    const int rel = pos_ - group_, unit = (unsigned)rel / (unsigned)each_, tile0 = rel - unit * each_;
     const int take = min(each_ - tile0, end_ - pos_);
     unit_ = pos_ - tile0;
     if (a_.paged) fill(p, s_, x_, unit);
@@ -285,15 +316,15 @@ class AttendSchedule {
     p->tok0 = t * a_.unit_tokens;
     p->n_tok = min(a_.unit_tokens, nq - p->tok0);
     if (a_.paged) {
-      p->nk = rows_of(s * a_.n_kv_heads + h);
+      p->nk = attend_rows(a_, s * a_.n_kv_heads + h);
       p->shift = p->q_row = p->k_row = 0;
-      p->n_all = paged_tiles(p->nk);
+      p->n_all = attend_paged_tiles(a_, p->nk);
     } else {
       p->nk = seq_keys(s);
       p->shift = p->nk - nq;
-      p->q_row = a_.cu_q[s];
-      p->k_row = a_.cu_k[s];
-      p->n_all = prompt_tiles(nq, p->nk, t);
+      p->q_row = first_query(s);
+      p->k_row = first_key(s);
+      p->n_all = attend_prompt_tiles(a_, nq, p->nk, t);
     }
     p->stop = 0;
   }

@@ -9,7 +9,7 @@ namespace {
 
 constexpr long long kMaxRows = (1ll << 31) - 512;      // tokens, rows of a pool: a tile behind the last one still has 32-bit coordinates
 constexpr int kMaxSegments = 1 << 20, kMaxLayerSegments = 16384;
-constexpr int kFmaRows = 64, kFmaFewRows = 16, kFmaKeys = 64;
+constexpr int kFmaRows = 64, kFmaFewRows = 16, kFmaKeyBits = 6;
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 bool dtype_ok(int dtype) { return dtype == SLKV_F32 || dtype == SLKV_BF16; }
@@ -45,7 +45,7 @@ void set_blocks(AttendShape* a, int dtype, long long max_tokens) {
     a->block_tokens = a->unit_tokens = a->part_rows / a->G;
     a->box_tokens = a->block_tokens;
     a->q_head_inner = 1;
-    a->tile_keys = kFmaKeys;
+    a->tile_bits = kFmaKeyBits;
     a->n_cta = attend_fma_ctas();
     a->used_rows = a->part_rows;
   } else {
@@ -53,7 +53,7 @@ void set_blocks(AttendShape* a, int dtype, long long max_tokens) {
     a->unit_tokens = 2 * a->block_tokens;
     a->part_rows = max_tokens <= a->block_tokens ? kAttendTile : 2 * kAttendTile;
     a->box_tokens = a->paged && max_tokens < a->block_tokens ? (int)max_tokens : a->block_tokens;
-    a->tile_keys = kAttendTile;
+    a->tile_bits = kAttendTileBits;
     a->n_cta = sm_count();
     a->used_rows = a->part_rows == kAttendTile ? a->box_tokens * a->G : a->part_rows;
   }
@@ -100,7 +100,7 @@ int check_prompt(const slkv_prompt_params* p, const int32_t* cu_q, const int32_t
       const int nq = cu_q[s + 1] - cu_q[s], nk = cu_k[s + 1] - cu_k[s];
       for (int t = 0; t * a->unit_tokens < nq; ++t) {
         const int end = (t + 1) * a->unit_tokens < nq ? (t + 1) * a->unit_tokens : nq, seen = end + nk - nq;
-        const long long n = seen > 0 ? (seen + a->tile_keys - 1) / a->tile_keys : 1;
+        const long long n = seen > 0 ? (seen + (1 << a->tile_bits) - 1) >> a->tile_bits : 1;
         tiles += n * p->n_kv_heads;
         if (n > most) most = n;
       }
@@ -161,7 +161,7 @@ int check_paged_attend(const slkv_paged_cache* c, const slkv_paged_attend_params
   if (c->dtype == SLKV_BF16) a->q_head_inner = a->q_head <= a->q_tok;
   a->lse_unit = p->lse_units == SLKV_LSE_LOG2 ? 1.0f : 0.69314718055994531f;
   const long long blocks = (a->n_tokens + a->unit_tokens - 1) / a->unit_tokens, longest = (long long)c->max_pages * c->page_rows;
-  const long long most = blocks * a->n_seqs * a->n_kv_heads * ((longest + a->tile_keys - 1) / a->tile_keys + a->has_new);
+  const long long most = blocks * a->n_seqs * a->n_kv_heads * (((longest + (1 << a->tile_bits) - 1) >> a->tile_bits) + a->has_new);
   if (most >= (1ll << 31)) return SLKV_ERR_BAD_SHAPE;      // tiles are counted in 32 bits
   if (most < a->n_cta) a->n_cta = (int)most;
   return SLKV_OK;

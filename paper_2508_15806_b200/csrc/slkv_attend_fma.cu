@@ -43,7 +43,10 @@ k_attend_fma(const __grid_constant__ AttendShape a) {
   pdl_launch_dependents();
   pdl_wait();
   if (tid == 0 && !a.spread) a.desc[2 * blockIdx.x].state = a.desc[2 * blockIdx.x + 1].state = 0;
-  AttendSchedule plan(a, blockIdx.x);            // every warp runs it
+  __shared__ AttendStart start;
+  attend_start(a, blockIdx.x, &start);
+  __syncthreads();
+  AttendSchedule plan(a, blockIdx.x, &start);    // every warp runs it
   const float sc = a.scale * kLog2e;
   for (;;) {
     AttendPiece p = {};

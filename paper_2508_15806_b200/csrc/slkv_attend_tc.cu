@@ -36,7 +36,10 @@ struct Smem {
   static constexpr int kStages = D == 128 ? 5 : 8;
   alignas(1024) unsigned char q[2][kTileBytes];
   alignas(1024) unsigned char kv[kStages][kTileBytes];
-  float2 ml[2][128];
+  union {
+    float2 ml[2][128];
+    AttendStart start;                           // before anything else
+  };
   AttendPiece piece[kUnits];
   unsigned long long unit_full[kUnits], unit_empty[kUnits], q_full[2], q_empty[2], kv_full[kStages], kv_empty[kStages], s_full[2],
       p_ready[2], o_full[2], merge_full, merge_done, drain;
@@ -650,8 +653,14 @@ k_attend_tc(const __grid_constant__ AttendTc t, const __grid_constant__ AttendMa
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
+  if (warp == kLoadWarp && lane < 5) {
+    const CUtensorMap* m = lane == 0 ? &maps.q : lane == 1 ? &maps.k : lane == 2 ? &maps.v : lane == 3 ? &maps.kn : &maps.vn;
+    if (lane < 3 || t.a.has_new) asm volatile("prefetch.tensormap [%0];" ::"l"(m) : "memory");
+  }
   pdl_launch_dependents();
   pdl_wait();
+  attend_start(t.a, blockIdx.x, &sm.start);
+  __syncthreads();
   if (warp >= 8) {
     regs_down<80>();
     if (warp == kLoadWarp) {
@@ -666,7 +675,7 @@ k_attend_tc(const __grid_constant__ AttendTc t, const __grid_constant__ AttendMa
       if (lane == 0) query_role<D>(t, maps, sm);
     } else if (warp == kPlanWarp) {
       if (lane == 0 && !t.a.spread) t.a.desc[2 * blockIdx.x].state = t.a.desc[2 * blockIdx.x + 1].state = 0;
-      AttendSchedule plan(t.a, blockIdx.x);
+      AttendSchedule plan(t.a, blockIdx.x, &sm.start);
       for (unsigned nth = 0;; ++nth) {
         AttendPiece p = {};
         const bool more = plan.next(&p);
