@@ -14,7 +14,7 @@ CALL = os.path.join(HERE, "_slkv_call.so")
 SOURCES = ["slkv_api.cu", "slkv_alloc.cu", "slkv_score_simt.cu", "slkv_score_tc.cu", "slkv_score_pipe.cu", "slkv_select.cu", "slkv_select_cluster.cu", "slkv_select_cta.cu",
            "slkv_layer_tc.cu", "slkv_layer_fma.cu", "slkv_bound.cu", "slkv_noalloc.cu", "slkv_behavior.cu", "slkv_cp.cu",
            "slkv_q4.cu", "slkv_q4_attend.cu", "slkv_q4_evict.cu", "slkv_q4_api.cu",
-           "slkv_attend_tc.cu", "slkv_attend_fma.cu", "slkv_paged.cu", "slkv_attend_api.cu"]
+           "slkv_attend_tc.cu", "slkv_attend_f32.cu", "slkv_attend_join.cu", "slkv_paged.cu", "slkv_attend_api.cu"]
 
 
 def _nvcc() -> str:

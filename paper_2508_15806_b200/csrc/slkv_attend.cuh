@@ -1,4 +1,4 @@
-// What the attention kernels of prompts and of paged caches share (slkv_attend_tc.cu, slkv_attend_fma.cu, slkv_attend_api.cu).
+// What the attention kernels of prompts and of paged caches share (slkv_attend_tc.cu, slkv_attend_f32.cu, slkv_attend_join.cu, slkv_attend_api.cu).
 //
 // Both are one problem: a unit is a block of query rows of one KV head -- some tokens times the G query heads that share its keys --
 // against tiles of 128 keys.  What differs is where a tile lies and which of its keys a row sees:
@@ -12,6 +12,7 @@
 namespace slkv {
 
 constexpr int kAttendTileBits = 7, kAttendTile = 1 << kAttendTileBits;                 // keys of a tile, query rows of a block
+constexpr int kF32TileBits = 6;                   // keys of a tile of fp32 rows: 64
 constexpr int kMaxDrafted = 64;                  // drafted tokens of a sequence: the bits of a mask
 constexpr int kMaxGroup = 64;                    // query heads of a KV head
 
@@ -53,9 +54,8 @@ struct AttendShape {
 
 size_t attend_workspace(int n_cta, int part_rows, int head_dim);
 void attend_bind(AttendShape* a, void* workspace);
-int attend_fma_ctas();
 cudaError_t launch_attend_tensor(const AttendShape& a, cudaStream_t st, int* launches);
-cudaError_t launch_attend_fma(const AttendShape& a, cudaStream_t st, int* launches);
+cudaError_t launch_attend_f32(const AttendShape& a, cudaStream_t st, int* launches);
 cudaError_t launch_attend_join(const AttendShape& a, bool f32, cudaStream_t st, int* launches);
 
 #ifdef __CUDACC__
@@ -72,8 +72,7 @@ struct AttendPiece {
   int stop;
 };
 
-// Row r of a unit: its token of the unit and its query head of the group; false: no row.  Rows come in blocks of 128 (the FMA kernel: one
-// block); in a block the query heads of a token lie next to each other, or the tokens of a query head (q_head_inner = 0).
+// Row r of a unit: its token of the unit and its query head of the group; false: no row.  Rows come in blocks of 128; in a block the query heads of a token lie next to each other, or the tokens of a query head (q_head_inner = 0).
 __device__ __forceinline__ bool attend_row(const AttendShape& a, int r, int* tok, int* head) {
   const int b = r >> 7, i = r & 127;
   int rt, rh;

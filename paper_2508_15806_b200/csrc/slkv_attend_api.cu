@@ -9,7 +9,6 @@ namespace {
 
 constexpr long long kMaxRows = (1ll << 31) - 512;      // tokens, rows of a pool: a tile behind the last one still has 32-bit coordinates
 constexpr int kMaxSegments = 1 << 20, kMaxLayerSegments = 16384;
-constexpr int kFmaRows = 64, kFmaFewRows = 16, kFmaKeyBits = 6;
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 bool dtype_ok(int dtype) { return dtype == SLKV_F32 || dtype == SLKV_BF16; }
@@ -38,25 +37,16 @@ int check_heads(int n_q_heads, int n_kv_heads, int head_dim, int dtype, int lse_
 
 // What follows from the types and shapes for both kernels: blocks, units, tiles.  max_tokens: of a sequence.
 void set_blocks(AttendShape* a, int dtype, long long max_tokens) {
-  a->ml_unit = dtype == SLKV_F32 ? 1.0f : a->scale * kLog2e;
-  if (dtype == SLKV_F32) {
-    // few rows: a block of 16, for which a thread has a quarter of the work
-    a->part_rows = max_tokens * a->G <= kFmaFewRows ? kFmaFewRows : kFmaRows;
-    a->block_tokens = a->unit_tokens = a->part_rows / a->G;
-    a->box_tokens = a->block_tokens;
-    a->q_head_inner = 1;
-    a->tile_bits = kFmaKeyBits;
-    a->n_cta = attend_fma_ctas();
-    a->used_rows = a->part_rows;
-  } else {
-    a->block_tokens = kAttendTile / a->G;
-    a->unit_tokens = 2 * a->block_tokens;
-    a->part_rows = max_tokens <= a->block_tokens ? kAttendTile : 2 * kAttendTile;
-    a->box_tokens = a->paged && max_tokens < a->block_tokens ? (int)max_tokens : a->block_tokens;
-    a->tile_bits = kAttendTileBits;
-    a->n_cta = sm_count();
-    a->used_rows = a->part_rows == kAttendTile ? a->box_tokens * a->G : a->part_rows;
-  }
+  a->ml_unit = a->scale * kLog2e;
+  const int blocks = dtype == SLKV_F32 ? 1 : 2;    // of 128 query rows in a unit
+  a->block_tokens = kAttendTile / a->G;
+  a->unit_tokens = blocks * a->block_tokens;
+  a->part_rows = max_tokens <= a->block_tokens ? kAttendTile : blocks * kAttendTile;
+  a->box_tokens = a->paged && max_tokens < a->block_tokens ? (int)max_tokens : a->block_tokens;
+  a->used_rows = a->part_rows == kAttendTile ? a->box_tokens * a->G : a->part_rows;
+  a->tile_bits = dtype == SLKV_F32 ? kF32TileBits : kAttendTileBits;
+  a->n_cta = sm_count();
+  a->q_head_inner = dtype == SLKV_F32 || a->q_head <= a->q_tok;
 }
 
 // ---- prompts
@@ -86,7 +76,6 @@ int check_prompt(const slkv_prompt_params* p, const int32_t* cu_q, const int32_t
   if (rc != SLKV_OK) return rc;
   a->scale = p->scale;
   set_blocks(a, p->dtype, longest);
-  if (p->dtype == SLKV_BF16) a->q_head_inner = a->q_head <= a->q_tok;
   a->lse_unit = p->lse_units == SLKV_LSE_LOG2 ? 1.0f : 0.69314718055994531f;
   // Three units or more for each CTA: whole ones, dealt out; fewer: all tiles in equal shares, pieces joined by another launch.
   long long units = 0;
@@ -158,7 +147,6 @@ int check_paged_attend(const slkv_paged_cache* c, const slkv_paged_attend_params
   a->has_new = p->has_new != 0;
   a->scale = p->scale;
   set_blocks(a, c->dtype, a->n_tokens);
-  if (c->dtype == SLKV_BF16) a->q_head_inner = a->q_head <= a->q_tok;
   a->lse_unit = p->lse_units == SLKV_LSE_LOG2 ? 1.0f : 0.69314718055994531f;
   const long long blocks = (a->n_tokens + a->unit_tokens - 1) / a->unit_tokens, longest = (long long)c->max_pages * c->page_rows;
   const long long most = blocks * a->n_seqs * a->n_kv_heads * (((longest + (1 << a->tile_bits) - 1) >> a->tile_bits) + a->has_new);
@@ -174,7 +162,7 @@ int attend(AttendShape* a, int dtype, void* workspace, size_t workspace_bytes, c
   if (!aligned16(workspace)) return SLKV_ERR_BAD_ALIGN;
   if (!a->spread) attend_bind(a, workspace);
   int launches = 0;
-  cudaError_t e = dtype == SLKV_F32 ? launch_attend_fma(*a, st, &launches) : launch_attend_tensor(*a, st, &launches);
+  cudaError_t e = dtype == SLKV_F32 ? launch_attend_f32(*a, st, &launches) : launch_attend_tensor(*a, st, &launches);
   if (e == cudaSuccess) e = launch_attend_join(*a, dtype == SLKV_F32, st, &launches);
   return report(e, launches);
 }

@@ -44,23 +44,27 @@ __device__ __forceinline__ void tc_st16(uint32_t taddr, const uint32_t (&r)[16])
       ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
         "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr) : "memory");
 }
+__device__ __forceinline__ void tc_st8(uint32_t taddr, const uint32_t (&r)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};"
+      ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(taddr) : "memory");
+}
 __device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // Matrix products.  A shared-memory descriptor is given by its low word alone, start address and leading stride; the high words are the
 // same for all operands here (128-byte-swizzled rows of 64 channels, 8-row groups 1024 bytes apart), so that a row of products costs one
-// addition each.  The leading stride matters to rows that are the summed index: the next 64 channels lie kHalfBytes further on.
+// addition each.  The leading stride matters to rows that are the summed index: the next 64 channels lie HALF bytes further on.
 constexpr uint32_t kDescHi = 64u | (1u << 14) | (2u << 29);
-__device__ __forceinline__ uint32_t desc_lo(uint32_t addr) { return ((addr >> 4) & 0x3FFFu) | ((uint32_t)(kHalfBytes >> 4) << 16); }
+template <int HALF = kHalfBytes>
+__device__ __forceinline__ uint32_t desc_lo(uint32_t addr) { return ((addr >> 4) & 0x3FFFu) | ((uint32_t)(HALF >> 4) << 16); }
 constexpr uint32_t kRowsB = 1u << 16;          // of an instruction descriptor: B's rows are the summed index
 // D (+)= A B, A and B in shared memory.
-template <bool ACC>
-__device__ __forceinline__ void tc_mma_ss(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t idesc) {
+__device__ __forceinline__ void tc_mma_ss(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t idesc, uint32_t acc) {
   asm volatile(
       "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\t"
       "setp.ne.u32 p, %5, 0;\n\t"
       "mov.b64 a, {%1, %4};\n\tmov.b64 b, {%2, %4};\n\t"
       "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n\t}"
-      ::"r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(idesc), "n"(kDescHi), "n"(ACC ? 1 : 0) : "memory");
+      ::"r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(idesc), "n"(kDescHi), "r"(acc) : "memory");
 }
 // The same with A in TMEM (a lane a row, two 16-bit values a column).
 __device__ __forceinline__ void tc_mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint32_t b_lo, uint32_t idesc, uint32_t acc) {
@@ -82,6 +86,12 @@ __device__ __forceinline__ bool mbar_poll(uint32_t bar, uint32_t parity, volatil
       if (now_ns() - t0 > kWaitLimitNs) { *abort_flag = 1; return false; }
     }
   }
+}
+
+// 32 bytes, from a 32-byte boundary.
+__device__ __forceinline__ void store32(void* to, const uint32_t* w) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]),
+               "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
 }
 
 __device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }

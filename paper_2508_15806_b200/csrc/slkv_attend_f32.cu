@@ -1,0 +1,566 @@
+// Attention of prompts and of tokens over a paged cache for fp32 rows, on the tensor cores.
+//
+// An fp32 number is the sum of three bf16 numbers, its significand in three parts of eight bits: x = x0 + x1 + x2 exactly.  A product
+// of two such sums needs six of the nine products (x0 y0, x0 y1, x1 y0, x1 y1, x0 y2, x2 y0; the others are below 2^-24 of it), which the
+// tensor cores add up in fp32: 375 TFLOP/s at six products each, against 74 on the FMA pipe.  Scores and outputs are made this way:
+//   K, V, Q   come in as fp32, are split by the warps that load them and lie in shared memory as three planes each
+//   S = Q K^T in TMEM, two buffers; a thread has a row, 64 keys a tile, with a running reference and sum in fp32
+//   P         = 2^(sc (x - m)) goes back to TMEM as three planes, two buffers; O += P V, rescaled only where m rises by more than 2^8
+// A CTA takes pieces of units (AttendSchedule) of one block of 128 query rows.
+//   warps 0-3  softmax, results      warps 4-7  K      warps 8-11  Q, V      warp 12  MMAs      warp 13  schedule
+// While the products of a tile run, the next one is loaded, split and, as soon as they are done, stored.
+//
+// A key that a row does not see gives it nothing: scores are replaced; keys behind the last one are rows of zeros; values that are not
+// finite, which 0 would not cancel, are left out of V, and rows that see them add them at the end.
+#include <atomic>
+
+#include "slkv_attend_device.cuh"
+
+namespace slkv {
+namespace {
+
+constexpr int kKeys = 1 << kF32TileBits;
+constexpr int kThreads = 512;
+constexpr int kKWarp = 4, kVWarp = 8, kMmaWarp = 12, kPlanWarp = 13;
+constexpr int kUnits = 3;                        // pieces the schedule is ahead by
+constexpr float kLift = 8.0f;                    // log2 of how far P may exceed 1 before the reference is raised
+constexpr int kTmemS = 0, kTmemP = 2 * kKeys, kPlaneCols = kKeys / 2, kTmemO = kTmemP + 2 * 3 * kPlaneCols;
+constexpr int kRowHalf = kKeys * 128;            // bytes of 64 channels of a tile's rows, one plane
+
+template <int D>
+struct Smem {
+  static constexpr int kHalves = D / 64;
+  static constexpr int kQPlane = kHalves * kHalfBytes, kKPlane = kHalves * kRowHalf;
+  alignas(1024) unsigned char q[3][kQPlane];
+  alignas(1024) unsigned char k[3][kKPlane];
+  alignas(1024) unsigned char v[3][kKPlane];
+  AttendPiece piece[kUnits];
+  unsigned long long unit_full[kUnits], unit_empty[kUnits], q_full, q_empty, k_full, k_empty, v_full, v_empty, s_full[2], p_ready[2], pv_done,
+      drain;
+  int odd_lo[2][4], odd_hi[2][4];                // tiles of a piece, by its parity, where a warp of V met values that are not finite
+  int abort;
+  uint32_t tmem;
+  AttendStart start;
+};
+
+struct AttendF32 {
+  AttendShape a;
+  int page_bits;
+  int wide;                                      // rows of out begin at 32-byte boundaries
+  int extra_arrival;                             // 1: a test makes the first CTA's wait for P run out
+};
+
+// Row j of a piece's tile, as it lies in memory; null: there is none.
+template <bool V>
+__device__ __forceinline__ const float* key_row(const AttendF32& t, const AttendPiece& p, int tile, int j) {
+  const AttendShape& a = t.a;
+  if (a.paged) {
+    if (a.has_new && tile == p.n_all - 1) {
+      if (j >= p.n_seq_tok) return nullptr;
+      return V ? static_cast<const float*>(a.v_new) + p.s * a.vn_seq + j * a.vn_tok + p.h * a.vn_head
+               : static_cast<const float*>(a.k_new) + p.s * a.kn_seq + j * a.kn_tok + p.h * a.kn_head;
+    }
+    const int row = tile * kKeys + j;
+    if (row >= p.nk) return nullptr;
+    const int id = __ldg(a.tables + (long long)(p.s * a.n_kv_heads + p.h) * a.max_pages + (row >> t.page_bits));
+    if ((unsigned)id >= (unsigned)a.n_pages) {
+      if (a.status) *a.status = SLKV_ERR_BAD_SHAPE;
+      return nullptr;
+    }
+    const long long at = (((long long)id << t.page_bits) + (row & (a.page_rows - 1))) * a.head_dim;
+    return static_cast<const float*>(V ? a.v : a.k) + at;
+  }
+  const int row = tile * kKeys + j;
+  if (row >= p.nk) return nullptr;
+  const long long at = p.k_row + row;
+  return V ? static_cast<const float*>(a.v) + at * a.v_tok + p.h * a.v_head : static_cast<const float*>(a.k) + at * a.k_tok + p.h * a.k_head;
+}
+
+// Three planes of eight numbers: the upper 16 bits of x, of what is left of it, and of what is left then.
+__device__ __forceinline__ void split8(const float (&x)[8], uint4& p0, uint4& p1, uint4& p2) {
+  uint32_t w[3][4];
+#pragma unroll
+  for (int e = 0; e < 8; e += 2) {
+    uint32_t b0[2], b1[2], b2[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float v = x[e + i];
+      b0[i] = __float_as_uint(v);
+      const float r = v - __uint_as_float(b0[i] & 0xffff0000u);
+      b1[i] = __float_as_uint(r);
+      b2[i] = __float_as_uint(r - __uint_as_float(b1[i] & 0xffff0000u));
+    }
+    w[0][e / 2] = __byte_perm(b0[0], b0[1], 0x7632);
+    w[1][e / 2] = __byte_perm(b1[0], b1[1], 0x7632);
+    w[2][e / 2] = __byte_perm(b2[0], b2[1], 0x7632);
+  }
+  p0 = make_uint4(w[0][0], w[0][1], w[0][2], w[0][3]);
+  p1 = make_uint4(w[1][0], w[1][1], w[1][2], w[1][3]);
+  p2 = make_uint4(w[2][0], w[2][1], w[2][2], w[2][3]);
+}
+
+// Eight channels of a row into three planes of 128-byte-swizzled rows.
+template <int HALF, int PLANE>
+__device__ __forceinline__ void store_planes(unsigned char* base, int row, int chunk, const float (&x)[8]) {
+  uint4 p0, p1, p2;
+  split8(x, p0, p1, p2);
+  unsigned char* at = base + (chunk >> 3) * HALF + row * 128 + (((chunk & 7) ^ (row & 7)) << 4);
+  *reinterpret_cast<uint4*>(at) = p0;
+  *reinterpret_cast<uint4*>(at + PLANE) = p1;
+  *reinterpret_cast<uint4*>(at + 2 * PLANE) = p2;
+}
+
+__device__ __forceinline__ void load8(const float* from, float (&x)[8]) {
+  const float4 a = *reinterpret_cast<const float4*>(from), b = *reinterpret_cast<const float4*>(from + 4);
+  x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
+  x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+}
+
+// The warps of K (V = false) or of Q and V.
+template <int D, bool V>
+__device__ __forceinline__ void rows_role(const AttendF32& t, Smem<D>& sm) {
+  using S = Smem<D>;
+  const AttendShape& a = t.a;
+  constexpr int kChunks = D / 8, kMine = kKeys * kChunks / 128;      // eight channels each: of a row, of a thread
+  const int tid = threadIdx.x & 127, lane = threadIdx.x & 31;
+  const int row0 = tid / kChunks, chunk = tid % kChunks;
+  unsigned long long* const full = V ? &sm.v_full : &sm.k_full;
+  unsigned long long* const empty = V ? &sm.v_empty : &sm.k_empty;
+  auto wait = [&](unsigned long long* bar, unsigned phase) {
+    return __all_sync(0xffffffffu, mbar_wait(smem_u32(bar), phase & 1, &sm.abort)) != 0;
+  };
+  unsigned done = 0, n_q = 0;                    // tiles, blocks of query rows
+  for (unsigned nth = 0;; ++nth) {
+    if (!wait(&sm.unit_full[nth % kUnits], nth / kUnits)) return;
+    const AttendPiece p = sm.piece[nth % kUnits];
+    __syncwarp();
+    if (lane == 0) mbar_arrive(smem_u32(&sm.unit_empty[nth % kUnits]));
+    if (p.stop) return;
+    if (p.n == 0) continue;
+    float x[kMine][8];
+    auto load = [&](int tile) {
+#pragma unroll
+      for (int u = 0; u < kMine; ++u) {
+        const float* from = key_row<V>(t, p, tile, row0 + u * (128 / kChunks));
+        if (from) {
+          load8(from + 8 * chunk, x[u]);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[u][e] = 0.0f;
+        }
+      }
+    };
+    load(p.tile0);
+    if (V) {
+      if (n_q > 0 && !wait(&sm.q_empty, n_q - 1)) return;
+      ++n_q;
+      const float* from = static_cast<const float*>(a.q) + (a.paged ? p.s * a.q_seq : p.q_row * a.q_tok) + p.tok0 * a.q_tok + p.h * a.G * a.q_head;
+      const int rows = p.n_tok * a.G;
+#pragma unroll 2
+      for (int r = row0; r < 128; r += 128 / kChunks) {
+        float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        const int rt = r / a.G;
+        if (r < rows) load8(from + rt * a.q_tok + (r - rt * a.G) * a.q_head + 8 * chunk, y);
+        store_planes<kHalfBytes, S::kQPlane>(sm.q[0], r, chunk, y);
+      }
+      fence_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&sm.q_full));
+    }
+    for (int i = 0; i < p.n; ++i, ++done) {
+      if (done > 0 && !wait(empty, done - 1)) return;
+      if (V && i == 0) {                         // the piece before the last one has been written
+        if (lane == 0) {
+          sm.odd_lo[nth & 1][tid >> 5] = 0x7fffffff;
+          sm.odd_hi[nth & 1][tid >> 5] = -1;
+        }
+        __syncwarp();
+      }
+      bool odd = false;
+#pragma unroll
+      for (int u = 0; u < kMine; ++u) {
+        if (V) {
+          bool here = false;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) here |= !(fabsf(x[u][e]) < INFINITY);
+          if (here) {
+            odd = true;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[u][e] = fabsf(x[u][e]) < INFINITY ? x[u][e] : 0.0f;
+          }
+        }
+        store_planes<kRowHalf, S::kKPlane>(V ? sm.v[0] : sm.k[0], row0 + u * (128 / kChunks), chunk, x[u]);
+      }
+      if (V && odd) {
+        atomicMin(&sm.odd_lo[nth & 1][tid >> 5], p.tile0 + i);
+        atomicMax(&sm.odd_hi[nth & 1][tid >> 5], p.tile0 + i);
+      }
+      fence_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(full));
+      if (i + 1 < p.n) load(p.tile0 + i + 1);
+    }
+  }
+}
+
+// The six products of three planes each, the small ones first: planes of A and of B, two bits each.
+constexpr int kPairs = 6;
+constexpr uint32_t kPlanesA = 0u | 2u << 2 | 1u << 4 | 0u << 6 | 1u << 8 | 0u << 10;
+constexpr uint32_t kPlanesB = 2u | 0u << 2 | 1u << 4 | 1u << 6 | 0u << 8 | 0u << 10;
+
+template <int D>
+__device__ __forceinline__ bool mma_role(const AttendF32& t, Smem<D>& sm) {
+  using S = Smem<D>;
+  const uint32_t tmem = sm.tmem;
+  const bool issuer = (threadIdx.x & 31) == 0;
+  constexpr uint32_t kIdS = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kKeys >> 3) << 17) | (8u << 24);
+  constexpr uint32_t kIdO = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(D >> 3) << 17) | (8u << 24) | kRowsB;
+  const uint32_t qa = desc_lo(smem_u32(sm.q[0])), ka = desc_lo(smem_u32(sm.k[0])), va = desc_lo<kRowHalf>(smem_u32(sm.v[0]));
+  auto wait = [&](unsigned long long* bar, unsigned phase) {
+    return __all_sync(0xffffffffu, mbar_poll(smem_u32(bar), phase & 1, &sm.abort)) != 0;
+  };
+  unsigned done = 0, n_q = 0;                    // tiles
+  for (unsigned nth = 0;; ++nth) {
+    if (!wait(&sm.unit_full[nth % kUnits], nth / kUnits)) return false;
+    const AttendPiece p = sm.piece[nth % kUnits];
+    __syncwarp();
+    if (issuer) mbar_arrive(smem_u32(&sm.unit_empty[nth % kUnits]));
+    if (p.stop) return true;
+    if (p.n == 0) continue;
+    if (!wait(&sm.q_full, n_q++)) return false;
+    for (int i = 0; i <= p.n; ++i) {
+      if (i < p.n) {
+        const unsigned no = done + i;
+        if (!wait(&sm.k_full, no)) return false;
+        tc_fence_after();
+        if (issuer) {
+          const uint32_t d = tmem + kTmemS + (no & 1) * kKeys;
+#pragma unroll 1
+          for (int c = 0; c < kPairs; ++c) {
+            const uint32_t ap = qa + ((kPlanesA >> (2 * c) & 3u) * S::kQPlane >> 4), bp = ka + ((kPlanesB >> (2 * c) & 3u) * S::kKPlane >> 4);
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k)
+              tc_mma_ss(d, ap + (((k >> 2) * kHalfBytes + (k & 3) * 32) >> 4), bp + (((k >> 2) * kRowHalf + (k & 3) * 32) >> 4), kIdS, k > 0 ? 1 : c > 0);
+          }
+          tc_commit(smem_u32(&sm.s_full[no & 1]));
+          tc_commit(smem_u32(&sm.k_empty));
+          if (i + 1 == p.n) tc_commit(smem_u32(&sm.q_empty));
+        }
+        __syncwarp();
+      }
+      if (i > 0) {
+        const unsigned no = done + i - 1;
+        if (!wait(&sm.v_full, no)) return false;
+        if (!wait(&sm.p_ready[no & 1], no >> 1)) return false;
+        tc_fence_after();
+        if (issuer) {
+          const uint32_t d = tmem + kTmemO, pa = tmem + kTmemP + (no & 1) * 3 * kPlaneCols;
+#pragma unroll 1
+          for (int c = 0; c < kPairs; ++c) {
+            const uint32_t ap = pa + (kPlanesA >> (2 * c) & 3u) * kPlaneCols, bp = va + ((kPlanesB >> (2 * c) & 3u) * S::kKPlane >> 4);
+#pragma unroll
+            for (int k = 0; k < kKeys / 16; ++k) tc_mma_ts(d, ap + 8 * k, bp + k * 128, kIdO, k > 0 ? 1 : i > 1 || c > 0);
+          }
+          tc_commit(smem_u32(&sm.v_empty));
+          tc_commit(smem_u32(&sm.pv_done));
+        }
+        __syncwarp();
+      }
+    }
+    done += p.n;
+  }
+}
+
+__device__ __forceinline__ uint32_t seen_below(int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u; }
+
+// Values of V that are not finite, of the tiles lo .. hi: rows that see them get them, in the results that the thread has written.
+__device__ __forceinline__ void put_back(const AttendF32& t, const AttendPiece& p, int lo, int hi, int bound, unsigned long long mask, float* out) {
+  const AttendShape& a = t.a;
+  for (int tile = lo; tile <= hi; ++tile)
+    for (int j = 0; j < kKeys; ++j) {
+      const bool drafted = a.has_new && tile == p.n_all - 1;
+      if (drafted ? !(mask >> j & 1) : !a.paged && tile * kKeys + j >= bound) continue;
+      const float* v = key_row<true>(t, p, tile, j);
+      if (!v) continue;
+      for (int ch = 0; ch < a.head_dim; ++ch)
+        if (!(fabsf(v[ch]) < INFINITY)) out[ch] += v[ch];
+    }
+}
+
+template <int D>
+__device__ __forceinline__ void softmax_role(const AttendF32& t, Smem<D>& sm) {
+  const AttendShape& a = t.a;
+  const int row = threadIdx.x, lane = threadIdx.x & 31;
+  const float sc = a.ml_unit;
+  const uint32_t lanes = sm.tmem + ((uint32_t)(row >> 5) << 21);
+  const f32x2 sc2 = pack2(sc, sc);
+  auto wait = [&](unsigned long long* bar, unsigned phase) {
+    return __all_sync(0xffffffffu, mbar_wait(smem_u32(bar), phase & 1, &sm.abort)) != 0;
+  };
+  unsigned done = 0;
+  for (unsigned nth = 0;; ++nth) {
+    if (!wait(&sm.unit_full[nth % kUnits], nth / kUnits)) return;
+    const AttendPiece p = sm.piece[nth % kUnits];
+    __syncwarp();
+    if (lane == 0) mbar_arrive(smem_u32(&sm.unit_empty[nth % kUnits]));
+    if (p.stop) return;
+    int rt, rh;
+    const bool there = attend_row(a, row, &rt, &rh) && rt < p.n_tok;
+    const int tok = p.tok0 + rt, bound = max(min(tok + 1 + p.shift, p.nk), 0);
+    unsigned long long mask = 0;
+    if (a.has_new && there) {
+      mask = a.tree ? a.tree[(long long)p.s * a.n_tokens + tok] : ~0ull >> (63 - tok);
+      mask &= ~0ull >> (64 - p.n_seq_tok);
+    }
+    const bool work = __any_sync(0xffffffffu, there);
+    float m = -INFINITY, l = 0.0f;
+#pragma unroll 1
+    for (int i = 0; i < p.n; ++i, ++done) {
+      const int tile = p.tile0 + i;
+      const bool drafted = a.has_new && tile == p.n_all - 1;
+      const int end = a.paged ? (drafted ? 0 : p.nk - tile * kKeys) : bound - tile * kKeys;     // keys that the row sees
+      if (!wait(&sm.s_full[done & 1], done >> 1)) return;
+      tc_fence_after();
+      if (work) {
+        uint32_t r[2][32];
+        const uint32_t ts = lanes + kTmemS + (done & 1) * kKeys, tp = lanes + kTmemP + (done & 1) * 3 * kPlaneCols;
+        tc_ld32(ts, r[0]);
+        tc_ld32(ts + 32, r[1]);
+        tc_wait_ld(r[0]);
+        tc_wait_ld(r[1]);
+        if (__any_sync(0xffffffffu, drafted || end < kKeys)) {
+#pragma unroll
+          for (int q = 0; q < 2; ++q) {
+            const uint32_t see = drafted ? (uint32_t)(mask >> (32 * q)) : seen_below(end - 32 * q);
+#pragma unroll
+            for (int e = 0; e < 32; ++e) r[q][e] = see >> e & 1u ? r[q][e] : 0xff800000u;
+          }
+        }
+        float mx[2];
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          mx[q] = __uint_as_float(r[q][0]);
+#pragma unroll
+          for (int e = 1; e < 31; e += 2) mx[q] = fmaxf(fmaxf(mx[q], __uint_as_float(r[q][e])), __uint_as_float(r[q][e + 1]));
+          mx[q] = fmaxf(mx[q], __uint_as_float(r[q][31]));
+        }
+        const float top = fmaxf(mx[0], mx[1]);
+        if (i == 0) {
+          m = top;
+        } else {
+          const bool lift = (top - m) * sc > kLift;        // m = -infinity: any score lifts it
+          if (__any_sync(0xffffffffu, lift)) {
+            if (!wait(&sm.pv_done, done - 1)) return;
+            tc_fence_after();
+            const float f = lift ? ex2((m - top) * sc) : 1.0f;
+            if (lift) { m = top; l *= f; }
+#pragma unroll 1
+            for (int ch = 0; ch < D; ch += 16) {
+              uint32_t o[16];
+              tc_ld16_issue(lanes + kTmemO + ch, o);
+              tc_ld_wait(o);
+#pragma unroll
+              for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+              tc_st16(lanes + kTmemO + ch, o);
+            }
+          }
+        }
+        // 2^(sc x - sc m) with one rounding of the difference, which is as large as sc m 2^-24: where that is much, differences first
+        float base = m == -INFINITY ? 0.0f : m;
+        if (__any_sync(0xffffffffu, fabsf(base) * sc > 0x1p20f)) {
+#pragma unroll
+          for (int q = 0; q < 2; ++q)
+#pragma unroll
+            for (int e = 0; e < 32; ++e) r[q][e] = __float_as_uint(__uint_as_float(r[q][e]) - base);
+          base = 0.0f;
+        }
+        const float nm = -base * sc;
+        const f32x2 nm2 = pack2(nm, nm);
+        f32x2 s0 = 0, s1 = 0;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {            // sixteen keys at a time
+          uint32_t w[3][8];
+          const uint32_t* x = r[q >> 1] + 16 * (q & 1);
+#pragma unroll
+          for (int e = 0; e < 16; e += 8) {
+            float y[8];
+#pragma unroll
+            for (int f = 0; f < 8; f += 2) {
+              const f32x2 pr = ex2_pair(fma2(pack2(__uint_as_float(x[e + f]), __uint_as_float(x[e + f + 1])), sc2, nm2));
+              if (f & 2) s1 = add2(s1, pr); else s0 = add2(s0, pr);
+              unpack2(pr, y[f], y[f + 1]);
+            }
+            uint4 p0, p1, p2;
+            split8(y, p0, p1, p2);
+            w[0][e / 2] = p0.x; w[0][e / 2 + 1] = p0.y; w[0][e / 2 + 2] = p0.z; w[0][e / 2 + 3] = p0.w;
+            w[1][e / 2] = p1.x; w[1][e / 2 + 1] = p1.y; w[1][e / 2 + 2] = p1.z; w[1][e / 2 + 3] = p1.w;
+            w[2][e / 2] = p2.x; w[2][e / 2 + 1] = p2.y; w[2][e / 2 + 2] = p2.z; w[2][e / 2 + 3] = p2.w;
+          }
+#pragma unroll
+          for (int c = 0; c < 3; ++c) tc_st8(tp + c * kPlaneCols + 8 * q, w[c]);
+        }
+        l += sum2(s0, s1);
+      }
+      tc_wait_st();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&sm.p_ready[done & 1]));
+    }
+    // ---- results
+    if (p.n > 0) {
+      // the last tile's scores came behind the product two tiles before it: one phase after the other
+      if (p.n > 1 && !wait(&sm.pv_done, done - 2)) return;
+      if (!wait(&sm.pv_done, done - 1)) return;
+      tc_fence_after();
+    }
+    if (!work) continue;
+    const bool whole = p.part < 0;
+    const float inv = !whole ? 1.0f : l > 0.0f || l != l ? 1.0f / l : 0.0f;
+    const long long place = (long long)(blockIdx.x * 2 + p.part) * a.part_rows + row;
+    float* const dst = whole ? static_cast<float*>(a.out) + (a.paged ? p.s * a.o_seq : p.q_row * a.o_tok) + tok * a.o_tok + (p.h * a.G + rh) * a.o_head
+                             : a.part + place * D;
+#pragma unroll 1
+    for (int ch = 0; ch < D; ch += 16) {
+      uint32_t o[16];
+      if (p.n > 0) {
+        tc_ld16_issue(lanes + kTmemO + ch, o);
+        tc_ld_wait(o);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[e] = 0;
+      }
+      if (there) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * inv);
+        if (t.wide || !whole) {
+          store32(dst + ch, o);
+          store32(dst + ch + 8, o + 8);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 16; e += 4) *reinterpret_cast<uint4*>(dst + ch + e) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+        }
+      }
+      __syncwarp();                              // the next load is the whole warp's
+    }
+    if (there) {
+      int lo = 0x7fffffff, hi = -1;
+#pragma unroll
+      for (int w = 0; w < 4 && p.n > 0; ++w) {
+        lo = min(lo, *(volatile int*)&sm.odd_lo[nth & 1][w]);
+        hi = max(hi, *(volatile int*)&sm.odd_hi[nth & 1][w]);
+      }
+      if (hi >= 0) put_back(t, p, lo, hi, bound, mask, dst);
+      if (whole) attend_lse(a, p.s, p.h * a.G + rh, tok, p.n_seq_tok, m * sc, l);
+      else a.ml[place] = make_float2(m, l);
+    }
+    __syncwarp();
+  }
+}
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1) k_attend_f32(const __grid_constant__ AttendF32 t) {
+  extern __shared__ __align__(1024) unsigned char raw[];
+  Smem<D>& sm = *reinterpret_cast<Smem<D>*>(raw);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kUnits; ++i) {
+      mbar_init(smem_u32(&sm.unit_full[i]), 1);
+      mbar_init(smem_u32(&sm.unit_empty[i]), 13);
+    }
+    mbar_init(smem_u32(&sm.q_full), 4);
+    mbar_init(smem_u32(&sm.q_empty), 1);
+    mbar_init(smem_u32(&sm.k_full), 4);
+    mbar_init(smem_u32(&sm.k_empty), 1);
+    mbar_init(smem_u32(&sm.v_full), 4);
+    mbar_init(smem_u32(&sm.v_empty), 1);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(smem_u32(&sm.s_full[i]), 1);
+      mbar_init(smem_u32(&sm.p_ready[i]), 4 + (blockIdx.x == 0 ? t.extra_arrival : 0));
+    }
+    mbar_init(smem_u32(&sm.pv_done), 1);
+    mbar_init(smem_u32(&sm.drain), 1);
+    sm.abort = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == kMmaWarp) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&sm.tmem)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  pdl_launch_dependents();
+  pdl_wait();
+  attend_start(t.a, blockIdx.x, &sm.start);
+  __syncthreads();
+  if (warp < kKWarp) {
+    softmax_role<D>(t, sm);
+  } else if (warp < kVWarp) {
+    rows_role<D, false>(t, sm);
+  } else if (warp < kMmaWarp) {
+    rows_role<D, true>(t, sm);
+  } else if (warp == kMmaWarp) {
+    if (!mma_role<D>(t, sm) && lane == 0) {      // a wait ran out: what is under way ends first
+      volatile int never = 0;
+      tc_commit(smem_u32(&sm.drain));
+      mbar_wait(smem_u32(&sm.drain), 0, &never);
+    }
+  } else if (warp == kPlanWarp) {
+    if (lane == 0 && !t.a.spread) t.a.desc[2 * blockIdx.x].state = t.a.desc[2 * blockIdx.x + 1].state = 0;
+    AttendSchedule plan(t.a, blockIdx.x, &sm.start);
+    for (unsigned nth = 0;; ++nth) {
+      AttendPiece p = {};
+      const bool more = plan.next(&p);
+      p.stop = !more;
+      if (nth >= (unsigned)kUnits) {
+        const bool ok = mbar_wait(smem_u32(&sm.unit_empty[nth % kUnits]), (nth / kUnits - 1) & 1, &sm.abort);
+        if (!__all_sync(0xffffffffu, ok)) break;
+      }
+      if (lane == 0) {
+        sm.piece[nth % kUnits] = p;
+        mbar_arrive(smem_u32(&sm.unit_full[nth % kUnits]));
+        if (more && p.part >= 0) attend_note(t.a, p.part, p, p.part == 1 ? plan.pieces() : 0);
+      }
+      if (!more) break;
+    }
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (sm.abort && threadIdx.x == 0) {
+    if (t.a.status) *t.a.status = SLKV_ERR_DEVICE_TIMEOUT;
+    if (!t.a.spread) t.a.desc[2 * blockIdx.x].state = t.a.desc[2 * blockIdx.x + 1].state = -1;
+  }
+  if (warp == kMmaWarp)
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(sm.tmem) : "memory");
+}
+
+template <int D>
+cudaError_t launch(const AttendF32& t, cudaStream_t st, int* launches) {
+  static_assert(sizeof(Smem<D>) <= kSmemLimit, "shared memory of a CTA");
+  static std::atomic<bool> allowed[16];
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev >= 16 || !allowed[dev].load(std::memory_order_relaxed)) {
+    e = cudaFuncSetAttribute(k_attend_f32<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Smem<D>));
+    if (e != cudaSuccess) return e;
+    if (dev < 16) allowed[dev].store(true, std::memory_order_relaxed);
+  }
+  LaunchScope scope(KID_ATTEND, st, launches);
+  return launch_pdl(k_attend_f32<D>, dim3((unsigned)t.a.n_cta), dim3(kThreads), sizeof(Smem<D>), st, 1, t);
+}
+
+}  // namespace
+
+cudaError_t launch_attend_f32(const AttendShape& a, cudaStream_t st, int* launches) {
+  AttendF32 t = {};
+  t.a = a;
+  for (t.page_bits = 0; a.paged && (1 << t.page_bits) < a.page_rows;) ++t.page_bits;
+  t.wide = reinterpret_cast<uintptr_t>(a.out) % 32 == 0 && a.o_tok % 8 == 0 && a.o_head % 8 == 0 && (!a.paged || a.o_seq % 8 == 0);
+  t.extra_arrival = take_expire_next_copy_wait() ? 1 : 0;
+  return a.head_dim == 128 ? launch<128>(t, st, launches) : launch<64>(t, st, launches);
+}
+
+}  // namespace slkv

@@ -253,11 +253,10 @@ __device__ __forceinline__ bool mma_role(const AttendTc& t, Smem<D>& sm) {
     auto qk = [&](int g, int i) {                // by the issuer
       const unsigned slot = (loads + b.k_load(b.tile(g, i))) % S::kStages, block = (n_q + (b.alt ? 0 : g)) & 1;
       const uint32_t qa = desc_lo(smem_u32(sm.q[block])), ka = desc_lo(smem_u32(sm.kv[slot])), d = tmem + kTmemS + 128 * g;
-      tc_mma_ss<false>(d, qa, ka, kIdS);
-#pragma unroll
-      for (int k = 1; k < D / 16; ++k) {
+      #pragma unroll
+      for (int k = 0; k < D / 16; ++k) {
         const uint32_t off = ((k >> 2) * kHalfBytes + (k & 3) * 32) >> 4;
-        tc_mma_ss<true>(d, qa + off, ka + off, kIdS);
+        tc_mma_ss(d, qa + off, ka + off, kIdS, k > 0);
       }
       tc_commit(smem_u32(&sm.s_full[g]));
       if (b.alt || g == 1) tc_commit(smem_u32(&sm.kv_empty[slot]));
@@ -393,12 +392,6 @@ __device__ __noinline__ void put_back(const AttendTc& t, const AttendPiece& p, i
       }
     }
   }
-}
-
-// 32 bytes, from a 32-byte boundary.
-__device__ __forceinline__ void store32(void* to, const uint32_t* w) {
-  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]),
-               "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
 }
 
 template <int D>
