@@ -212,7 +212,6 @@ template <int D>
 __device__ __forceinline__ bool mma_role(const AttendF32& t, Smem<D>& sm) {
   using S = Smem<D>;
   const uint32_t tmem = sm.tmem;
-  const bool issuer = (threadIdx.x & 31) == 0;
   constexpr uint32_t kIdS = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kKeys >> 3) << 17) | (8u << 24);
   constexpr uint32_t kIdO = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(D >> 3) << 17) | (8u << 24) | kRowsB;
   const uint32_t qa = desc_lo(smem_u32(sm.q[0])), ka = desc_lo(smem_u32(sm.k[0])), va = desc_lo<kRowHalf>(smem_u32(sm.v[0]));
@@ -224,7 +223,7 @@ __device__ __forceinline__ bool mma_role(const AttendF32& t, Smem<D>& sm) {
     if (!wait(&sm.unit_full[nth % kUnits], nth / kUnits)) return false;
     const AttendPiece p = sm.piece[nth % kUnits];
     __syncwarp();
-    if (issuer) mbar_arrive(smem_u32(&sm.unit_empty[nth % kUnits]));
+    if (elect_one()) mbar_arrive(smem_u32(&sm.unit_empty[nth % kUnits]));
     if (p.stop) return true;
     if (p.n == 0) continue;
     if (!wait(&sm.q_full, n_q++)) return false;
@@ -233,7 +232,7 @@ __device__ __forceinline__ bool mma_role(const AttendF32& t, Smem<D>& sm) {
         const unsigned no = done + i;
         if (!wait(&sm.k_full, no)) return false;
         tc_fence_after();
-        if (issuer) {
+        if (elect_one()) {
           const uint32_t d = tmem + kTmemS + (no & 1) * kKeys;
 #pragma unroll 1
           for (int c = 0; c < kPairs; ++c) {
@@ -253,7 +252,7 @@ __device__ __forceinline__ bool mma_role(const AttendF32& t, Smem<D>& sm) {
         if (!wait(&sm.v_full, no)) return false;
         if (!wait(&sm.p_ready[no & 1], no >> 1)) return false;
         tc_fence_after();
-        if (issuer) {
+        if (elect_one()) {
           const uint32_t d = tmem + kTmemO, pa = tmem + kTmemP + (no & 1) * 3 * kPlaneCols;
 #pragma unroll 1
           for (int c = 0; c < kPairs; ++c) {
@@ -500,7 +499,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_f32(const __grid_constan
   } else if (warp < kMmaWarp) {
     rows_role<D, true>(t, sm);
   } else if (warp == kMmaWarp) {
-    if (!mma_role<D>(t, sm) && lane == 0) {      // a wait ran out: what is under way ends first
+    if (!mma_role<D>(t, sm) && elect_one()) {    // a wait ran out: what is under way ends first
       volatile int never = 0;
       tc_commit(smem_u32(&sm.drain));
       mbar_wait(smem_u32(&sm.drain), 0, &never);

@@ -227,7 +227,6 @@ __device__ __forceinline__ bool mma_role(const AttendTc& t, Smem<D>& sm) {
   using S = Smem<D>;
   const AttendShape& a = t.a;
   const uint32_t tmem = sm.tmem;
-  const bool issuer = (threadIdx.x & 31) == 0;
   constexpr uint32_t kIdS = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kAttendTile >> 3) << 17) | (8u << 24);
   constexpr uint32_t kIdO = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(D >> 3) << 17) | (8u << 24) | kRowsB;
   unsigned loads = 0, n_q = 0, n_p[2] = {0, 0};
@@ -238,7 +237,7 @@ __device__ __forceinline__ bool mma_role(const AttendTc& t, Smem<D>& sm) {
     if (!wait(&sm.unit_full[nth % kUnits], nth / kUnits)) return false;
     const AttendPiece p = sm.piece[nth % kUnits];
     __syncwarp();
-    if (issuer) mbar_arrive(smem_u32(&sm.unit_empty[nth % kUnits]));
+    if (elect_one()) mbar_arrive(smem_u32(&sm.unit_empty[nth % kUnits]));
     if (p.stop) return true;
     if (p.n == 0) continue;
     const Blocks b(t, p);
@@ -267,12 +266,12 @@ __device__ __forceinline__ bool mma_role(const AttendTc& t, Smem<D>& sm) {
         const unsigned block = n_q + g;
         if (!wait(&sm.q_full[block & 1], block >> 1)) return false;
         // a block that sees none of the tiles
-        if (b.n[g] == 0 && issuer) mbar_arrive(smem_u32(&sm.q_empty[block & 1]));
+        if (b.n[g] == 0 && elect_one()) mbar_arrive(smem_u32(&sm.q_empty[block & 1]));
       }
       if (b.n[g] == 0) continue;
       if (!k_there(g, 0)) return false;
       tc_fence_after();
-      if (issuer) qk(g, 0);
+      if (elect_one()) qk(g, 0);
       __syncwarp();
     }
     const int steps = max(b.n[0], b.n[1]);
@@ -292,7 +291,7 @@ __device__ __forceinline__ bool mma_role(const AttendTc& t, Smem<D>& sm) {
         const uint32_t va = desc_lo(smem_u32(sm.kv[slot])), d = tmem + kTmemO + 128 * g, pa = tmem + kTmemS + 128 * g;
         if (!wait(&sm.p_ready[g], n_p[g]++)) return false;
         tc_fence_after();
-        if (issuer) {
+        if (elect_one()) {
           if (used == kAttendTile) {
 #pragma unroll
             for (int k = 0; k < kAttendTile / 16; ++k) tc_mma_ts(d, pa + 8 * k, va + k * 128, kIdO, k > 0 ? 1 : i > 0);
@@ -659,7 +658,7 @@ k_attend_tc(const __grid_constant__ AttendTc t, const __grid_constant__ AttendMa
     if (warp == kLoadWarp) {
       load_role<D>(t, maps, sm);
     } else if (warp == kMmaWarp) {
-      if (!mma_role<D>(t, sm) && lane == 0) {    // a wait ran out: what is under way ends first
+      if (!mma_role<D>(t, sm) && elect_one()) {  // a wait ran out: what is under way ends first
         volatile int never = 0;
         tc_commit(smem_u32(&sm.drain));
         mbar_wait(smem_u32(&sm.drain), 0, &never);
