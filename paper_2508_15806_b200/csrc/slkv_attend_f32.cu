@@ -5,10 +5,13 @@
 // tensor cores add up in fp32: 375 TFLOP/s at six products each, against 74 on the FMA pipe.  Scores and outputs are made this way:
 //   K, V, Q   come in as fp32, are split by the warps that load them and lie in shared memory as three planes each
 //   S = Q K^T in TMEM, two buffers; a thread has a row, 64 keys a tile, with a running reference and sum in fp32
-//   P         = 2^(sc (x - m)) goes back to TMEM as three planes, two buffers; O += P V, rescaled only where m rises by more than 2^8
+//   P         = 2^(sc (x - m)) goes back to TMEM as three planes; O += P V, rescaled only where m rises by more than 2^8
+// The tensor cores cut off what they add to an accumulator: over 16000 keys the outputs came out 2 10^-5 too small.  So O holds
+// kFlush tiles, whose sum the softmax warps add to that of the tiles before, rounded to nearest (1.7 10^-6 off, as sums in fp32 are).
 // A CTA takes pieces of units (AttendSchedule) of one block of 128 query rows.
 //   warps 0-3  softmax, results      warps 4-7  K      warps 8-11  Q, V      warp 12  MMAs      warp 13  schedule
-// While the products of a tile run, the next one is loaded, split and, as soon as they are done, stored.
+// K and V are handed over in blocks of 64 channels, two buffers each: while the products with one block run, the next is split and stored,
+// and the one behind it is on its way into registers.
 //
 // A key that a row does not see gives it nothing: scores are replaced; keys behind the last one are rows of zeros; values that are not
 // finite, which 0 would not cancel, are left out of V, and rows that see them add them at the end.
@@ -24,19 +27,21 @@ constexpr int kThreads = 512;
 constexpr int kKWarp = 4, kVWarp = 8, kMmaWarp = 12, kPlanWarp = 13;
 constexpr int kUnits = 3;                        // pieces the schedule is ahead by
 constexpr float kLift = 8.0f;                    // log2 of how far P may exceed 1 before the reference is raised
-constexpr int kTmemS = 0, kTmemP = 2 * kKeys, kPlaneCols = kKeys / 2, kTmemO = kTmemP + 2 * 3 * kPlaneCols;
-constexpr int kRowHalf = kKeys * 128;            // bytes of 64 channels of a tile's rows, one plane
+constexpr int kFlush = 8;                        // tiles whose products are added up in TMEM
+constexpr int kTmemS = 0, kTmemP = 2 * kKeys, kPlaneCols = kKeys / 2, kTmemO = 256, kTmemSum = 384;   // P has 3 kPlaneCols columns
+static_assert(kTmemP + 3 * kPlaneCols <= kTmemO, "columns");
+constexpr int kPlane = kKeys * 128;              // bytes of a block of K or V, 64 channels of a tile's rows, one plane
 
 template <int D>
 struct Smem {
   static constexpr int kHalves = D / 64;
-  static constexpr int kQPlane = kHalves * kHalfBytes, kKPlane = kHalves * kRowHalf;
+  static constexpr int kQPlane = kHalves * kHalfBytes;
   alignas(1024) unsigned char q[3][kQPlane];
-  alignas(1024) unsigned char k[3][kKPlane];
-  alignas(1024) unsigned char v[3][kKPlane];
+  alignas(1024) unsigned char k[2][3][kPlane];
+  alignas(1024) unsigned char v[2][3][kPlane];
   AttendPiece piece[kUnits];
-  unsigned long long unit_full[kUnits], unit_empty[kUnits], q_full, q_empty, k_full, k_empty, v_full, v_empty, s_full[2], p_ready[2], pv_done,
-      drain;
+  unsigned long long unit_full[kUnits], unit_empty[kUnits], q_full, q_empty, k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_ready,
+      pv_done, drain;
   int odd_lo[2][4], odd_hi[2][4];                // tiles of a piece, by its parity, where a warp of V met values that are not finite
   int abort;
   uint32_t tmem;
@@ -46,19 +51,18 @@ struct Smem {
 struct AttendF32 {
   AttendShape a;
   int page_bits;
-  int wide;                                      // rows of out begin at 32-byte boundaries
+  int wide, wide_k, wide_v;                      // rows of out, of K, of V (drafted ones too) begin at 32-byte boundaries
   int extra_arrival;                             // 1: a test makes the first CTA's wait for P run out
 };
 
 // Row j of a piece's tile, as it lies in memory; null: there is none.
-template <bool V>
-__device__ __forceinline__ const float* key_row(const AttendF32& t, const AttendPiece& p, int tile, int j) {
+__device__ __forceinline__ const float* key_row(const AttendF32& t, const AttendPiece& p, bool v, int tile, int j) {
   const AttendShape& a = t.a;
   if (a.paged) {
     if (a.has_new && tile == p.n_all - 1) {
       if (j >= p.n_seq_tok) return nullptr;
-      return V ? static_cast<const float*>(a.v_new) + p.s * a.vn_seq + j * a.vn_tok + p.h * a.vn_head
-               : static_cast<const float*>(a.k_new) + p.s * a.kn_seq + j * a.kn_tok + p.h * a.kn_head;
+      return static_cast<const float*>(v ? a.v_new : a.k_new) + p.s * (v ? a.vn_seq : a.kn_seq) + j * (v ? a.vn_tok : a.kn_tok) +
+             p.h * (v ? a.vn_head : a.kn_head);
     }
     const int row = tile * kKeys + j;
     if (row >= p.nk) return nullptr;
@@ -68,12 +72,11 @@ __device__ __forceinline__ const float* key_row(const AttendF32& t, const Attend
       return nullptr;
     }
     const long long at = (((long long)id << t.page_bits) + (row & (a.page_rows - 1))) * a.head_dim;
-    return static_cast<const float*>(V ? a.v : a.k) + at;
+    return static_cast<const float*>(v ? a.v : a.k) + at;
   }
   const int row = tile * kKeys + j;
   if (row >= p.nk) return nullptr;
-  const long long at = p.k_row + row;
-  return V ? static_cast<const float*>(a.v) + at * a.v_tok + p.h * a.v_head : static_cast<const float*>(a.k) + at * a.k_tok + p.h * a.k_head;
+  return static_cast<const float*>(v ? a.v : a.k) + (long long)(p.k_row + row) * (v ? a.v_tok : a.k_tok) + p.h * (v ? a.v_head : a.k_head);
 }
 
 // Three planes of eight numbers: the upper 16 bits of x, of what is left of it, and of what is left then.
@@ -99,37 +102,45 @@ __device__ __forceinline__ void split8(const float (&x)[8], uint4& p0, uint4& p1
   p2 = make_uint4(w[2][0], w[2][1], w[2][2], w[2][3]);
 }
 
-// Eight channels of a row into three planes of 128-byte-swizzled rows.
-template <int HALF, int PLANE>
+// Eight channels of a row into three planes of 128-byte-swizzled rows of 64 channels.
+template <int PLANE>
 __device__ __forceinline__ void store_planes(unsigned char* base, int row, int chunk, const float (&x)[8]) {
   uint4 p0, p1, p2;
   split8(x, p0, p1, p2);
-  unsigned char* at = base + (chunk >> 3) * HALF + row * 128 + (((chunk & 7) ^ (row & 7)) << 4);
+  unsigned char* at = base + row * 128 + ((chunk ^ (row & 7)) << 4);
   *reinterpret_cast<uint4*>(at) = p0;
   *reinterpret_cast<uint4*>(at + PLANE) = p1;
   *reinterpret_cast<uint4*>(at + 2 * PLANE) = p2;
 }
 
-__device__ __forceinline__ void load8(const float* from, float (&x)[8]) {
-  const float4 a = *reinterpret_cast<const float4*>(from), b = *reinterpret_cast<const float4*>(from + 4);
-  x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
-  x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+// Whole sectors at a time where rows begin at them; K and V pass by L1, they are read once.
+__device__ __forceinline__ void load8(const float* from, bool wide, float (&x)[8]) {
+  if (wide) {
+    asm volatile("ld.global.L1::no_allocate.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]), "=f"(x[4]), "=f"(x[5]), "=f"(x[6]), "=f"(x[7]) : "l"(from));
+  } else {
+    const float4 a = *reinterpret_cast<const float4*>(from), b = *reinterpret_cast<const float4*>(from + 4);
+    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
+    x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+  }
 }
 
-// The warps of K (V = false) or of Q and V.
-template <int D, bool V>
-__device__ __forceinline__ void rows_role(const AttendF32& t, Smem<D>& sm) {
+// The warps of K, or of Q and V (v).  One code for both, a block at a time: what runs side by side here has to stay in the instruction
+// cache (with a code each and both blocks of a tile unrolled, 8000 tokens took 4540 us, waiting for instructions for the most part).
+template <int D>
+__device__ __forceinline__ void rows_role(const AttendF32& t, Smem<D>& sm, const bool v) {
   using S = Smem<D>;
   const AttendShape& a = t.a;
-  constexpr int kChunks = D / 8, kMine = kKeys * kChunks / 128;      // eight channels each: of a row, of a thread
-  const int tid = threadIdx.x & 127, lane = threadIdx.x & 31;
-  const int row0 = tid / kChunks, chunk = tid % kChunks;
-  unsigned long long* const full = V ? &sm.v_full : &sm.k_full;
-  unsigned long long* const empty = V ? &sm.v_empty : &sm.k_empty;
+  constexpr int kMine = kKeys / 16;              // rows of a block that a thread has eight channels of
+  const int tid = threadIdx.x & 127, lane = threadIdx.x & 31, row0 = tid >> 3, chunk = tid & 7;
+  const bool wide = v ? t.wide_v : t.wide_k;
+  unsigned long long* const full = v ? sm.v_full : sm.k_full;
+  unsigned long long* const empty = v ? sm.v_empty : sm.k_empty;
+  unsigned char* const planes = v ? sm.v[0][0] : sm.k[0][0];
   auto wait = [&](unsigned long long* bar, unsigned phase) {
     return __all_sync(0xffffffffu, mbar_wait(smem_u32(bar), phase & 1, &sm.abort)) != 0;
   };
-  unsigned done = 0, n_q = 0;                    // tiles, blocks of query rows
+  unsigned done = 0, n_q = 0;                    // blocks of keys, of query rows
   for (unsigned nth = 0;; ++nth) {
     if (!wait(&sm.unit_full[nth % kUnits], nth / kUnits)) return;
     const AttendPiece p = sm.piece[nth % kUnits];
@@ -138,72 +149,77 @@ __device__ __forceinline__ void rows_role(const AttendF32& t, Smem<D>& sm) {
     if (p.stop) return;
     if (p.n == 0) continue;
     float x[kMine][8];
-    auto load = [&](int tile) {
+    auto load = [&](int block) {                 // of the piece
+      const int tile = p.tile0 + block / S::kHalves, ch = 64 * (block % S::kHalves) + 8 * chunk;
 #pragma unroll
       for (int u = 0; u < kMine; ++u) {
-        const float* from = key_row<V>(t, p, tile, row0 + u * (128 / kChunks));
+        const float* from = key_row(t, p, v, tile, row0 + 16 * u);
         if (from) {
-          load8(from + 8 * chunk, x[u]);
+          load8(from + ch, wide, x[u]);
         } else {
 #pragma unroll
           for (int e = 0; e < 8; ++e) x[u][e] = 0.0f;
         }
       }
     };
-    load(p.tile0);
-    if (V) {
+    load(0);
+    if (v) {
       if (n_q > 0 && !wait(&sm.q_empty, n_q - 1)) return;
       ++n_q;
       const float* from = static_cast<const float*>(a.q) + (a.paged ? p.s * a.q_seq : p.q_row * a.q_tok) + p.tok0 * a.q_tok + p.h * a.G * a.q_head;
       const int rows = p.n_tok * a.G;
-#pragma unroll 2
-      for (int r = row0; r < 128; r += 128 / kChunks) {
+#pragma unroll 1
+      for (int i = 0; i < 8 * S::kHalves; ++i) {
+        const int r = row0 + 16 * (i / S::kHalves), h = i % S::kHalves, rt = r / a.G;
         float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        const int rt = r / a.G;
-        if (r < rows) load8(from + rt * a.q_tok + (r - rt * a.G) * a.q_head + 8 * chunk, y);
-        store_planes<kHalfBytes, S::kQPlane>(sm.q[0], r, chunk, y);
+        if (r < rows) load8(from + rt * a.q_tok + (r - rt * a.G) * a.q_head + 64 * h + 8 * chunk, false, y);
+        store_planes<S::kQPlane>(sm.q[0] + h * kHalfBytes, r, chunk, y);
       }
       fence_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&sm.q_full));
     }
-    for (int i = 0; i < p.n; ++i, ++done) {
-      if (done > 0 && !wait(empty, done - 1)) return;
-      if (V && i == 0) {                         // the piece before the last one has been written
-        if (lane == 0) {
-          sm.odd_lo[nth & 1][tid >> 5] = 0x7fffffff;
-          sm.odd_hi[nth & 1][tid >> 5] = -1;
+#pragma unroll 1
+    for (int i = 0; i < p.n * S::kHalves; ++i, ++done) {
+      const unsigned slot = done & 1;
+      if (done > 1 && !wait(empty + slot, (done >> 1) - 1)) return;
+      if (v) {
+        if (i == 0) {                            // the piece before the last one has been written
+          if (lane == 0) {
+            sm.odd_lo[nth & 1][tid >> 5] = 0x7fffffff;
+            sm.odd_hi[nth & 1][tid >> 5] = -1;
+          }
+          __syncwarp();
         }
-        __syncwarp();
-      }
-      bool odd = false;
+        bool odd = false;
 #pragma unroll
-      for (int u = 0; u < kMine; ++u) {
-        if (V) {
-          bool here = false;
+        for (int u = 0; u < kMine; ++u) {
+          float top = 0.0f;                      // 0 times what is not finite is NaN
 #pragma unroll
-          for (int e = 0; e < 8; ++e) here |= !(fabsf(x[u][e]) < INFINITY);
-          if (here) {
-            odd = true;
+          for (int e = 0; e < 8; ++e) top = fmaf(0.0f, x[u][e], top);
+          odd |= top != 0.0f;
+        }
+        if (odd) {
+#pragma unroll
+          for (int u = 0; u < kMine; ++u)
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[u][e] = fabsf(x[u][e]) < INFINITY ? x[u][e] : 0.0f;
-          }
+          const int tile = p.tile0 + i / S::kHalves;
+          atomicMin(&sm.odd_lo[nth & 1][tid >> 5], tile);
+          atomicMax(&sm.odd_hi[nth & 1][tid >> 5], tile);
         }
-        store_planes<kRowHalf, S::kKPlane>(V ? sm.v[0] : sm.k[0], row0 + u * (128 / kChunks), chunk, x[u]);
       }
-      if (V && odd) {
-        atomicMin(&sm.odd_lo[nth & 1][tid >> 5], p.tile0 + i);
-        atomicMax(&sm.odd_hi[nth & 1][tid >> 5], p.tile0 + i);
-      }
+#pragma unroll
+      for (int u = 0; u < kMine; ++u) store_planes<kPlane>(planes + slot * 3 * kPlane, row0 + 16 * u, chunk, x[u]);
       fence_async_smem();
       __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(full));
-      if (i + 1 < p.n) load(p.tile0 + i + 1);
+      if (lane == 0) mbar_arrive(smem_u32(full + slot));
+      if (i + 1 < p.n * S::kHalves) load(i + 1);
     }
   }
 }
 
-// The six products of three planes each, the small ones first: planes of A and of B, two bits each.
+// The six products of three planes each, the small ones first, of all channels (what is cut off then is cut off small sums): planes of A and of B, two bits each.
 constexpr int kPairs = 6;
 constexpr uint32_t kPlanesA = 0u | 2u << 2 | 1u << 4 | 0u << 6 | 1u << 8 | 0u << 10;
 constexpr uint32_t kPlanesB = 2u | 0u << 2 | 1u << 4 | 1u << 6 | 0u << 8 | 0u << 10;
@@ -213,8 +229,8 @@ __device__ __forceinline__ bool mma_role(const AttendF32& t, Smem<D>& sm) {
   using S = Smem<D>;
   const uint32_t tmem = sm.tmem;
   constexpr uint32_t kIdS = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kKeys >> 3) << 17) | (8u << 24);
-  constexpr uint32_t kIdO = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(D >> 3) << 17) | (8u << 24) | kRowsB;
-  const uint32_t qa = desc_lo(smem_u32(sm.q[0])), ka = desc_lo(smem_u32(sm.k[0])), va = desc_lo<kRowHalf>(smem_u32(sm.v[0]));
+  constexpr uint32_t kIdO = (1u << 4) | (1u << 7) | (1u << 10) | (8u << 17) | (8u << 24) | kRowsB;      // 64 channels
+  const uint32_t qa = desc_lo(smem_u32(sm.q[0]));
   auto wait = [&](unsigned long long* bar, unsigned phase) {
     return __all_sync(0xffffffffu, mbar_poll(smem_u32(bar), phase & 1, &sm.abort)) != 0;
   };
@@ -230,40 +246,53 @@ __device__ __forceinline__ bool mma_role(const AttendF32& t, Smem<D>& sm) {
     for (int i = 0; i <= p.n; ++i) {
       if (i < p.n) {
         const unsigned no = done + i;
-        if (!wait(&sm.k_full, no)) return false;
-        tc_fence_after();
-        if (elect_one()) {
-          const uint32_t d = tmem + kTmemS + (no & 1) * kKeys;
-#pragma unroll 1
-          for (int c = 0; c < kPairs; ++c) {
-            const uint32_t ap = qa + ((kPlanesA >> (2 * c) & 3u) * S::kQPlane >> 4), bp = ka + ((kPlanesB >> (2 * c) & 3u) * S::kKPlane >> 4);
+        const uint32_t d = tmem + kTmemS + (no & 1) * kKeys;
 #pragma unroll
-            for (int k = 0; k < D / 16; ++k)
-              tc_mma_ss(d, ap + (((k >> 2) * kHalfBytes + (k & 3) * 32) >> 4), bp + (((k >> 2) * kRowHalf + (k & 3) * 32) >> 4), kIdS, k > 0 ? 1 : c > 0);
-          }
+        for (int h = 0; h < S::kHalves; ++h) {
+          const unsigned block = no * S::kHalves + h;
+          if (!wait(&sm.k_full[block & 1], block >> 1)) return false;
+        }
+        tc_fence_after();
+        const uint32_t ka = desc_lo(smem_u32(sm.k[0][0])), first = no * S::kHalves & 1;
+        if (elect_one()) {
+#pragma unroll 1
+          for (int c = 0; c < kPairs; ++c)
+#pragma unroll
+            for (int h = 0; h < S::kHalves; ++h) {
+              const uint32_t ap = qa + (((kPlanesA >> (2 * c) & 3u) * S::kQPlane + h * kHalfBytes) >> 4);
+              const uint32_t bp = ka + (((first ^ h) * 3 * kPlane + (kPlanesB >> (2 * c) & 3u) * kPlane) >> 4);
+#pragma unroll
+              for (int k = 0; k < 4; ++k) tc_mma_ss(d, ap + 2 * k, bp + 2 * k, kIdS, c > 0 || h > 0 || k > 0);
+              if (c + 1 == kPairs) tc_commit(smem_u32(&sm.k_empty[first ^ h]));
+            }
           tc_commit(smem_u32(&sm.s_full[no & 1]));
-          tc_commit(smem_u32(&sm.k_empty));
           if (i + 1 == p.n) tc_commit(smem_u32(&sm.q_empty));
         }
         __syncwarp();
       }
       if (i > 0) {
         const unsigned no = done + i - 1;
-        if (!wait(&sm.v_full, no)) return false;
-        if (!wait(&sm.p_ready[no & 1], no >> 1)) return false;
+        if (!wait(&sm.p_ready, no)) return false;
         tc_fence_after();
-        if (elect_one()) {
-          const uint32_t d = tmem + kTmemO, pa = tmem + kTmemP + (no & 1) * 3 * kPlaneCols;
+        const uint32_t pa = tmem + kTmemP, first = (i - 1) % kFlush != 0;
 #pragma unroll 1
-          for (int c = 0; c < kPairs; ++c) {
-            const uint32_t ap = pa + (kPlanesA >> (2 * c) & 3u) * kPlaneCols, bp = va + ((kPlanesB >> (2 * c) & 3u) * S::kKPlane >> 4);
+        for (int h = 0; h < S::kHalves; ++h) {
+          const unsigned block = no * S::kHalves + h;
+          if (!wait(&sm.v_full[block & 1], block >> 1)) return false;
+          tc_fence_after();
+          const uint32_t va = desc_lo(smem_u32(sm.v[block & 1][0])), d = tmem + kTmemO + 64 * h;
+          if (elect_one()) {
+#pragma unroll 1
+            for (int c = 0; c < kPairs; ++c) {
+              const uint32_t ap = pa + (kPlanesA >> (2 * c) & 3u) * kPlaneCols, bp = va + ((kPlanesB >> (2 * c) & 3u) * kPlane >> 4);
 #pragma unroll
-            for (int k = 0; k < kKeys / 16; ++k) tc_mma_ts(d, ap + 8 * k, bp + k * 128, kIdO, k > 0 ? 1 : i > 1 || c > 0);
+              for (int k = 0; k < kKeys / 16; ++k) tc_mma_ts(d, ap + 8 * k, bp + k * 128, kIdO, c > 0 || k > 0 ? 1u : first);
+            }
+            tc_commit(smem_u32(&sm.v_empty[block & 1]));
+            if (h + 1 == S::kHalves) tc_commit(smem_u32(&sm.pv_done));
           }
-          tc_commit(smem_u32(&sm.v_empty));
-          tc_commit(smem_u32(&sm.pv_done));
+          __syncwarp();
         }
-        __syncwarp();
       }
     }
     done += p.n;
@@ -279,7 +308,7 @@ __device__ __forceinline__ void put_back(const AttendF32& t, const AttendPiece& 
     for (int j = 0; j < kKeys; ++j) {
       const bool drafted = a.has_new && tile == p.n_all - 1;
       if (drafted ? !(mask >> j & 1) : !a.paged && tile * kKeys + j >= bound) continue;
-      const float* v = key_row<true>(t, p, tile, j);
+      const float* v = key_row(t, p, true, tile, j);
       if (!v) continue;
       for (int ch = 0; ch < a.head_dim; ++ch)
         if (!(fabsf(v[ch]) < INFINITY)) out[ch] += v[ch];
@@ -321,73 +350,86 @@ __device__ __forceinline__ void softmax_role(const AttendF32& t, Smem<D>& sm) {
       if (!wait(&sm.s_full[done & 1], done >> 1)) return;
       tc_fence_after();
       if (work) {
-        uint32_t r[2][32];
-        const uint32_t ts = lanes + kTmemS + (done & 1) * kKeys, tp = lanes + kTmemP + (done & 1) * 3 * kPlaneCols;
-        tc_ld32(ts, r[0]);
-        tc_ld32(ts + 32, r[1]);
-        tc_wait_ld(r[0]);
-        tc_wait_ld(r[1]);
-        if (__any_sync(0xffffffffu, drafted || end < kKeys)) {
-#pragma unroll
-          for (int q = 0; q < 2; ++q) {
+        const uint32_t ts = lanes + kTmemS + (done & 1) * kKeys, tp = lanes + kTmemP;
+        const bool masked = __any_sync(0xffffffffu, drafted || end < kKeys);
+        // 32 keys at a time, once for the maximum and once more: half the code, see rows_role
+        uint32_t r[32];
+        auto load = [&](int q) {
+          tc_ld32(ts + 32 * q, r);
+          tc_wait_ld(r);
+          if (masked) {
             const uint32_t see = drafted ? (uint32_t)(mask >> (32 * q)) : seen_below(end - 32 * q);
 #pragma unroll
-            for (int e = 0; e < 32; ++e) r[q][e] = see >> e & 1u ? r[q][e] : 0xff800000u;
+            for (int e = 0; e < 32; ++e) r[e] = see >> e & 1u ? r[e] : 0xff800000u;
           }
-        }
-        float mx[2];
-#pragma unroll
+        };
+        float top = -INFINITY;
+#pragma unroll 1
         for (int q = 0; q < 2; ++q) {
-          mx[q] = __uint_as_float(r[q][0]);
+          load(q);
+          float mx[2] = {__uint_as_float(r[0]), __uint_as_float(r[1])};
 #pragma unroll
-          for (int e = 1; e < 31; e += 2) mx[q] = fmaxf(fmaxf(mx[q], __uint_as_float(r[q][e])), __uint_as_float(r[q][e + 1]));
-          mx[q] = fmaxf(mx[q], __uint_as_float(r[q][31]));
+          for (int e = 2; e < 30; e += 4) {
+            mx[0] = fmaxf(fmaxf(mx[0], __uint_as_float(r[e])), __uint_as_float(r[e + 1]));
+            mx[1] = fmaxf(fmaxf(mx[1], __uint_as_float(r[e + 2])), __uint_as_float(r[e + 3]));
+          }
+          mx[0] = fmaxf(fmaxf(mx[0], __uint_as_float(r[30])), __uint_as_float(r[31]));
+          top = fmaxf(top, fmaxf(mx[0], mx[1]));
         }
-        const float top = fmaxf(mx[0], mx[1]);
-        if (i == 0) {
-          m = top;
-        } else {
-          const bool lift = (top - m) * sc > kLift;        // m = -infinity: any score lifts it
-          if (__any_sync(0xffffffffu, lift)) {
-            if (!wait(&sm.pv_done, done - 1)) return;
-            tc_fence_after();
-            const float f = lift ? ex2((m - top) * sc) : 1.0f;
-            if (lift) { m = top; l *= f; }
+        const bool lift = i > 0 && (top - m) * sc > kLift;           // m = -infinity: any score lifts it
+        const float f = lift ? ex2((m - top) * sc) : 1.0f;
+        const bool scaled = __any_sync(0xffffffffu, lift);
+        if (i == 0 || lift) m = top;
+        l *= f;
+        if (i > 0) {                             // P and O belong to the product before until it is done
+          if (!wait(&sm.pv_done, done - 1)) return;
+          tc_fence_after();
+          const bool flush = i % kFlush == 0, have = i > kFlush;     // O goes to the sum; which is there already
+          if (flush || scaled) {
 #pragma unroll 1
             for (int ch = 0; ch < D; ch += 16) {
-              uint32_t o[16];
+              uint32_t o[16], z[16];
               tc_ld16_issue(lanes + kTmemO + ch, o);
+              if (have) tc_ld16_issue(lanes + kTmemSum + ch, z);
               tc_ld_wait(o);
+              if (have) {
+                tc_ld_wait(z);
+              } else {
 #pragma unroll
-              for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-              tc_st16(lanes + kTmemO + ch, o);
+                for (int e = 0; e < 16; ++e) z[e] = 0;
+              }
+#pragma unroll
+              for (int e = 0; e < 16; ++e) {
+                if (flush) z[e] = __float_as_uint((__uint_as_float(z[e]) + __uint_as_float(o[e])) * f);
+                else { z[e] = __float_as_uint(__uint_as_float(z[e]) * f); o[e] = __float_as_uint(__uint_as_float(o[e]) * f); }
+              }
+              if (!flush) tc_st16(lanes + kTmemO + ch, o);
+              if (flush || have) tc_st16(lanes + kTmemSum + ch, z);
             }
           }
         }
         // 2^(sc x - sc m) with one rounding of the difference, which is as large as sc m 2^-24: where that is much, differences first
-        float base = m == -INFINITY ? 0.0f : m;
-        if (__any_sync(0xffffffffu, fabsf(base) * sc > 0x1p20f)) {
-#pragma unroll
-          for (int q = 0; q < 2; ++q)
-#pragma unroll
-            for (int e = 0; e < 32; ++e) r[q][e] = __float_as_uint(__uint_as_float(r[q][e]) - base);
-          base = 0.0f;
-        }
+        float base = m == -INFINITY ? 0.0f : m, less = 0.0f;
+        if (__any_sync(0xffffffffu, fabsf(base) * sc > 0x1p20f)) { less = base; base = 0.0f; }
         const float nm = -base * sc;
         const f32x2 nm2 = pack2(nm, nm);
         f32x2 s0 = 0, s1 = 0;
+#pragma unroll 1
+        for (int q = 0; q < 2; ++q) {
+          load(q);
+          if (less != 0.0f) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {            // sixteen keys at a time
-          uint32_t w[3][8];
-          const uint32_t* x = r[q >> 1] + 16 * (q & 1);
+            for (int e = 0; e < 32; ++e) r[e] = __float_as_uint(__uint_as_float(r[e]) - less);
+          }
+          uint32_t w[3][16];
 #pragma unroll
-          for (int e = 0; e < 16; e += 8) {
+          for (int e = 0; e < 32; e += 8) {
             float y[8];
 #pragma unroll
-            for (int f = 0; f < 8; f += 2) {
-              const f32x2 pr = ex2_pair(fma2(pack2(__uint_as_float(x[e + f]), __uint_as_float(x[e + f + 1])), sc2, nm2));
-              if (f & 2) s1 = add2(s1, pr); else s0 = add2(s0, pr);
-              unpack2(pr, y[f], y[f + 1]);
+            for (int k = 0; k < 8; k += 2) {
+              const f32x2 pr = ex2_pair(fma2(pack2(__uint_as_float(r[e + k]), __uint_as_float(r[e + k + 1])), sc2, nm2));
+              if (k & 2) s1 = add2(s1, pr); else s0 = add2(s0, pr);
+              unpack2(pr, y[k], y[k + 1]);
             }
             uint4 p0, p1, p2;
             split8(y, p0, p1, p2);
@@ -396,19 +438,19 @@ __device__ __forceinline__ void softmax_role(const AttendF32& t, Smem<D>& sm) {
             w[2][e / 2] = p2.x; w[2][e / 2 + 1] = p2.y; w[2][e / 2 + 2] = p2.z; w[2][e / 2 + 3] = p2.w;
           }
 #pragma unroll
-          for (int c = 0; c < 3; ++c) tc_st8(tp + c * kPlaneCols + 8 * q, w[c]);
+          for (int c = 0; c < 3; ++c) tc_st16(tp + c * kPlaneCols + 16 * q, w[c]);
         }
         l += sum2(s0, s1);
+      } else if (i > 0) {
+        if (!wait(&sm.pv_done, done - 1)) return;
       }
       tc_wait_st();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&sm.p_ready[done & 1]));
+      if (lane == 0) mbar_arrive(smem_u32(&sm.p_ready));
     }
     // ---- results
     if (p.n > 0) {
-      // the last tile's scores came behind the product two tiles before it: one phase after the other
-      if (p.n > 1 && !wait(&sm.pv_done, done - 2)) return;
       if (!wait(&sm.pv_done, done - 1)) return;
       tc_fence_after();
     }
@@ -427,6 +469,13 @@ __device__ __forceinline__ void softmax_role(const AttendF32& t, Smem<D>& sm) {
       } else {
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[e] = 0;
+      }
+      if (p.n > kFlush) {
+        uint32_t z[16];
+        tc_ld16_issue(lanes + kTmemSum + ch, z);
+        tc_ld_wait(z);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) + __uint_as_float(z[e]));
       }
       if (there) {
 #pragma unroll
@@ -468,14 +517,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_f32(const __grid_constan
     }
     mbar_init(smem_u32(&sm.q_full), 4);
     mbar_init(smem_u32(&sm.q_empty), 1);
-    mbar_init(smem_u32(&sm.k_full), 4);
-    mbar_init(smem_u32(&sm.k_empty), 1);
-    mbar_init(smem_u32(&sm.v_full), 4);
-    mbar_init(smem_u32(&sm.v_empty), 1);
     for (int i = 0; i < 2; ++i) {
+      mbar_init(smem_u32(&sm.k_full[i]), 4);
+      mbar_init(smem_u32(&sm.k_empty[i]), 1);
+      mbar_init(smem_u32(&sm.v_full[i]), 4);
+      mbar_init(smem_u32(&sm.v_empty[i]), 1);
       mbar_init(smem_u32(&sm.s_full[i]), 1);
-      mbar_init(smem_u32(&sm.p_ready[i]), 4 + (blockIdx.x == 0 ? t.extra_arrival : 0));
     }
+    mbar_init(smem_u32(&sm.p_ready), 4 + (blockIdx.x == 0 ? t.extra_arrival : 0));
     mbar_init(smem_u32(&sm.pv_done), 1);
     mbar_init(smem_u32(&sm.drain), 1);
     sm.abort = 0;
@@ -494,10 +543,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_f32(const __grid_constan
   __syncthreads();
   if (warp < kKWarp) {
     softmax_role<D>(t, sm);
-  } else if (warp < kVWarp) {
-    rows_role<D, false>(t, sm);
   } else if (warp < kMmaWarp) {
-    rows_role<D, true>(t, sm);
+    rows_role<D>(t, sm, warp >= kVWarp);
   } else if (warp == kMmaWarp) {
     if (!mma_role<D>(t, sm) && elect_one()) {    // a wait ran out: what is under way ends first
       volatile int never = 0;
@@ -557,7 +604,12 @@ cudaError_t launch_attend_f32(const AttendShape& a, cudaStream_t st, int* launch
   AttendF32 t = {};
   t.a = a;
   for (t.page_bits = 0; a.paged && (1 << t.page_bits) < a.page_rows;) ++t.page_bits;
-  t.wide = reinterpret_cast<uintptr_t>(a.out) % 32 == 0 && a.o_tok % 8 == 0 && a.o_head % 8 == 0 && (!a.paged || a.o_seq % 8 == 0);
+  auto wide = [&](const void* base, long long tok, long long head, long long seq) {
+    return reinterpret_cast<uintptr_t>(base) % 32 == 0 && (tok | head | seq) % 8 == 0;
+  };
+  t.wide = wide(a.out, a.o_tok, a.o_head, a.paged ? a.o_seq : 0);
+  t.wide_k = a.paged ? wide(a.k, 0, 0, 0) && (!a.has_new || wide(a.k_new, a.kn_tok, a.kn_head, a.kn_seq)) : wide(a.k, a.k_tok, a.k_head, 0);
+  t.wide_v = a.paged ? wide(a.v, 0, 0, 0) && (!a.has_new || wide(a.v_new, a.vn_tok, a.vn_head, a.vn_seq)) : wide(a.v, a.v_tok, a.v_head, 0);
   t.extra_arrival = take_expire_next_copy_wait() ? 1 : 0;
   return a.head_dim == 128 ? launch<128>(t, st, launches) : launch<64>(t, st, launches);
 }
