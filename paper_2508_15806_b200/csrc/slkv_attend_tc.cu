@@ -42,7 +42,7 @@ struct Smem {
   };
   AttendPiece piece[kUnits];
   unsigned long long unit_full[kUnits], unit_empty[kUnits], q_full[2], q_empty[2], kv_full[kStages], kv_empty[kStages], s_full[2],
-      p_ready[2], o_full[2], merge_full, merge_done, drain;
+      p_most[2], p_ready[2], o_full[2], merge_full, merge_done, drain;
   int odd[2];                                    // number + 1 of the piece that found V values that are not finite, by its parity
   int abort;
   uint32_t tmem;
@@ -289,12 +289,22 @@ __device__ __forceinline__ bool mma_role(const AttendTc& t, Smem<D>& sm) {
         const int used = columns(t, p, p.tile0 + b.tile(g, i), tok, min(a.block_tokens, p.n_seq_tok - tok)).used;
         const unsigned slot = (loads + b.v_load(b.tile(g, i), p.n)) % S::kStages;
         const uint32_t va = desc_lo(smem_u32(sm.kv[slot])), d = tmem + kTmemO + 128 * g, pa = tmem + kTmemS + 128 * g;
+        constexpr int kMost = 6;                 // products with P's first three quarters
+        if (!wait(&sm.p_most[g], n_p[g])) return false;
+        if (used == kAttendTile) {
+          tc_fence_after();
+          if (elect_one()) {
+#pragma unroll
+            for (int k = 0; k < kMost; ++k) tc_mma_ts(d, pa + 8 * k, va + k * 128, kIdO, k > 0 ? 1 : i > 0);
+          }
+          __syncwarp();
+        }
         if (!wait(&sm.p_ready[g], n_p[g]++)) return false;
         tc_fence_after();
         if (elect_one()) {
           if (used == kAttendTile) {
 #pragma unroll
-            for (int k = 0; k < kAttendTile / 16; ++k) tc_mma_ts(d, pa + 8 * k, va + k * 128, kIdO, k > 0 ? 1 : i > 0);
+            for (int k = kMost; k < kAttendTile / 16; ++k) tc_mma_ts(d, pa + 8 * k, va + k * 128, kIdO, 1);
           } else {
 #pragma unroll 1
             for (int k = 0; k < used / 16; ++k) tc_mma_ts(d, pa + 8 * k, va + k * 128, kIdO, k > 0 || i > 0);
@@ -310,17 +320,8 @@ __device__ __forceinline__ bool mma_role(const AttendTc& t, Smem<D>& sm) {
   }
 }
 
-// What a thread's row sees of a tile, a bit per key.
-struct Seen { uint32_t w[4]; };
-__device__ __forceinline__ Seen seen_below(int n) {
-  Seen s;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int k = min(max(n - 32 * i, 0), 32);
-    s.w[i] = k == 32 ? 0xffffffffu : (1u << k) - 1u;
-  }
-  return s;
-}
+// The first n of 32 keys, a bit each.
+__device__ __forceinline__ uint32_t seen_below(int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u; }
 
 // V rows all .. used of a tile: those from `end` on become zero, and what is not finite in the others too.  Returns whether there was any.
 template <int D>
@@ -402,6 +403,12 @@ __device__ __forceinline__ void softmax_role(const AttendTc& t, Smem<D>& sm, int
   const uint32_t ts = lanes + kTmemS + 128 * g, to = lanes + kTmemO + 128 * g;
   const f32x2 sc2 = pack2(t.sc, t.sc);
   unsigned loads = 0, n_s = 0, n_o = 0, n_merge = 0;
+  auto say_most = [&] {
+    tc_wait_st();
+    tc_fence_before();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(smem_u32(&sm.p_most[g]));
+  };
   for (unsigned nth = 0;; ++nth) {
     bool ok = mbar_wait(smem_u32(&sm.unit_full[nth % kUnits]), (nth / kUnits) & 1, &sm.abort);
     if (!__all_sync(0xffffffffu, ok)) return;
@@ -423,10 +430,11 @@ __device__ __forceinline__ void softmax_role(const AttendTc& t, Smem<D>& sm, int
     const bool work = __any_sync(0xffffffffu, there);
     float m = -INFINITY, l = 0.0f;
     const int n = b.n[g];
+    const int all = a.paged ? p.nk : min(tok0 + 1 + p.shift, p.nk);      // keys that every row sees
 #pragma unroll 1
     for (int i = 0; i < n; ++i, ++n_s) {
       const int tl = b.tile(g, i), tile = p.tile0 + tl;
-      const Columns c = columns(t, p, tile, tok0, n_tok);
+      const bool drafted = a.has_new && tile == p.n_all - 1, edge = drafted || (tile + 1) * kAttendTile > all;
       ok = mbar_wait(smem_u32(&sm.s_full[g]), n_s & 1, &sm.abort);
       if (!__all_sync(0xffffffffu, ok)) return;
       tc_fence_after();
@@ -436,17 +444,14 @@ __device__ __forceinline__ void softmax_role(const AttendTc& t, Smem<D>& sm, int
         for (int q = 0; q < 4; ++q) tc_ld32(ts + 32 * q, r[q]);
 #pragma unroll
         for (int q = 0; q < 4; ++q) tc_wait_ld(r[q]);
-        if (c.all < kAttendTile) {
-          Seen see;
-          if (a.has_new && tile == p.n_all - 1) {
-            see.w[0] = (uint32_t)mask; see.w[1] = (uint32_t)(mask >> 32); see.w[2] = see.w[3] = 0;
-          } else {
-            see = seen_below(a.paged ? c.end : bound - tile * kAttendTile);
+        if (edge) {
+          const int end = (a.paged ? p.nk : bound) - tile * kAttendTile;             // keys that the row sees
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const uint32_t see = drafted ? (q < 2 ? (uint32_t)(mask >> (32 * q)) : 0u) : seen_below(end - 32 * q);
+#pragma unroll
+            for (int e = 0; e < 32; ++e) r[q][e] = see >> e & 1u ? r[q][e] : 0xff800000u;
           }
-#pragma unroll
-          for (int q = 0; q < 4; ++q)
-#pragma unroll
-            for (int e = 0; e < 32; ++e) r[q][e] = see.w[q] >> e & 1u ? r[q][e] : 0xff800000u;
         }
         float mx[4];
 #pragma unroll
@@ -502,9 +507,13 @@ __device__ __forceinline__ void softmax_role(const AttendTc& t, Smem<D>& sm, int
             w[e / 2 + 1] = bf16_pair(p1);
           }
           tc_st16(ts + 16 * q, w);
+          if (q == 2 && !edge) say_most();       // three quarters of the product with V can begin
         }
         l += sum2(s0, s1);
+      } else if (!edge) {
+        say_most();
       }
+      const Columns c = edge ? columns(t, p, tile, tok0, n_tok) : Columns{0, 0, 0};
       if (c.all < c.used) {
         const unsigned no = loads + b.v_load(tl, p.n), slot = no % S::kStages;
         ok = mbar_wait(smem_u32(&sm.kv_full[slot]), (no / S::kStages) & 1, &sm.abort);
@@ -512,6 +521,7 @@ __device__ __forceinline__ void softmax_role(const AttendTc& t, Smem<D>& sm, int
         if (clean_rows<D>(sm.kv[slot], c, tid)) *(volatile int*)&sm.odd[nth & 1] = (int)nth + 1;
         fence_async_smem();
       }
+      if (edge) say_most();
       tc_wait_st();
       tc_fence_before();
       __syncwarp();
@@ -628,6 +638,7 @@ k_attend_tc(const __grid_constant__ AttendTc t, const __grid_constant__ AttendMa
       mbar_init(smem_u32(&sm.q_full[g]), 1);
       mbar_init(smem_u32(&sm.q_empty[g]), 1);
       mbar_init(smem_u32(&sm.s_full[g]), 1);
+      mbar_init(smem_u32(&sm.p_most[g]), 4);
       mbar_init(smem_u32(&sm.p_ready[g]), blockIdx.x == 0 ? t.arrivals : 4);
       mbar_init(smem_u32(&sm.o_full[g]), 1);
       sm.odd[g] = 0;
