@@ -40,7 +40,8 @@ struct AttendShape {
   int32_t* status;                               // may be null
   float scale, lse_unit;                         // lse_unit: log2 units -> the caller's
   // how the units are shared out
-  int spread;                                    // 1: whole units in turn, the longest first; 0: every CTA as many tiles as the others
+  int spread;                                    // 1: whole units in turn, the longest first; 0: equal shares
+  int whole;                                     // equal shares of whole units: nothing is joined; 2: all units count alike
   int n_cta;
   int levels;                                    // spread: blocks of the longest sequence
   // partial results of units that several CTAs share
@@ -57,6 +58,8 @@ void attend_bind(AttendShape* a, void* workspace);
 cudaError_t launch_attend_tensor(const AttendShape& a, cudaStream_t st, int* launches);
 cudaError_t launch_attend_f32(const AttendShape& a, cudaStream_t st, int* launches);
 cudaError_t launch_attend_join(const AttendShape& a, bool f32, cudaStream_t st, int* launches);
+
+constexpr int kUnitCost = 3;                     // see AttendSchedule
 
 #ifdef __CUDACC__
 // A piece of a unit: its tiles tile0 .. tile0 + n - 1 of n_all.
@@ -95,7 +98,10 @@ __device__ __forceinline__ void attend_lse(const AttendShape& a, int s, int qh, 
 //   spread       whole units, to the CTAs in turn and back (0 .. n - 1, n - 1 .. 0, ..), the ones with the most tiles of their
 //                sequence first: shares differ by about the last units, which are short, and CTAs that run beside each other read the
 //                same keys
-//   not spread   the tiles of all units in one row, cut into equal shares: for few units.  A unit without tiles counts one.
+//   not spread   all units in one row, cut into equal shares: for few units.  A unit is as long as its tiles and kUnitCost more, which is
+//                about what beginning and ending it costs beside them (units of one tile, 2000 tokens: a CTA with 15 of them took
+//                119 us, one with a unit of 15 tiles 55).  Where shares are long, parts have two tiles or more;
+//                with `whole`, through none: the unit is the share's that its middle lies in (whole = 2: no more units than CTAs, one each).
 // The first piece is what a launch waits for, and most of that is instructions that come in for the first time: the threads of the CTA
 // look for it together (attend_start), a few segments each, in little code.
 __device__ __forceinline__ int attend_tokens(const AttendShape& a, int s) {
@@ -114,19 +120,21 @@ __device__ __forceinline__ int attend_prompt_tiles(const AttendShape& a, int nq,
 __device__ __forceinline__ int attend_paged_tiles(const AttendShape& a, int rows) {
   return ((rows + (1 << a.tile_bits) - 1) >> a.tile_bits) + a.has_new;
 }
-// Tiles of all units of a segment (paged) or a sequence (prompt); a unit without any counts one.
+__device__ __forceinline__ int attend_length(const AttendShape& a, int tiles) { return a.whole == 2 ? 1 : tiles + kUnitCost; }
+// How long all units of a segment (paged) or a sequence (prompt) are.
 __device__ __forceinline__ int attend_weight(const AttendShape& a, int i) {
-  if (a.paged) return attend_blocks(a, attend_tokens(a, (unsigned)i / (unsigned)a.n_kv_heads)) * max(attend_paged_tiles(a, attend_rows(a, i)), 1);
+  if (a.paged)
+    return attend_blocks(a, attend_tokens(a, (unsigned)i / (unsigned)a.n_kv_heads)) * attend_length(a, attend_paged_tiles(a, attend_rows(a, i)));
   const int nq = attend_tokens(a, i), nk = max(a.cu_k[i + 1] - a.cu_k[i], 0);
   int sum = 0;
-  for (int t = 0; t * a.unit_tokens < nq; ++t) sum += max(attend_prompt_tiles(a, nq, nk, t), 1);
+  for (int t = 0; t * a.unit_tokens < nq; ++t) sum += attend_length(a, attend_prompt_tiles(a, nq, nk, t));
   return sum * a.n_kv_heads;
 }
-// Where a CTA's share of the tiles begins.
+// Where a CTA's share begins.
 struct AttendStart {
   int warp_sum[32];
   int total;
-  int group, before;             // segment or sequence that the share begins in, tiles in front of it
+  int group, before;             // segment or sequence that the share begins in, what lies in front of it
 };
 // By all threads of a CTA, 32 times n_warps; two barriers inside, one left to the caller.
 __device__ __forceinline__ void attend_start(const AttendShape& a, int cta, AttendStart* st) {
@@ -184,7 +192,7 @@ class AttendSchedule {
       count_ = level_count(level_);
       return;
     }
-    // the first `more` CTAs have each + 1 tiles, the others each; where there are fewer tiles than CTAs the last ones have none
+    // the first `more` shares are longer by one; where there is less than one for each CTA the last ones have none
     const int total = st->total;
     share_ = (unsigned)total / (unsigned)a_.n_cta;
     more_ = total - share_ * a_.n_cta;
@@ -202,8 +210,10 @@ class AttendSchedule {
     load_group();
   }
   __device__ __forceinline__ bool next(AttendPiece* p) { return a_.spread ? next_spread(p) : next_share(p); }
-  // Of the piece at hand, one of several: how many pieces its unit has.
-  __device__ __forceinline__ int pieces() const { return cta_of(unit_ + each_ - 1) - cta_of(unit_) + 1; }
+  // Of the piece at hand, one of several: how many pieces its unit has.  One more than there are shares that begin where it is cut.
+  __device__ __forceinline__ int pieces() const {
+    return 1 + cta_of(unit_ + each_ - least_part()) - cta_of(unit_ + kUnitCost + least_part() - 1);
+  }
 
  private:
   const AttendShape& a_;
@@ -216,10 +226,11 @@ class AttendSchedule {
   // shares: the group of units with the same tiles (prompt: a block of tokens, all KV heads; paged: a segment, all blocks)
   int pos_, end_, group_;        // group_: first position of the group
   int s_, x_;                    // sequence; prompt: block of tokens, paged: KV head
-  int inner_, each_, blocks_;    // units of the group, tiles counted for each; blocks of the sequence
+  int inner_, each_, tiles_, blocks_;      // units of the group, their length and tiles; blocks of the sequence
   int unit_;                     // first position of the unit at hand
   int share_, more_;
 
+  __device__ __forceinline__ int least_part() const { return share_ < 8 ? 1 : 2; }     // tiles of a part
   __device__ __forceinline__ int cta_of(int pos) const {
     const int big = more_ * (share_ + 1);
     return pos < big ? pos / (share_ + 1) : more_ + (pos - big) / max(share_, 1);
@@ -282,30 +293,44 @@ class AttendSchedule {
     blocks_ = attend_blocks(a_, nq);
     if (a_.paged) {
       inner_ = blocks_;
-      each_ = max(attend_paged_tiles(a_, attend_rows(a_, s_ * a_.n_kv_heads + x_)), 1);
+      tiles_ = attend_paged_tiles(a_, attend_rows(a_, s_ * a_.n_kv_heads + x_));
     } else {
       inner_ = x_ < blocks_ ? a_.n_kv_heads : 0;
-      each_ = max(attend_prompt_tiles(a_, nq, seq_keys(s_), x_), 1);
+      tiles_ = attend_prompt_tiles(a_, nq, seq_keys(s_), x_);
     }
+    each_ = attend_length(a_, tiles_);
+  }
+  // Tiles of a unit of length each_ that lie in front of a cut at v.
+  __device__ __forceinline__ int cut(int v) const {
+    const int n = tiles_;
+    if (v >= each_) return n;
+    if (v <= 0) return 0;
+    if (a_.whole) return 2 * v < each_ ? 0 : n;
+    const int t = v - kUnitCost, least = least_part();
+    return t < least ? 0 : t > n - least ? n : t;
   }
   __device__ __forceinline__ bool next_share(AttendPiece* p) {
-    if (pos_ >= end_) return false;
-    while (pos_ >= group_ + inner_ * each_) {
-      group_ += inner_ * each_;
-      if (++x_ >= (a_.paged ? a_.n_kv_heads : blocks_)) { x_ = 0; ++s_; }
-      if (s_ >= a_.n_seqs) return false;                       // lengths on the device that are not the host's
-      load_group();
+    while (pos_ < end_) {
+      while (pos_ >= group_ + inner_ * each_) {
+        group_ += inner_ * each_;
+        if (++x_ >= (a_.paged ? a_.n_kv_heads : blocks_)) { x_ = 0; ++s_; }
+        if (s_ >= a_.n_seqs) return false;                     // lengths on the device that are not the host's
+        load_group();
+      }
+      const int rel = pos_ - group_, unit = (unsigned)rel / (unsigned)each_, v0 = rel - unit * each_;
+      const int v1 = min(each_, v0 + end_ - pos_), n = tiles_;
+      const int tile0 = cut(v0), tile1 = cut(v1);
+      unit_ = pos_ - v0;
+      pos_ += v1 - v0;
+      if (n == 0 ? v0 > 0 : tile0 == tile1) continue;
+      if (a_.paged) fill(p, s_, x_, unit);
+      else fill(p, s_, unit, x_);
+      p->tile0 = tile0;
+      p->n = tile1 - tile0;
+      p->part = p->n == n ? -1 : (tile0 == 0 ? 1 : 0);
+      return true;
     }
-    const int rel = pos_ - group_, unit = (unsigned)rel / (unsigned)each_, tile0 = rel - unit * each_;
-    const int take = min(each_ - tile0, end_ - pos_);
-    unit_ = pos_ - tile0;
-    if (a_.paged) fill(p, s_, x_, unit);
-    else fill(p, s_, unit, x_);
-    p->tile0 = tile0;
-    p->n = p->n_all == 0 ? 0 : take;
-    p->part = take == each_ ? -1 : (tile0 == 0 ? 1 : 0);
-    pos_ += take;
-    return true;
+    return false;
   }
   __device__ __forceinline__ void fill(AttendPiece* p, int s, int h, int t) const {
     p->s = s;

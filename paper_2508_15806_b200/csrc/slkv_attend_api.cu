@@ -1,5 +1,4 @@
 // extern "C" entry points of the prompt attention and of the paged cache: argument checks, then one launcher each.
-#include <cmath>
 
 #include "slkv_attend.cuh"
 #include "slkv_paged.cuh"
@@ -49,7 +48,43 @@ void set_blocks(AttendShape* a, int dtype, long long max_tokens) {
   a->q_head_inner = dtype == SLKV_F32 || a->q_head <= a->q_tok;
 }
 
+// Segments of so many tiles are not cut: the second launch costs more.
+constexpr int kWholeTiles = 4;
+// What pieces and the launch that joins them cost, in the time of a tile.
+constexpr int kJoinCost = 8;
+
 // ---- prompts
+// Whole units dealt out, or equal shares of all tiles whose pieces another launch joins?  By the time of the CTA that has the most to do,
+// in tiles: for few units it is added up, in the order in which they are dealt out; many are always dealt out.  Both sides, us: 1000 tokens
+// (128 units) 33 / 39, 2000 51 / 71, 3000 90 / 114; four chunks behind 24000 tokens 400 / 223.  Returns the number of units.
+long long spread_or_share(const int32_t* cu_q, const int32_t* cu_k, AttendShape* a) {
+  const int tile = 1 << a->tile_bits;
+  long long units = 0;
+  for (int s = 0; s < a->n_seqs; ++s) units += (cu_q[s + 1] - cu_q[s] + a->unit_tokens - 1) / a->unit_tokens;
+  units *= a->n_kv_heads;
+  a->spread = 1;
+  constexpr int kMostCtas = 512;
+  if (units >= 3ll * a->n_cta || (long long)a->n_seqs * a->levels > (1 << 16) || a->n_cta > kMostCtas) return units;
+  long long load[kMostCtas] = {};
+  long long total = 0, item = 0, most = 0;
+  for (int level = a->levels - 1; level >= 0; --level)
+    for (int s = 0; s < a->n_seqs; ++s) {
+      const long long nq = cu_q[s + 1] - cu_q[s], nk = cu_k[s + 1] - cu_k[s], first = (long long)level * a->unit_tokens;
+      if (first >= nq) continue;
+      const long long seen = (first + a->unit_tokens < nq ? first + a->unit_tokens : nq) + nk - nq;
+      const long long length = (seen > 0 ? (seen + tile - 1) / tile : 0) + kUnitCost;
+      total += length * a->n_kv_heads;
+      for (int h = 0; h < a->n_kv_heads; ++h, ++item) {
+        const long long round = item / a->n_cta, place = item % a->n_cta;
+        long long& l = load[round & 1 ? a->n_cta - 1 - place : place];
+        l += length;
+        if (l > most) most = l;
+      }
+    }
+  if (most > total / a->n_cta + kJoinCost && total < (1ll << 31)) a->spread = 0;
+  return units;
+}
+
 int check_prompt(const slkv_prompt_params* p, const int32_t* cu_q, const int32_t* cu_k, AttendShape* a) {
   if (!p || !cu_q) return SLKV_ERR_NULL_PTR;
   if (!cu_k) cu_k = cu_q;
@@ -77,27 +112,8 @@ int check_prompt(const slkv_prompt_params* p, const int32_t* cu_q, const int32_t
   a->scale = p->scale;
   set_blocks(a, p->dtype, longest);
   a->lse_unit = p->lse_units == SLKV_LSE_LOG2 ? 1.0f : 0.69314718055994531f;
-  // Three units or more for each CTA: whole ones, dealt out; fewer: all tiles in equal shares, pieces joined by another launch.
-  long long units = 0;
-  for (int s = 0; s < p->n_seqs; ++s) units += (cu_q[s + 1] - cu_q[s] + a->unit_tokens - 1) / a->unit_tokens;
-  units *= p->n_kv_heads;
   a->levels = (int)((longest + a->unit_tokens - 1) / a->unit_tokens);
-  a->spread = units >= 3ll * a->n_cta;
-  if (!a->spread) {
-    long long most = 0, tiles = 0;
-    for (int s = 0; s < p->n_seqs; ++s) {
-      const int nq = cu_q[s + 1] - cu_q[s], nk = cu_k[s + 1] - cu_k[s];
-      for (int t = 0; t * a->unit_tokens < nq; ++t) {
-        const int end = (t + 1) * a->unit_tokens < nq ? (t + 1) * a->unit_tokens : nq, seen = end + nk - nq;
-        const long long n = seen > 0 ? (seen + (1 << a->tile_bits) - 1) >> a->tile_bits : 1;
-        tiles += n * p->n_kv_heads;
-        if (n > most) most = n;
-      }
-    }
-    // units that are short all the same
-    if (units > 0 && (most <= 2 || tiles >= (1ll << 31))) a->spread = 1;
-    if (!a->spread && tiles < a->n_cta) a->n_cta = (int)tiles;
-  }
+  const long long units = spread_or_share(cu_q, cu_k, a);
   if (a->spread && units < a->n_cta) a->n_cta = (int)(units > 0 ? units : 1);
   return SLKV_OK;
 }
@@ -149,18 +165,19 @@ int check_paged_attend(const slkv_paged_cache* c, const slkv_paged_attend_params
   set_blocks(a, c->dtype, a->n_tokens);
   a->lse_unit = p->lse_units == SLKV_LSE_LOG2 ? 1.0f : 0.69314718055994531f;
   const long long blocks = (a->n_tokens + a->unit_tokens - 1) / a->unit_tokens, longest = (long long)c->max_pages * c->page_rows;
-  const long long most = blocks * a->n_seqs * a->n_kv_heads * (((longest + (1 << a->tile_bits) - 1) >> a->tile_bits) + a->has_new);
-  if (most >= (1ll << 31)) return SLKV_ERR_BAD_SHAPE;      // tiles are counted in 32 bits
-  if (most < a->n_cta) a->n_cta = (int)most;
+  const long long units = blocks * a->n_seqs * a->n_kv_heads, tiles = ((longest + (1 << a->tile_bits) - 1) >> a->tile_bits) + a->has_new;
+  if (units * (tiles + kUnitCost) >= (1ll << 31)) return SLKV_ERR_BAD_SHAPE;             // counted in 32 bits
+  a->whole = tiles <= kWholeTiles ? (units <= a->n_cta ? 2 : 1) : 0;
+  if (a->whole && units < a->n_cta) a->n_cta = (int)units;
   return SLKV_OK;
 }
 
-size_t workspace_of(const AttendShape& a) { return a.spread ? 256 : attend_workspace(a.n_cta, a.part_rows, a.head_dim); }
+size_t workspace_of(const AttendShape& a) { return a.spread || a.whole ? 256 : attend_workspace(a.n_cta, a.part_rows, a.head_dim); }
 
 int attend(AttendShape* a, int dtype, void* workspace, size_t workspace_bytes, cudaStream_t st) {
   if (!workspace || workspace_bytes < workspace_of(*a)) return SLKV_ERR_WORKSPACE;
   if (!aligned16(workspace)) return SLKV_ERR_BAD_ALIGN;
-  if (!a->spread) attend_bind(a, workspace);
+  if (!a->spread && !a->whole) attend_bind(a, workspace);
   int launches = 0;
   cudaError_t e = dtype == SLKV_F32 ? launch_attend_f32(*a, st, &launches) : launch_attend_tensor(*a, st, &launches);
   if (e == cudaSuccess) e = launch_attend_join(*a, dtype == SLKV_F32, st, &launches);

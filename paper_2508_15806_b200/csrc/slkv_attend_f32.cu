@@ -325,6 +325,8 @@ __device__ __forceinline__ void softmax_role(const AttendF32& t, Smem<D>& sm) {
   auto wait = [&](unsigned long long* bar, unsigned phase) {
     return __all_sync(0xffffffffu, mbar_wait(smem_u32(bar), phase & 1, &sm.abort)) != 0;
   };
+  int rt, rh;                                    // the thread's row: token of the block, query head of the group
+  if (!attend_row(a, row, &rt, &rh)) rt = 1 << 20;
   unsigned done = 0;
   for (unsigned nth = 0;; ++nth) {
     if (!wait(&sm.unit_full[nth % kUnits], nth / kUnits)) return;
@@ -332,8 +334,7 @@ __device__ __forceinline__ void softmax_role(const AttendF32& t, Smem<D>& sm) {
     __syncwarp();
     if (lane == 0) mbar_arrive(smem_u32(&sm.unit_empty[nth % kUnits]));
     if (p.stop) return;
-    int rt, rh;
-    const bool there = attend_row(a, row, &rt, &rh) && rt < p.n_tok;
+    const bool there = rt < p.n_tok;
     const int tok = p.tok0 + rt, bound = max(min(tok + 1 + p.shift, p.nk), 0);
     unsigned long long mask = 0;
     if (a.has_new && there) {
@@ -552,7 +553,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_f32(const __grid_constan
       mbar_wait(smem_u32(&sm.drain), 0, &never);
     }
   } else if (warp == kPlanWarp) {
-    if (lane == 0 && !t.a.spread) t.a.desc[2 * blockIdx.x].state = t.a.desc[2 * blockIdx.x + 1].state = 0;
+    if (lane == 0 && t.a.desc) t.a.desc[2 * blockIdx.x].state = t.a.desc[2 * blockIdx.x + 1].state = 0;
     AttendSchedule plan(t.a, blockIdx.x, &sm.start);
     for (unsigned nth = 0;; ++nth) {
       AttendPiece p = {};
@@ -576,7 +577,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_f32(const __grid_constan
   tc_fence_after();
   if (sm.abort && threadIdx.x == 0) {
     if (t.a.status) *t.a.status = SLKV_ERR_DEVICE_TIMEOUT;
-    if (!t.a.spread) t.a.desc[2 * blockIdx.x].state = t.a.desc[2 * blockIdx.x + 1].state = -1;
+    if (t.a.desc) t.a.desc[2 * blockIdx.x].state = t.a.desc[2 * blockIdx.x + 1].state = -1;
   }
   if (warp == kMmaWarp)
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(sm.tmem) : "memory");

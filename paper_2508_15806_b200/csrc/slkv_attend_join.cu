@@ -68,7 +68,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) k_attend_join(const __grid_co
 }  // namespace
 
 cudaError_t launch_attend_join(const AttendShape& a, bool f32, cudaStream_t st, int* launches) {
-  if (a.spread || a.n_cta < 2) return cudaSuccess;
+  if (a.spread || a.whole || a.n_cta < 2) return cudaSuccess;
   LaunchScope scope(KID_ATTEND_JOIN, st, launches);
   const dim3 grid((unsigned)(a.n_cta - 1), (unsigned)((a.used_rows + kJoinRows - 1) / kJoinRows)), block(kJoinWarps * 32);
   if (a.head_dim == 128) return f32 ? launch_pdl(k_attend_join<128, true>, grid, block, 0, st, 1, a) : launch_pdl(k_attend_join<128, false>, grid, block, 0, st, 1, a);

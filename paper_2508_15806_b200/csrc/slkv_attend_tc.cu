@@ -403,6 +403,8 @@ __device__ __forceinline__ void softmax_role(const AttendTc& t, Smem<D>& sm, int
   const uint32_t ts = lanes + kTmemS + 128 * g, to = lanes + kTmemO + 128 * g;
   const f32x2 sc2 = pack2(t.sc, t.sc);
   unsigned loads = 0, n_s = 0, n_o = 0, n_merge = 0;
+  int rt, rh;                                    // the thread's row: token of the block, query head of the group
+  if (!attend_row(a, tid, &rt, &rh)) rt = 1 << 20;
   auto say_most = [&] {
     tc_wait_st();
     tc_fence_before();
@@ -418,8 +420,7 @@ __device__ __forceinline__ void softmax_role(const AttendTc& t, Smem<D>& sm, int
     if (p.stop) return;
     const Blocks b(t, p);
     const int tok0 = p.tok0 + (b.alt ? 0 : g * a.block_tokens), n_tok = min(a.block_tokens, p.n_seq_tok - tok0);
-    int rt, rh;
-    const bool there = attend_row(a, tid, &rt, &rh) && rt < n_tok;
+    const bool there = rt < n_tok;
     const int tok = tok0 + rt;
     const int bound = max(min(tok + 1 + p.shift, p.nk), 0);
     unsigned long long mask = 0;
@@ -677,7 +678,7 @@ k_attend_tc(const __grid_constant__ AttendTc t, const __grid_constant__ AttendMa
     } else if (warp == kQueryWarp) {
       if (lane == 0) query_role<D>(t, maps, sm);
     } else if (warp == kPlanWarp) {
-      if (lane == 0 && !t.a.spread) t.a.desc[2 * blockIdx.x].state = t.a.desc[2 * blockIdx.x + 1].state = 0;
+      if (lane == 0 && t.a.desc) t.a.desc[2 * blockIdx.x].state = t.a.desc[2 * blockIdx.x + 1].state = 0;
       AttendSchedule plan(t.a, blockIdx.x, &sm.start);
       for (unsigned nth = 0;; ++nth) {
         AttendPiece p = {};
@@ -705,7 +706,7 @@ k_attend_tc(const __grid_constant__ AttendTc t, const __grid_constant__ AttendMa
   tc_fence_after();
   if (sm.abort && threadIdx.x == 0) {
     if (t.a.status) *t.a.status = SLKV_ERR_DEVICE_TIMEOUT;
-    if (!t.a.spread) t.a.desc[2 * blockIdx.x].state = t.a.desc[2 * blockIdx.x + 1].state = -1;
+    if (t.a.desc) t.a.desc[2 * blockIdx.x].state = t.a.desc[2 * blockIdx.x + 1].state = -1;
   }
   if (warp == kMmaWarp)
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(sm.tmem) : "memory");
