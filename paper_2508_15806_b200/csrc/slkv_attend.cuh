@@ -51,6 +51,7 @@ struct AttendShape {
   struct AttendPart* desc;                       // [n_cta][2]
   int part_rows, used_rows;                      // rows of a unit there is room for, and at most in use
   int q_head_inner, box_tokens;                  // how a block's rows lie: see attend_row; tokens of a block in shared memory
+  int row_inverse;                               // 2^16 / G or 2^16 / box_tokens, rounded up: exact for rows below 128
 };
 
 size_t attend_workspace(int n_cta, int part_rows, int head_dim);
@@ -78,9 +79,8 @@ struct AttendPiece {
 // Row r of a unit: its token of the unit and its query head of the group; false: no row.  Rows come in blocks of 128; in a block the query heads of a token lie next to each other, or the tokens of a query head (q_head_inner = 0).
 __device__ __forceinline__ bool attend_row(const AttendShape& a, int r, int* tok, int* head) {
   const int b = r >> 7, i = r & 127;
-  int rt, rh;
-  if (a.q_head_inner) { rt = i / a.G; rh = i - rt * a.G; }
-  else { rh = i / a.box_tokens; rt = i - rh * a.box_tokens; }
+  const int quotient = i * a.row_inverse >> 16, rest = i - quotient * (a.q_head_inner ? a.G : a.box_tokens);
+  const int rt = a.q_head_inner ? quotient : rest, rh = a.q_head_inner ? rest : quotient;
   *tok = b * a.block_tokens + rt;
   *head = rh;
   return rt < a.block_tokens && rh < a.G;

@@ -46,6 +46,8 @@ void set_blocks(AttendShape* a, int dtype, long long max_tokens) {
   a->tile_bits = dtype == SLKV_F32 ? kF32TileBits : kAttendTileBits;
   a->n_cta = sm_count();
   a->q_head_inner = dtype == SLKV_F32 || a->q_head <= a->q_tok;
+  const int inner = a->q_head_inner ? a->G : a->box_tokens;
+  a->row_inverse = (65536 + inner - 1) / inner;
 }
 
 // Segments of so many tiles are not cut: the second launch costs more.
