@@ -589,8 +589,8 @@ int slkv_prompt_attend(const slkv_prompt_params* p, const void* q, const void* k
  * device arrays that the host never reads: lengths beyond max_pages pages are cut to them, entries of tables outside the pool are read as
  * pages of zeros (status: SLKV_ERR_BAD_SHAPE).
  * Everything is enqueued on `stream`, nothing is allocated, every call can be captured.  A cache and a workspace belong to one call at a
- * time.  n_seqs * n_kv_heads <= 16384, n_layers times that <= 2^20, n_pages and max_pages times page_rows <= 2^31 - 512; pages, rows and workspaces
- * 16-byte aligned.
+ * time.  n_seqs * n_kv_heads <= 16384, n_layers times that <= 2^20, that times max_pages < 2^31; n_pages and max_pages times page_rows
+ * <= 2^31 - 512; pages, rows and workspaces 16-byte aligned.
  */
 typedef struct slkv_paged_cache {
   int32_t n_layers, n_seqs, n_kv_heads;

@@ -131,6 +131,7 @@ int check_cache(const slkv_paged_cache* c) {
   if (c->page_rows != 16 && c->page_rows != 32 && c->page_rows != 64 && c->page_rows != 128) return SLKV_ERR_BAD_SHAPE;
   if (c->n_pages < 1 || (long long)c->n_pages * c->page_rows > kMaxRows) return SLKV_ERR_BAD_SHAPE;
   if (c->max_pages < 1 || (long long)c->max_pages * c->page_rows > kMaxRows) return SLKV_ERR_BAD_SHAPE;
+  if ((long long)c->n_layers * c->n_seqs * c->n_kv_heads * c->max_pages >= (1ll << 31)) return SLKV_ERR_BAD_SHAPE;
   if (!aligned16(c->k_pages) || !aligned16(c->v_pages)) return SLKV_ERR_BAD_ALIGN;
   return SLKV_OK;
 }
@@ -233,7 +234,8 @@ int slkv_paged_plan(const slkv_paged_cache* c, int32_t mode, const int32_t* want
   if ((lens_out == nullptr) != (n_free_out == nullptr)) return SLKV_ERR_NULL_PTR;
   PagedPlanArgs a = {};
   a.n_seqs = c->n_seqs; a.n_kv_heads = c->n_kv_heads; a.n_seg = (int)n_seg;
-  a.page_rows = c->page_rows; a.n_pages = c->n_pages; a.max_pages = c->max_pages;
+  for (a.page_bits = 0; (1 << a.page_bits) < c->page_rows;) ++a.page_bits;
+  a.n_pages = c->n_pages; a.max_pages = c->max_pages;
   a.mode = mode; a.slot_width = slot_width;
   a.tables = c->tables; a.lens = c->lens; a.lens_out = lens_out ? lens_out : c->lens;
   a.free_pages = c->free_pages; a.n_free = c->n_free; a.n_free_out = n_free_out ? n_free_out : c->n_free;

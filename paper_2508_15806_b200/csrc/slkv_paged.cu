@@ -12,203 +12,218 @@ namespace cg = cooperative_groups;
 constexpr int kPlanThreads = 1024, kPlanWarps = kPlanThreads / 32, kPlanCluster = 8;
 constexpr int kSlotsHere = 1 << 16;              // ragged slots that the planning launch writes itself
 
-// Exclusive prefix over the block of one value a thread; *total: of all.
-__device__ __forceinline__ long long block_scan(long long v, long long* warp_sums, long long* total) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  long long incl = v;
+// Exclusive prefix over the block of two values a thread (32 bits each, sums below 2^31 of the lower one); *total: of all.
+__device__ __forceinline__ unsigned long long block_scan(unsigned long long v, unsigned long long* warp_sums, unsigned long long* total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n_warps = blockDim.x >> 5;
+  unsigned long long incl = v;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
-    const long long o = __shfl_up_sync(0xffffffffu, incl, d);
+    const unsigned long long o = __shfl_up_sync(0xffffffffu, incl, d);
     if (lane >= d) incl += o;
+  }
+  if (n_warps == 1) {
+    *total = __shfl_sync(0xffffffffu, incl, 31);
+    return incl - v;
   }
   if (lane == 31) warp_sums[warp] = incl;
   __syncthreads();
-  long long w = lane < kPlanWarps ? warp_sums[lane] : 0, wi = w;
-#pragma unroll
-  for (int d = 1; d < 32; d <<= 1) {
-    const long long o = __shfl_up_sync(0xffffffffu, wi, d);
-    if (lane >= d) wi += o;
+  unsigned long long before = 0, all = 0;
+#pragma unroll 4
+  for (int w = 0; w < n_warps; ++w) {
+    const unsigned long long x = warp_sums[w];
+    if (w < warp) before += x;
+    all += x;
   }
-  *total = __shfl_sync(0xffffffffu, wi, 31);
-  const long long before = __shfl_sync(0xffffffffu, wi - w, warp);
+  *total = all;
   __syncthreads();                               // warp_sums may be written again
   return before + incl - v;
 }
+__device__ __forceinline__ unsigned long long pack(unsigned hi, unsigned lo) { return (unsigned long long)hi << 32 | lo; }
 
 struct Segment { int len, want, have, need; };
 
 __device__ __forceinline__ Segment segment(const PagedPlanArgs& a, int seg) {
   Segment x;
-  const long long most = (long long)a.max_pages * a.page_rows;
-  x.len = (int)min((long long)max(a.lens[seg], 0), most);
+  const int most = a.max_pages << a.page_bits;
+  x.len = min(max(a.lens[seg], 0), most);
   long long want;
   if (a.mode == SLKV_PAGED_LENGTHS) {
     want = a.want[seg];
   } else if (a.mode == SLKV_PAGED_OFFSETS) {
-    const int per = a.n_seqs * a.n_kv_heads, layer = seg / per;
-    const int32_t* o = a.want + (long long)layer * (per + 1) + (seg - layer * per);
+    const int per = a.n_seqs * a.n_kv_heads, layer = (unsigned)seg / (unsigned)per;
+    const int32_t* o = a.want + seg + layer;     // a layer has one offset more than segments
     want = (long long)o[1] - o[0];
   } else {
-    want = (long long)x.len + max(a.want[seg / a.n_kv_heads % a.n_seqs], 0);
+    want = (long long)x.len + max(a.want[(unsigned)seg / (unsigned)a.n_kv_heads % (unsigned)a.n_seqs], 0);
   }
-  x.want = (int)min(max(want, 0ll), most);
-  x.have = (x.len + a.page_rows - 1) / a.page_rows;
-  x.need = (x.want + a.page_rows - 1) / a.page_rows;
+  x.want = (int)min(max(want, 0ll), (long long)most);
+  const int mask = (1 << a.page_bits) - 1;
+  x.have = (x.len + mask) >> a.page_bits;
+  x.need = (x.want + mask) >> a.page_bits;
   return x;
 }
 
-// One cluster.  A CTA has a run of segments, 1024 at a time a thread each; what lies before a segment is what the CTAs before this one
-// come to (exchanged through their shared memory) and a scan.  Pages are moved by the segment's thread, or by its warp where there are
-// many.  What bounds it: three or four dependent reads of L2 and the barriers between them, the data is a few hundred KB.
+__device__ __forceinline__ int slot_of(const PagedPlanArgs& a, long long table, int row) {
+  return (a.tables[table + (row >> a.page_bits)] << a.page_bits) + (row & ((1 << a.page_bits) - 1));
+}
+
+// dst[to + TO i] = src[from + FROM i] for i below each lane's count, where that lies below `limit`: by the lane itself where all have
+// few, else by the warp, one lane's after the other.
+template <int TO, int FROM>
+__device__ __forceinline__ void move_run(int32_t* dst, long long to, long long limit, const int32_t* src, long long from, int count) {
+  const int lane = threadIdx.x & 31;
+  constexpr int kFew = 4;
+  if (__all_sync(0xffffffffu, count <= kFew)) {
+#pragma unroll
+    for (int i = 0; i < kFew; ++i)
+      if (i < count && (unsigned long long)(to + TO * i) < (unsigned long long)limit) dst[to + TO * i] = __ldcg(src + from + FROM * i);
+  } else {
+    for (unsigned todo = __ballot_sync(0xffffffffu, count > 0); todo; todo &= todo - 1) {
+      const int l = __ffs(todo) - 1, n = __shfl_sync(0xffffffffu, count, l);
+      const long long t = __shfl_sync(0xffffffffu, to, l), f = __shfl_sync(0xffffffffu, from, l);
+      for (int i = lane; i < n; i += 32)
+        if ((unsigned long long)(t + TO * i) < (unsigned long long)limit) dst[t + TO * i] = __ldcg(src + f + FROM * i);
+    }
+  }
+  __syncwarp();
+}
+
+// One cluster, or one CTA where that does.  A CTA has a run of segments, a thread each at a time; what lies before a segment is what the
+// CTAs before this one come to (exchanged through their shared memory) and a scan.  What bounds it: three or four dependent reads of L2
+// and the barriers between them, the data is a few hundred KB at most; so lengths are read once where a thread has one segment, and
+// pages returned and taken are counted in one scan.
 __global__ void __launch_bounds__(kPlanThreads) k_paged_plan(const __grid_constant__ PagedPlanArgs a) {
   cg::cluster_group cluster = cg::this_cluster();
-  __shared__ long long warp_sums[kPlanWarps];
-  __shared__ long long totals[3];                // of this CTA: pages returned, pages wanted, rows that come in
+  __shared__ unsigned long long warp_sums[kPlanWarps];
+  __shared__ unsigned long long totals[2];       // of this CTA: pages returned and wanted; rows that come in
   const int rank = (int)cluster.block_rank(), n_cta = (int)cluster.num_blocks();
-  const int tid = threadIdx.x, lane = tid & 31;
+  const int tid = threadIdx.x, lane = tid & 31, threads = blockDim.x;
+  auto sync = [&] {
+    if (n_cta == 1) __syncthreads();
+    else cluster.sync();
+  };
   pdl_launch_dependents();
   pdl_wait();
   const int first = (int)((long long)a.n_seg * rank / n_cta), last = (int)((long long)a.n_seg * (rank + 1) / n_cta);
-
-  long long gone = 0, more = 0;
-  for (int seg = first + tid; seg < last; seg += kPlanThreads) {
-    const Segment x = segment(a, seg);
-    gone += max(x.have - x.need, 0);
-    more += max(x.need - x.have, 0);
-  }
-  long long sum;
-  block_scan(gone, warp_sums, &sum);
-  if (tid == 0) totals[0] = sum;
-  block_scan(more, warp_sums, &sum);
-  if (tid == 0) totals[1] = sum;
+  const bool once = last - first <= threads;     // a segment a thread: x and its place stay in registers
   const long long n_free = min(max(a.n_free[0], 0), a.n_pages);
-  cluster.sync();
-  long long gone_before = 0, gone_all = 0, more_before = 0, more_all = 0;
-  for (int r = 0; r < n_cta; ++r) {
-    const long long* t = cluster.map_shared_rank(totals, r);
-    if (r == rank) { gone_before = gone_all; more_before = more_all; }
-    gone_all += t[0];
-    more_all += t[1];
+
+  Segment x = {};
+  unsigned long long place = 0, sum = 0, all = 0;
+  for (int s0 = first; s0 < last; s0 += threads) {
+    x = Segment{};
+    if (s0 + tid < last) x = segment(a, s0 + tid);
+    place = all + block_scan(pack(max(x.have - x.need, 0), max(x.need - x.have, 0)), warp_sums, &sum);
+    all += sum;
   }
+  unsigned long long before = 0, total = all;
+  if (n_cta > 1) {
+    if (tid == 0) totals[0] = all;
+    cluster.sync();
+    total = 0;
+    for (int r = 0; r < n_cta; ++r) {
+      if (r == rank) before = total;
+      total += cluster.map_shared_rank(totals, r)[0];
+    }
+  }
+  const long long gone_all = total >> 32, more_all = total & 0xffffffffu;
   const long long stack = n_free + gone_all;     // pages on it once all are returned
+  // The segments again, with what lies before each: returned pages in the upper word, wanted ones in the lower.
+  auto again = [&](auto body) {
+    if (once) {
+      body(first + tid, x, before + place);
+      return;
+    }
+    unsigned long long run = before;
+    for (int s0 = first; s0 < last; s0 += threads) {
+      Segment y = {};
+      if (s0 + tid < last) y = segment(a, s0 + tid);
+      const unsigned long long at = run + block_scan(pack(max(y.have - y.need, 0), max(y.need - y.have, 0)), warp_sums, &sum);
+      run += sum;
+      body(s0 + tid, y, at);
+    }
+  };
 
   if (gone_all > 0) {                            // the first segment's first page ends up on top
-    long long before = gone_before;
-    for (int s0 = first; s0 < last; s0 += kPlanThreads) {
-      const int seg = s0 + tid;
-      Segment x = {};
-      if (seg < last) x = segment(a, seg);
-      const int n = max(x.have - x.need, 0);
-      const long long at = before + block_scan(n, warp_sums, &sum);
-      before += sum;
-      unsigned todo = __ballot_sync(0xffffffffu, n > 0);
-      for (; todo; todo &= todo - 1) {
-        const int l = __ffs(todo) - 1;
-        const int m = __shfl_sync(0xffffffffu, n, l), need = __shfl_sync(0xffffffffu, x.need, l);
-        const long long to = stack - 1 - __shfl_sync(0xffffffffu, at, l);
-        const int32_t* row = a.tables + (long long)(seg - lane + l) * a.max_pages + need;
-        for (int i = lane; i < m; i += 32)
-          if (to - i >= 0 && to - i < a.n_pages) a.free_pages[to - i] = row[i];
-      }
-    }
-    cluster.sync();                              // some are taken again below
+    again([&](int seg, const Segment& y, unsigned long long at) {
+      move_run<-1, 1>(a.free_pages, stack - 1 - (long long)(at >> 32), a.n_pages, a.tables, (long long)seg * a.max_pages + y.need,
+                      max(y.have - y.need, 0));
+    });
+    sync();                                      // some are taken again below
   }
 
   // pages taken and new lengths; rows that come in
-  const long long fits = min(stack, (long long)a.n_pages);
-  bool short_of = false;
-  auto new_length = [&](const Segment& x, long long at, int* granted) {
-    const int wanted = max(x.need - x.have, 0);
-    *granted = (int)min(max(fits - at, 0ll), (long long)wanted);
-    return (int)min((long long)x.want, (long long)(min(x.have, x.need) + *granted) * a.page_rows);
+  const long long fits = min(stack, (long long)a.n_pages), entries = (long long)a.n_seg * a.max_pages;
+  auto new_length = [&](const Segment& y, unsigned long long at, int* granted) {
+    const int wanted = max(y.need - y.have, 0);
+    *granted = (int)min(max(fits - (long long)(at & 0xffffffffu), 0ll), (long long)wanted);
+    return min(y.want, (min(y.have, y.need) + *granted) << a.page_bits);
   };
   const bool ragged = a.slots && a.slot_width == 0;
-  long long rows_before = 0, rows_all = 0;
-  if (ragged) {
-    long long before = more_before, rows = 0;
-    for (int s0 = first; s0 < last; s0 += kPlanThreads) {
-      const int seg = s0 + tid;
-      Segment x = {};
-      if (seg < last) x = segment(a, seg);
-      const long long at = before + block_scan(max(x.need - x.have, 0), warp_sums, &sum);
-      before += sum;
+  unsigned long long rows_before = 0, rows_all = 0;
+  if (ragged && n_cta > 1) {
+    unsigned long long rows = 0;
+    again([&](int, const Segment& y, unsigned long long at) {
       int granted;
-      rows += max(new_length(x, at, &granted) - x.len, 0);
-    }
-    block_scan(rows, warp_sums, &sum);
-    if (tid == 0) totals[2] = sum;
+      block_scan((unsigned long long)max(new_length(y, at, &granted) - y.len, 0), warp_sums, &sum);
+      rows += sum;
+    });
+    if (tid == 0) totals[1] = rows;
     cluster.sync();
     for (int r = 0; r < n_cta; ++r) {
       if (r == rank) rows_before = rows_all;
-      rows_all += cluster.map_shared_rank(totals, r)[2];
+      rows_all += cluster.map_shared_rank(totals, r)[1];
     }
   }
-  long long before = more_before;
-  for (int s0 = first; s0 < last; s0 += kPlanThreads) {
-    const int seg = s0 + tid;
-    Segment x = {};
-    if (seg < last) x = segment(a, seg);
-    const long long at = before + block_scan(max(x.need - x.have, 0), warp_sums, &sum);
-    before += sum;
-    int granted = 0;
-    const int len = new_length(x, at, &granted);
-    const int added = max(len - x.len, 0);
-    if (seg < last) {
-      short_of |= len < x.want;
+  bool short_of = false;
+  again([&](int seg, const Segment& y, unsigned long long at) {
+    int granted;
+    const int len = new_length(y, at, &granted), added = max(len - y.len, 0);
+    const bool mine = seg < last;
+    if (mine) {
+      short_of |= len < y.want;
       a.lens_out[seg] = len;
     }
-    unsigned todo = __ballot_sync(0xffffffffu, granted > 0);
-    for (; todo; todo &= todo - 1) {
-      const int l = __ffs(todo) - 1;
-      const int m = __shfl_sync(0xffffffffu, granted, l), have = __shfl_sync(0xffffffffu, x.have, l);
-      const long long from = fits - 1 - __shfl_sync(0xffffffffu, at, l);
-      int32_t* row = a.tables + (long long)(seg - lane + l) * a.max_pages + have;
-      for (int i = lane; i < m; i += 32) row[i] = __ldcg(a.free_pages + from - i);
-    }
+    const long long row0 = (long long)seg * a.max_pages;
+    move_run<1, -1>(a.tables, row0 + y.have, entries, a.free_pages, fits - 1 - (long long)(at & 0xffffffffu), mine ? granted : 0);
     if (ragged) {
-      const long long to = rows_before + block_scan(added, warp_sums, &sum);
+      const unsigned long long to = rows_before + block_scan((unsigned long long)added, warp_sums, &sum);
       rows_before += sum;
-      if (seg < last) {
-        a.slot_offsets[seg] = (int)min(to, (long long)0x7fffffff);
-        if (seg == a.n_seg - 1) a.slot_offsets[a.n_seg] = (int)min(to + added, (long long)0x7fffffff);
+      if (mine) {
+        a.slot_offsets[seg] = (int)min(to, 0x7fffffffull);
+        if (seg == a.n_seg - 1) a.slot_offsets[a.n_seg] = (int)min(to + added, 0x7fffffffull);
       }
       if (a.n_slots <= kSlotsHere) {
-        todo = __ballot_sync(0xffffffffu, added > 0);
-        for (; todo; todo &= todo - 1) {
-          const int l = __ffs(todo) - 1;
-          const int m = __shfl_sync(0xffffffffu, added, l), r0 = __shfl_sync(0xffffffffu, x.len, l);
-          const long long t0 = __shfl_sync(0xffffffffu, to, l);
-          const int32_t* row = a.tables + (long long)(seg - lane + l) * a.max_pages;
-          __syncwarp();
-          for (int i = lane; i < m && t0 + i < a.n_slots; i += 32) {
-            const int pg = (r0 + i) / a.page_rows;
-            a.slots[t0 + i] = row[pg] * a.page_rows + r0 + i - pg * a.page_rows;
-          }
+        for (unsigned todo = __ballot_sync(0xffffffffu, added > 0); todo; todo &= todo - 1) {
+          const int l = __ffs(todo) - 1, m = __shfl_sync(0xffffffffu, added, l), r0 = __shfl_sync(0xffffffffu, y.len, l);
+          const unsigned long long t0 = __shfl_sync(0xffffffffu, to, l);
+          const long long table = __shfl_sync(0xffffffffu, row0, l);
+          for (int i = lane; i < m && t0 + i < (unsigned long long)a.n_slots; i += 32) a.slots[t0 + i] = slot_of(a, table, r0 + i);
         }
       }
     } else if (a.slots) {
-      // 32 segments' slots are one run of the output
-      __syncwarp();
-      const int here = min(last - (seg - lane), 32);
-      for (int i0 = 0; i0 < here * a.slot_width; i0 += 32) {
-        const int i = i0 + lane, l = min(i / a.slot_width, 31), e = i - l * a.slot_width;
-        const int m = __shfl_sync(0xffffffffu, added, l), r = __shfl_sync(0xffffffffu, x.len, l) + e;
-        if (i >= here * a.slot_width) continue;
-        const long long sg = seg - lane + l;
-        const int pg = r / a.page_rows;
-        a.slots[sg * a.slot_width + e] = e < m ? a.tables[sg * a.max_pages + pg] * a.page_rows + r - pg * a.page_rows : -1;
+      short_of |= mine && added > a.slot_width;
+      if (a.slot_width <= 16) {                  // a lane its own segment's
+        if (mine)
+          for (int e = 0; e < a.slot_width; ++e) a.slots[(long long)seg * a.slot_width + e] = e < added ? slot_of(a, row0, y.len + e) : -1;
+      } else {
+        for (unsigned todo = __ballot_sync(0xffffffffu, mine); todo; todo &= todo - 1) {
+          const int l = __ffs(todo) - 1, m = __shfl_sync(0xffffffffu, added, l), r0 = __shfl_sync(0xffffffffu, y.len, l);
+          const long long table = __shfl_sync(0xffffffffu, row0, l), to = (long long)(seg - lane + l) * a.slot_width;
+          for (int e = lane; e < a.slot_width; e += 32) a.slots[to + e] = e < m ? slot_of(a, table, r0 + e) : -1;
+        }
       }
-      short_of |= seg < last && added > a.slot_width;
     }
-  }
+  });
   if (ragged) {
-    short_of |= rows_all > a.n_slots;
+    if (n_cta == 1) rows_all = rows_before;
+    short_of |= rows_all > (unsigned long long)a.n_slots;
     if (a.n_slots <= kSlotsHere)
-      for (long long i = rows_all + rank * kPlanThreads + tid; i < a.n_slots; i += (long long)n_cta * kPlanThreads) a.slots[i] = -1;
+      for (long long i = (long long)rows_all + rank * threads + tid; i < a.n_slots; i += (long long)n_cta * threads) a.slots[i] = -1;
   }
   if (short_of && a.status) *a.status = SLKV_ERR_CAPACITY;
   if (rank == 0 && tid == 0) a.n_free_out[0] = (int)max(fits - more_all, 0ll);
-  cluster.sync();                                // no CTA's shared memory goes while another reads it
+  if (n_cta > 1) cluster.sync();                 // no CTA's shared memory goes while another reads it
 }
 
 // Ragged slots, where there are many: a thread each, its segment by bisection.
@@ -223,8 +238,7 @@ __global__ void __launch_bounds__(256) k_paged_slots(const __grid_constant__ Pag
     const int mid = (lo + hi) >> 1;
     if (a.slot_offsets[mid] <= i) lo = mid; else hi = mid;
   }
-  const int r = a.lens_out[lo] - a.slot_offsets[lo + 1] + (int)i, pg = r / a.page_rows;
-  a.slots[i] = a.tables[(long long)lo * a.max_pages + pg] * a.page_rows + r - pg * a.page_rows;
+  a.slots[i] = slot_of(a, (long long)lo * a.max_pages, a.lens_out[lo] - a.slot_offsets[lo + 1] + (int)i);
 }
 
 // 16 bytes of a K and a V row a thread, of kWriteRows rows at once: their slots are read first, then the rows.
@@ -263,10 +277,13 @@ __global__ void __launch_bounds__(kWriteThreads) k_paged_write(const __grid_cons
 
 cudaError_t launch_paged_plan(const PagedPlanArgs& a, cudaStream_t st, int* launches) {
   {
+    // a segment a thread as far as a cluster goes
     int ctas = 1;
-    while (ctas < kPlanCluster && (long long)ctas * 256 < a.n_seg) ctas *= 2;
+    while (ctas < kPlanCluster && ctas * kPlanThreads / 2 < a.n_seg) ctas *= 2;
+    int threads = (a.n_seg + ctas - 1) / ctas;
+    threads = threads >= kPlanThreads ? kPlanThreads : (threads + 31) / 32 * 32;
     LaunchScope scope(KID_PAGED_PLAN, st, launches);
-    const cudaError_t e = launch_pdl(k_paged_plan, dim3((unsigned)ctas), dim3(kPlanThreads), 0, st, ctas, a);
+    const cudaError_t e = launch_pdl(k_paged_plan, dim3((unsigned)ctas), dim3((unsigned)threads), 0, st, ctas, a);
     if (e != cudaSuccess) return e;
   }
   if (!a.slots || a.slot_width != 0 || a.n_slots <= kSlotsHere) return cudaSuccess;

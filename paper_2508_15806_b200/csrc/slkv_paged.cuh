@@ -6,7 +6,7 @@
 namespace slkv {
 
 struct PagedPlanArgs {
-  int n_seqs, n_kv_heads, n_seg, page_rows, n_pages, max_pages, mode, slot_width;
+  int n_seqs, n_kv_heads, n_seg, page_bits, n_pages, max_pages, mode, slot_width;     // page_bits: log2 of a page's rows
   int32_t* tables;
   const int32_t* lens;
   int32_t* lens_out;
