@@ -67,25 +67,29 @@ __device__ __forceinline__ int slot_of(const PagedPlanArgs& a, long long table, 
   return (a.tables[table + (row >> a.page_bits)] << a.page_bits) + (row & ((1 << a.page_bits) - 1));
 }
 
-// dst[to + TO i] = src[from + FROM i] for i below each lane's count, where that lies below `limit`: by the lane itself where all have
-// few, else by the warp, one lane's after the other.
+// dst[to + TO i] = src[from + FROM i] for i below each thread's count, where that lies below `limit`: by the thread itself where all have
+// few, else by all warps of the CTA, one thread's run each at a time.
+struct Run { long long to, from; int count; };
 template <int TO, int FROM>
-__device__ __forceinline__ void move_run(int32_t* dst, long long to, long long limit, const int32_t* src, long long from, int count) {
-  const int lane = threadIdx.x & 31;
+__device__ __forceinline__ void move_runs(int32_t* dst, long long limit, const int32_t* src, Run mine, Run* runs) {
   constexpr int kFew = 4;
-  if (__all_sync(0xffffffffu, count <= kFew)) {
+  auto move = [&](const Run& r, int i) {
+    if ((unsigned long long)(r.to + TO * i) < (unsigned long long)limit) dst[r.to + TO * i] = __ldcg(src + r.from + FROM * i);
+  };
+  if (!__syncthreads_or(mine.count > kFew)) {
 #pragma unroll
     for (int i = 0; i < kFew; ++i)
-      if (i < count && (unsigned long long)(to + TO * i) < (unsigned long long)limit) dst[to + TO * i] = __ldcg(src + from + FROM * i);
+      if (i < mine.count) move(mine, i);
   } else {
-    for (unsigned todo = __ballot_sync(0xffffffffu, count > 0); todo; todo &= todo - 1) {
-      const int l = __ffs(todo) - 1, n = __shfl_sync(0xffffffffu, count, l);
-      const long long t = __shfl_sync(0xffffffffu, to, l), f = __shfl_sync(0xffffffffu, from, l);
-      for (int i = lane; i < n; i += 32)
-        if ((unsigned long long)(t + TO * i) < (unsigned long long)limit) dst[t + TO * i] = __ldcg(src + f + FROM * i);
+    runs[threadIdx.x] = mine;
+    __syncthreads();
+    for (int t = threadIdx.x >> 5; t < (int)blockDim.x; t += (int)blockDim.x >> 5) {
+      const Run r = runs[t];
+#pragma unroll 4
+      for (int i = threadIdx.x & 31; i < r.count; i += 32) move(r, i);
     }
   }
-  __syncwarp();
+  __syncthreads();                               // the entries are there for the slots; runs may be written again
 }
 
 // One cluster, or one CTA where that does.  A CTA has a run of segments, a thread each at a time; what lies before a segment is what the
@@ -95,6 +99,7 @@ __device__ __forceinline__ void move_run(int32_t* dst, long long to, long long l
 __global__ void __launch_bounds__(kPlanThreads) k_paged_plan(const __grid_constant__ PagedPlanArgs a) {
   cg::cluster_group cluster = cg::this_cluster();
   __shared__ unsigned long long warp_sums[kPlanWarps];
+  __shared__ Run runs[kPlanThreads];
   __shared__ unsigned long long totals[2];       // of this CTA: pages returned and wanted; rows that come in
   const int rank = (int)cluster.block_rank(), n_cta = (int)cluster.num_blocks();
   const int tid = threadIdx.x, lane = tid & 31, threads = blockDim.x;
@@ -146,8 +151,8 @@ __global__ void __launch_bounds__(kPlanThreads) k_paged_plan(const __grid_consta
 
   if (gone_all > 0) {                            // the first segment's first page ends up on top
     again([&](int seg, const Segment& y, unsigned long long at) {
-      move_run<-1, 1>(a.free_pages, stack - 1 - (long long)(at >> 32), a.n_pages, a.tables, (long long)seg * a.max_pages + y.need,
-                      max(y.have - y.need, 0));
+      move_runs<-1, 1>(a.free_pages, a.n_pages, a.tables,
+                       {stack - 1 - (long long)(at >> 32), (long long)seg * a.max_pages + y.need, max(y.have - y.need, 0)}, runs);
     });
     sync();                                      // some are taken again below
   }
@@ -185,7 +190,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_paged_plan(const __grid_consta
       a.lens_out[seg] = len;
     }
     const long long row0 = (long long)seg * a.max_pages;
-    move_run<1, -1>(a.tables, row0 + y.have, entries, a.free_pages, fits - 1 - (long long)(at & 0xffffffffu), mine ? granted : 0);
+    move_runs<1, -1>(a.tables, entries, a.free_pages, {row0 + y.have, fits - 1 - (long long)(at & 0xffffffffu), mine ? granted : 0}, runs);
     if (ragged) {
       const unsigned long long to = rows_before + block_scan((unsigned long long)added, warp_sums, &sum);
       rows_before += sum;
@@ -226,19 +231,28 @@ __global__ void __launch_bounds__(kPlanThreads) k_paged_plan(const __grid_consta
   if (n_cta > 1) cluster.sync();                 // no CTA's shared memory goes while another reads it
 }
 
-// Ragged slots, where there are many: a thread each, its segment by bisection.
-__global__ void __launch_bounds__(256) k_paged_slots(const __grid_constant__ PagedPlanArgs a) {
+// Ragged slots, where there are many: 256 in a row to a warp, which finds the first one's segment by bisection; from there each lane goes on.
+constexpr int kSlotThreads = 256, kSlotsOfWarp = 256;
+__global__ void __launch_bounds__(kSlotThreads) k_paged_slots(const __grid_constant__ PagedPlanArgs a) {
   pdl_launch_dependents();
   pdl_wait();
-  const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
-  if (i >= a.n_slots) return;
-  if (i >= a.slot_offsets[a.n_seg]) { a.slots[i] = -1; return; }
-  int lo = 0, hi = a.n_seg;                      // the last segment whose offset is not above i
+  const long long first = ((long long)blockIdx.x * (kSlotThreads / 32) + (threadIdx.x >> 5)) * kSlotsOfWarp;
+  if (first >= a.n_slots) return;
+  const int rows = a.slot_offsets[a.n_seg];
+  int lo = 0, hi = a.n_seg;                      // the last segment whose offset is not above the first slot
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
-    if (a.slot_offsets[mid] <= i) lo = mid; else hi = mid;
+    if (a.slot_offsets[mid] <= first) lo = mid; else hi = mid;
   }
-  a.slots[i] = slot_of(a, (long long)lo * a.max_pages, a.lens_out[lo] - a.slot_offsets[lo + 1] + (int)i);
+#pragma unroll 2
+  for (long long i = first + (threadIdx.x & 31); i < first + kSlotsOfWarp && i < a.n_slots; i += 32) {
+    int slot = -1;
+    if (i < rows) {
+      while (a.slot_offsets[lo + 1] <= i) ++lo;
+      slot = slot_of(a, (long long)lo * a.max_pages, a.lens_out[lo] - a.slot_offsets[lo + 1] + (int)i);
+    }
+    a.slots[i] = slot;
+  }
 }
 
 // 16 bytes of a K and a V row a thread, of kWriteRows rows at once: their slots are read first, then the rows.
@@ -282,13 +296,15 @@ cudaError_t launch_paged_plan(const PagedPlanArgs& a, cudaStream_t st, int* laun
     while (ctas < kPlanCluster && ctas * kPlanThreads / 2 < a.n_seg) ctas *= 2;
     int threads = (a.n_seg + ctas - 1) / ctas;
     threads = threads >= kPlanThreads ? kPlanThreads : (threads + 31) / 32 * 32;
+    if (a.mode != SLKV_PAGED_ADD) threads = kPlanThreads;      // whole segments come and go: the warps move their pages
     LaunchScope scope(KID_PAGED_PLAN, st, launches);
     const cudaError_t e = launch_pdl(k_paged_plan, dim3((unsigned)ctas), dim3((unsigned)threads), 0, st, ctas, a);
     if (e != cudaSuccess) return e;
   }
   if (!a.slots || a.slot_width != 0 || a.n_slots <= kSlotsHere) return cudaSuccess;
   LaunchScope scope(KID_PAGED_PLAN, st, launches);
-  return launch_pdl(k_paged_slots, dim3((unsigned)((a.n_slots + 255) / 256)), dim3(256), 0, st, 1, a);
+  const long long per = kSlotThreads / 32 * kSlotsOfWarp;
+  return launch_pdl(k_paged_slots, dim3((unsigned)((a.n_slots + per - 1) / per)), dim3(kSlotThreads), 0, st, 1, a);
 }
 
 cudaError_t launch_paged_write(const PagedWriteArgs& a, cudaStream_t st, int* launches) {
