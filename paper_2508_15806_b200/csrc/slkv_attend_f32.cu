@@ -6,8 +6,8 @@
 //   K, V, Q   come in as fp32, are split by the warps that load them and lie in shared memory as three planes each
 //   S = Q K^T in TMEM, two buffers; a thread has a row, 64 keys a tile, with a running reference and sum in fp32
 //   P         = 2^(sc (x - m)) goes back to TMEM as three planes; O += P V, rescaled only where m rises by more than 2^8
-// The tensor cores cut off what they add to an accumulator: over 16000 keys the outputs came out 2 10^-5 too small.  So O holds
-// kFlush tiles, whose sum the softmax warps add to that of the tiles before, rounded to nearest (1.7 10^-6 off, as sums in fp32 are).
+// The tensor cores cut off what they add to an accumulator: over 16000 keys the outputs came out 2 10^-5 too small.  So O holds one tile's
+// products, the small ones first, and the softmax warps add it to the sum of the tiles before, rounded to nearest (3 10^-7 off).
 // A CTA takes pieces of units (AttendSchedule) of one block of 128 query rows.
 //   warps 0-3  softmax, results      warps 4-7  K      warps 8-11  Q, V      warp 12  MMAs      warp 13  schedule
 // K and V are handed over in blocks of 64 channels, two buffers each: while the products with one block run, the next is split and stored,
@@ -27,7 +27,6 @@ constexpr int kThreads = 512;
 constexpr int kKWarp = 4, kVWarp = 8, kMmaWarp = 12, kPlanWarp = 13;
 constexpr int kUnits = 3;                        // pieces the schedule is ahead by
 constexpr float kLift = 8.0f;                    // log2 of how far P may exceed 1 before the reference is raised
-constexpr int kFlush = 8;                        // tiles whose products are added up in TMEM
 constexpr int kTmemS = 0, kTmemP = 2 * kKeys, kPlaneCols = kKeys / 2, kTmemO = 256, kTmemSum = 384;   // P has 3 kPlaneCols columns
 static_assert(kTmemP + 3 * kPlaneCols <= kTmemO, "columns");
 constexpr int kPlane = kKeys * 128;              // bytes of a block of K or V, 64 channels of a tile's rows, one plane
@@ -274,7 +273,7 @@ __device__ __forceinline__ bool mma_role(const AttendF32& t, Smem<D>& sm) {
         const unsigned no = done + i - 1;
         if (!wait(&sm.p_ready, no)) return false;
         tc_fence_after();
-        const uint32_t pa = tmem + kTmemP, first = (i - 1) % kFlush != 0;
+        const uint32_t pa = tmem + kTmemP;
 #pragma unroll 1
         for (int h = 0; h < S::kHalves; ++h) {
           const unsigned block = no * S::kHalves + h;
@@ -286,7 +285,7 @@ __device__ __forceinline__ bool mma_role(const AttendF32& t, Smem<D>& sm) {
             for (int c = 0; c < kPairs; ++c) {
               const uint32_t ap = pa + (kPlanesA >> (2 * c) & 3u) * kPlaneCols, bp = va + ((kPlanesB >> (2 * c) & 3u) * kPlane >> 4);
 #pragma unroll
-              for (int k = 0; k < kKeys / 16; ++k) tc_mma_ts(d, ap + 8 * k, bp + k * 128, kIdO, c > 0 || k > 0 ? 1u : first);
+              for (int k = 0; k < kKeys / 16; ++k) tc_mma_ts(d, ap + 8 * k, bp + k * 128, kIdO, c > 0 || k > 0);
             }
             tc_commit(smem_u32(&sm.v_empty[block & 1]));
             if (h + 1 == S::kHalves) tc_commit(smem_u32(&sm.pv_done));
@@ -352,86 +351,72 @@ __device__ __forceinline__ void softmax_role(const AttendF32& t, Smem<D>& sm) {
       tc_fence_after();
       if (work) {
         const uint32_t ts = lanes + kTmemS + (done & 1) * kKeys, tp = lanes + kTmemP;
-        const bool masked = __any_sync(0xffffffffu, drafted || end < kKeys);
-        // 32 keys at a time, once for the maximum and once more: half the code, see rows_role
-        uint32_t r[32];
-        auto load = [&](int q) {
-          tc_ld32(ts + 32 * q, r);
-          tc_wait_ld(r);
-          if (masked) {
+        uint32_t r[2][32];
+        tc_ld32(ts, r[0]);
+        tc_ld32(ts + 32, r[1]);
+        tc_wait_ld(r[0]);
+        tc_wait_ld(r[1]);
+        if (__any_sync(0xffffffffu, drafted || end < kKeys)) {
+#pragma unroll
+          for (int q = 0; q < 2; ++q) {
             const uint32_t see = drafted ? (uint32_t)(mask >> (32 * q)) : seen_below(end - 32 * q);
 #pragma unroll
-            for (int e = 0; e < 32; ++e) r[e] = see >> e & 1u ? r[e] : 0xff800000u;
+            for (int e = 0; e < 32; ++e) r[q][e] = see >> e & 1u ? r[q][e] : 0xff800000u;
           }
-        };
-        float top = -INFINITY;
-#pragma unroll 1
-        for (int q = 0; q < 2; ++q) {
-          load(q);
-          float mx[2] = {__uint_as_float(r[0]), __uint_as_float(r[1])};
-#pragma unroll
-          for (int e = 2; e < 30; e += 4) {
-            mx[0] = fmaxf(fmaxf(mx[0], __uint_as_float(r[e])), __uint_as_float(r[e + 1]));
-            mx[1] = fmaxf(fmaxf(mx[1], __uint_as_float(r[e + 2])), __uint_as_float(r[e + 3]));
-          }
-          mx[0] = fmaxf(fmaxf(mx[0], __uint_as_float(r[30])), __uint_as_float(r[31]));
-          top = fmaxf(top, fmaxf(mx[0], mx[1]));
         }
+        float mx[2];
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          mx[q] = __uint_as_float(r[q][0]);
+#pragma unroll
+          for (int e = 1; e < 31; e += 2) mx[q] = fmaxf(fmaxf(mx[q], __uint_as_float(r[q][e])), __uint_as_float(r[q][e + 1]));
+          mx[q] = fmaxf(mx[q], __uint_as_float(r[q][31]));
+        }
+        const float top = fmaxf(mx[0], mx[1]);
         const bool lift = i > 0 && (top - m) * sc > kLift;           // m = -infinity: any score lifts it
         const float f = lift ? ex2((m - top) * sc) : 1.0f;
-        const bool scaled = __any_sync(0xffffffffu, lift);
         if (i == 0 || lift) m = top;
         l *= f;
-        if (i > 0) {                             // P and O belong to the product before until it is done
-          if (!wait(&sm.pv_done, done - 1)) return;
-          tc_fence_after();
-          const bool flush = i % kFlush == 0, have = i > kFlush;     // O goes to the sum; which is there already
-          if (flush || scaled) {
-#pragma unroll 1
-            for (int ch = 0; ch < D; ch += 16) {
-              uint32_t o[16], z[16];
-              tc_ld16_issue(lanes + kTmemO + ch, o);
-              if (have) tc_ld16_issue(lanes + kTmemSum + ch, z);
-              tc_ld_wait(o);
-              if (have) {
-                tc_ld_wait(z);
-              } else {
-#pragma unroll
-                for (int e = 0; e < 16; ++e) z[e] = 0;
-              }
-#pragma unroll
-              for (int e = 0; e < 16; ++e) {
-                if (flush) z[e] = __float_as_uint((__uint_as_float(z[e]) + __uint_as_float(o[e])) * f);
-                else { z[e] = __float_as_uint(__uint_as_float(z[e]) * f); o[e] = __float_as_uint(__uint_as_float(o[e]) * f); }
-              }
-              if (!flush) tc_st16(lanes + kTmemO + ch, o);
-              if (flush || have) tc_st16(lanes + kTmemSum + ch, z);
-            }
-          }
-        }
         // 2^(sc x - sc m) with one rounding of the difference, which is as large as sc m 2^-24: where that is much, differences first
-        float base = m == -INFINITY ? 0.0f : m, less = 0.0f;
-        if (__any_sync(0xffffffffu, fabsf(base) * sc > 0x1p20f)) { less = base; base = 0.0f; }
+        float base = m == -INFINITY ? 0.0f : m;
+        if (__any_sync(0xffffffffu, fabsf(base) * sc > 0x1p20f)) {
+#pragma unroll
+          for (int q = 0; q < 2; ++q)
+#pragma unroll
+            for (int e = 0; e < 32; ++e) r[q][e] = __float_as_uint(__uint_as_float(r[q][e]) - base);
+          base = 0.0f;
+        }
         const float nm = -base * sc;
         const f32x2 nm2 = pack2(nm, nm);
         f32x2 s0 = 0, s1 = 0;
-#pragma unroll 1
-        for (int q = 0; q < 2; ++q) {
-          load(q);
-          if (less != 0.0f) {
 #pragma unroll
-            for (int e = 0; e < 32; ++e) r[e] = __float_as_uint(__uint_as_float(r[e]) - less);
+        for (int q = 0; q < 2; ++q)
+#pragma unroll
+          for (int e = 0; e < 32; e += 4) {
+            const f32x2 p0 = ex2_pair(fma2(pack2(__uint_as_float(r[q][e]), __uint_as_float(r[q][e + 1])), sc2, nm2));
+            const f32x2 p1 = ex2_pair(fma2(pack2(__uint_as_float(r[q][e + 2]), __uint_as_float(r[q][e + 3])), sc2, nm2));
+            s0 = add2(s0, p0);
+            s1 = add2(s1, p1);
+            float y[4];
+            unpack2(p0, y[0], y[1]);
+            unpack2(p1, y[2], y[3]);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) r[q][e + k] = __float_as_uint(y[k]);
           }
-          uint32_t w[3][16];
+        l += sum2(s0, s1);
+        // P and O belong to the product before until it is done; what can be is computed by then
+        if (i > 0) {
+          if (!wait(&sm.pv_done, done - 1)) return;
+          tc_fence_after();
+        }
 #pragma unroll
-          for (int e = 0; e < 32; e += 8) {
+        for (int q = 0; q < 4; ++q) {            // sixteen keys at a time
+          uint32_t w[3][8];
+#pragma unroll
+          for (int e = 0; e < 16; e += 8) {
             float y[8];
 #pragma unroll
-            for (int k = 0; k < 8; k += 2) {
-              const f32x2 pr = ex2_pair(fma2(pack2(__uint_as_float(r[e + k]), __uint_as_float(r[e + k + 1])), sc2, nm2));
-              if (k & 2) s1 = add2(s1, pr); else s0 = add2(s0, pr);
-              unpack2(pr, y[k], y[k + 1]);
-            }
+            for (int k = 0; k < 8; ++k) y[k] = __uint_as_float(r[q >> 1][16 * (q & 1) + e + k]);
             uint4 p0, p1, p2;
             split8(y, p0, p1, p2);
             w[0][e / 2] = p0.x; w[0][e / 2 + 1] = p0.y; w[0][e / 2 + 2] = p0.z; w[0][e / 2 + 3] = p0.w;
@@ -439,9 +424,21 @@ __device__ __forceinline__ void softmax_role(const AttendF32& t, Smem<D>& sm) {
             w[2][e / 2] = p2.x; w[2][e / 2 + 1] = p2.y; w[2][e / 2 + 2] = p2.z; w[2][e / 2 + 3] = p2.w;
           }
 #pragma unroll
-          for (int c = 0; c < 3; ++c) tc_st16(tp + c * kPlaneCols + 16 * q, w[c]);
+          for (int c = 0; c < 3; ++c) tc_st8(tp + c * kPlaneCols + 8 * q, w[c]);
         }
-        l += sum2(s0, s1);
+        if (i > 0) {                             // the product before goes to the sum, which begins with the first one
+#pragma unroll 1
+          for (int ch = 0; ch < D; ch += 32) {
+            uint32_t o[32], z[32];
+            tc_ld32(lanes + kTmemO + ch, o);
+            tc_ld32(lanes + kTmemSum + ch, z);
+            tc_wait_ld(o);
+            tc_wait_ld(z);
+#pragma unroll
+            for (int e = 0; e < 32; ++e) z[e] = __float_as_uint(((i > 1 ? __uint_as_float(z[e]) : 0.0f) + __uint_as_float(o[e])) * f);
+            tc_st32(lanes + kTmemSum + ch, z);
+          }
+        }
       } else if (i > 0) {
         if (!wait(&sm.pv_done, done - 1)) return;
       }
@@ -471,7 +468,7 @@ __device__ __forceinline__ void softmax_role(const AttendF32& t, Smem<D>& sm) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[e] = 0;
       }
-      if (p.n > kFlush) {
+      if (p.n > 1) {
         uint32_t z[16];
         tc_ld16_issue(lanes + kTmemSum + ch, z);
         tc_ld_wait(z);
