@@ -144,6 +144,7 @@ __device__ __forceinline__ void attend_start(const AttendShape& a, int cta, Atte
   const int per = (unsigned)n <= blockDim.x ? 1 : (int)((unsigned)(n + blockDim.x - 1) / blockDim.x);
   const int first = threadIdx.x * per, last = min(first + per, n);
   int sum = 0;
+#pragma unroll 4
   for (int i = first; i < last; ++i) sum += attend_weight(a, i);
   int incl = sum;
 #pragma unroll 1
@@ -223,6 +224,7 @@ class AttendSchedule {
   // spread
   long long item_, base_, count_;
   int level_, round_;
+  int scan_s_ = 0, scan_before_ = 0;       // sequences looked through for this level; those of them that have such a block
   // shares: the group of units with the same tiles (prompt: a block of tokens, all KV heads; paged: a segment, all blocks)
   int pos_, end_, group_;        // group_: first position of the group
   int s_, x_;                    // sequence; prompt: block of tokens, paged: KV head
@@ -261,22 +263,23 @@ class AttendSchedule {
   __device__ __forceinline__ bool next_spread(AttendPiece* p) {
     while (level_ >= 0 && item_ >= base_ + count_) {
       base_ += count_;
+      scan_s_ = scan_before_ = 0;
       if (--level_ >= 0) count_ = level_count(level_);
     }
     if (level_ < 0) return false;
     const unsigned rel = (unsigned)(item_ - base_);            // fewer than 2^31 sequences times heads
-    int nth = (int)(rel / (unsigned)a_.n_kv_heads);
+    const int nth = (int)(rel / (unsigned)a_.n_kv_heads);      // of the sequences that have such a block
     const int h = (int)(rel - (unsigned)nth * (unsigned)a_.n_kv_heads);
     int s = 0;
-    for (int s0 = 0; s0 < a_.n_seqs; s0 += 32) {
-      unsigned m = __ballot_sync(0xffffffffu, lane_blocks(s0) > level_);
+    for (; scan_s_ < a_.n_seqs; scan_s_ += 32) {               // on from where the last item was: items come in ascending order
+      unsigned m = __ballot_sync(0xffffffffu, lane_blocks(scan_s_) > level_);
       const int n = __popc(m);
-      if (nth < n) {
-        for (; nth > 0; --nth) m &= m - 1;
-        s = s0 + __ffs(m) - 1;
+      if (nth < scan_before_ + n) {
+        for (int skip = nth - scan_before_; skip > 0; --skip) m &= m - 1;
+        s = scan_s_ + __ffs(m) - 1;
         break;
       }
-      nth -= n;
+      scan_before_ += n;
     }
     fill(p, s, h, level_);
     p->tile0 = 0;

@@ -259,3 +259,8 @@ def test_a_wait_that_runs_out():
     B.slkv_prompt_attend(p, q, k, v, c, [0, 300], out, ws, status=status)
     torch.cuda.synchronize()
     assert int(status) == 0 and torch.equal(out[:300], good[:300])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_thousands_of_sequences(dtype):
+    run([1 + i % 3 if i % 7 else 0 for i in range(3001)], hkv=1, G=2, d=64, dtype=dtype, window=2)
