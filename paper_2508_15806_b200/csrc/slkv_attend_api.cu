@@ -232,6 +232,7 @@ int slkv_paged_plan(const slkv_paged_cache* c, int32_t mode, const int32_t* want
     if (slot_width == 0 && !slot_offsets_opt) return SLKV_ERR_NULL_PTR;
   }
   if ((lens_out == nullptr) != (n_free_out == nullptr)) return SLKV_ERR_NULL_PTR;
+  if (lens_out && lens_out != c->lens && lens_out < c->lens + n_seg && c->lens < lens_out + n_seg) return SLKV_ERR_BAD_SHAPE;
   PagedPlanArgs a = {};
   a.n_seqs = c->n_seqs; a.n_kv_heads = c->n_kv_heads; a.n_seg = (int)n_seg;
   for (a.page_bits = 0; (1 << a.page_bits) < c->page_rows;) ++a.page_bits;
