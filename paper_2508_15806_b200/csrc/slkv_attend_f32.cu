@@ -25,7 +25,8 @@ namespace {
 constexpr int kKeys = 1 << kF32TileBits;
 constexpr int kThreads = 512;
 constexpr int kKWarp = 4, kVWarp = 8, kMmaWarp = 12, kPlanWarp = 13;
-constexpr int kUnits = 3;                        // pieces the schedule is ahead by
+constexpr int kUnits = 3;                        // pieces the schedule is ahead by: nobody is more than these ahead of a warp that is at one
+constexpr int kAhead = 2 * kUnits;
 constexpr float kLift = 8.0f;                    // log2 of how far P may exceed 1 before the reference is raised
 constexpr int kTmemS = 0, kTmemP = 2 * kKeys, kPlaneCols = kKeys / 2, kTmemO = 256, kTmemSum = 384;   // P has 3 kPlaneCols columns
 static_assert(kTmemP + 3 * kPlaneCols <= kTmemO, "columns");
@@ -41,7 +42,7 @@ struct Smem {
   AttendPiece piece[kUnits];
   unsigned long long unit_full[kUnits], unit_empty[kUnits], q_full, q_empty, k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_ready,
       pv_done, drain;
-  int odd_lo[2][4], odd_hi[2][4];                // tiles of a piece, by its parity, where a warp of V met values that are not finite
+  int odd_lo[kAhead][4], odd_hi[kAhead][4];      // tiles of a piece where a warp of V met values that are not finite
   int abort;
   uint32_t tmem;
   AttendStart start;
@@ -183,10 +184,10 @@ __device__ __forceinline__ void rows_role(const AttendF32& t, Smem<D>& sm, const
       const unsigned slot = done & 1;
       if (done > 1 && !wait(empty + slot, (done >> 1) - 1)) return;
       if (v) {
-        if (i == 0) {                            // the piece before the last one has been written
+        if (i == 0) {                            // results are at most kUnits pieces behind
           if (lane == 0) {
-            sm.odd_lo[nth & 1][tid >> 5] = 0x7fffffff;
-            sm.odd_hi[nth & 1][tid >> 5] = -1;
+            sm.odd_lo[nth % kAhead][tid >> 5] = 0x7fffffff;
+            sm.odd_hi[nth % kAhead][tid >> 5] = -1;
           }
           __syncwarp();
         }
@@ -204,8 +205,8 @@ __device__ __forceinline__ void rows_role(const AttendF32& t, Smem<D>& sm, const
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[u][e] = fabsf(x[u][e]) < INFINITY ? x[u][e] : 0.0f;
           const int tile = p.tile0 + i / S::kHalves;
-          atomicMin(&sm.odd_lo[nth & 1][tid >> 5], tile);
-          atomicMax(&sm.odd_hi[nth & 1][tid >> 5], tile);
+          atomicMin(&sm.odd_lo[nth % kAhead][tid >> 5], tile);
+          atomicMax(&sm.odd_hi[nth % kAhead][tid >> 5], tile);
         }
       }
 #pragma unroll
@@ -492,8 +493,8 @@ __device__ __forceinline__ void softmax_role(const AttendF32& t, Smem<D>& sm) {
       int lo = 0x7fffffff, hi = -1;
 #pragma unroll
       for (int w = 0; w < 4 && p.n > 0; ++w) {
-        lo = min(lo, *(volatile int*)&sm.odd_lo[nth & 1][w]);
-        hi = max(hi, *(volatile int*)&sm.odd_hi[nth & 1][w]);
+        lo = min(lo, *(volatile int*)&sm.odd_lo[nth % kAhead][w]);
+        hi = max(hi, *(volatile int*)&sm.odd_hi[nth % kAhead][w]);
       }
       if (hi >= 0) put_back(t, p, lo, hi, bound, mask, dst);
       if (whole) attend_lse(a, p.s, p.h * a.G + rh, tok, p.n_seq_tok, m * sc, l);

@@ -25,7 +25,8 @@ namespace {
 
 constexpr int kThreads = 384;
 constexpr int kLoadWarp = 8, kMmaWarp = 9, kPlanWarp = 10, kQueryWarp = 11;
-constexpr int kUnits = 4;                        // pieces the schedule is ahead by
+constexpr int kUnits = 4;                        // pieces the schedule is ahead by: nobody is more than these ahead of a warp that is at one
+constexpr int kAhead = 2 * kUnits;
 constexpr float kLift = 8.0f;                    // log2 of how far P may exceed 1 before the reference is raised
 constexpr int kTmemS = 0, kTmemO = 256;          // columns: S of block b at 128 b, O at 256 + 128 b
 
@@ -43,7 +44,7 @@ struct Smem {
   AttendPiece piece[kUnits];
   unsigned long long unit_full[kUnits], unit_empty[kUnits], q_full[2], q_empty[2], kv_full[kStages], kv_empty[kStages], s_full[2],
       p_most[2], p_ready[2], o_full[2], merge_full, merge_done, drain;
-  int odd[2];                                    // number + 1 of the piece that found V values that are not finite, by its parity
+  int odd[kAhead];                               // number + 1 of the piece that found V values that are not finite
   int abort;
   uint32_t tmem;
 };
@@ -519,7 +520,7 @@ __device__ __forceinline__ void softmax_role(const AttendTc& t, Smem<D>& sm, int
         const unsigned no = loads + b.v_load(tl, p.n), slot = no % S::kStages;
         ok = mbar_wait(smem_u32(&sm.kv_full[slot]), (no / S::kStages) & 1, &sm.abort);
         if (!__all_sync(0xffffffffu, ok)) return;
-        if (clean_rows<D>(sm.kv[slot], c, tid)) *(volatile int*)&sm.odd[nth & 1] = (int)nth + 1;
+        if (clean_rows<D>(sm.kv[slot], c, tid)) *(volatile int*)&sm.odd[nth % kAhead] = (int)nth + 1;
         fence_async_smem();
       }
       if (edge) say_most();
@@ -599,7 +600,7 @@ __device__ __forceinline__ void softmax_role(const AttendTc& t, Smem<D>& sm, int
         }
         __syncwarp();                            // the next load is the whole warp's
       }
-      if (there && *(volatile int*)&sm.odd[nth & 1] == (int)nth + 1) {
+      if (there && *(volatile int*)&sm.odd[nth % kAhead] == (int)nth + 1) {
         if (whole) put_back<true>(t, p, bound, mask, ch0, ch1, dst);
         else put_back<false>(t, p, bound, mask, ch0, ch1, dst);
       }
@@ -642,8 +643,8 @@ k_attend_tc(const __grid_constant__ AttendTc t, const __grid_constant__ AttendMa
       mbar_init(smem_u32(&sm.p_most[g]), 4);
       mbar_init(smem_u32(&sm.p_ready[g]), blockIdx.x == 0 ? t.arrivals : 4);
       mbar_init(smem_u32(&sm.o_full[g]), 1);
-      sm.odd[g] = 0;
     }
+    for (int i = 0; i < kAhead; ++i) sm.odd[i] = 0;
     mbar_init(smem_u32(&sm.merge_full), 8);
     mbar_init(smem_u32(&sm.merge_done), 8);
     mbar_init(smem_u32(&sm.drain), 1);

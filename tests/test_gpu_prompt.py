@@ -264,3 +264,16 @@ def test_a_wait_that_runs_out():
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_thousands_of_sequences(dtype):
     run([1 + i % 3 if i % 7 else 0 for i in range(3001)], hkv=1, G=2, d=64, dtype=dtype, window=2)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_values_that_are_not_finite_in_many_short_sequences(d, dtype):
+    """Units of one tile, many of one CTA: what is noted of one while others are loaded ahead of its results."""
+    nq = [1 + 11 * i % 60 for i in range(400)]
+    q, k, v = inputs(nq, nq, 2, 2, d, dtype, seed=9)
+    at = cu(nq)
+    for s in range(0, len(nq), 3):
+        v[at[s] + nq[s] // 2, s % 2, s % d] = float("inf") if s % 2 else float("nan")
+    out, lse, before = attend(q, k, v, nq)
+    R.check_prompt(q, k, v, at, at, out, lse, 32, d ** -0.5, before, torch.full_like(lse, 5.0))
