@@ -560,9 +560,11 @@ int slkv_q4_evict(const slkv_q4_cache* from, const slkv_q4_cache* to, const int3
  *                 before its first query are left as they are.  With the window of slkv_params this is the lse_opt of slkv_score and
  *                 slkv_compress (SLKV_ALL_CAUSAL), which spares them their pass over K for it.
  *   status        dev, optional: SLKV_ERR_DEVICE_TIMEOUT if a wait inside a kernel ran out; rows concerned are then left as they were or NaN
- * Limits: n_q_heads / n_kv_heads <= 64, fewer than 2^31 - 512 tokens.  Scores below fp32's range in magnitude.
- * fp32 accumulation throughout; with bf16, probabilities are rounded to bf16 for the product with V (2^-8 of each term).  Results are the
- * same bit for bit from call to call.  A workspace belongs to one call at a time.
+ * Limits: n_q_heads / n_kv_heads <= 64, fewer than 2^31 - 512 tokens, n_seqs * n_kv_heads < 2^31.  Scores below fp32's range in
+ * magnitude: where a query or a key that it sees is not finite, its results may be NaN.
+ * fp32 accumulation throughout; with bf16, probabilities are rounded to bf16 for the product with V (2^-8 of each term).  fp32 rows are
+ * exact sums of three bf16 parts, whose products with less than 2^-24 of a term are left out.  Results are the same bit for bit from call
+ * to call.  out is none of the inputs.  A workspace belongs to one call at a time.
  */
 typedef struct slkv_prompt_params {
   int32_t n_seqs;
@@ -623,6 +625,7 @@ typedef struct slkv_paged_cache {
  *                    Rows beyond n_slots or slot_width get none (status: SLKV_ERR_CAPACITY).
  *   lens_out, n_free_out   dev, optional, both or neither: take the new values in place of c->lens and c->n_free, which then keep the old
  *                    ones: c still describes the cache as it was (tokens that are drafted), until a plan from there takes the pages again.
+ *                    lens_out is c->lens or does not overlap it.
  * OFFSETS behind slkv_compress_overlapped calls on the same stream needs no slkv_join: what is queued there goes out first.
  */
 enum { SLKV_PAGED_LENGTHS = 0, SLKV_PAGED_OFFSETS = 1, SLKV_PAGED_ADD = 2 };

@@ -92,7 +92,8 @@ int check_prompt(const slkv_prompt_params* p, const int32_t* cu_q, const int32_t
   if (!cu_k) cu_k = cu_q;
   int rc = check_heads(p->n_q_heads, p->n_kv_heads, p->head_dim, p->dtype, p->lse_units, p->scale);
   if (rc != SLKV_OK) return rc;
-  if (p->n_seqs < 1 || p->window < 1 || cu_q[0] != 0 || cu_k[0] != 0) return SLKV_ERR_BAD_SHAPE;
+  if (p->n_seqs < 1 || p->window < 1 || (long long)p->n_seqs * p->n_kv_heads >= (1ll << 31)) return SLKV_ERR_BAD_SHAPE;
+  if (cu_q[0] != 0 || cu_k[0] != 0) return SLKV_ERR_BAD_SHAPE;
   long long longest = 0;
   for (int s = 0; s < p->n_seqs; ++s) {
     if (cu_q[s + 1] < cu_q[s] || cu_k[s + 1] < cu_k[s]) return SLKV_ERR_BAD_SHAPE;

@@ -29,7 +29,7 @@ def call_prompt(p, q=P, k=P, v=P, cu_dev=P, host=None, cu_k_dev=None, k_host=Non
 
 
 @pytest.mark.parametrize("kw,code", [
-    (dict(n_seqs=0), "BAD_SHAPE"), (dict(n_q_heads=9), "BAD_SHAPE"), (dict(n_q_heads=0), "BAD_SHAPE"), (dict(n_kv_heads=0), "BAD_SHAPE"),
+    (dict(n_seqs=0), "BAD_SHAPE"), (dict(n_seqs=1 << 30), "BAD_SHAPE"), (dict(n_q_heads=9), "BAD_SHAPE"), (dict(n_q_heads=0), "BAD_SHAPE"), (dict(n_kv_heads=0), "BAD_SHAPE"),
     (dict(n_q_heads=130), "BAD_SHAPE"), (dict(head_dim=96), "BAD_SHAPE"), (dict(window=0), "BAD_SHAPE"), (dict(dtype=2), "BAD_DTYPE"),
     (dict(lse_units=2), "BAD_DTYPE"), (dict(scale=0.0), "BAD_SHAPE"), (dict(scale=-1.0), "BAD_SHAPE"), (dict(scale=float("nan")), "BAD_SHAPE"),
     (dict(scale=float("inf")), "BAD_SHAPE"), (dict(scale=2.0 ** 55), "BAD_SHAPE"), (dict(scale=2.0 ** -55), "BAD_SHAPE"),
