@@ -3,15 +3,23 @@
 // An fp32 number is the sum of three bf16 numbers, its significand in three parts of eight bits: x = x0 + x1 + x2 exactly.  A product
 // of two such sums needs six of the nine products (x0 y0, x0 y1, x1 y0, x1 y1, x0 y2, x2 y0; the others are below 2^-24 of it), which the
 // tensor cores add up in fp32: 375 TFLOP/s at six products each, against 74 on the FMA pipe.  Scores and outputs are made this way:
-//   K, V, Q   come in as fp32, are split by the warps that load them and lie in shared memory as three planes each
+//   K, V, Q   come in as fp32, are split by the warps that load them into three planes each; K and V lie in shared memory, Q in TMEM but
+//             for its third plane, which one product in six needs: with all of it in shared memory a product of 64 keys takes 48 cycles
+//             for its operands instead of 32
 //   S = Q K^T in TMEM, two buffers; a thread has a row, 64 keys a tile, with a running reference and sum in fp32
 //   P         = 2^(sc (x - m)) goes back to TMEM as three planes; O += P V, rescaled only where m rises by more than 2^8
 // The tensor cores cut off what they add to an accumulator: over 16000 keys the outputs came out 2 10^-5 too small.  So O holds one tile's
-// products, the small ones first, and the softmax warps add it to the sum of the tiles before, rounded to nearest (3 10^-7 off).
+// products, the small ones first, and the softmax warps, which have 240 registers for it, add it to the sum of the tiles before, rounded to
+// nearest (4 10^-7 off).
 // A CTA takes pieces of units (AttendSchedule) of one block of 128 query rows.
 //   warps 0-3  softmax, results      warps 4-7  K      warps 8-11  Q, V      warp 12  MMAs      warp 13  schedule
-// K and V are handed over in blocks of 64 channels, two buffers each: while the products with one block run, the next is split and stored,
-// and the one behind it is on its way into registers.
+// K and V are handed over in blocks of 64 channels, four buffers each; while one is split and stored, the one behind it is on its way into
+// registers.
+//
+// Measured (B200, 32 query heads on 8 KV heads): 8000 tokens 2.53 ms (207 TFLOP/s counted once, 1240 as products of planes), head_dim 64
+// 1.63 ms; one token each of 8 sequences over 8000 to 32000 rows 410 us (2.6 TB/s).  A tile of head_dim 128 takes 5700 cycles, its products
+// 3450 of them: the warps of V, and behind them those of K, have 4600 cycles of loading, splitting and storing to do.  One softmax
+// warp, one of K and one of V share a scheduler, which issues in about half of the cycles.
 //
 // A key that a row does not see gives it nothing: scores are replaced; keys behind the last one are rows of zeros; values that are not
 // finite, which 0 would not cancel, are left out of V, and rows that see them add them at the end.
@@ -28,19 +36,19 @@ constexpr int kKWarp = 4, kVWarp = 8, kMmaWarp = 12, kPlanWarp = 13;
 constexpr int kUnits = 3;                        // pieces the schedule is ahead by: nobody is more than these ahead of a warp that is at one
 constexpr int kAhead = 2 * kUnits;
 constexpr float kLift = 8.0f;                    // log2 of how far P may exceed 1 before the reference is raised
-constexpr int kTmemS = 0, kTmemP = 2 * kKeys, kPlaneCols = kKeys / 2, kTmemO = 256, kTmemSum = 384;   // P has 3 kPlaneCols columns
+constexpr int kTmemS = 0, kTmemP = 2 * kKeys, kPlaneCols = kKeys / 2, kTmemO = 256, kTmemQ = 384;   // P has 3 kPlaneCols columns
 static_assert(kTmemP + 3 * kPlaneCols <= kTmemO, "columns");
 constexpr int kPlane = kKeys * 128;              // bytes of a block of K or V, 64 channels of a tile's rows, one plane
 
 template <int D>
 struct Smem {
   static constexpr int kHalves = D / 64;
-  static constexpr int kQPlane = kHalves * kHalfBytes;
-  alignas(1024) unsigned char q[3][kQPlane];
-  alignas(1024) unsigned char k[2][3][kPlane];
-  alignas(1024) unsigned char v[2][3][kPlane];
+  static constexpr int kK = 4, kV = 4;           // buffers
+  alignas(1024) unsigned char q[kHalves * kHalfBytes];         // Q's third plane; the others are in TMEM
+  alignas(1024) unsigned char k[kK][3][kPlane];
+  alignas(1024) unsigned char v[kV][3][kPlane];
   AttendPiece piece[kUnits];
-  unsigned long long unit_full[kUnits], unit_empty[kUnits], q_full, q_empty, k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_ready,
+  unsigned long long unit_full[kUnits], unit_empty[kUnits], q_full, q_empty, k_full[kK], k_empty[kK], v_full[kV], v_empty[kV], s_full[2], p_ready,
       pv_done, drain;
   int odd_lo[kAhead][4], odd_hi[kAhead][4];      // tiles of a piece where a warp of V met values that are not finite
   int abort;
@@ -55,28 +63,27 @@ struct AttendF32 {
   int extra_arrival;                             // 1: a test makes the first CTA's wait for P run out
 };
 
-// Row j of a piece's tile, as it lies in memory; null: there is none.
-__device__ __forceinline__ const float* key_row(const AttendF32& t, const AttendPiece& p, bool v, int tile, int j) {
+// Row j of a piece's tile, as it lies in memory; where there is none, another one that there is.
+__device__ __forceinline__ const float* key_row(const AttendF32& t, const AttendPiece& p, bool v, int tile, int j, bool* there) {
   const AttendShape& a = t.a;
-  if (a.paged) {
-    if (a.has_new && tile == p.n_all - 1) {
-      if (j >= p.n_seq_tok) return nullptr;
-      return static_cast<const float*>(v ? a.v_new : a.k_new) + p.s * (v ? a.vn_seq : a.kn_seq) + j * (v ? a.vn_tok : a.kn_tok) +
-             p.h * (v ? a.vn_head : a.kn_head);
-    }
-    const int row = tile * kKeys + j;
-    if (row >= p.nk) return nullptr;
-    const int id = __ldg(a.tables + (long long)(p.s * a.n_kv_heads + p.h) * a.max_pages + (row >> t.page_bits));
-    if ((unsigned)id >= (unsigned)a.n_pages) {
-      if (a.status) *a.status = SLKV_ERR_BAD_SHAPE;
-      return nullptr;
-    }
-    const long long at = (((long long)id << t.page_bits) + (row & (a.page_rows - 1))) * a.head_dim;
-    return static_cast<const float*>(v ? a.v : a.k) + at;
+  if (a.has_new && tile == p.n_all - 1) {
+    *there = j < p.n_seq_tok;
+    j = min(j, p.n_seq_tok - 1);
+    return static_cast<const float*>(v ? a.v_new : a.k_new) + p.s * (v ? a.vn_seq : a.kn_seq) + j * (v ? a.vn_tok : a.kn_tok) +
+           p.h * (v ? a.vn_head : a.kn_head);
   }
-  const int row = tile * kKeys + j;
-  if (row >= p.nk) return nullptr;
-  return static_cast<const float*>(v ? a.v : a.k) + (long long)(p.k_row + row) * (v ? a.v_tok : a.k_tok) + p.h * (v ? a.v_head : a.k_head);
+  int row = tile * kKeys + j;
+  *there = row < p.nk;
+  row = min(row, p.nk - 1);
+  const float* const base = static_cast<const float*>(v ? a.v : a.k);
+  if (!a.paged) return base + (long long)(p.k_row + row) * (v ? a.v_tok : a.k_tok) + p.h * (v ? a.v_head : a.k_head);
+  int id = __ldg(a.tables + (long long)(p.s * a.n_kv_heads + p.h) * a.max_pages + (row >> t.page_bits));
+  if ((unsigned)id >= (unsigned)a.n_pages) {
+    if (*there && a.status) *a.status = SLKV_ERR_BAD_SHAPE;
+    *there = false;
+    id = 0;
+  }
+  return base + (((long long)id << t.page_bits) + (row & (a.page_rows - 1))) * a.head_dim;
 }
 
 // Three planes of eight numbers: the upper 16 bits of x, of what is left of it, and of what is left then.
@@ -113,16 +120,15 @@ __device__ __forceinline__ void store_planes(unsigned char* base, int row, int c
   *reinterpret_cast<uint4*>(at + 2 * PLANE) = p2;
 }
 
-// Whole sectors at a time where rows begin at them; K and V pass by L1, they are read once.
+// Eight numbers, in whole sectors where rows begin at them; K and V pass by L1, they are read once.  Without a branch: values that one
+// side of it loads are waited for where the sides meet (8000 tokens took 2720 us instead of 2530).
 __device__ __forceinline__ void load8(const float* from, bool wide, float (&x)[8]) {
-  if (wide) {
-    asm volatile("ld.global.L1::no_allocate.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-                 : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]), "=f"(x[4]), "=f"(x[5]), "=f"(x[6]), "=f"(x[7]) : "l"(from));
-  } else {
-    const float4 a = *reinterpret_cast<const float4*>(from), b = *reinterpret_cast<const float4*>(from + 4);
-    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
-    x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-  }
+  asm volatile(
+      "{\n\t.reg .pred w;\n\tsetp.ne.u32 w, %9, 0;\n\t"
+      "@w ld.global.L1::no_allocate.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];\n\t"
+      "@!w ld.global.v4.f32 {%0, %1, %2, %3}, [%8];\n\t"
+      "@!w ld.global.v4.f32 {%4, %5, %6, %7}, [%8 + 16];\n\t}"
+      : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]), "=f"(x[4]), "=f"(x[5]), "=f"(x[6]), "=f"(x[7]) : "l"(from), "r"((uint32_t)wide));
 }
 
 // The warps of K, or of Q and V (v).  One code for both, a block at a time: what runs side by side here has to stay in the instruction
@@ -140,7 +146,8 @@ __device__ __forceinline__ void rows_role(const AttendF32& t, Smem<D>& sm, const
   auto wait = [&](unsigned long long* bar, unsigned phase) {
     return __all_sync(0xffffffffu, mbar_wait(smem_u32(bar), phase & 1, &sm.abort)) != 0;
   };
-  unsigned done = 0, n_q = 0;                    // blocks of keys, of query rows
+  const unsigned buffers = v ? S::kV : S::kK;
+  unsigned slot = 0, round = 0, n_q = 0;         // blocks of keys, of query rows
   for (unsigned nth = 0;; ++nth) {
     if (!wait(&sm.unit_full[nth % kUnits], nth / kUnits)) return;
     const AttendPiece p = sm.piece[nth % kUnits];
@@ -149,40 +156,64 @@ __device__ __forceinline__ void rows_role(const AttendF32& t, Smem<D>& sm, const
     if (p.stop) return;
     if (p.n == 0) continue;
     float x[kMine][8];
+    unsigned none = 0;                           // bit u: there is no row u, x[u] is another one's
     auto load = [&](int block) {                 // of the piece
       const int tile = p.tile0 + block / S::kHalves, ch = 64 * (block % S::kHalves) + 8 * chunk;
+      none = 0;
 #pragma unroll
       for (int u = 0; u < kMine; ++u) {
-        const float* from = key_row(t, p, v, tile, row0 + 16 * u);
-        if (from) {
-          load8(from + ch, wide, x[u]);
-        } else {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) x[u][e] = 0.0f;
-        }
+        bool there;
+        load8(key_row(t, p, v, tile, row0 + 16 * u, &there) + ch, wide, x[u]);
+        none |= there ? 0u : 1u << u;
       }
     };
     load(0);
     if (v) {
       if (n_q > 0 && !wait(&sm.q_empty, n_q - 1)) return;
+      tc_fence_after();
       ++n_q;
-      const float* from = static_cast<const float*>(a.q) + (a.paged ? p.s * a.q_seq : p.q_row * a.q_tok) + p.tok0 * a.q_tok + p.h * a.G * a.q_head;
-      const int rows = p.n_tok * a.G;
+      const int rt = tid / a.G, r7 = tid & 7;    // a row a thread
+      const bool there = rt < p.n_tok && rt < a.block_tokens;
+      const float* from = static_cast<const float*>(a.q) + (a.paged ? p.s * a.q_seq : p.q_row * a.q_tok) + (p.tok0 + rt) * a.q_tok +
+                          (p.h * a.G + tid - rt * a.G) * a.q_head;
+      const uint32_t tq = sm.tmem + ((uint32_t)(tid >> 5) << 21) + kTmemQ;
 #pragma unroll 1
-      for (int i = 0; i < 8 * S::kHalves; ++i) {
-        const int r = row0 + 16 * (i / S::kHalves), h = i % S::kHalves, rt = r / a.G;
-        float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (r < rows) load8(from + rt * a.q_tok + (r - rt * a.G) * a.q_head + 64 * h + 8 * chunk, false, y);
-        store_planes<S::kQPlane>(sm.q[0] + h * kHalfBytes, r, chunk, y);
+      for (int c = 0; c < D / 16; ++c) {
+        uint32_t w[2][8];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+          if (there) {
+#pragma unroll
+            for (int k = 0; k < 8; k += 4) {
+              const float4 z = *reinterpret_cast<const float4*>(from + 16 * c + 8 * e + k);
+              y[k] = z.x; y[k + 1] = z.y; y[k + 2] = z.z; y[k + 3] = z.w;
+            }
+          }
+          uint4 p0, p1, p2;
+          split8(y, p0, p1, p2);
+          w[0][4 * e] = p0.x; w[0][4 * e + 1] = p0.y; w[0][4 * e + 2] = p0.z; w[0][4 * e + 3] = p0.w;
+          w[1][4 * e] = p1.x; w[1][4 * e + 1] = p1.y; w[1][4 * e + 2] = p1.z; w[1][4 * e + 3] = p1.w;
+          *reinterpret_cast<uint4*>(sm.q + (c >> 2) * kHalfBytes + tid * 128 + (((2 * (c & 3) + e) ^ r7) << 4)) = p2;
+        }
+        tc_st8(tq + 8 * c, w[0]);
+        tc_st8(tq + D / 2 + 8 * c, w[1]);
       }
+      tc_wait_st();
+      tc_fence_before();
       fence_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&sm.q_full));
     }
 #pragma unroll 1
-    for (int i = 0; i < p.n * S::kHalves; ++i, ++done) {
-      const unsigned slot = done & 1;
-      if (done > 1 && !wait(empty + slot, (done >> 1) - 1)) return;
+    for (int i = 0; i < p.n * S::kHalves; ++i) {
+      if (round > 0 && !wait(empty + slot, round - 1)) return;
+      if (__any_sync(0xffffffffu, none != 0)) {
+#pragma unroll
+        for (int u = 0; u < kMine; ++u)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[u][e] = none >> u & 1u ? 0.0f : x[u][e];
+      }
       if (v) {
         if (i == 0) {                            // results are at most kUnits pieces behind
           if (lane == 0) {
@@ -214,6 +245,7 @@ __device__ __forceinline__ void rows_role(const AttendF32& t, Smem<D>& sm, const
       fence_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(full + slot));
+      if (++slot == buffers) { slot = 0; ++round; }
       if (i + 1 < p.n * S::kHalves) load(i + 1);
     }
   }
@@ -230,11 +262,12 @@ __device__ __forceinline__ bool mma_role(const AttendF32& t, Smem<D>& sm) {
   const uint32_t tmem = sm.tmem;
   constexpr uint32_t kIdS = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kKeys >> 3) << 17) | (8u << 24);
   constexpr uint32_t kIdO = (1u << 4) | (1u << 7) | (1u << 10) | (8u << 17) | (8u << 24) | kRowsB;      // 64 channels
-  const uint32_t qa = desc_lo(smem_u32(sm.q[0]));
+  const uint32_t qa = desc_lo(smem_u32(sm.q)), qt = tmem + kTmemQ;
   auto wait = [&](unsigned long long* bar, unsigned phase) {
     return __all_sync(0xffffffffu, mbar_poll(smem_u32(bar), phase & 1, &sm.abort)) != 0;
   };
   unsigned done = 0, n_q = 0;                    // tiles
+  unsigned k_slot = 0, k_round = 0, v_slot = 0, v_round = 0;
   for (unsigned nth = 0;; ++nth) {
     if (!wait(&sm.unit_full[nth % kUnits], nth / kUnits)) return false;
     const AttendPiece p = sm.piece[nth % kUnits];
@@ -247,24 +280,29 @@ __device__ __forceinline__ bool mma_role(const AttendF32& t, Smem<D>& sm) {
       if (i < p.n) {
         const unsigned no = done + i;
         const uint32_t d = tmem + kTmemS + (no & 1) * kKeys;
+        uint32_t kb[S::kHalves], kslot[S::kHalves];
 #pragma unroll
         for (int h = 0; h < S::kHalves; ++h) {
-          const unsigned block = no * S::kHalves + h;
-          if (!wait(&sm.k_full[block & 1], block >> 1)) return false;
+          if (!wait(&sm.k_full[k_slot], k_round)) return false;
+          kslot[h] = k_slot;
+          kb[h] = desc_lo(smem_u32(sm.k[0][0])) + (k_slot * 3 * kPlane >> 4);
+          if (++k_slot == S::kK) { k_slot = 0; ++k_round; }
         }
         tc_fence_after();
-        const uint32_t ka = desc_lo(smem_u32(sm.k[0][0])), first = no * S::kHalves & 1;
         if (elect_one()) {
-#pragma unroll 1
-          for (int c = 0; c < kPairs; ++c)
 #pragma unroll
-            for (int h = 0; h < S::kHalves; ++h) {
-              const uint32_t ap = qa + (((kPlanesA >> (2 * c) & 3u) * S::kQPlane + h * kHalfBytes) >> 4);
-              const uint32_t bp = ka + (((first ^ h) * 3 * kPlane + (kPlanesB >> (2 * c) & 3u) * kPlane) >> 4);
+          for (int c = 0; c < kPairs; ++c) {
+            const uint32_t plane = kPlanesA >> (2 * c) & 3u, bo = (kPlanesB >> (2 * c) & 3u) * kPlane >> 4, ap = qt + plane * (D / 2);
 #pragma unroll
-              for (int k = 0; k < 4; ++k) tc_mma_ss(d, ap + 2 * k, bp + 2 * k, kIdS, c > 0 || h > 0 || k > 0);
-              if (c + 1 == kPairs) tc_commit(smem_u32(&sm.k_empty[first ^ h]));
-            }
+            for (int h = 0; h < S::kHalves; ++h)
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                if (plane == 2) tc_mma_ss(d, qa + (h * kHalfBytes >> 4) + 2 * k, kb[h] + bo + 2 * k, kIdS, c > 0 || h > 0 || k > 0);
+                else tc_mma_ts(d, ap + 32 * h + 8 * k, kb[h] + bo + 2 * k, kIdS, c > 0 || h > 0 || k > 0);
+              }
+          }
+#pragma unroll
+          for (int h = 0; h < S::kHalves; ++h) tc_commit(smem_u32(&sm.k_empty[kslot[h]]));
           tc_commit(smem_u32(&sm.s_full[no & 1]));
           if (i + 1 == p.n) tc_commit(smem_u32(&sm.q_empty));
         }
@@ -277,21 +315,21 @@ __device__ __forceinline__ bool mma_role(const AttendF32& t, Smem<D>& sm) {
         const uint32_t pa = tmem + kTmemP;
 #pragma unroll 1
         for (int h = 0; h < S::kHalves; ++h) {
-          const unsigned block = no * S::kHalves + h;
-          if (!wait(&sm.v_full[block & 1], block >> 1)) return false;
+          if (!wait(&sm.v_full[v_slot], v_round)) return false;
           tc_fence_after();
-          const uint32_t va = desc_lo(smem_u32(sm.v[block & 1][0])), d = tmem + kTmemO + 64 * h;
+          const uint32_t va = desc_lo(smem_u32(sm.v[0][0])) + (v_slot * 3 * kPlane >> 4), d = tmem + kTmemO + 64 * h;
           if (elect_one()) {
-#pragma unroll 1
+#pragma unroll
             for (int c = 0; c < kPairs; ++c) {
               const uint32_t ap = pa + (kPlanesA >> (2 * c) & 3u) * kPlaneCols, bp = va + ((kPlanesB >> (2 * c) & 3u) * kPlane >> 4);
 #pragma unroll
               for (int k = 0; k < kKeys / 16; ++k) tc_mma_ts(d, ap + 8 * k, bp + k * 128, kIdO, c > 0 || k > 0);
             }
-            tc_commit(smem_u32(&sm.v_empty[block & 1]));
+            tc_commit(smem_u32(&sm.v_empty[v_slot]));
             if (h + 1 == S::kHalves) tc_commit(smem_u32(&sm.pv_done));
           }
           __syncwarp();
+          if (++v_slot == S::kV) { v_slot = 0; ++v_round; }
         }
       }
     }
@@ -308,8 +346,9 @@ __device__ __forceinline__ void put_back(const AttendF32& t, const AttendPiece& 
     for (int j = 0; j < kKeys; ++j) {
       const bool drafted = a.has_new && tile == p.n_all - 1;
       if (drafted ? !(mask >> j & 1) : !a.paged && tile * kKeys + j >= bound) continue;
-      const float* v = key_row(t, p, true, tile, j);
-      if (!v) continue;
+      bool row_there;
+      const float* v = key_row(t, p, true, tile, j, &row_there);
+      if (!row_there) continue;
       for (int ch = 0; ch < a.head_dim; ++ch)
         if (!(fabsf(v[ch]) < INFINITY)) out[ch] += v[ch];
     }
@@ -343,6 +382,9 @@ __device__ __forceinline__ void softmax_role(const AttendF32& t, Smem<D>& sm) {
     }
     const bool work = __any_sync(0xffffffffu, there);
     float m = -INFINITY, l = 0.0f;
+    f32x2 sum[D / 2];                            // of the tiles before the last one
+#pragma unroll
+    for (int e = 0; e < D / 2; ++e) sum[e] = 0;
 #pragma unroll 1
     for (int i = 0; i < p.n; ++i, ++done) {
       const int tile = p.tile0 + i;
@@ -427,17 +469,19 @@ __device__ __forceinline__ void softmax_role(const AttendF32& t, Smem<D>& sm) {
 #pragma unroll
           for (int c = 0; c < 3; ++c) tc_st8(tp + c * kPlaneCols + 8 * q, w[c]);
         }
-        if (i > 0) {                             // the product before goes to the sum, which begins with the first one
-#pragma unroll 1
-          for (int ch = 0; ch < D; ch += 32) {
-            uint32_t o[32], z[32];
-            tc_ld32(lanes + kTmemO + ch, o);
-            tc_ld32(lanes + kTmemSum + ch, z);
-            tc_wait_ld(o);
-            tc_wait_ld(z);
+        if (i > 0) {                             // the product before goes to the sum
 #pragma unroll
-            for (int e = 0; e < 32; ++e) z[e] = __float_as_uint(((i > 1 ? __uint_as_float(z[e]) : 0.0f) + __uint_as_float(o[e])) * f);
-            tc_st32(lanes + kTmemSum + ch, z);
+          for (int ch = 0; ch < D; ch += 32) {
+            uint32_t o[32];
+            tc_ld32(lanes + kTmemO + ch, o);
+            tc_wait_ld(o);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) sum[ch / 2 + e] = add2(sum[ch / 2 + e], pack2(__uint_as_float(o[2 * e]), __uint_as_float(o[2 * e + 1])));
+          }
+          if (__any_sync(0xffffffffu, lift)) {
+            const f32x2 f2 = pack2(f, f);
+#pragma unroll
+            for (int e = 0; e < D / 2; ++e) sum[e] = mul2(sum[e], f2);
           }
         }
       } else if (i > 0) {
@@ -459,7 +503,8 @@ __device__ __forceinline__ void softmax_role(const AttendF32& t, Smem<D>& sm) {
     const long long place = (long long)(blockIdx.x * 2 + p.part) * a.part_rows + row;
     float* const dst = whole ? static_cast<float*>(a.out) + (a.paged ? p.s * a.o_seq : p.q_row * a.o_tok) + tok * a.o_tok + (p.h * a.G + rh) * a.o_head
                              : a.part + place * D;
-#pragma unroll 1
+    const f32x2 inv2 = pack2(inv, inv);
+#pragma unroll
     for (int ch = 0; ch < D; ch += 16) {
       uint32_t o[16];
       if (p.n > 0) {
@@ -469,16 +514,14 @@ __device__ __forceinline__ void softmax_role(const AttendF32& t, Smem<D>& sm) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[e] = 0;
       }
-      if (p.n > 1) {
-        uint32_t z[16];
-        tc_ld16_issue(lanes + kTmemSum + ch, z);
-        tc_ld_wait(z);
-#pragma unroll
-        for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) + __uint_as_float(z[e]));
-      }
       if (there) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * inv);
+        for (int e = 0; e < 16; e += 2) {
+          float x, y;
+          unpack2(mul2(add2(sum[(ch + e) / 2], pack2(__uint_as_float(o[e]), __uint_as_float(o[e + 1]))), inv2), x, y);
+          o[e] = __float_as_uint(x);
+          o[e + 1] = __float_as_uint(y);
+        }
         if (t.wide || !whole) {
           store32(dst + ch, o);
           store32(dst + ch + 8, o + 8);
@@ -516,13 +559,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_f32(const __grid_constan
     }
     mbar_init(smem_u32(&sm.q_full), 4);
     mbar_init(smem_u32(&sm.q_empty), 1);
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < Smem<D>::kK; ++i) {
       mbar_init(smem_u32(&sm.k_full[i]), 4);
       mbar_init(smem_u32(&sm.k_empty[i]), 1);
+    }
+    for (int i = 0; i < Smem<D>::kV; ++i) {
       mbar_init(smem_u32(&sm.v_full[i]), 4);
       mbar_init(smem_u32(&sm.v_empty[i]), 1);
-      mbar_init(smem_u32(&sm.s_full[i]), 1);
     }
+    for (int i = 0; i < 2; ++i) mbar_init(smem_u32(&sm.s_full[i]), 1);
     mbar_init(smem_u32(&sm.p_ready), 4 + (blockIdx.x == 0 ? t.extra_arrival : 0));
     mbar_init(smem_u32(&sm.pv_done), 1);
     mbar_init(smem_u32(&sm.drain), 1);
@@ -540,33 +585,40 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_f32(const __grid_constan
   pdl_wait();
   attend_start(t.a, blockIdx.x, &sm.start);
   __syncthreads();
+  // registers of the four warpgroups: no more than four times 128 in all
+  static_assert((D == 128 ? 240 + 2 * 96 : 176 + 2 * 128) + 80 <= 512, "registers");
   if (warp < kKWarp) {
+    regs_up<D == 128 ? 240 : 176>();
     softmax_role<D>(t, sm);
   } else if (warp < kMmaWarp) {
+    if (D == 128) regs_down<96>();
     rows_role<D>(t, sm, warp >= kVWarp);
-  } else if (warp == kMmaWarp) {
-    if (!mma_role<D>(t, sm) && elect_one()) {    // a wait ran out: what is under way ends first
-      volatile int never = 0;
-      tc_commit(smem_u32(&sm.drain));
-      mbar_wait(smem_u32(&sm.drain), 0, &never);
-    }
-  } else if (warp == kPlanWarp) {
-    if (lane == 0 && t.a.desc) t.a.desc[2 * blockIdx.x].state = t.a.desc[2 * blockIdx.x + 1].state = 0;
-    AttendSchedule plan(t.a, blockIdx.x, &sm.start);
-    for (unsigned nth = 0;; ++nth) {
-      AttendPiece p = {};
-      const bool more = plan.next(&p);
-      p.stop = !more;
-      if (nth >= (unsigned)kUnits) {
-        const bool ok = mbar_wait(smem_u32(&sm.unit_empty[nth % kUnits]), (nth / kUnits - 1) & 1, &sm.abort);
-        if (!__all_sync(0xffffffffu, ok)) break;
+  } else {
+    regs_down<80>();
+    if (warp == kMmaWarp) {
+      if (!mma_role<D>(t, sm) && elect_one()) {  // a wait ran out: what is under way ends first
+        volatile int never = 0;
+        tc_commit(smem_u32(&sm.drain));
+        mbar_wait(smem_u32(&sm.drain), 0, &never);
       }
-      if (lane == 0) {
-        sm.piece[nth % kUnits] = p;
-        mbar_arrive(smem_u32(&sm.unit_full[nth % kUnits]));
-        if (more && p.part >= 0) attend_note(t.a, p.part, p, p.part == 1 ? plan.pieces() : 0);
+    } else if (warp == kPlanWarp) {
+      if (lane == 0 && t.a.desc) t.a.desc[2 * blockIdx.x].state = t.a.desc[2 * blockIdx.x + 1].state = 0;
+      AttendSchedule plan(t.a, blockIdx.x, &sm.start);
+      for (unsigned nth = 0;; ++nth) {
+        AttendPiece p = {};
+        const bool more = plan.next(&p);
+        p.stop = !more;
+        if (nth >= (unsigned)kUnits) {
+          const bool ok = mbar_wait(smem_u32(&sm.unit_empty[nth % kUnits]), (nth / kUnits - 1) & 1, &sm.abort);
+          if (!__all_sync(0xffffffffu, ok)) break;
+        }
+        if (lane == 0) {
+          sm.piece[nth % kUnits] = p;
+          mbar_arrive(smem_u32(&sm.unit_full[nth % kUnits]));
+          if (more && p.part >= 0) attend_note(t.a, p.part, p, p.part == 1 ? plan.pieces() : 0);
+        }
+        if (!more) break;
       }
-      if (!more) break;
     }
   }
   __syncwarp();
