@@ -780,8 +780,11 @@ def make_paged_cache(k_pages: torch.Tensor, v_pages: torch.Tensor, tables: torch
     assert n_seqs >= 1 and n_kv_heads >= 1 and lens.numel() % (n_seqs * n_kv_heads) == 0
     c = SlkvPagedCache(lens.numel() // (n_seqs * n_kv_heads), n_seqs, n_kv_heads, dim, _DTYPES[k_pages.dtype], page_rows, n_pages,
                        tables.size(1), *(t.data_ptr() for t in tensors))
-    c.tensors, c.device, c.element = tensors, k_pages.device, k_pages.dtype
+    c.tensors, c.device, c.element, c.dim = tensors, k_pages.device, k_pages.dtype, dim
     c.index = k_pages.get_device() if k_pages.is_cuda else -2
+    # what calls check, once for all: fields of the structure are slow to read
+    c.wanted = (lens.numel(), lens.numel() + c.n_layers, n_seqs)       # by mode of slkv_paged_plan
+    c.same = (c.tables, c.free_pages, c.n_layers, n_seqs, n_kv_heads, c.max_pages)
     return c
 
 
@@ -794,10 +797,8 @@ def slkv_paged_plan(cache: SlkvPagedCache, mode: int, want: torch.Tensor, slots:
     d = cache.index
     if not d == want.get_device() == _current_device():
         _q4_elsewhere()
-    per = cache.n_seqs * cache.n_kv_heads
-    n_seg = cache.n_layers * per
-    assert want.dtype is _I32 and want.is_contiguous()
-    assert want.numel() == {SLKV_PAGED_LENGTHS: n_seg, SLKV_PAGED_OFFSETS: n_seg + cache.n_layers, SLKV_PAGED_ADD: cache.n_seqs}[mode]
+    n_seg = cache.wanted[SLKV_PAGED_LENGTHS]
+    assert want.dtype is _I32 and want.is_contiguous() and 0 <= mode <= 2 and want.numel() == cache.wanted[mode]
     width = n_slots = 0
     if slots is not None:
         assert slots.dtype is _I32 and slots.is_contiguous() and slots.get_device() == d
@@ -812,8 +813,7 @@ def slkv_paged_plan(cache: SlkvPagedCache, mode: int, want: torch.Tensor, slots:
             assert slot_offsets.get_device() == d
     lens_out = n_free_out = None
     if after is not None:
-        assert after.tables == cache.tables and after.free_pages == cache.free_pages and after.n_layers == cache.n_layers
-        assert after.n_seqs == cache.n_seqs and after.n_kv_heads == cache.n_kv_heads and after.max_pages == cache.max_pages
+        assert after.same == cache.same
         lens_out, n_free_out = after.tensors[3], after.tensors[5]
     if status is not None:
         _q4_status(cache, status)
@@ -838,8 +838,9 @@ def slkv_paged_write(cache: SlkvPagedCache, k: torch.Tensor, v: torch.Tensor, sl
         ns, nt, hkv, dim = k.shape
         ks, kt, kh, k1 = k.stride()
         vs, vt, vh, v1 = v.stride()
-    assert k1 == v1 == 1 and dim == cache.head_dim and ns * hkv > 0 and slots.numel() % (ns * hkv) == 0
-    width = slots.numel() // (ns * hkv)
+    assert k1 == v1 == 1 and dim == cache.dim and ns * hkv > 0
+    width, rest = divmod(slots.numel(), ns * hkv)
+    assert rest == 0
     if take is not None:
         assert take.dtype is _I32 and take.is_contiguous() and take.numel() == ns * width and take.get_device() == d
     rc = _fn["slkv_paged_write"](stream, cache, k, v, ns, hkv, nt, ks, kt, kh, vs, vt, vh, slots, width, take)
