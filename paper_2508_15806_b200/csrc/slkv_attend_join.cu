@@ -12,7 +12,9 @@ __device__ __forceinline__ float exp2_of(float x) {
 
 // One CTA's unit that goes on in the next ones: the pieces' outputs by their references.  What bounds it is latency -- what the pieces are,
 // then their references, sums and outputs, kAtOnce pieces at a time, then the result -- so nothing else stands between the loads.  A row is
-// a warp's; where the rows are few (tokens that decode over long segments, many pieces), the eight warps of a CTA share its pieces.
+// a warp's; where the rows are few (tokens that decode over long segments, many pieces), the eight warps of a CTA share its pieces: one user
+// over 8000 rows 25.9 us without, 17.0 with it.  The launch takes 5 us by itself, 1 to 2 behind the other one, 12 where four chunks of
+// 512 tokens leave 256 rows a unit (39 MB of pieces).
 constexpr int kJoinWarps = 8, kAtOnce = 4;
 constexpr int kFewRows = 16;
 template <int D, bool F32, int SHARE>                          // SHARE: warps of a row
