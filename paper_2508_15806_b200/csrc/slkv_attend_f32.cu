@@ -60,7 +60,7 @@ struct AttendF32 {
   AttendShape a;
   int page_bits;
   int wide, wide_k, wide_v;                      // rows of out, of K, of V (drafted ones too) begin at 32-byte boundaries
-  int extra_arrival;                             // 1: a test makes the first CTA's wait for P run out
+  int extra_arrival;                             // 1: a test makes the waits for P run out
 };
 
 // Row j of a piece's tile, as it lies in memory; where there is none, another one that there is.
@@ -568,7 +568,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_f32(const __grid_constan
       mbar_init(smem_u32(&sm.v_empty[i]), 1);
     }
     for (int i = 0; i < 2; ++i) mbar_init(smem_u32(&sm.s_full[i]), 1);
-    mbar_init(smem_u32(&sm.p_ready), 4 + (blockIdx.x == 0 ? t.extra_arrival : 0));
+    mbar_init(smem_u32(&sm.p_ready), 4 + t.extra_arrival);
     mbar_init(smem_u32(&sm.pv_done), 1);
     mbar_init(smem_u32(&sm.drain), 1);
     sm.abort = 0;

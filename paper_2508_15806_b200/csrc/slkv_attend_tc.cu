@@ -362,14 +362,6 @@ __device__ __forceinline__ bool clean_rows(unsigned char* v, const Columns& c, i
   return odd;
 }
 
-template <int D>
-struct Rows {                                    // of a softmax thread, for the piece at hand
-  int tok, head;                                 // its row's token in the sequence, query head
-  bool there;
-  int bound;                                     // prompt: keys that the row sees
-  unsigned long long mask;                       // paged: drafted tokens that it sees
-};
-
 // Values of V that are not finite and were taken out, in the channels ch0 .. ch1 - 1: rows that see them get them back, in the results
 // that the thread has written.
 template <bool WHOLE>
@@ -651,7 +643,7 @@ k_attend_tc(const __grid_constant__ AttendTc t, const __grid_constant__ AttendMa
       mbar_init(smem_u32(&sm.q_empty[g]), 1);
       mbar_init(smem_u32(&sm.s_full[g]), 1);
       mbar_init(smem_u32(&sm.p_most[g]), 4);
-      mbar_init(smem_u32(&sm.p_ready[g]), blockIdx.x == 0 ? t.arrivals : 4);
+      mbar_init(smem_u32(&sm.p_ready[g]), t.arrivals);
       mbar_init(smem_u32(&sm.o_full[g]), 1);
     }
     for (int i = 0; i < kAhead; ++i) sm.odd[i] = 0;

@@ -469,3 +469,71 @@ def test_prompt_to_accepted_tokens(dtype):
         rk, rv = c.rows(seg)
         assert torch.equal(rk, torch.cat([old[seg][0], kn[s, idx, h]])) and torch.equal(rv, torch.cat([old[seg][1], vn[s, idx, h]]))
     check_attend(c, G, 1, seed=31)
+
+
+def test_attend_far_rows_in_fp32():
+    """Pages whose offsets pass 2^31 elements and 2^33 bytes."""
+    n_pages = (1 << 31) // (128 * 64) + 3
+    k_pages = torch.zeros(n_pages, 128, 64, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(3)
+    k_pages[-2:] = torch.randn(2, 128, 64, device="cuda", generator=g)
+    c = B.make_paged_cache(k_pages, k_pages, dev([[n_pages - 1, 0, n_pages - 2]]), dev([384]), torch.zeros(n_pages, dtype=torch.int32, device="cuda"),
+                           dev([0]), 1, 1)
+    q = torch.randn(1, 1, 4, 64, device="cuda", generator=g)
+    out = torch.zeros_like(q)
+    p = B.make_paged_attend(c, q, out)
+    B.slkv_paged_attend(c, p, q, out, B.new_paged_workspace(c, p))
+    rows = torch.cat([k_pages[-1], k_pages[0], k_pages[-2]])
+    for h in range(4):
+        R.check(out[0, :, h], None, R.rows(q[0, :, h], rows, rows, torch.ones(1, 384, dtype=torch.bool, device="cuda"), 0.125), False, 64)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attend_a_wait_that_runs_out(dtype):
+    c = Cache([3000, 200, 1700, 900], 2, 2, 64, dtype, 32)
+    q, k, v, good, lse, _ = attend(c, 4, 3)
+    out, status = torch.full_like(good, 7.0), dev([0])
+    p = B.make_paged_attend(c.c, q, out, k, v)
+    ws = B.new_paged_workspace(c.c, p)
+    B.slkv_debug_expire_next_wait(5)
+    B.slkv_paged_attend(c.c, p, q, out, ws, k, v, status=status)
+    torch.cuda.synchronize()
+    assert int(status) == B.ERR["DEVICE_TIMEOUT"]
+    fine = (out == good) | (out == 7.0) | torch.isnan(out)
+    assert fine.all() and not torch.equal(out, good)
+    status.zero_()
+    B.slkv_paged_attend(c.c, p, q, out, ws, k, v, status=status)
+    torch.cuda.synchronize()
+    assert int(status) == 0 and torch.equal(out, good)
+
+
+@pytest.mark.parametrize("sizes", [(1, 5, 700), (3, 11, 300), (8, 8, 64), (1, 40, 33)])
+def test_plan_few_segments_of_many_pages(sizes):
+    """Warps that share the pages of few segments; clusters where whole segments come and go; back again, and in part."""
+    ns, hkv, most = sizes
+    r = random.Random(sum(sizes))
+    n_seg = ns * hkv
+    pages = 16
+    full = [r.randint(0, most * pages) for _ in range(n_seg)]
+    c = Cache([0] * n_seg, ns, hkv, 64, "bf16", pages, spare=n_seg * most, room=most)
+    before = c.tables.clone(), c.free.clone(), c.n_free.clone()
+    slots, so = torch.full((sum(full) + 5,), 9, dtype=torch.int32, device="cuda"), torch.zeros(n_seg + 1, dtype=torch.int32, device="cuda")
+    status = dev([0])
+    B.slkv_paged_plan(c.c, B.SLKV_PAGED_LENGTHS, dev(full), slots=slots, slot_offsets=so, status=status)
+    assert int(status) == 0 and c.lens.tolist() == full
+    tables, got, taken = c.tables.cpu(), slots.tolist(), []
+    for s, n in enumerate(full):
+        need = -(-n // pages)
+        taken += tables[s, :need].tolist()
+        assert got[int(so[s]):int(so[s]) + n] == [int(tables[s, i // pages]) * pages + i % pages for i in range(n)]
+    assert got[sum(full):] == [-1] * 5
+    stack = before[1].tolist()[:int(before[2])]
+    assert taken == stack[::-1][:len(taken)]                              # from the top, in order
+    assert int(c.n_free) == len(stack) - len(taken)
+    half = [n // 2 for n in full]
+    B.slkv_paged_plan(c.c, B.SLKV_PAGED_LENGTHS, dev(half))
+    assert c.lens.tolist() == half
+    B.slkv_paged_plan(c.c, B.SLKV_PAGED_LENGTHS, dev(full))
+    assert torch.equal(c.tables.cpu(), tables)                            # taking and returning are each other's inverse
+    B.slkv_paged_plan(c.c, B.SLKV_PAGED_LENGTHS, dev([0] * n_seg))
+    assert torch.equal(c.free, before[1]) and torch.equal(c.n_free, before[2])

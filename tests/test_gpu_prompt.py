@@ -277,3 +277,75 @@ def test_values_that_are_not_finite_in_many_short_sequences(d, dtype):
         v[at[s] + nq[s] // 2, s % 2, s % d] = float("inf") if s % 2 else float("nan")
     out, lse, before = attend(q, k, v, nq)
     R.check_prompt(q, k, v, at, at, out, lse, 32, d ** -0.5, before, torch.full_like(lse, 5.0))
+
+
+def test_a_wait_that_runs_out_in_fp32():
+    q, k, v = inputs([40], [900], 1, 4, 64, "f32", seed=13)           # units shared by several CTAs
+    good, _, before = attend(q, k, v, [40], [900])
+    out, status = before.clone(), torch.zeros(1, dtype=torch.int32, device="cuda")
+    c, ck = (torch.tensor([0, n], dtype=torch.int32, device="cuda") for n in (40, 900))
+    p = B.make_prompt(q, k, v, out, 1)
+    ws = B.new_prompt_workspace(p, [0, 40], [0, 900])
+    for expire in (True, False):
+        status.zero_()
+        if expire:
+            B.slkv_debug_expire_next_wait(5)
+        B.slkv_prompt_attend(p, q, k, v, c, [0, 40], out, ws, cu_k=ck, cu_k_host=[0, 900], status=status)
+        torch.cuda.synchronize()
+        if expire:
+            assert int(status) == B.ERR["DEVICE_TIMEOUT"]
+            fine = (out == good) | (out == 7.0) | torch.isnan(out)
+            assert fine[:40].all() and not torch.equal(out[:40], good[:40])
+        else:
+            assert int(status) == 0 and torch.equal(out, good)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_calls_side_by_side(dtype):
+    """Two streams with a workspace each, several calls of both under way."""
+    shapes = [([300, 5], [1700, 5]), ([64], [2000])]
+    made = []
+    for i, (nq, nk) in enumerate(shapes):
+        q, k, v = inputs(nq, nk, 2, 4, 128, dtype, seed=14 + i)
+        want = attend(q, k, v, nq, nk)[0]
+        c, ck = (torch.tensor(cu(x), dtype=torch.int32, device="cuda") for x in (nq, nk))
+        outs = [torch.full_like(q, 7.0) for _ in range(6)]
+        p = B.make_prompt(q, k, v, outs[0], len(nq))
+        made.append((p, q, k, v, c, cu(nq), ck, cu(nk), outs, B.new_prompt_workspace(p, cu(nq), cu(nk)), want, torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for turn in range(6):
+        for p, q, k, v, c, cq, ck, chk, outs, ws, _, stream in made:
+            B.slkv_prompt_attend(p, q, k, v, c, cq, outs[turn], ws, cu_k=ck, cu_k_host=chk, stream=stream)
+    torch.cuda.synchronize()
+    for *_, outs, _, want, _ in made:
+        for out in outs:
+            assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_graphs_that_share_a_workspace(dtype):
+    """Two captured calls of different shape in one workspace, replayed in turn on one stream."""
+    shapes = [([30], [1500]), ([1, 90], [800, 900])]
+    made, ws = [], torch.empty(0, dtype=torch.uint8, device="cuda")
+    for i, (nq, nk) in enumerate(shapes):
+        q, k, v = inputs(nq, nk, 2, 4, 64, dtype, seed=16 + i)
+        want = attend(q, k, v, nq, nk)[0]
+        c, ck = (torch.tensor(cu(x), dtype=torch.int32, device="cuda") for x in (nq, nk))
+        out = torch.full_like(q, 7.0)
+        p = B.make_prompt(q, k, v, out, len(nq))
+        made.append([p, q, k, v, c, cu(nq), ck, cu(nk), out, want])
+        one = B.new_prompt_workspace(p, cu(nq), cu(nk))
+        ws = one if one.numel() > ws.numel() else ws
+    graphs = []
+    for p, q, k, v, c, cq, ck, chk, out, _ in made:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            B.slkv_prompt_attend(p, q, k, v, c, cq, out, ws, cu_k=ck, cu_k_host=chk)
+    for _ in range(3):
+        for x in made:
+            x[8].fill_(7.0)
+        for g in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        for x in made:
+            assert torch.equal(x[8], x[9])
