@@ -118,15 +118,16 @@ cudaError_t launch_attend_join(const AttendShape& a, bool f32, cudaStream_t st, 
   return f32 ? launch_join<64, true>(a, st) : launch_join<64, false>(a, st);
 }
 
-// Workspace: outputs of pieces, their references and sums, what they belong to.
+// Workspace: outputs of pieces, their references and sums, what they belong to, each from a 256-byte boundary: outputs are written 32 bytes at a
+// time.  A caller's workspace begins at any 16-byte boundary, so there is room for the way to the first of them.
 static size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 size_t attend_workspace(int n_cta, int part_rows, int head_dim) {
   const size_t places = 2 * (size_t)n_cta * part_rows;
-  return up256(places * head_dim * sizeof(float)) + up256(places * sizeof(float2)) + up256(2 * n_cta * sizeof(AttendPart));
+  return 256 + up256(places * head_dim * sizeof(float)) + up256(places * sizeof(float2)) + up256(2 * n_cta * sizeof(AttendPart));
 }
 void attend_bind(AttendShape* a, void* workspace) {
   const size_t places = 2 * (size_t)a->n_cta * a->part_rows;
-  char* w = static_cast<char*>(workspace);
+  char* w = reinterpret_cast<char*>(up256(reinterpret_cast<uintptr_t>(workspace)));
   a->part = reinterpret_cast<float*>(w);
   w += up256(places * a->head_dim * sizeof(float));
   a->ml = reinterpret_cast<float2*>(w);

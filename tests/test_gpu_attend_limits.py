@@ -1,0 +1,49 @@
+"""Prompt attention and the paged cache at what their documentation allows: workspaces, queued layers, drafted rows of several blocks, large tables."""
+import pytest
+import torch
+
+import test_gpu_paged as G
+import test_gpu_prompt as T
+from paper_2508_15806_b200 import binding as B
+
+pytestmark = pytest.mark.gpu
+
+
+# ---- workspaces ---------------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("offset", [16, 32, 48, 240])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_workspaces_from_any_16_byte_boundary(dtype, offset):
+    """Of the size asked for and no more, in units that several CTAs share; what lies around them stays as it is."""
+    def carve(n):
+        buf = torch.full((n + 512,), 0xA5, dtype=torch.uint8, device="cuda")
+        assert buf.data_ptr() % 256 == 0
+        return buf, buf[offset:offset + n]
+
+    def untouched(buf, ws):
+        assert (buf[:offset] == 0xA5).all() and (buf[offset + ws.numel():] == 0xA5).all()
+
+    nq, nk = [33, 5], [1900, 700]
+    q, k, v = T.inputs(nq, nk, 2, 4, 128, dtype, seed=21)
+    want, want_lse, _ = T.attend(q, k, v, nq, nk)
+    c_q, c_k = T.cu(nq), T.cu(nk)
+    dev = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")      # noqa: E731
+    out, lse = torch.full_like(q, 7.0), torch.full_like(want_lse, 5.0)
+    p = B.make_prompt(q, k, v, out, len(nq), window=32)
+    buf, ws = carve(B.slkv_prompt_attend_workspace_bytes(p, c_q, c_k))
+    B.slkv_prompt_attend(p, q, k, v, dev(c_q), c_q, out, ws, cu_k=dev(c_k), cu_k_host=c_k, lse=lse)
+    torch.cuda.synchronize()
+    assert B.slkv_last_launch_count() == 2                                 # pieces and the launch that joins them
+    assert torch.equal(out, want) and torch.equal(lse, want_lse)
+    untouched(buf, ws)
+
+    c = G.Cache([3000, 200, 1700, 900], 2, 2, 64, dtype, 32)
+    for n in (3, 64):                                                        # one block of query rows, more
+        q, k, v, want, _, _ = G.attend(c, 4, n)
+        out = torch.full_like(q, 7.0)
+        p = B.make_paged_attend(c.c, q, out, k, v)
+        buf, ws = carve(B.slkv_paged_attend_workspace_bytes(c.c, p))
+        B.slkv_paged_attend(c.c, p, q, out, ws, k, v)
+        torch.cuda.synchronize()
+        assert B.slkv_last_launch_count() == 2
+        assert torch.equal(out, want)
+        untouched(buf, ws)
