@@ -485,9 +485,10 @@ __device__ __forceinline__ void softmax_role(const AttendTc& t, Smem<D>& sm, int
             }
           }
         }
-        // 2^(x - m sc) with one rounding of the difference, which is as large as m sc 2^-24: where that is much, differences first
+        // 2^(x - m sc) with one rounding of the difference, which is as large as m sc 2^-24: where that is much, differences first.  That
+        // changes last bits, so rows that there are not, whose scores are what shared memory held, have no say in it.
         float base = m == -INFINITY ? 0.0f : m;
-        if (__any_sync(0xffffffffu, fabsf(base) * t.sc > 0x1p20f)) {
+        if (__any_sync(0xffffffffu, there && fabsf(base) * t.sc > 0x1p20f)) {
 #pragma unroll
           for (int q = 0; q < 4; ++q)
 #pragma unroll

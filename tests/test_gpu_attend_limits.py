@@ -47,3 +47,22 @@ def test_workspaces_from_any_16_byte_boundary(dtype, offset):
         assert B.slkv_last_launch_count() == 2
         assert torch.equal(out, want)
         untouched(buf, ws)
+
+
+# ---- the same bit for bit --------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("heads,n", [(4, 1), (4, 3), (3, 40), (5, 64)])
+def test_results_do_not_depend_on_what_ran_before(heads, n):
+    """Blocks with rows that no query has: whatever an earlier launch left in shared memory there, results are the same bit for bit."""
+    c = G.Cache([3000, 200, 1700, 900], 2, 2, 128, "bf16", 32)
+    q, k, v = T.inputs([3000], [3000], 8, 4, 128, "bf16", seed=22, behind=0)
+    got = []
+    for factor in (0.0, 1.0, 2.0 ** 30, 2.0 ** 60):
+        T.attend(q * factor, k, v, [3000])                                # queries of this size in every CTA's buffers
+        got.append(G.attend(c, heads, n)[3:5])
+        nq, nk = [20, 5], [900, 5]
+        x = T.inputs(nq, nk, 2, heads, 128, "bf16", seed=23)
+        T.attend(q * factor, k, v, [3000])
+        got[-1] = got[-1] + T.attend(*x, nq, nk)[:2]
+    for other in got[1:]:
+        for x, y in zip(got[0], other):
+            assert torch.equal(x, y)
