@@ -518,7 +518,10 @@ __device__ __forceinline__ void softmax_role(const AttendTc& t, Smem<D>& sm, int
       } else if (!edge) {
         say_most();
       }
-      const Columns c = edge ? columns(t, p, tile, tok0, n_tok) : Columns{0, 0, 0};
+      // Drafted rows are the first warpgroup's to clean, for both blocks.  Both would look through the same ones, and the one that comes
+      // second find nothing, so that nothing orders what the other notes in front of its results; the first one's note lies in front of
+      // both blocks' products, which are issued in this order.  In prompts no row of the first block sees what the second one cleans.
+      const Columns c = edge && (b.alt || g == 0 || !drafted) ? columns(t, p, tile, tok0, n_tok) : Columns{0, 0, 0};
       if (c.all < c.used) {
         const unsigned no = loads + b.v_load(tl, p.n), slot = no % S::kStages;
         ok = mbar_wait(smem_u32(&sm.kv_full[slot]), (no / S::kStages) & 1, &sm.abort);

@@ -66,3 +66,27 @@ def test_results_do_not_depend_on_what_ran_before(heads, n):
     for other in got[1:]:
         for x, y in zip(got[0], other):
             assert torch.equal(x, y)
+
+
+# ---- drafted rows ------------------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("heads,n", [(4, 33), (4, 40), (4, 64), (16, 8), (16, 24), (5, 61), (1, 64)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_drafted_values_that_are_not_finite_in_two_blocks(dtype, heads, n):
+    """Both blocks of a unit see the same drafted rows: values that are not finite reach every token that sees them, in both, and no other."""
+    c = G.Cache([200, 300, 0, 128], 2, 2, 128, dtype, 32, junk=float("nan"), seed=4)
+    counts = [n - 1, n]
+
+    def edit(q, k, v):
+        inf = float("inf")
+        v[0, 1, :, 4], v[0, n // 2, :, 64], v[0, n - 2, :, 127], v[1, 0, :, 0], v[1, n - 1, :, 100] = float("nan"), inf, -inf, inf, -inf
+        k[0, n - 1], v[0, n - 1] = float("nan"), float("nan")              # padding
+    for seed in range(3):
+        masks = G.tree_masks(2, n, seed)
+        for s in range(2):
+            for i in range(seed, n):
+                masks[s][i] |= 1 << (n // 2) if i % 3 == 0 else 1          # seen from both blocks
+        G.check_attend(c, heads, n, masks, counts=counts, edit=edit, seed=seed)
+    first = G.attend(c, heads, n, masks, counts, edit=edit)[3]
+    for _ in range(20):
+        again = G.attend(c, heads, n, masks, counts, edit=edit)[3]
+        assert torch.equal(torch.isfinite(again), torch.isfinite(first)) and torch.equal(again.nan_to_num(), first.nan_to_num())
