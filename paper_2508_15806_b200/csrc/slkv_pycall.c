@@ -16,6 +16,7 @@
 
 #define MAX_ARGS 28
 #define STACK_INTS 512
+#define MAX_LISTS 4 /* that do not fit there: an entry point takes two at most */
 
 static PyObject *s_data_ptr, *s_cuda_stream;
 static PyObject *f_get_device, *f_raw_stream, *f_current_stream, *f_initialized;
@@ -80,10 +81,10 @@ static int invoke(void* f, W* a) {
 static PyObject* call(PyObject* self, PyObject* const* args, Py_ssize_t n) {
   W a[MAX_ARGS] = {0};
   int32_t small[STACK_INTS];
-  int32_t* heap = NULL;
+  int32_t* heap[MAX_LISTS];
   Py_ssize_t used = 0;
   Py_buffer views[4];
-  int n_views = 0, ok = 0, rc = 0;
+  int n_heap = 0, n_views = 0, ok = 0, rc = 0;
   (void)self;
   if (n < 2 || n - 1 > MAX_ARGS) {
     PyErr_SetString(PyExc_TypeError, "call(address, stream, *args)");
@@ -112,10 +113,10 @@ static PyObject* call(PyObject* self, PyObject* const* args, Py_ssize_t n) {
         buf = small + used;
         used += len;
       } else {
-        if (heap) { PyErr_SetString(PyExc_TypeError, "too many long lists"); goto done; }
-        heap = (int32_t*)malloc((size_t)len * sizeof(int32_t));
-        if (!heap) { PyErr_NoMemory(); goto done; }
-        buf = heap;
+        if (n_heap == MAX_LISTS) { PyErr_SetString(PyExc_TypeError, "too many long lists"); goto done; }
+        buf = (int32_t*)malloc((size_t)len * sizeof(int32_t));
+        if (!buf) { PyErr_NoMemory(); goto done; }
+        heap[n_heap++] = buf;
       }
       for (Py_ssize_t j = 0; j < len; ++j) {
         PyObject* e = PySequence_Fast_GET_ITEM(o, j);
@@ -150,7 +151,7 @@ static PyObject* call(PyObject* self, PyObject* const* args, Py_ssize_t n) {
   ok = 1;
 done:
   while (n_views > 0) PyBuffer_Release(&views[--n_views]);
-  free(heap);
+  while (n_heap > 0) free(heap[--n_heap]);
   return ok ? PyLong_FromLong(rc) : NULL;
 }
 

@@ -22,3 +22,27 @@ def test_workspaces_have_room_from_any_16_byte_boundary(paged):
     n_pieces = places // 128                                           # of 128 rows: few tokens; 32 bytes each for what it belongs to
     for d in (64, 128):
         assert size(d) >= up256(places * d * 4) + up256(places * 8) + up256(n_pieces * 32) + 16
+
+
+class Stream:
+    cuda_stream = 0
+
+
+@pytest.mark.parametrize("n", [3, 255, 256, 511, 512, 600, 5000])
+def test_two_lists_of_any_length(n):
+    """The binding hands over host offsets of queries and of keys, both as long as there are sequences."""
+    p = T.prompt(n_seqs=n)
+    call = B._fn["slkv_prompt_attend"]
+
+    def status(cu_q, cu_k):
+        return call(Stream, p, None, T.P, T.P, T.P, cu_q, T.P, cu_k, None, None, None, T.P, 1 << 40)
+
+    none, keys = [0] * (n + 1), list(range(0, 3 * (n + 1), 3))
+    assert status(none, keys) == status(tuple(none), tuple(keys)) == B.SLKV_OK      # no query: nothing to do, but both lists are looked through
+    for i in (1, n // 2 + 1, n):
+        bad = list(keys)
+        bad[i] = -1
+        assert status(none, bad) == B.ERR["BAD_SHAPE"], i
+        bad = list(none)
+        bad[i - 1] = 7
+        assert status(bad, keys) == B.ERR["BAD_SHAPE"], i

@@ -90,3 +90,10 @@ def test_drafted_values_that_are_not_finite_in_two_blocks(dtype, heads, n):
     for _ in range(20):
         again = G.attend(c, heads, n, masks, counts, edit=edit)[3]
         assert torch.equal(torch.isfinite(again), torch.isfinite(first)) and torch.equal(again.nan_to_num(), first.nan_to_num())
+
+
+# ---- many sequences ----------------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_many_sequences_behind_keys_of_their_own(dtype):
+    nq = [1 + i % 4 if i % 9 else 0 for i in range(700)]
+    T.run(nq, [n + i % 5 * 31 for i, n in enumerate(nq)], hkv=1, G=2, d=64, dtype=dtype, window=2)
