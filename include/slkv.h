@@ -258,7 +258,10 @@ int slkv_compress(const slkv_params* p, const void* q_win, const void* k, const 
  *     queued and makes `stream` wait for every overlapped call made so far on the current device (no host wait);
  *     consume outputs, or free / overwrite any input, output or workspace buffer -- q_win, k, v, cu_seqlens_dev
  *     and budgets included -- only behind it.  cu_seqlens_host is read during the call only.  Any other slkv_*
- *     call that uses a workspace joins by itself first.  Of the slkv_q4_* calls, slkv_q4_pack sends out what is queued on its
+ *     call that uses a workspace joins by itself first, but for these.  slkv_prompt_attend and slkv_paged_attend leave what is queued
+ *     where it is, so that a prefill's layers still come together into lists; where their workspace overlaps that of overlapped calls, or their
+ *     lse_opt one that a queued layer takes, what is concerned goes out, and `stream` waits for it, first.  slkv_paged_plan and
+ *     slkv_paged_write send out what is queued on their own stream.  Of the slkv_q4_* calls, slkv_q4_pack sends out what is queued on its
  *     own stream, so that it finds the rows of calls made there before it; the others do not look at queued layers, and no
  *     slkv_q4_* call waits for another stream: a cache that is filled on one and read on another needs an order from the caller.
  *   - Streams and host threads: the calls made on one stream form one sequence (queue, workspace);
@@ -565,6 +568,8 @@ int slkv_q4_evict(const slkv_q4_cache* from, const slkv_q4_cache* to, const int3
  * fp32 accumulation throughout; with bf16, probabilities are rounded to bf16 for the product with V (2^-8 of each term).  fp32 rows are
  * exact sums of three bf16 parts, whose products with less than 2^-24 of a term are left out.  Results are the same bit for bit from call
  * to call.  out is none of the inputs.  A workspace belongs to one call at a time.
+ * Layers queued by slkv_compress_overlapped stay queued, but for those that take the log-sum-exps which lse_opt overwrites (see there); their other
+ * inputs and outputs are not to be overwritten in front of slkv_join, by out neither.
  */
 typedef struct slkv_prompt_params {
   int32_t n_seqs;

@@ -572,6 +572,32 @@ cudaError_t send_queued_layers(cudaStream_t st, int* launches) {
   return e;
 }
 
+// In front of a call on `st` that leaves queued layers where they are, so that a prefill's layers still come together into lists, and writes `ws`
+// and `lse`: overlapped calls, of any stream, whose workspace or whose queued layers' log-sum-exps those overlap go out, and `st` waits for them.
+cudaError_t send_layers_using(const void* ws, size_t ws_bytes, const float* lse, size_t lse_bytes, cudaStream_t st, int* launches) {
+  std::lock_guard<std::mutex> lock(g_lists_mu);
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess || dev < 0 || dev >= kMaxDevices || !g_lists[dev]) return e;
+  auto overlap = [](const void* a, size_t an, const void* b, size_t bn) {
+    const char *x = static_cast<const char*>(a), *y = static_cast<const char*>(b);
+    return x && y && x < y + bn && y < x + an;
+  };
+  DeviceStates* d = g_lists[dev];
+  for (int i = 0; i < kStatesPerDevice; ++i) {
+    ListState& s = d->st[i];
+    if (!d->used[i] || (s.n == 0 && !s.in_flight)) continue;
+    bool used = overlap(ws, ws_bytes, s.ws, s.ws_bytes);
+    const size_t rows = (size_t)s.p.n_seqs * s.p.n_q_heads * s.p.window;
+    for (int k = 0; k < s.n && !used; ++k) used = overlap(lse, lse_bytes, s.score[k].lse.lse_opt, rows * sizeof(float));
+    if (!used) continue;
+    e = flush_list(&s, d->owner[i], launches);
+    if (e == cudaSuccess) e = order_behind(&s, d->owner[i], st);
+    if (e != cudaSuccess) return e;
+  }
+  return cudaSuccess;
+}
+
 int report(cudaError_t e, int launches) {
   g_last_launches = launches;
   return e == cudaSuccess ? SLKV_OK : cuda_fail(e);

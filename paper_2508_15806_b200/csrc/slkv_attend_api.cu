@@ -183,7 +183,9 @@ int attend(AttendShape* a, int dtype, void* workspace, size_t workspace_bytes, c
   if (!aligned16(workspace)) return SLKV_ERR_BAD_ALIGN;
   if (!a->spread && !a->whole) attend_bind(a, workspace);
   int launches = 0;
-  cudaError_t e = dtype == SLKV_F32 ? launch_attend_f32(*a, st, &launches) : launch_attend_tensor(*a, st, &launches);
+  const size_t lse_rows = (size_t)a->n_seqs * a->n_q_heads * (a->paged ? a->n_tokens : a->window);
+  cudaError_t e = send_layers_using(workspace, a->spread || a->whole ? 0 : workspace_of(*a), a->lse, lse_rows * sizeof(float), st, &launches);
+  if (e == cudaSuccess) e = dtype == SLKV_F32 ? launch_attend_f32(*a, st, &launches) : launch_attend_tensor(*a, st, &launches);
   if (e == cudaSuccess) e = launch_attend_join(*a, dtype == SLKV_F32, st, &launches);
   return report(e, launches);
 }

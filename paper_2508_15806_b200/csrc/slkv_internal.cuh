@@ -341,6 +341,7 @@ cudaError_t launch_q4_evict(const Q4CacheView& from, const Q4CacheView& to, int 
                             const int32_t* newest, int32_t* status, void* workspace, cudaStream_t st, int* launches);
 // What slkv_compress_overlapped has queued on this stream goes out (slkv_api.cu).
 cudaError_t send_queued_layers(cudaStream_t st, int* launches);
+cudaError_t send_layers_using(const void* ws, size_t ws_bytes, const float* lse, size_t lse_bytes, cudaStream_t st, int* launches);
 // A call's status for the caller, its CUDA error and its launches kept for this thread.
 int report(cudaError_t e, int launches);
 

@@ -97,3 +97,50 @@ def test_drafted_values_that_are_not_finite_in_two_blocks(dtype, heads, n):
 def test_many_sequences_behind_keys_of_their_own(dtype):
     nq = [1 + i % 4 if i % 9 else 0 for i in range(700)]
     T.run(nq, [n + i % 5 * 31 for i, n in enumerate(nq)], hkv=1, G=2, d=64, dtype=dtype, window=2)
+
+
+# ---- beside overlapped compressions --------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("shared", ["nothing", "lse", "workspace", "both"])
+def test_prompts_between_overlapped_compressions(shared):
+    """Layer by layer, prompt attention and the compression that takes its log-sum-exps, which may stay queued.  One buffer of log-sum-exps for all
+    layers, one workspace for everything: the results are those of calls without overlap.  With buffers of their own, layers stay queued."""
+    nq, nk, hkv, g, d, w = [40, 20], [900, 700], 4, 4, 128, 16
+    c_q, c_k = T.cu(nq), T.cu(nk)
+    dev = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")      # noqa: E731
+    dq, dk, budgets = dev(c_q), dev(c_k), dev([60, 100, 33, 250])
+    layers, ws, lse = [], None, torch.zeros(2, hkv * g, w, device="cuda")
+    for i in range(3):
+        q, k, v = T.inputs(nq, nk, hkv, g, d, "bf16", seed=40 + i, behind=0)
+        q_win = torch.stack([q[e - w:e] for e in c_q[1:]])
+        pp, pc = B.make_prompt(q, k, v, torch.empty_like(q), 2, window=w), B.make_params(q_win, k, v, w, 5, softmax_domain=B.SLKV_ALL_CAUSAL)
+        sizes = B.slkv_workspace_bytes_overlapped(pc, c_k), B.slkv_prompt_attend_workspace_bytes(pp, c_q, c_k)
+        if ws is None:
+            ws = [torch.full((max(sizes),), 0xff, dtype=torch.uint8, device="cuda") for _ in range(2)]
+        cap = B.slkv_packed_rows_upper_bound(pc, c_k)
+
+        def outs():
+            return (*(torch.zeros(cap, d, dtype=k.dtype, device="cuda") for _ in range(2)), torch.zeros(2 * hkv + 1, dtype=torch.int32, device="cuda"),
+                    torch.zeros(cap, dtype=torch.int32, device="cuda"))
+        layers.append((q, k, v, q_win, pp, pc, torch.empty_like(q), lse if shared in ("lse", "both") else torch.zeros_like(lse), outs(), outs()))
+    own, wants = [], []
+    for q, k, v, q_win, pp, pc, out, _, _, want in layers:                 # one behind the other
+        x = torch.zeros_like(lse)
+        B.slkv_prompt_attend(pp, q, k, v, dq, c_q, out, ws[0], cu_k=dk, cu_k_host=c_k, lse=x)
+        own.append(B.slkv_last_launch_count())
+        B.slkv_compress(pc, q_win, k, v, dk, c_k, budgets, *want, ws[1], lse=x)
+        wants.append(out.clone())
+    torch.cuda.synchronize()
+    counts = []
+    for q, k, v, q_win, pp, pc, out, x, got, _ in layers:
+        out.zero_()
+        B.slkv_prompt_attend(pp, q, k, v, dq, c_q, out, ws[0], cu_k=dk, cu_k_host=c_k, lse=x)
+        counts.append(B.slkv_last_launch_count())
+        B.slkv_compress_overlapped(pc, q_win, k, v, dk, c_k, budgets, *got, ws[0 if shared in ("workspace", "both") else 1], lse=x)
+        assert B.slkv_last_launch_count() == 0                              # queued
+    B.slkv_join()
+    torch.cuda.synchronize()
+    for (_, _, _, _, _, _, out, _, got, want), o in zip(layers, wants):
+        assert torch.equal(out, o)
+        n = int(want[2][-1])
+        assert torch.equal(got[2], want[2]) and all(torch.equal(got[i][:n], want[i][:n]) for i in (0, 1, 3))
+    assert counts[0] == own[0] and all(n == m if shared == "nothing" else n > m for n, m in zip(counts[1:], own[1:])), (counts, own)
