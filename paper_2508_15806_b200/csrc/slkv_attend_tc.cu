@@ -523,6 +523,11 @@ __device__ __forceinline__ void softmax_role(const AttendTc& t, Smem<D>& sm, int
       // both blocks' products, which are issued in this order.  In prompts no row of the first block sees what the second one cleans.
       const Columns c = edge && (b.alt || g == 0 || !drafted) ? columns(t, p, tile, tok0, n_tok) : Columns{0, 0, 0};
       if (c.all < c.used) {
+        // The only wait on this barrier here, so phases before this one are passed over, and a parity tells this phase from the one before only if
+        // that is done: load no - kStages of the ring has to have landed.  S of tile t is there, and its products were issued behind waits for
+        // K's loads up to tile t and V's up to t - 1 (tiles in turn: t - 2) of the piece, and for all of earlier pieces.  The latest of which nothing
+        // is known are, with tiles in turn, V of t - 1 and K of t + 1, the two loads in front of V of t.
+        static_assert(S::kStages >= 3, "a ring shorter than what nobody here has waited for");
         const unsigned no = loads + b.v_load(tl, p.n), slot = no % S::kStages;
         ok = mbar_wait(smem_u32(&sm.kv_full[slot]), (no / S::kStages) & 1, &sm.abort);
         if (!__all_sync(0xffffffffu, ok)) return;
