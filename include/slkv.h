@@ -563,8 +563,9 @@ int slkv_q4_evict(const slkv_q4_cache* from, const slkv_q4_cache* to, const int3
  *                 before its first query are left as they are.  With the window of slkv_params this is the lse_opt of slkv_score and
  *                 slkv_compress (SLKV_ALL_CAUSAL), which spares them their pass over K for it.
  *   status        dev, optional: SLKV_ERR_DEVICE_TIMEOUT if a wait inside a kernel ran out; rows concerned are then left as they were or NaN
- * Limits: n_q_heads / n_kv_heads <= 64, fewer than 2^31 - 512 tokens, n_seqs * n_kv_heads < 2^31.  Scores below fp32's range in
- * magnitude: where a query or a key that it sees is not finite, its results may be NaN.
+ * Limits: n_q_heads / n_kv_heads <= 64, at most 2^31 - 512 tokens, n_seqs * n_kv_heads < 2^31.  Strides of axes longer than one: head_dim at
+ * least, below 2^38, multiples of 16 bytes, as are addresses.  Scores below fp32's range in magnitude: where a query or a key that it sees is not
+ * finite, its results may be NaN.
  * fp32 accumulation throughout; with bf16, probabilities are rounded to bf16 for the product with V (2^-8 of each term).  fp32 rows are
  * exact sums of three bf16 parts, whose products with less than 2^-24 of a term are left out.  Results are the same bit for bit from call
  * to call.  out is none of the inputs.  A workspace belongs to one call at a time.
@@ -660,7 +661,9 @@ int slkv_paged_write(const slkv_paged_cache* c, const void* k, const void* v, in
  *   tree_opt       dev, optional, uint64[n_seqs][n_tokens]; NULL: token i sees the tokens 0 .. i
  *   n_new_opt      dev, optional, int32[n_seqs]: tokens of each sequence; the rows behind them are padding: not read by others, outputs left as they are
  *   lse_opt        dev, optional out, float[n_seqs][n_q_heads][n_tokens] in lse_units
- * Limits, precision, status and workspace as slkv_prompt_attend.
+ * Limits, precision, status and workspace as slkv_prompt_attend.  Tiles are counted in 32 bits, whatever lengths there are: n_seqs * n_kv_heads
+ * times the blocks of 2 * (128 / G) tokens (fp32: of 128 / G; G = n_q_heads / n_kv_heads, quotients rounded down) that n_tokens make times
+ * max_pages * page_rows / 128 + 4 (fp32: / 64) < 2^31, counts rounded up.
  */
 typedef struct slkv_paged_attend_params {
   int32_t n_q_heads;        /* multiple of the cache's n_kv_heads */

@@ -46,3 +46,22 @@ def test_two_lists_of_any_length(n):
         bad = list(none)
         bad[i - 1] = 7
         assert status(bad, keys) == B.ERR["BAD_SHAPE"], i
+
+
+@pytest.mark.parametrize("dtype,tile,blocks", [(B.SLKV_BF16, 128, 2), (B.SLKV_F32, 64, 1)])
+@pytest.mark.parametrize("n_q_heads,n_tokens", [(8, 64), (8, 5), (24, 64), (128, 3)])
+def test_tiles_of_a_layer_are_counted_in_32_bits(dtype, tile, blocks, n_q_heads, n_tokens):
+    """Where the documentation draws the line, whatever the dimensions: the longest tables that are taken, and one page more."""
+    G = n_q_heads // 2
+    per = -(-n_tokens // (blocks * (128 // G)))
+    segments = 1 << 14
+    for new in (0, 1):
+        most = ((1 << 31) - 1) // (segments * per) - 3 - new           # tiles of a table
+        pages = most * tile // 64
+        p = T.tree(n_q_heads=n_q_heads, n_tokens=n_tokens, layer=0, has_new=new)
+        for n, good in ((pages, True), (pages + 1 + tile // 64, False)):
+            c = T.cache(n_layers=1, n_seqs=segments // 2, page_rows=64, max_pages=n, dtype=dtype)
+            if segments * n >= 1 << 31:                                  # the cache itself is refused
+                continue
+            assert (B.lib().slkv_paged_attend_workspace_bytes(c, p) > 0) == good
+            assert T.attend(c, p, ws=None) == B.ERR["WORKSPACE" if good else "BAD_SHAPE"]
