@@ -1,4 +1,6 @@
 """Prompt attention and the paged cache at what their documentation allows: workspaces, queued layers, drafted rows of several blocks, large tables."""
+import random
+
 import pytest
 import torch
 
@@ -144,3 +146,49 @@ def test_prompts_between_overlapped_compressions(shared):
         n = int(want[2][-1])
         assert torch.equal(got[2], want[2]) and all(torch.equal(got[i][:n], want[i][:n]) for i in (0, 1, 3))
     assert counts[0] == own[0] and all(n == m if shared == "nothing" else n > m for n, m in zip(counts[1:], own[1:])), (counts, own)
+
+
+# ---- plans of many segments ------------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("layers,ns,hkv", [(33, 32, 8), (32, 64, 8), (3, 2048, 8), (40, 300, 1)])
+def test_plan_more_segments_than_threads(layers, ns, hkv):
+    """Several segments a thread, in rounds that write lengths in place: by lengths up and down, ragged and wide slots, by rows added, there and back."""
+    r = random.Random(layers + ns)
+    n = layers * ns * hkv
+    assert n > 8192
+    c = G.Cache([r.choice([0, 1, 16, 17, 32, r.randint(0, 70)]) for _ in range(n)], ns, hkv, 64, "bf16", 16, spare=3 * n, room=4)
+    before = [list(t) for t in c.host_tables], list(c.host_lens), list(c.host_free)
+    up = [x + r.choice([0, 0, 1, 5, 40]) for x in c.host_lens]
+    G.check_plan(c, B.SLKV_PAGED_LENGTHS, up, up)
+    G.check_plan(c, B.SLKV_PAGED_LENGTHS, before[1], before[1], width=3)
+    assert (c.host_lens, c.host_free) == before[1:]
+    want = [r.choice([x, 0, x + 1, max(0, x - 20), r.randint(0, 70)]) for x in c.host_lens]
+    G.check_plan(c, B.SLKV_PAGED_LENGTHS, want, want)
+    add = [r.randint(-1, 4) for _ in range(ns)]
+    lengths = [x + max(add[i // hkv % ns], 0) for i, x in enumerate(c.host_lens)]
+    after = B.make_paged_cache(c.k, c.v, c.tables, torch.zeros_like(c.lens), c.free, torch.zeros_like(c.n_free), ns, hkv)
+    first = G.check_plan(c, B.SLKV_PAGED_ADD, add, lengths, width=4, after=after)
+    assert torch.equal(first, G.check_plan(c, B.SLKV_PAGED_ADD, add, lengths, width=4))
+
+
+def test_plan_many_segments_run_out():
+    """Pages that run out in a later round, in the middle of a CTA's segments."""
+    r = random.Random(9)
+    n, ns = 9000, 9000 // 8
+    for spare in (100, 6000, 15000):
+        c = G.Cache([r.randint(0, 20) for _ in range(n)], ns, 8, 64, "f32", 16, spare=spare, room=5)
+        want = [x + r.randint(0, 60) for x in c.host_lens]
+        G.check_plan(c, B.SLKV_PAGED_LENGTHS, want, want)
+
+
+@pytest.mark.parametrize("layers,ns,hkv", [(32, 16, 8), (32, 512, 1), (2, 300, 8)])
+def test_plan_few_that_grow_among_many(layers, ns, hkv):
+    """One sequence comes in and another goes while the others stay: new rows of a layer and of the next lie far apart, long runs of segments without."""
+    r = random.Random(ns)
+    n, per = layers * ns * hkv, ns * hkv
+    c = G.Cache([r.randint(1, 40) for _ in range(n)], ns, hkv, 64, "bf16", 32, spare=12 * layers * hkv, room=12)
+    comes, goes = r.sample(range(ns), 2)
+    want = [r.randint(200, 380) if i % per // hkv == comes else 0 if i % per // hkv == goes else x for i, x in enumerate(c.host_lens)]
+    G.check_plan(c, B.SLKV_PAGED_LENGTHS, want, want)
+    last = [x + (i in (0, n - 1)) * 50 for i, x in enumerate(c.host_lens)]                # the first and the last one only
+    G.check_plan(c, B.SLKV_PAGED_LENGTHS, last, last)
+    G.check_plan(c, B.SLKV_PAGED_LENGTHS, last, last)                                      # nothing comes in at all
