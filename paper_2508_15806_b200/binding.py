@@ -792,7 +792,7 @@ def slkv_paged_plan(cache: SlkvPagedCache, mode: int, want: torch.Tensor, slots:
                     slot_offsets: Optional[torch.Tensor] = None, after: Optional[SlkvPagedCache] = None,
                     status: Optional[torch.Tensor] = None, stream=None) -> None:
     """want int32: [n_segments] (SLKV_PAGED_LENGTHS), [n_layers, n_seqs * n_kv_heads + 1] (SLKV_PAGED_OFFSETS) or [n_seqs]
-    (SLKV_PAGED_ADD).  slots int32: [n] with slot_offsets int32 [n_segments + 1], or [n_segments, width] without.  after: the same cache
+    (SLKV_PAGED_ADD).  slots int32: [n] with slot_offsets int32 [n_segments + 1], or [n_segments, width] without (width 0: as no slots).  after: the same cache
     with lengths and a count of free pages of its own, which take the new ones."""
     d = cache.index
     if not d == want.get_device() == _current_device():
@@ -811,6 +811,8 @@ def slkv_paged_plan(cache: SlkvPagedCache, mode: int, want: torch.Tensor, slots:
         else:
             assert slot_offsets.dtype is _I32 and slot_offsets.is_contiguous() and slot_offsets.numel() == n_seg + 1
             assert slot_offsets.get_device() == d
+            if n_slots == 0:                     # an empty tensor has no address, which says that no slots are asked for; none is written
+                slots = slot_offsets
     lens_out = n_free_out = None
     if after is not None:
         assert after.same == cache.same

@@ -192,3 +192,11 @@ def test_plan_few_that_grow_among_many(layers, ns, hkv):
     last = [x + (i in (0, n - 1)) * 50 for i, x in enumerate(c.host_lens)]                # the first and the last one only
     G.check_plan(c, B.SLKV_PAGED_LENGTHS, last, last)
     G.check_plan(c, B.SLKV_PAGED_LENGTHS, last, last)                                      # nothing comes in at all
+
+
+@pytest.mark.parametrize("grows", [False, True])
+def test_plan_without_room_for_a_slot(grows):
+    """An empty tensor of slots, as many as no row needs: offsets are written all the same, and the status tells where rows do come in."""
+    c = G.Cache([3, 0, 40, 16], 2, 2, 64, "bf16", 16, spare=9, room=3)
+    want = [3, 0, 41, 16] if grows else [3, 0, 20, 0]
+    G.check_plan(c, B.SLKV_PAGED_LENGTHS, want, want, n_slots=0)
