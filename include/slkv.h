@@ -565,7 +565,7 @@ int slkv_q4_evict(const slkv_q4_cache* from, const slkv_q4_cache* to, const int3
  *   status        dev, optional: SLKV_ERR_DEVICE_TIMEOUT if a wait inside a kernel ran out; rows concerned are then left as they were or NaN
  * Limits: n_q_heads / n_kv_heads <= 64, at most 2^31 - 512 tokens, n_seqs * n_kv_heads < 2^31.  Strides of axes longer than one: head_dim at
  * least, below 2^38, multiples of 16 bytes, as are addresses.  Scores below fp32's range in magnitude: where a query or a key that it sees is not
- * finite, its results may be NaN.
+ * finite, its results may be NaN.  An infinite value that a query sees makes the output infinite, or NaN where its probability rounds to 0.
  * fp32 accumulation throughout; with bf16, probabilities are rounded to bf16 for the product with V (2^-8 of each term).  fp32 rows are
  * exact sums of three bf16 parts, whose products with less than 2^-24 of a term are left out.  Results are the same bit for bit from call
  * to call.  out is none of the inputs.  A workspace belongs to one call at a time.

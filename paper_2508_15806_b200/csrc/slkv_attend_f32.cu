@@ -2,7 +2,7 @@
 //
 // An fp32 number is the sum of three bf16 numbers, its significand in three parts of eight bits: x = x0 + x1 + x2 exactly.  A product
 // of two such sums needs six of the nine products (x0 y0, x0 y1, x1 y0, x1 y1, x0 y2, x2 y0; the others are below 2^-24 of it), which the
-// tensor cores add up in fp32: 375 TFLOP/s at six products each, against 74 on the FMA pipe.  Scores and outputs are made this way:
+// tensor cores add up in fp32: 278 TFLOP/s at six products each (a sixth of cuBLAS' measured bf16 rate), against 74 on the FMA pipe.  Scores and outputs are made this way:
 //   K, V, Q   come in as fp32, are split by the warps that load them into three planes each; K and V lie in shared memory, Q in TMEM but
 //             for its third plane, which one product in six needs: with all of it in shared memory a product of 64 keys takes 48 cycles
 //             for its operands instead of 32

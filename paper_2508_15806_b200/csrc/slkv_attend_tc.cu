@@ -13,13 +13,14 @@
 //   warp 8  TMA loads of K, V      warp 9  MMAs      warp 10  schedule      warp 11  TMA loads of Q
 // P is rounded to bf16 for the product (2^-8 of each term); the sum of a row is taken of what is not rounded, in fp32.
 //
-// Measured (B200, head_dim 128, 32 query heads on 8 KV heads): 32000 tokens 8.0 ms, 1050 TFLOP/s, 8000 tokens 480 us; drafted trees of 64
-// over segments of 8000 to 32000 rows 217 us, 5.8 TB/s.  What bounds prompts is the chain of a block: a tile's softmax takes 2280 cycles (loads
+// Measured (B200, head_dim 128, 32 query heads on 8 KV heads; in a row, the same inputs): 32000 tokens 7.7 ms, 1090 TFLOP/s, 8000 tokens 459 us,
+// 1140 TFLOP/s (other inputs from call to call: 8.1 ms, 480 us); drafted trees of 64 over segments of 8000 to 32000 rows 217 us, 5.8 TB/s.  What bounds prompts is the chain of a block: a tile's softmax takes 2280 cycles (loads
 // from TMEM 170, maximum 400, exponentials 1220 to 1320 beside the other block's, the rest conversions, stores and barriers), the products
 // before and behind it 1300 more, of which 1024 are the matrix unit's; two blocks in turn keep it busy 57 % of the time, the exponentials'
 // unit as long.  There is no TMEM for a third block or a second S.  Tried, 8000 tokens: four warps more, two threads to a row (8.7 ms at
-// 32000 tokens); halves of 64 keys with S in two buffers (550 us); two warps that issue products; a part of the exponentials as polynomials
-// (466 us for an eighth of them, 479 for a quarter, 530 for half); the maximum beside the exponentials of the reference before (506 to 524 us).
+// 32000 tokens); halves of 64 keys with S in two buffers and a softmax each (550 us); two warps that issue products; a part of the exponentials as polynomials
+// (beside it in one call, in turn: none 459 us, an eighth of them 467, a quarter 479, half 510; at 32000 tokens 7.71 ms, 7.86, 7.99, 8.42); the maximum beside the
+// exponentials of the reference before (506 to 524 us, 479 without in that call).
 //
 // A key that a row does not see gives it nothing, whatever K and V hold there: scores are replaced, not biased, and since 0 times an
 // infinity is not 0, the V rows of a tile that not every row of the block sees are looked through first: rows behind the last key become 0 in
